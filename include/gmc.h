@@ -505,8 +505,167 @@ gmc_status gmc_calib_copy(void* hip_stream, float* dst_dev, const float* src_dev
 gmc_status gmc_calib_stream(void* hip_stream, float* e_dev, const float* g_dev, int64_t row_pitch, int32_t K,
                             int64_t d);
 
-/* Message for the last non-OK status of this context (or of gmc_init when
- * ctx is NULL); never NULL. */
+/* ---------------------------------------------------------------------------
+ * The operators of a worker's own pass, between its data and the gradient
+ * g_{t,k} that gmc_step takes: dropout, group norm with its activation, and
+ * two losses with their gradients.  None of them needs a context.
+ *
+ * Conventions shared by them:
+ *   - Work is enqueued on hip_stream (a hipStream_t; NULL: the null stream) of
+ *     the current device and is asynchronous.  Nothing is allocated and
+ *     nothing is kept between calls: scratch is the caller's workspace_dev, of
+ *     at least the bytes the *_workspace function gives (its contents need not
+ *     be set and mean nothing afterwards; calls that may overlap need one
+ *     each).  A *_workspace function returns -1 for sizes the call refuses.
+ *     The calls may be captured into a HIP graph.
+ *   - Activations and logits are of a GMC_F32, GMC_BF16 or GMC_F16 type;
+ *     statistics, parameters, log-probabilities and losses are fp32.
+ *     Arithmetic is binary32 or wider, and a 16-bit result is rounded once, to
+ *     nearest even, from the 32-bit one.
+ *   - Pitches count elements.  Any element alignment is accepted.  The
+ *     innermost axis (columns, channels, vocabulary) is contiguous.
+ *   - Sums are taken in a fixed order: the same call gives the same bits (the
+ *     losses' order follows the logits' alignment to 16 bytes).
+ *   - An output may be an input's own buffer where the call says so, with the
+ *     same pitches; overlaps of another kind are refused.
+ *   - Invalid arguments return GMC_EINVAL before any device work, reported
+ *     through gmc_last_error(NULL).
+ */
+enum { GMC_F32 = 0, GMC_BF16 = 1, GMC_F16 = 2 };
+
+/*
+ * Dropout with a mask that is never stored, with or without the residual add,
+ * and its own backward pass:
+ *   y[r][c] = (kept ? x[r][c] * scale : 0) + residual[r][c]
+ * Forward: x the branch, residual the stream it joins or NULL.  Backward:
+ * x = dL/dy, no residual, the same p, seed, t, worker and site (the residual's
+ * gradient is dL/dy itself).
+ *   Mask: with i = r * cols + c, kept = bits(i) >= level, level =
+ *   floor(65536 p + 1/2); bits(i) are the 16 bits from bit 16 (i mod 4) of the
+ *   draw mix64(state + (i / 4 + 1) * 0x9e3779b97f4a7c15) of a SplitMix64 stream
+ *   with state = seed XOR mix64(t + 1) XOR mix64((worker + 1) << 32 | (site + 1)):
+ *   the workers share a seed, as the compressors' draws do, and differ by
+ *   their number.  scale = fl32(65536 / (65536 - level)), the reciprocal of
+ *   the probability the mask really has (p in units of 2^-16); level 65536
+ *   keeps nothing.  A dropped x is not looked at: NaN there gives 0.
+ *   rows, cols  >= 0, rows * cols <= 2^40 (0: nothing to do)
+ *   p           [0, 1]
+ *   t           step, >= 0; worker in [0, GMC_MAX_WORKERS); site >= 0, the
+ *               dropout's number in the model
+ *   y_dev       may be x_dev or residual_dev
+ */
+gmc_status gmc_dropout(void* hip_stream, int32_t dtype, int64_t rows, int64_t cols, const void* x_dev,
+                       int64_t x_pitch, const void* residual_dev, int64_t residual_pitch, void* y_dev,
+                       int64_t y_pitch, double p, uint64_t seed, int64_t t, int32_t worker, int32_t site);
+
+/* Activations of gmc_group_norm: none, max(z, 0), z / (1 + e^-z). */
+enum { GMC_ACT_NONE = 0, GMC_ACT_RELU = 1, GMC_ACT_SILU = 2 };
+
+/*
+ * Group norm and its activation over N channels-last images of S pixels with C
+ * channels in G groups of C / G neighbours: over each image's group of m =
+ * S C / G values, mean and rstd = 1 / sqrt(variance + eps) (variance over m,
+ * about the mean), then y = act(z), z = ((x - mean) * rstd) * gamma + beta.
+ * Statistics are the image's own: they do not depend on the worker's batch.
+ *   x_dev       x[n * x_image + s * x_pixel + c]; x_pixel >= C
+ *   gamma_dev, beta_dev  [C] fp32 or NULL (ones, zeros); may lie inside w
+ *   eps         [0, 1]
+ *   y_dev       may be x_dev
+ *   mean_dev, rstd_dev   [N][G] fp32 out, for the backward pass
+ *   N >= 0, 1 <= S < 2^31, N S C <= 2^40
+ */
+gmc_status gmc_group_norm(void* hip_stream, int32_t dtype, int64_t N, int64_t S, int32_t C, int32_t G,
+                          const void* x_dev, int64_t x_image, int64_t x_pixel, const float* gamma_dev,
+                          const float* beta_dev, double eps, int32_t act, void* y_dev, int64_t y_image,
+                          int64_t y_pixel, float* mean_dev, float* rstd_dev, void* workspace_dev,
+                          int64_t workspace_bytes);
+
+/*
+ * Its backward pass: from dL/dy and the forward pass's x, mean and rstd,
+ *   dz = dy act'(z) (z as above, bit for bit; relu's derivative at 0 is 0),
+ *   dgamma[c] = sum dz hat, dbeta[c] = sum dz over images and pixels,
+ *   dx = rstd (gamma dz - (s1 + hat s2) / m), s1 = sum gamma dz and s2 = sum
+ *   gamma dz hat over the image's group.
+ *   dx_dev      may be dy_dev or x_dev
+ *   dgamma_dev, dbeta_dev  [C] fp32 out or NULL; may lie inside a row of the
+ *               gradients gmc_step takes
+ */
+gmc_status gmc_group_norm_backward(void* hip_stream, int32_t dtype, int64_t N, int64_t S, int32_t C, int32_t G,
+                                   const void* dy_dev, int64_t dy_image, int64_t dy_pixel, const void* x_dev,
+                                   int64_t x_image, int64_t x_pixel, const float* mean_dev, const float* rstd_dev,
+                                   const float* gamma_dev, const float* beta_dev, int32_t act, void* dx_dev,
+                                   int64_t dx_image, int64_t dx_pixel, float* dgamma_dev, float* dbeta_dev,
+                                   void* workspace_dev, int64_t workspace_bytes);
+
+/* Scratch bytes of the two calls above (backward = 0, 1); a caller may pass
+ * one workspace of the larger to both. */
+int64_t gmc_group_norm_workspace(int32_t dtype, int64_t N, int64_t S, int32_t C, int32_t G, int32_t backward);
+
+/*
+ * The clipped policy loss with a KL term over R sequences of T tokens, from
+ * the tokens' logits over a vocabulary of V, and the logits' gradient:
+ *   logp  = log softmax(logits / temperature)[label]
+ *   ratio = exp(logp - old_logp),  A = the token's advantage
+ *   l     = -min(ratio A, clip(ratio, 1 - clip_lo, 1 + clip_hi) A)
+ *           + kl_coef (exp(ref_logp - logp) - (ref_logp - logp) - 1)
+ *   loss  = sum of weight * l; weight = 1 / (tokens that count), or with
+ *           by_sequence 1 / (the sequence's tokens that count * sequences
+ *           that have any)
+ *   grad  = grad_scale * dloss / dlogits; where the clipped term is the smaller
+ *           one it has no gradient
+ * A token whose label is `ignore` counts nowhere: its logits, old_logp,
+ * ref_logp and advantage are not read, its logp is 0 and its gradient row 0.
+ * A label outside [0, V) that is not `ignore` makes the token's logp, the
+ * loss and its gradient row NaN.  With no token at all the loss is 0.
+ *   logits_dev   [r * seq_pitch + t * tok_pitch + v]; tok_pitch >= V (any
+ *                for T = 1); a view without each sequence's last token is fine
+ *   labels_dev   int64 [R][T], rows label_pitch apart
+ *   old_logp_dev fp32 [R][T], or NULL: the present ones (ratio 1)
+ *   ref_logp_dev fp32 [R][T], or NULL: no KL term
+ *   adv_dev      fp32, adv_dev[r * adv_seq + t * adv_tok]; adv_tok 0: one per
+ *                sequence
+ *   stats_dev    fp32 [3] out: loss, the weighted mean of the KL term (without
+ *                kl_coef), the weighted share of clipped tokens
+ *   logp_dev     fp32 [R][T] out
+ *   grad_dev     out, with pitches of its own, or NULL; may be logits_dev
+ *   R T < 2^22, 1 <= V < 2^30
+ * workspace_dev is 16-byte aligned.
+ */
+gmc_status gmc_policy_loss(void* hip_stream, int32_t dtype, int64_t R, int64_t T, int64_t V, const void* logits_dev,
+                           int64_t seq_pitch, int64_t tok_pitch, const int64_t* labels_dev, int64_t label_pitch,
+                           int64_t ignore, const float* old_logp_dev, const float* ref_logp_dev, const float* adv_dev,
+                           int64_t adv_seq, int64_t adv_tok, double clip_lo, double clip_hi, double kl_coef,
+                           double temperature, int32_t by_sequence, double grad_scale, float* stats_dev,
+                           float* logp_dev, void* grad_dev, int64_t grad_seq, int64_t grad_tok, void* workspace_dev,
+                           int64_t workspace_bytes);
+int64_t gmc_policy_loss_workspace(int64_t R, int64_t T);
+
+/*
+ * The preference loss of P pairs of answers (paired log ratios), from the
+ * logits of 2 P sequences of T tokens, pair p's chosen answer in sequence p and
+ * its rejected one in sequence P + p, and the logits' gradient:
+ *   reward = beta * sum over the answer's tokens of (logp - ref_logp), divided
+ *            by their number with `average` (0 for an empty answer)
+ *   h      = reward of the chosen - reward of the rejected answer
+ *   l      = -(1 - smoothing) log sigmoid(h) - smoothing log sigmoid(-h)
+ *   loss   = the mean of l over the pairs; grad = grad_scale * dloss / dlogits
+ * `ignore`, labels out of range, pitches and grad_dev as in gmc_policy_loss.
+ *   ref_logp_dev  fp32 [2 P][T], or NULL: zeros
+ *   smoothing     [0, 1]
+ *   loss_dev      fp32 [1] out (0 for P = 0); pair_loss_dev fp32 [P] out;
+ *   rewards_dev   fp32 [2 P] out; logp_dev fp32 [2 P][T] out
+ * workspace_dev is 8-byte aligned.
+ */
+gmc_status gmc_preference_loss(void* hip_stream, int32_t dtype, int64_t P, int64_t T, int64_t V,
+                               const void* logits_dev, int64_t seq_pitch, int64_t tok_pitch, const int64_t* labels_dev,
+                               int64_t label_pitch, int64_t ignore, const float* ref_logp_dev, double beta,
+                               double smoothing, int32_t average, double grad_scale, float* loss_dev,
+                               float* pair_loss_dev, float* rewards_dev, float* logp_dev, void* grad_dev,
+                               int64_t grad_seq, int64_t grad_tok, void* workspace_dev, int64_t workspace_bytes);
+int64_t gmc_preference_loss_workspace(int64_t P, int64_t T);
+
+/* Message for the last non-OK status of this context (or of gmc_init and the
+ * calls without a context when ctx is NULL); never NULL. */
 const char* gmc_last_error(const gmc_ctx* ctx);
 
 /* Free the context and its scratch (synchronises its stream).  NULL is a no-op. */

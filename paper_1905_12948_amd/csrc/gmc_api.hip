@@ -12,6 +12,7 @@
 
 #include "../../include/gmc.h"
 #include "gmc_internal.h"
+#include "gmc_ops.h"
 
 using namespace gmc;
 
@@ -122,6 +123,19 @@ gmc_status fail(gmc_ctx* ctx, gmc_status st, const std::string& msg) {
     if (ctx) ctx->err = msg; else g_init_error = msg;
     return st;
 }
+
+}  // namespace
+
+gmc_status gmc::op_error(gmc_status st, const char* where, const char* what) noexcept {
+    try {
+        g_init_error.assign(where).append(": ").append(what);
+    } catch (...) {
+        g_init_error.clear();
+    }
+    return st;
+}
+
+namespace {
 
 gmc_status hip_fail(gmc_ctx* ctx, hipError_t e, const char* what) {
     std::string m = std::string(what) + ": " + hipGetErrorString(e);

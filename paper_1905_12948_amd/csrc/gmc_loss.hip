@@ -1,0 +1,718 @@
+// The clipped policy loss with its KL term and the preference loss, from logits,
+// with the logits' gradient (gmc_policy_loss and gmc_preference_loss in
+// include/gmc.h).
+//
+// Both gradients have the form  dlogits_j = c (delta_jy - p_j)  with p the
+// token's softmax and c a scalar of the token.  A row of logits is a token's
+// vocabulary; with M its maximum, e_j = 2^((x_j - M) L), L = log2(e) / tau, and
+// s = sum e_j:  log p_y = ((x_y - M) L - log2 s) ln 2  and  c p_j = (c / s) e_j.
+// The maximum is subtracted first, so that any finite logits are in range
+// (rows at the type's lowest value among them) and -inf entries give zeros.
+//
+// Policy: c depends on the token alone, so a workgroup keeps the row in its
+// registers: the logits are read once and the gradient is written once, the
+// floor of the bytes.  Preference: c needs the pair's sums over all its tokens;
+// the rows are read for the statistics and again for the gradient.
+// Ignored tokens' logits are never read, and their gradient is zero.
+#include <math.h>
+
+#include "gmc_ops.h"
+
+namespace gmc {
+
+namespace {
+
+constexpr int kHeldVecs = 8;         // vectors of a row a thread holds ...
+constexpr int kHeldVecsLong = 16;    // ... of a long one
+constexpr int kRowThreads = 1024;
+constexpr int kStatThreads = 1024;
+
+// A row of V elements as a head and a tail of single elements and a body of
+// 16-byte aligned vectors.
+template <int DT>
+struct Row {
+    typedef typename Elem<DT>::T T;
+    static constexpr int N = 16 / Elem<DT>::kSize;
+    const T* p;
+    int V, head, nb, tail;
+
+    __device__ __forceinline__ Row(const T* q, int v) : p(q), V(v) {
+        const int off = (int)((reinterpret_cast<uintptr_t>(q) & 15u) / Elem<DT>::kSize);
+        head = off ? N - off : 0;
+        if (head > V) head = V;
+        nb = (V - head) / N;
+        tail = V - head - nb * N;
+    }
+    // The index of thread `tid`'s single element, -1 for most threads.
+    __device__ __forceinline__ int edge(int tid) const {
+        if (tid < head) return tid;
+        if (tid >= 32 && tid < 32 + tail) return V - tail + (tid - 32);
+        return -1;
+    }
+};
+
+// Workgroup-wide (max, sum of 2^((x - max) L)) from every thread's own; one
+// barrier, every thread gets the result.  kWaves = 1: a wavefront's own row.
+template <int kWaves>
+__device__ __forceinline__ void join_stats(float L, float& m, float& s, float2* lds) {
+    const float wm = wave_max(m);
+    const float base = wm == -INFINITY ? 0.0f : wm;
+    s = wave_sum(s * exp2_fast((m - base) * L));
+    m = wm;
+    if (kWaves == 1) return;
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = make_float2(m, s);
+    __syncthreads();
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, lds[w].x);
+    const float b = top == -INFINITY ? 0.0f : top;
+    float t = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) t += lds[w].y * exp2_fast((lds[w].x - b) * L);
+    m = top;
+    s = t;
+}
+
+// e_j of a vector, the maximum subtracted.
+template <int N>
+__device__ __forceinline__ void exps(float (&f)[N], float base, float L) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = exp2_fast((f[i] - base) * L);
+}
+
+// (max, sum) over the thread's share of a row, read in passes of four vectors.
+template <int DT, int kThreads>
+__device__ __forceinline__ void stream_stats(const Row<DT>& row, int tid, float L, float& m, float& s) {
+    constexpr int N = Row<DT>::N;
+    typedef Vec<DT, N> V;
+    m = -INFINITY;
+    s = 0.0f;
+    const int e = row.edge(tid);
+    if (e >= 0) {
+        m = Elem<DT>::up(row.p[e]);
+        s = m == -INFINITY ? 0.0f : m == m && m < INFINITY ? 1.0f : NAN;
+    }
+    for (int v0 = tid; v0 < row.nb; v0 += 4 * kThreads) {
+        V x[4];
+        float f[N];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (v0 + k * kThreads < row.nb) x[k] = V::load(row.p + row.head + (int64_t)(v0 + k * kThreads) * N);
+        float cm = m;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (v0 + k * kThreads < row.nb) {
+                x[k].unpack(f);
+#pragma unroll
+                for (int i = 0; i < N; ++i) cm = fmaxf(cm, f[i]);
+            }
+        const float base = cm == -INFINITY ? 0.0f : cm;
+        s *= exp2_fast((m - base) * L);
+        m = cm;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (v0 + k * kThreads < row.nb) {
+                x[k].unpack(f);
+                exps<N>(f, base, L);
+#pragma unroll
+                for (int i = 0; i < N; ++i) s += f[i];
+            }
+    }
+}
+
+// A vector of the gradient: c (delta - p), at = the label's place in it or
+// outside [0, N).
+template <int N>
+__device__ __forceinline__ void gradient(float (&f)[N], float base, float L, float k, float c, int at) {
+    exps<N>(f, base, L);
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = f[i] * k;
+    if ((unsigned)at < (unsigned)N)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i == at) f[i] += c;
+}
+
+template <int DT>
+__device__ __forceinline__ void zero_row(typename Elem<DT>::T* out, int V, int tid, int threads) {
+    constexpr int N = Row<DT>::N;
+    const Row<DT> row(out, V);
+    Vec<DT, N> z;
+    const float f[N] = {};
+    z.pack(f);
+    for (int v = tid; v < row.nb; v += threads) z.store(out + row.head + (int64_t)v * N);
+    const int e = row.edge(tid);
+    if (e >= 0) out[e] = Elem<DT>::down(0.0f);
+}
+
+// The gradient of a row read from memory, element by element in its own thread
+// (so it may be written over the logits).
+template <int DT>
+__device__ __forceinline__ void stream_gradient(const Row<DT>& row, typename Elem<DT>::T* out, int tid, int threads,
+                                                float base, float L, float k, float c, int y) {
+    constexpr int N = Row<DT>::N;
+    typedef Vec<DT, N> V;
+    for (int v0 = tid; v0 < row.nb; v0 += 4 * threads) {
+        V x[4];
+        float f[N];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (v0 + u * threads < row.nb) x[u] = V::load(row.p + row.head + (int64_t)(v0 + u * threads) * N);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (v0 + u * threads < row.nb) {
+                const int j = row.head + (v0 + u * threads) * N;
+                x[u].unpack(f);
+                gradient<N>(f, base, L, k, c, y - j);
+                x[u].pack(f);
+                x[u].store(out + j);
+            }
+    }
+    const int e = row.edge(tid);
+    if (e >= 0) {
+        float f[1] = {Elem<DT>::up(row.p[e])};
+        gradient<1>(f, base, L, k, c, y - e);
+        out[e] = Elem<DT>::down(f[0]);
+    }
+}
+
+__device__ __forceinline__ float logp_of(float xy, float M, float L, float s) {
+    const float base = M == -INFINITY ? 0.0f : M;
+    return ((xy - base) * L - __log2f(s)) * kLn2;
+}
+
+// -- policy -------------------------------------------------------------------
+
+struct PolicyArgs {
+    const void* logits;
+    void* grad;  // NULL: the loss alone
+    int64_t seq, tok, grad_seq, grad_tok;
+    const int64_t* labels;
+    int64_t label_pitch, ignore;
+    const float* old_logp;  // NULL: the present ones
+    const float* ref_logp;  // NULL: no KL term
+    const float* adv;
+    int64_t adv_seq, adv_tok;
+    int64_t R, T, rows;
+    int32_t V;
+    float lo, hi, kl, L, inv_tau, scale;
+    int32_t by_sequence;
+    float* logp;
+    const float* weight;  // [R] one token's weight, or [1]
+    float4* tokens;       // per token: weighted loss, KL, clipped
+};
+
+// Weights of the mean over tokens, or of the mean over sequences of their
+// means: how many tokens each sequence keeps (one wavefront a sequence) ...
+__global__ __launch_bounds__(256) void policy_counts(PolicyArgs a, float* weight) {
+    const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (r >= a.R) return;
+    int n = 0;
+    for (int64_t t = threadIdx.x & 63; t < a.T; t += 64) n += a.labels[r * a.label_pitch + t] != a.ignore;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o);
+    if ((threadIdx.x & 63) == 0) weight[1 + r] = (float)n;
+}
+
+// ... and the reciprocal of all tokens, or of the sequences that keep any.
+__global__ __launch_bounds__(1024) void policy_weight(PolicyArgs a, float* weight) {
+    __shared__ double lds[16];
+    double n = 0.0;
+    for (int64_t r = threadIdx.x; r < a.R; r += 1024) {
+        const float c = weight[1 + r];
+        n += a.by_sequence ? (c > 0.0f ? 1.0 : 0.0) : (double)c;
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = n;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double t = 0.0;
+        for (int w = 0; w < 16; ++w) t += lds[w];
+        weight[0] = t > 0.0 ? (float)(1.0 / t) : 0.0f;
+    }
+}
+
+// What a token adds to the loss, and c.
+struct Token {
+    float logp, loss, kl, clipped, c;
+};
+
+__device__ __forceinline__ Token policy_token(const PolicyArgs& a, int64_t r, int64_t t, float logp) {
+    Token k;
+    float w = a.weight[0];
+    if (a.by_sequence) w = w / a.weight[1 + r];
+    const float A = a.adv[r * a.adv_seq + t * a.adv_tok];
+    const float ratio = a.old_logp ? expf(logp - a.old_logp[r * a.T + t]) : logp == logp ? 1.0f : NAN;
+    const float unclipped = ratio * A;
+    const float clipped = fminf(fmaxf(ratio, 1.0f - a.lo), 1.0f + a.hi) * A;
+    const bool free = !(unclipped > clipped);  // the smaller one, which the gradient follows
+    float slope = free ? -unclipped : 0.0f;
+    float kl = 0.0f;
+    if (a.ref_logp) {
+        const float d = a.ref_logp[r * a.T + t] - logp;
+        const float e = expm1f(d);
+        kl = e - d;
+        slope = slope - a.kl * e;
+    }
+    k.logp = logp;
+    k.loss = w * (-(free ? unclipped : clipped) + a.kl * kl);
+    k.kl = w * kl;
+    k.clipped = free ? 0.0f : w;
+    k.c = a.scale * a.inv_tau * w * slope;
+    return k;
+}
+
+__device__ __forceinline__ void policy_write(const PolicyArgs& a, int64_t i, const Token& k) {
+    a.logp[i] = k.logp;
+    a.tokens[i] = make_float4(k.loss, k.kl, k.clipped, 0.0f);
+}
+
+// One row of logits per kThreads threads, held in kHeld vectors a thread.
+template <int DT, int kThreads, int kHeld>
+__global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void policy_held(PolicyArgs a) {
+    typedef typename Elem<DT>::T T;
+    constexpr int N = Row<DT>::N;
+    constexpr int kWaves = kThreads / 64;
+    typedef Vec<DT, N> V;
+    __shared__ float2 lds[kWaves];
+    const int tid = threadIdx.x % kThreads;
+    const int64_t i = (int64_t)blockIdx.x * (blockDim.x / kThreads) + threadIdx.x / kThreads;
+    if (i >= a.rows) return;
+    const int64_t r = i / a.T, t = i - r * a.T;
+    const int64_t label = a.labels[r * a.label_pitch + t];
+    T* out = static_cast<T*>(a.grad) + r * a.grad_seq + t * a.grad_tok;
+    if (label == a.ignore) {
+        if (tid == 0) policy_write(a, i, Token{0.0f, 0.0f, 0.0f, 0.0f, 0.0f});
+        if (a.grad) zero_row<DT>(out, a.V, tid, kThreads);
+        return;
+    }
+    const Row<DT> row(static_cast<const T*>(a.logits) + r * a.seq + t * a.tok, a.V);
+    V x[kHeld];
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k)
+        if (tid + k * kThreads < row.nb) x[k] = V::load(row.p + row.head + (int64_t)(tid + k * kThreads) * N);
+    const int e = row.edge(tid);
+    const float ex = e >= 0 ? Elem<DT>::up(row.p[e]) : -INFINITY;
+    const bool known = (uint64_t)label < (uint64_t)a.V;
+    const int y = known ? (int)label : -1;
+    const float xy = known ? Elem<DT>::up(row.p[y]) : NAN;
+    float m = ex, s, f[N];
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k)
+        if (tid + k * kThreads < row.nb) {
+            x[k].unpack(f);
+#pragma unroll
+            for (int q = 0; q < N; ++q) m = fmaxf(m, f[q]);
+        }
+    // the wavefront's maximum first: its exponentials are then final up to a factor
+    m = wave_max(m);
+    const float own = m == -INFINITY ? 0.0f : m;
+    s = e >= 0 ? exp2_fast((ex - own) * a.L) : 0.0f;
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k)
+        if (tid + k * kThreads < row.nb) {
+            x[k].unpack(f);
+            exps<N>(f, own, a.L);
+#pragma unroll
+            for (int q = 0; q < N; ++q) s += f[q];
+        }
+    join_stats<kWaves>(a.L, m, s, lds);
+    const Token tk = policy_token(a, r, t, logp_of(xy, m, a.L, s));
+    if (tid == 0) policy_write(a, i, tk);
+    if (!a.grad) return;
+    const float base = m == -INFINITY ? 0.0f : m;
+    const float k1 = -tk.c / s;
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k)
+        if (tid + k * kThreads < row.nb) {
+            const int j = row.head + (tid + k * kThreads) * N;
+            x[k].unpack(f);
+            gradient<N>(f, base, a.L, k1, tk.c, y - j);
+            x[k].pack(f);
+            x[k].store(out + j);
+        }
+    if (e >= 0) {
+        float g[1] = {ex};
+        gradient<1>(g, base, a.L, k1, tk.c, y - e);
+        out[e] = Elem<DT>::down(g[0]);
+    }
+}
+
+// Rows longer than a workgroup's registers: two reads.
+template <int DT>
+__global__ __launch_bounds__(kRowThreads) void policy_long(PolicyArgs a) {
+    typedef typename Elem<DT>::T T;
+    __shared__ float2 lds[kRowThreads / 64];
+    const int64_t i = blockIdx.x, r = i / a.T, t = i - r * a.T;
+    const int64_t label = a.labels[r * a.label_pitch + t];
+    T* out = static_cast<T*>(a.grad) + r * a.grad_seq + t * a.grad_tok;
+    if (label == a.ignore) {
+        if (threadIdx.x == 0) policy_write(a, i, Token{0.0f, 0.0f, 0.0f, 0.0f, 0.0f});
+        if (a.grad) zero_row<DT>(out, a.V, threadIdx.x, kRowThreads);
+        return;
+    }
+    const Row<DT> row(static_cast<const T*>(a.logits) + r * a.seq + t * a.tok, a.V);
+    const bool known = (uint64_t)label < (uint64_t)a.V;
+    const int y = known ? (int)label : -1;
+    const float xy = known ? Elem<DT>::up(row.p[y]) : NAN;
+    float m, s;
+    stream_stats<DT, kRowThreads>(row, threadIdx.x, a.L, m, s);
+    join_stats<kRowThreads / 64>(a.L, m, s, lds);
+    const Token tk = policy_token(a, r, t, logp_of(xy, m, a.L, s));
+    if (threadIdx.x == 0) policy_write(a, i, tk);
+    if (a.grad)
+        stream_gradient<DT>(row, out, threadIdx.x, kRowThreads, m == -INFINITY ? 0.0f : m, a.L, -tk.c / s, tk.c, y);
+}
+
+// The three sums over the tokens, in 64 bits and a fixed order.
+__global__ __launch_bounds__(1024) void policy_finish(const float4* tokens, int64_t rows, float* stats) {
+    __shared__ double lds[3][16];
+    double v[3] = {0.0, 0.0, 0.0};
+    for (int64_t i = threadIdx.x; i < rows; i += 1024) {
+        const float4 k = tokens[i];
+        v[0] += k.x;
+        v[1] += k.y;
+        v[2] += k.z;
+    }
+#pragma unroll
+    for (int q = 0; q < 3; ++q) {
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) v[q] += __shfl_xor(v[q], o);
+        if ((threadIdx.x & 63) == 0) lds[q][threadIdx.x >> 6] = v[q];
+    }
+    __syncthreads();
+    if (threadIdx.x < 3) {
+        double t = 0.0;
+        for (int w = 0; w < 16; ++w) t += lds[threadIdx.x][w];
+        stats[threadIdx.x] = (float)t;
+    }
+}
+
+// -- preference -----------------------------------------------------------------
+
+struct PrefArgs {
+    const void* logits;
+    void* grad;
+    int64_t seq, tok, grad_seq, grad_tok;
+    const int64_t* labels;
+    int64_t label_pitch, ignore;
+    const float* ref_logp;  // NULL: zero
+    int64_t P, T;
+    int64_t first, pairs;  // this launch's pairs
+    int32_t V;
+    float beta, smoothing, scale;
+    int32_t average;
+    float* logp;       // [2P][T]
+    float* rewards;    // [2P]
+    float* pair_loss;  // [P]
+    float2* stats;     // [2P][T] (max, sum)
+    float* coef;       // [2P]
+};
+
+// The token of row i of a launch: the chosen answers of its pairs, then the
+// rejected ones.
+__device__ __forceinline__ int64_t pref_sequence(const PrefArgs& a, int64_t local) {
+    return local < a.pairs ? a.first + local : a.P + a.first + (local - a.pairs);
+}
+
+template <int DT, int kThreads>
+__global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void pref_logp(PrefArgs a) {
+    typedef typename Elem<DT>::T T;
+    constexpr int kWaves = kThreads / 64;
+    __shared__ float2 lds[kWaves];
+    const int tid = threadIdx.x % kThreads;
+    const int64_t i = (int64_t)blockIdx.x * (blockDim.x / kThreads) + threadIdx.x / kThreads;
+    if (i >= 2 * a.pairs * a.T) return;
+    const int64_t local = i / a.T, t = i - local * a.T, r = pref_sequence(a, local);
+    const int64_t label = a.labels[r * a.label_pitch + t];
+    if (label == a.ignore) {
+        if (tid == 0) a.logp[r * a.T + t] = 0.0f;
+        return;
+    }
+    const Row<DT> row(static_cast<const T*>(a.logits) + r * a.seq + t * a.tok, a.V);
+    const bool known = (uint64_t)label < (uint64_t)a.V;
+    const float xy = known ? Elem<DT>::up(row.p[label]) : NAN;
+    float m, s;
+    stream_stats<DT, kThreads>(row, tid, kLog2e, m, s);
+    join_stats<kWaves>(kLog2e, m, s, lds);
+    if (tid == 0) {
+        a.logp[r * a.T + t] = logp_of(xy, m, kLog2e, s);
+        a.stats[r * a.T + t] = make_float2(m, s);
+    }
+}
+
+// One workgroup a pair: the two implicit rewards, the loss and both c.
+__global__ __launch_bounds__(256) void pref_pair(PrefArgs a) {
+    __shared__ double lds[2][4];
+    __shared__ int cnt[2][4];
+    const int64_t p = a.first + blockIdx.x;
+    double sum[2];
+    int n[2];
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+        const int64_t r = side ? a.P + p : p;
+        sum[side] = 0.0;
+        n[side] = 0;
+        for (int64_t t = threadIdx.x; t < a.T; t += 256) {
+            if (a.labels[r * a.label_pitch + t] == a.ignore) continue;
+            sum[side] += (double)a.logp[r * a.T + t] - (a.ref_logp ? (double)a.ref_logp[r * a.T + t] : 0.0);
+            ++n[side];
+        }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+            sum[side] += __shfl_xor(sum[side], o);
+            n[side] += __shfl_xor(n[side], o);
+        }
+        if ((threadIdx.x & 63) == 0) {
+            lds[side][threadIdx.x >> 6] = sum[side];
+            cnt[side][threadIdx.x >> 6] = n[side];
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x) return;
+    double share[2];
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+        double s = 0.0;
+        int k = 0;
+        for (int w = 0; w < 4; ++w) {
+            s += lds[side][w];
+            k += cnt[side][w];
+        }
+        share[side] = a.average ? 1.0 / (k > 0 ? k : 1) : 1.0;
+        sum[side] = (double)a.beta * s * share[side];
+        a.rewards[side ? a.P + p : p] = (float)sum[side];
+    }
+    const double h = sum[0] - sum[1], eps = a.smoothing;
+    const double low = log1p(exp(-fabs(h)));  // -log sigmoid(|h|)
+    a.pair_loss[p] = (float)((1.0 - eps) * (low + fmax(-h, 0.0)) + eps * (low + fmax(h, 0.0)));
+    // sigmoid(h) - (1 - eps) = eps sigmoid(h) - (1 - eps) sigmoid(-h)
+    const double z = exp(-fabs(h)), big = 1.0 / (1.0 + z), small = z / (1.0 + z);
+    const double up = h >= 0.0 ? big : small, down = h >= 0.0 ? small : big;
+    const double slope = (double)a.beta * (eps * up - (1.0 - eps) * down) / (double)a.P * (double)a.scale;
+    a.coef[p] = (float)(slope * share[0]);
+    a.coef[a.P + p] = (float)(-slope * share[1]);
+}
+
+template <int DT, int kThreads>
+__global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void pref_gradient(PrefArgs a) {
+    typedef typename Elem<DT>::T T;
+    const int tid = threadIdx.x % kThreads;
+    const int64_t i = (int64_t)blockIdx.x * (blockDim.x / kThreads) + threadIdx.x / kThreads;
+    if (i >= 2 * a.pairs * a.T) return;
+    const int64_t local = i / a.T, t = i - local * a.T, r = pref_sequence(a, local);
+    const int64_t label = a.labels[r * a.label_pitch + t];
+    T* out = static_cast<T*>(a.grad) + r * a.grad_seq + t * a.grad_tok;
+    if (label == a.ignore) {
+        zero_row<DT>(out, a.V, tid, kThreads);
+        return;
+    }
+    const Row<DT> row(static_cast<const T*>(a.logits) + r * a.seq + t * a.tok, a.V);
+    const float2 st = a.stats[r * a.T + t];
+    const float c = a.coef[r];
+    const int y = (uint64_t)label < (uint64_t)a.V ? (int)label : -1;
+    stream_gradient<DT>(row, out, tid, kThreads, st.x == -INFINITY ? 0.0f : st.x, kLog2e, -c / st.y, c, y);
+}
+
+__global__ __launch_bounds__(1024) void pref_mean(const float* pair_loss, int64_t P, float* loss) {
+    __shared__ double lds[16];
+    double v = 0.0;
+    for (int64_t i = threadIdx.x; i < P; i += 1024) v += pair_loss[i];
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double t = 0.0;
+        for (int w = 0; w < 16; ++w) t += lds[w];
+        loss[0] = P > 0 ? (float)(t / (double)P) : 0.0f;
+    }
+}
+
+// -- host -----------------------------------------------------------------------
+
+constexpr int64_t kMostRows = 0xffffffffll / 1024;
+
+gmc_status logits_check(const char* me, int32_t dtype, int64_t R, int64_t T, int64_t V, const void* logits,
+                        int64_t seq, int64_t tok, const void* grad, int64_t grad_seq, int64_t grad_tok,
+                        const void* labels, int64_t label_pitch) {
+    if (!known_type(dtype)) return op_error(GMC_EINVAL, me, "unknown element type");
+    if (R < 0 || T < 0 || V < 1 || V > 0x3fffffff)
+        return op_error(GMC_EINVAL, me, "need R >= 0, T >= 0 and 1 <= V < 2^30");
+    if (R == 0 || T == 0) return GMC_OK;
+    if (R > kMostRows / T) return op_error(GMC_EINVAL, me, "more than 2^22 - 1 tokens");
+    if (!logits || !labels) return op_error(GMC_EINVAL, me, "NULL argument");
+    const auto fits = [&](int64_t s, int64_t k) {
+        constexpr int64_t kMost = int64_t(1) << 50;
+        if (T > 1 && (k < V || k > kMost / T)) return false;
+        return R == 1 || (s >= (T - 1) * (T > 1 ? k : 0) + V && s <= kMost / R);
+    };
+    if (!fits(seq, tok) || (grad && !fits(grad_seq, grad_tok)))
+        return op_error(GMC_EINVAL, me, "a pitch is shorter than what it steps over");
+    if (R > 1 && (label_pitch < T || label_pitch > (int64_t(1) << 50) / R))
+        return op_error(GMC_EINVAL, me, "the label pitch is shorter than a row");
+    if (grad) {
+        const int64_t b = type_size(dtype);
+        const auto span = [&](int64_t s, int64_t k) {
+            return ((R - 1) * (R > 1 ? s : 0) + (T - 1) * (T > 1 ? k : 0) + V) * b;
+        };
+        const bool same = logits == grad && (R == 1 || seq == grad_seq) && (T == 1 || tok == grad_tok);
+        if (!same && overlap(logits, span(seq, tok), grad, span(grad_seq, grad_tok)))
+            return op_error(GMC_EINVAL, me, "the gradient overlaps the logits without being them");
+    }
+    return GMC_OK;
+}
+
+}  // namespace
+
+}  // namespace gmc
+
+using namespace gmc;
+
+extern "C" {
+
+int64_t gmc_policy_loss_workspace(int64_t R, int64_t T) {
+    if (R < 0 || T < 0 || (T > 0 && R > kMostRows / T)) return -1;
+    return R * T * (int64_t)sizeof(float4) + (1 + R) * (int64_t)sizeof(float);
+}
+
+gmc_status gmc_policy_loss(void* hip_stream, int32_t dtype, int64_t R, int64_t T, int64_t V, const void* logits_dev,
+                           int64_t seq_pitch, int64_t tok_pitch, const int64_t* labels_dev, int64_t label_pitch,
+                           int64_t ignore, const float* old_logp_dev, const float* ref_logp_dev, const float* adv_dev,
+                           int64_t adv_seq, int64_t adv_tok, double clip_lo, double clip_hi, double kl_coef,
+                           double temperature, int32_t by_sequence, double grad_scale, float* stats_dev,
+                           float* logp_dev, void* grad_dev, int64_t grad_seq, int64_t grad_tok, void* workspace_dev,
+                           int64_t workspace_bytes) {
+    const char* me = "gmc_policy_loss";
+    const gmc_status ok = logits_check(me, dtype, R, T, V, logits_dev, seq_pitch, tok_pitch, grad_dev, grad_seq,
+                                       grad_tok, labels_dev, label_pitch);
+    if (ok != GMC_OK) return ok;
+    if (!(clip_lo >= 0.0 && clip_lo <= 1.0 && clip_hi >= 0.0 && isfinite(clip_hi)))
+        return op_error(GMC_EINVAL, me, "need 0 <= clip_lo <= 1 and 0 <= clip_hi");
+    if (!isfinite(kl_coef) || !isfinite(grad_scale)) return op_error(GMC_EINVAL, me, "kl_coef and grad_scale must be finite");
+    if (!(temperature > 0.0 && isfinite(temperature))) return op_error(GMC_EINVAL, me, "temperature must be > 0 and finite");
+    if (!stats_dev) return op_error(GMC_EINVAL, me, "NULL argument");
+    if (workspace_bytes < gmc_policy_loss_workspace(R, T) || !workspace_dev)
+        return op_error(GMC_EINVAL, me, "the workspace is too small");
+    if (reinterpret_cast<uintptr_t>(workspace_dev) & 15u)
+        return op_error(GMC_EINVAL, me, "the workspace is not 16-byte aligned");
+    hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+    PolicyArgs a{};
+    a.rows = R * T;
+    a.tokens = static_cast<float4*>(workspace_dev);
+    if (a.rows) {
+        if (!adv_dev || !logp_dev) return op_error(GMC_EINVAL, me, "NULL argument");
+        float* weight = reinterpret_cast<float*>(a.tokens + a.rows);
+        a.logits = logits_dev;
+        a.grad = grad_dev;
+        a.seq = seq_pitch;
+        a.tok = tok_pitch;
+        a.grad_seq = grad_seq;
+        a.grad_tok = grad_tok;
+        a.labels = labels_dev;
+        a.label_pitch = label_pitch;
+        a.ignore = ignore;
+        a.old_logp = old_logp_dev;
+        a.ref_logp = ref_logp_dev;
+        a.adv = adv_dev;
+        a.adv_seq = adv_seq;
+        a.adv_tok = adv_tok;
+        a.R = R;
+        a.T = T;
+        a.V = (int32_t)V;
+        a.lo = (float)clip_lo;
+        a.hi = (float)clip_hi;
+        a.kl = (float)kl_coef;
+        a.L = (float)(1.4426950408889634 / temperature);
+        a.inv_tau = (float)(1.0 / temperature);
+        a.scale = (float)grad_scale;
+        a.by_sequence = by_sequence != 0;
+        a.logp = logp_dev;
+        a.weight = weight;
+        policy_counts<<<dim3((unsigned)((R + 3) / 4)), 256, 0, st>>>(a, weight);
+        policy_weight<<<1, 1024, 0, st>>>(a, weight);
+        const int64_t vecs = V * type_size(dtype) / 16;  // at most, whatever the alignment
+        const dim3 rows((unsigned)a.rows), quads((unsigned)((a.rows + 3) / 4));
+        GMC_BY_TYPE(dtype, {
+            if (vecs <= 64 * kHeldVecs) policy_held<DT, 64, kHeldVecs><<<quads, 256, 0, st>>>(a);
+            else if (vecs <= 256 * kHeldVecs) policy_held<DT, 256, kHeldVecs><<<rows, 256, 0, st>>>(a);
+            else if (vecs <= 1024 * kHeldVecs) policy_held<DT, 1024, kHeldVecs><<<rows, 1024, 0, st>>>(a);
+            else if (vecs <= 1024 * kHeldVecsLong) policy_held<DT, 1024, kHeldVecsLong><<<rows, 1024, 0, st>>>(a);
+            else policy_long<DT><<<rows, kRowThreads, 0, st>>>(a);
+        });
+    }
+    policy_finish<<<1, 1024, 0, st>>>(a.tokens, a.rows, stats_dev);
+    return op_launched(me);
+}
+
+int64_t gmc_preference_loss_workspace(int64_t P, int64_t T) {
+    if (P < 0 || T < 0 || (T > 0 && P > kMostRows / 2 / T)) return -1;
+    return 2 * P * T * (int64_t)sizeof(float2) + 2 * P * (int64_t)sizeof(float);
+}
+
+gmc_status gmc_preference_loss(void* hip_stream, int32_t dtype, int64_t P, int64_t T, int64_t V,
+                               const void* logits_dev, int64_t seq_pitch, int64_t tok_pitch, const int64_t* labels_dev,
+                               int64_t label_pitch, int64_t ignore, const float* ref_logp_dev, double beta,
+                               double smoothing, int32_t average, double grad_scale, float* loss_dev,
+                               float* pair_loss_dev, float* rewards_dev, float* logp_dev, void* grad_dev,
+                               int64_t grad_seq, int64_t grad_tok, void* workspace_dev, int64_t workspace_bytes) {
+    const char* me = "gmc_preference_loss";
+    if (P < 0 || P > kMostRows / 2) return op_error(GMC_EINVAL, me, "need 0 <= P < 2^21");
+    const gmc_status ok = logits_check(me, dtype, 2 * P, T, V, logits_dev, seq_pitch, tok_pitch, grad_dev, grad_seq,
+                                       grad_tok, labels_dev, label_pitch);
+    if (ok != GMC_OK) return ok;
+    if (!isfinite(beta) || !isfinite(grad_scale)) return op_error(GMC_EINVAL, me, "beta and grad_scale must be finite");
+    if (!(smoothing >= 0.0 && smoothing <= 1.0)) return op_error(GMC_EINVAL, me, "smoothing must be in [0, 1]");
+    if (!loss_dev) return op_error(GMC_EINVAL, me, "NULL argument");
+    hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+    if (P > 0) {
+        if (!pair_loss_dev || !rewards_dev || (T > 0 && !logp_dev)) return op_error(GMC_EINVAL, me, "NULL argument");
+        if (!workspace_dev || workspace_bytes < gmc_preference_loss_workspace(P, T))
+            return op_error(GMC_EINVAL, me, "the workspace is too small");
+        if (reinterpret_cast<uintptr_t>(workspace_dev) & 7u)
+            return op_error(GMC_EINVAL, me, "the workspace is not 8-byte aligned");
+        PrefArgs a{};
+        a.logits = logits_dev;
+        a.grad = grad_dev;
+        a.seq = seq_pitch;
+        a.tok = tok_pitch;
+        a.grad_seq = grad_seq;
+        a.grad_tok = grad_tok;
+        a.labels = labels_dev;
+        a.label_pitch = label_pitch;
+        a.ignore = ignore;
+        a.ref_logp = ref_logp_dev;
+        a.P = P;
+        a.T = T;
+        a.first = 0;
+        a.pairs = P;
+        a.V = (int32_t)V;
+        a.beta = (float)beta;
+        a.smoothing = (float)smoothing;
+        a.scale = (float)grad_scale;
+        a.average = average != 0;
+        a.logp = logp_dev;
+        a.rewards = rewards_dev;
+        a.pair_loss = pair_loss_dev;
+        a.stats = static_cast<float2*>(workspace_dev);
+        a.coef = reinterpret_cast<float*>(a.stats + 2 * P * T);
+        const int64_t tokens = 2 * P * T, vecs = V * type_size(dtype) / 16;
+        const dim3 rows((unsigned)tokens), quads((unsigned)((tokens + 3) / 4));
+        GMC_BY_TYPE(dtype, {
+            if (tokens) {
+                if (vecs <= 64 * kHeldVecs) pref_logp<DT, 64><<<quads, 256, 0, st>>>(a);
+                else pref_logp<DT, kStatThreads><<<rows, kStatThreads, 0, st>>>(a);
+            }
+            pref_pair<<<dim3((unsigned)P), 256, 0, st>>>(a);
+            if (tokens && a.grad) {
+                if (vecs <= 64 * kHeldVecs) pref_gradient<DT, 64><<<quads, 256, 0, st>>>(a);
+                else pref_gradient<DT, kStatThreads><<<rows, kStatThreads, 0, st>>>(a);
+            }
+        });
+    }
+    pref_mean<<<1, 1024, 0, st>>>(pair_loss_dev, P, loss_dev);
+    return op_launched(me);
+}
+
+}  // extern "C"

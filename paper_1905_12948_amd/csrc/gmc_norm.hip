@@ -1,0 +1,889 @@
+// Group norm with its activation over channels-last images, forward and
+// backward (gmc_group_norm and gmc_group_norm_backward in include/gmc.h).
+//
+//   hat = (x - mean) rstd,  z = hat gamma + beta,  y = act(z)
+//   dz = dy act'(z),  dgamma = sum dz hat,  dbeta = sum dz  (images, pixels)
+//   dx = rstd (gamma dz - (s1 + hat s2) / m),  s1 = sum gamma dz,
+//   s2 = sum gamma dz hat over the m values of an image's group
+//
+// A thread owns 16 bytes of neighbouring channels and walks over pixels, so
+// that a wavefront reads whole lines of the channels-last layout; sums are
+// taken per channel and then folded into groups, so groups may have any width.
+//
+// Held form: one workgroup has all pixels of a block of whole groups in its
+// registers: x (and dy) are read once and the result is written once, which is
+// the floor of the bytes; the variance is the second pass over the registers,
+// about the mean.  Split form, for images whose groups do not fit: per-channel
+// moments of pieces of the image, joined about the common mean, and a second
+// launch that reads the images again.  z is formed in the order written, one
+// rounding each, in both directions: a sign of z that decides the gradient is
+// the sign the forward pass saw.  All sums are 32-bit, in a fixed order.
+#include <math.h>
+
+#include "gmc_ops.h"
+
+namespace gmc {
+
+namespace {
+
+constexpr int kHeldThreads = 1024;
+constexpr int kHeldMost = 16;      // vectors of x a thread holds (16 bytes each)
+constexpr int kHeldMostBack = 8;   // ... of x and of dy
+constexpr int kHeldChannels = 256; // threads across channels, at most
+constexpr int kSplitThreads = 256;
+constexpr int kSplitTile = 8;      // pixels a thread joins at once
+
+struct NormArgs {
+    const void* x;
+    const void* dy;
+    void* out;  // y, or dx
+    int64_t x_image, x_pixel, dy_image, dy_pixel, out_image, out_pixel;
+    const float* gamma;  // NULL: ones
+    const float* beta;   // NULL: zeros
+    float* mean;         // [N][G]: written forward, read backward
+    float* rstd;
+    float* part;         // scratch
+    float* part2;
+    int64_t N;
+    int32_t S, C, G, cpg;
+    int32_t gw, cb, blocks;  // held: groups and channels per workgroup, workgroups per image
+    int32_t tc, tp_log2;     // threads across channels, and the power of two above
+    int32_t chunk, chunks;   // split: pixels per workgroup, workgroups per image
+    int32_t cblocks;         // split: workgroups across channels
+    float eps;
+    int32_t act;
+};
+
+__device__ __forceinline__ float activate(float z, int act) {
+    if (act == GMC_ACT_RELU) return z > 0.0f ? z : (z != z ? z : 0.0f);
+    if (act == GMC_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.0f + exp2_fast(-kLog2e * z));
+    return z;
+}
+
+// dy act'(z)
+__device__ __forceinline__ float back_act(float dy, float z, int act) {
+    if (act == GMC_ACT_RELU) return z > 0.0f ? dy : 0.0f;
+    if (act == GMC_ACT_SILU) {
+        const float gate = __builtin_amdgcn_rcpf(1.0f + exp2_fast(-kLog2e * z));
+        return dy * (gate * (1.0f + z * (1.0f - gate)));
+    }
+    return dy;
+}
+
+// A workgroup's place in its block of channels.
+struct Place {
+    int cv, r, rows, waves;  // channel vector, pixel row, pixel rows, wavefronts
+    bool on;
+};
+
+__device__ __forceinline__ Place place(const NormArgs& a) {
+    Place p;
+    p.cv = threadIdx.x & ((1 << a.tp_log2) - 1);
+    p.r = threadIdx.x >> a.tp_log2;
+    p.rows = blockDim.x >> a.tp_log2;
+    p.waves = blockDim.x >> 6;
+    p.on = p.cv < a.tc;
+    return p;
+}
+
+// chan[c] = the sum over the workgroup's threads of v for channel c.  Lanes of
+// one channel vector are folded by shuffles, wavefronts (or, where a channel
+// block is wider than a wavefront, pixel rows) through LDS, in a fixed order.
+template <int VEC>
+__device__ __forceinline__ void channel_sums(float (&v)[VEC], const NormArgs& a, const Place& p, float* part,
+                                             float* chan) {
+    const int width = VEC << a.tp_log2;
+    int slots;
+    if (a.tp_log2 < 6) {
+        for (int o = 1 << a.tp_log2; o < 64; o <<= 1)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) v[i] += __shfl_xor(v[i], o);
+        slots = p.waves;
+        const int lane = threadIdx.x & 63;
+        if (lane < (1 << a.tp_log2))
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) part[(threadIdx.x >> 6) * width + lane * VEC + i] = v[i];
+    } else {
+        slots = p.rows;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) part[p.r * width + p.cv * VEC + i] = v[i];
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < a.tc * VEC; c += blockDim.x) {
+        float s = 0.0f;
+        for (int k = 0; k < slots; ++k) s += part[k * width + c];
+        chan[c] = s;
+    }
+    __syncthreads();
+}
+
+// grp[g] = the sum of chan over group g's channels, one wavefront a group.
+__device__ __forceinline__ void group_sums(const float* chan, const NormArgs& a, float* grp) {
+    for (int g = threadIdx.x >> 6; g < a.gw; g += blockDim.x >> 6) {
+        float s = 0.0f;
+        for (int c = threadIdx.x & 63; c < a.cpg; c += 64) s += chan[g * a.cpg + c];
+        s = wave_sum(s);
+        if ((threadIdx.x & 63) == 0) grp[g] = s;
+    }
+    __syncthreads();
+}
+
+template <int VEC>
+__device__ __forceinline__ void load_params(const NormArgs& a, int c0, bool on, float (&ga)[VEC], float (&be)[VEC]) {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+        ga[i] = on && a.gamma ? a.gamma[c0 + i] : 1.0f;
+        be[i] = on && a.beta ? a.beta[c0 + i] : 0.0f;
+    }
+}
+
+extern __shared__ float norm_lds[];
+
+template <int DT, int VEC, int KP>
+__global__ __launch_bounds__(kHeldThreads) void norm_forward_held(NormArgs a) {
+    typedef typename Elem<DT>::T T;
+    typedef Vec<DT, VEC> V;
+    const Place p = place(a);
+    float* part = norm_lds;
+    float* chan = part + (((a.tp_log2 < 6 ? p.waves : p.rows) * VEC) << a.tp_log2);
+    float* grp = chan + (VEC << a.tp_log2);
+    const int64_t n = blockIdx.x / (unsigned)a.blocks;
+    const int blk = (int)(blockIdx.x - n * a.blocks);
+    const int c0 = blk * a.cb + p.cv * VEC;
+    const T* px = static_cast<const T*>(a.x) + n * a.x_image + c0;
+    T* py = static_cast<T*>(a.out) + n * a.out_image + c0;
+    V xv[KP];
+#pragma unroll
+    for (int k = 0; k < KP; ++k) {
+        const int s = p.r + k * p.rows;
+        if (p.on && s < a.S) xv[k] = V::load(px + s * a.x_pixel);
+    }
+    float ga[VEC], be[VEC], mu[VEC], rs[VEC];
+    load_params<VEC>(a, c0, p.on, ga, be);
+    const float m = (float)((int64_t)a.S * a.cpg);
+    float sum[VEC], f[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) sum[i] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < KP; ++k)
+        if (p.on && p.r + k * p.rows < a.S) {
+            xv[k].unpack(f);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) sum[i] += f[i];
+        }
+    channel_sums<VEC>(sum, a, p, part, chan);
+    group_sums(chan, a, grp);
+    int gi[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+        gi[i] = p.on ? (p.cv * VEC + i) / a.cpg : 0;
+        mu[i] = grp[gi[i]] / m;
+        sum[i] = 0.0f;
+    }
+    __syncthreads();  // grp is read
+    for (int g = threadIdx.x; g < a.gw; g += blockDim.x) a.mean[n * a.G + blk * a.gw + g] = grp[g] / m;
+#pragma unroll
+    for (int k = 0; k < KP; ++k)
+        if (p.on && p.r + k * p.rows < a.S) {
+            xv[k].unpack(f);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const float d = f[i] - mu[i];
+                sum[i] = __builtin_fmaf(d, d, sum[i]);
+            }
+        }
+    channel_sums<VEC>(sum, a, p, part, chan);
+    group_sums(chan, a, grp);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) rs[i] = 1.0f / sqrtf(grp[gi[i]] / m + a.eps);
+    for (int g = threadIdx.x; g < a.gw; g += blockDim.x) a.rstd[n * a.G + blk * a.gw + g] = 1.0f / sqrtf(grp[g] / m + a.eps);
+#pragma unroll
+    for (int k = 0; k < KP; ++k) {
+        const int s = p.r + k * p.rows;
+        if (p.on && s < a.S) {
+            xv[k].unpack(f);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) f[i] = activate((f[i] - mu[i]) * rs[i] * ga[i] + be[i], a.act);
+            xv[k].pack(f);
+            xv[k].store(py + s * a.out_pixel);
+        }
+    }
+}
+
+// Mean and rstd of the thread's channels, from [N][G].
+template <int VEC>
+__device__ __forceinline__ void load_stats(const NormArgs& a, int64_t n, int c0, bool on, float (&mu)[VEC],
+                                           float (&rs)[VEC]) {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+        const int64_t at = n * a.G + (on ? (c0 + i) / a.cpg : 0);
+        mu[i] = a.mean[at];
+        rs[i] = a.rstd[at];
+    }
+}
+
+template <int DT, int VEC, int KP>
+__global__ __launch_bounds__(kHeldThreads) void norm_backward_held(NormArgs a) {
+    typedef typename Elem<DT>::T T;
+    typedef Vec<DT, VEC> V;
+    const Place p = place(a);
+    float* part = norm_lds;
+    float* chan = part + (((a.tp_log2 < 6 ? p.waves : p.rows) * VEC) << a.tp_log2);
+    float* grp1 = chan + (VEC << a.tp_log2);
+    float* grp2 = grp1 + a.gw;
+    const int64_t n = blockIdx.x / (unsigned)a.blocks;
+    const int blk = (int)(blockIdx.x - n * a.blocks);
+    const int c0 = blk * a.cb + p.cv * VEC;
+    const T* px = static_cast<const T*>(a.x) + n * a.x_image + c0;
+    const T* pd = static_cast<const T*>(a.dy) + n * a.dy_image + c0;
+    T* po = static_cast<T*>(a.out) + n * a.out_image + c0;
+    V xv[KP], dv[KP];
+#pragma unroll
+    for (int k = 0; k < KP; ++k) {
+        const int s = p.r + k * p.rows;
+        if (p.on && s < a.S) {
+            xv[k] = V::load(px + s * a.x_pixel);
+            dv[k] = V::load(pd + s * a.dy_pixel);
+        }
+    }
+    float ga[VEC], be[VEC], mu[VEC], rs[VEC], s1[VEC], s2[VEC];
+    load_params<VEC>(a, c0, p.on, ga, be);
+    load_stats<VEC>(a, n, c0, p.on, mu, rs);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) s1[i] = s2[i] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < KP; ++k)
+        if (p.on && p.r + k * p.rows < a.S) {
+            float f[VEC], d[VEC];
+            xv[k].unpack(f);
+            dv[k].unpack(d);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const float hat = (f[i] - mu[i]) * rs[i];
+                const float dz = back_act(d[i], hat * ga[i] + be[i], a.act);
+                s1[i] += dz;
+                s2[i] = __builtin_fmaf(dz, hat, s2[i]);
+            }
+        }
+    // per image: this workgroup's channels' sums, for dbeta and dgamma
+    channel_sums<VEC>(s1, a, p, part, chan);
+    for (int c = threadIdx.x; c < a.cb; c += blockDim.x) {
+        const float v = chan[c];
+        a.part[n * a.C + blk * a.cb + c] = v;
+        chan[c] = a.gamma ? v * a.gamma[blk * a.cb + c] : v;
+    }
+    __syncthreads();
+    group_sums(chan, a, grp1);
+    channel_sums<VEC>(s2, a, p, part, chan);
+    for (int c = threadIdx.x; c < a.cb; c += blockDim.x) {
+        const float v = chan[c];
+        a.part2[n * a.C + blk * a.cb + c] = v;
+        chan[c] = a.gamma ? v * a.gamma[blk * a.cb + c] : v;
+    }
+    __syncthreads();
+    group_sums(chan, a, grp2);
+    const float m = (float)((int64_t)a.S * a.cpg);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+        const int g = p.on ? (p.cv * VEC + i) / a.cpg : 0;
+        s1[i] = grp1[g] / m;
+        s2[i] = grp2[g] / m;
+    }
+#pragma unroll
+    for (int k = 0; k < KP; ++k) {
+        const int s = p.r + k * p.rows;
+        if (p.on && s < a.S) {
+            float f[VEC], d[VEC];
+            xv[k].unpack(f);
+            dv[k].unpack(d);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const float hat = (f[i] - mu[i]) * rs[i];
+                const float dz = back_act(d[i], hat * ga[i] + be[i], a.act);
+                f[i] = rs[i] * (dz * ga[i] - __builtin_fmaf(hat, s2[i], s1[i]));
+            }
+            xv[k].pack(f);
+            xv[k].store(po + s * a.out_pixel);
+        }
+    }
+}
+
+// -- split form ---------------------------------------------------------------
+
+// Workgroup (channel block, chunk, image) of the split kernels.
+struct Piece {
+    int64_t n;
+    int c0, first, last, chunk;
+};
+
+template <int VEC>
+__device__ __forceinline__ Piece piece(const NormArgs& a, Place& p) {
+    Piece q;
+    const unsigned per = (unsigned)(a.chunks * a.cblocks);
+    q.n = blockIdx.x / per;
+    const unsigned rest = blockIdx.x - (unsigned)q.n * per;
+    q.chunk = (int)(rest / (unsigned)a.cblocks);
+    const int cblk = (int)(rest - (unsigned)q.chunk * a.cblocks);
+    const int tv = cblk * a.tc + p.cv;
+    q.c0 = tv * VEC;
+    p.on = p.on && q.c0 < a.C;
+    q.first = q.chunk * a.chunk;
+    q.last = q.first + a.chunk < a.S ? q.first + a.chunk : a.S;
+    return q;
+}
+
+// Per (image, chunk, channel): the mean and the sum of squares about it.
+template <int DT, int VEC>
+__global__ __launch_bounds__(kSplitThreads) void norm_moments(NormArgs a) {
+    typedef typename Elem<DT>::T T;
+    typedef Vec<DT, VEC> V;
+    Place p = place(a);
+    const Piece q = piece<VEC>(a, p);
+    float* part = norm_lds;
+    float* chan = part + (((a.tp_log2 < 6 ? p.waves : p.rows) * VEC) << a.tp_log2);
+    const T* px = static_cast<const T*>(a.x) + q.n * a.x_image + q.c0;
+    float mean[VEC], sq[VEC], f[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) mean[i] = sq[i] = 0.0f;
+    float have = 0.0f;
+    for (int s0 = q.first + p.r; s0 < q.last && p.on; s0 += kSplitTile * p.rows) {
+        V xv[kSplitTile];
+        int cnt = 0;
+#pragma unroll
+        for (int k = 0; k < kSplitTile; ++k)
+            if (s0 + k * p.rows < q.last) {
+                xv[k] = V::load(px + (int64_t)(s0 + k * p.rows) * a.x_pixel);
+                ++cnt;
+            }
+        // the tile's own mean and squares about it, then joined with what is there
+        float tm[VEC], ts[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) tm[i] = ts[i] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < kSplitTile; ++k)
+            if (k < cnt) {
+                xv[k].unpack(f);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) tm[i] += f[i];
+            }
+        const float inv = 1.0f / (float)cnt, all = have + (float)cnt;
+        const float share = (float)cnt / all, cross = have * share;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) tm[i] *= inv;
+#pragma unroll
+        for (int k = 0; k < kSplitTile; ++k)
+            if (k < cnt) {
+                xv[k].unpack(f);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    const float d = f[i] - tm[i];
+                    ts[i] = __builtin_fmaf(d, d, ts[i]);
+                }
+            }
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            const float d = tm[i] - mean[i];
+            mean[i] = __builtin_fmaf(d, share, mean[i]);
+            sq[i] += ts[i] + d * d * cross;
+        }
+        have = all;
+    }
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) f[i] = have * mean[i];
+    channel_sums<VEC>(f, a, p, part, chan);
+    const float inv = 1.0f / (float)(q.last - q.first);
+    const int64_t at = (q.n * a.chunks + q.chunk) * a.C + (q.c0 - p.cv * VEC);
+    const int width = a.tc * VEC;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+        const float d = mean[i] - chan[p.on ? p.cv * VEC + i : 0] * inv;
+        f[i] = sq[i] + have * d * d;
+    }
+    for (int c = threadIdx.x; c < width; c += blockDim.x)
+        if (q.c0 - p.cv * VEC + c < a.C) a.part[at + c] = chan[c] * inv;
+    __syncthreads();
+    channel_sums<VEC>(f, a, p, part, chan);
+    for (int c = threadIdx.x; c < width; c += blockDim.x)
+        if (q.c0 - p.cv * VEC + c < a.C) a.part2[at + c] = chan[c];
+}
+
+__device__ __forceinline__ float block_sum(float v, float* lds) {
+    v = wave_sum(v);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    float s = 0.0f;
+    for (int w = 0; w < (int)(blockDim.x >> 6); ++w) s += lds[w];
+    __syncthreads();
+    return s;
+}
+
+// One workgroup per (image, group): joins the chunks' channel moments.
+__global__ __launch_bounds__(kSplitThreads) void norm_join(NormArgs a) {
+    __shared__ float lds[kSplitThreads / 64];
+    const int64_t n = blockIdx.x / (unsigned)a.G;
+    const int g = (int)(blockIdx.x - n * a.G);
+    const int total = a.chunks * a.cpg;
+    const float* mean = a.part + n * a.chunks * a.C + (int64_t)g * a.cpg;
+    const float* sq = a.part2 + n * a.chunks * a.C + (int64_t)g * a.cpg;
+    const float m = (float)((int64_t)a.S * a.cpg);
+    const int short_one = a.S - (a.chunks - 1) * a.chunk;
+    float s = 0.0f;
+    for (int e = threadIdx.x; e < total; e += blockDim.x) {
+        const int k = e / a.cpg, c = e - k * a.cpg;
+        s += (float)(k == a.chunks - 1 ? short_one : a.chunk) * mean[(int64_t)k * a.C + c];
+    }
+    const float mu = block_sum(s, lds) / m;
+    s = 0.0f;
+    for (int e = threadIdx.x; e < total; e += blockDim.x) {
+        const int k = e / a.cpg, c = e - k * a.cpg;
+        const float d = mean[(int64_t)k * a.C + c] - mu;
+        s += sq[(int64_t)k * a.C + c] + (float)(k == a.chunks - 1 ? short_one : a.chunk) * d * d;
+    }
+    const float var = block_sum(s, lds) / m;
+    if (threadIdx.x == 0) {
+        a.mean[n * a.G + g] = mu;
+        a.rstd[n * a.G + g] = 1.0f / sqrtf(var + a.eps);
+    }
+}
+
+template <int DT, int VEC>
+__global__ __launch_bounds__(kSplitThreads) void norm_forward_split(NormArgs a) {
+    typedef typename Elem<DT>::T T;
+    typedef Vec<DT, VEC> V;
+    Place p = place(a);
+    const Piece q = piece<VEC>(a, p);
+    if (!p.on) return;
+    const T* px = static_cast<const T*>(a.x) + q.n * a.x_image + q.c0;
+    T* py = static_cast<T*>(a.out) + q.n * a.out_image + q.c0;
+    float ga[VEC], be[VEC], mu[VEC], rs[VEC], f[VEC];
+    load_params<VEC>(a, q.c0, true, ga, be);
+    load_stats<VEC>(a, q.n, q.c0, true, mu, rs);
+    for (int s0 = q.first + p.r; s0 < q.last; s0 += 4 * p.rows) {
+        V xv[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (s0 + k * p.rows < q.last) xv[k] = V::load(px + (int64_t)(s0 + k * p.rows) * a.x_pixel);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (s0 + k * p.rows < q.last) {
+                xv[k].unpack(f);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) f[i] = activate((f[i] - mu[i]) * rs[i] * ga[i] + be[i], a.act);
+                xv[k].pack(f);
+                xv[k].store(py + (int64_t)(s0 + k * p.rows) * a.out_pixel);
+            }
+    }
+}
+
+// Per (image, chunk, channel): the sums of dz and of dz hat.
+template <int DT, int VEC>
+__global__ __launch_bounds__(kSplitThreads) void norm_back_sums(NormArgs a) {
+    typedef typename Elem<DT>::T T;
+    typedef Vec<DT, VEC> V;
+    Place p = place(a);
+    const Piece q = piece<VEC>(a, p);
+    float* part = norm_lds;
+    float* chan = part + (((a.tp_log2 < 6 ? p.waves : p.rows) * VEC) << a.tp_log2);
+    const T* px = static_cast<const T*>(a.x) + q.n * a.x_image + q.c0;
+    const T* pd = static_cast<const T*>(a.dy) + q.n * a.dy_image + q.c0;
+    float ga[VEC], be[VEC], mu[VEC], rs[VEC], s1[VEC], s2[VEC];
+    load_params<VEC>(a, q.c0, p.on, ga, be);
+    load_stats<VEC>(a, q.n, q.c0, p.on, mu, rs);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) s1[i] = s2[i] = 0.0f;
+    for (int s0 = q.first + p.r; s0 < q.last && p.on; s0 += 4 * p.rows) {
+        V xv[4], dv[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (s0 + k * p.rows < q.last) {
+                xv[k] = V::load(px + (int64_t)(s0 + k * p.rows) * a.x_pixel);
+                dv[k] = V::load(pd + (int64_t)(s0 + k * p.rows) * a.dy_pixel);
+            }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (s0 + k * p.rows < q.last) {
+                float f[VEC], d[VEC];
+                xv[k].unpack(f);
+                dv[k].unpack(d);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    const float hat = (f[i] - mu[i]) * rs[i];
+                    const float dz = back_act(d[i], hat * ga[i] + be[i], a.act);
+                    s1[i] += dz;
+                    s2[i] = __builtin_fmaf(dz, hat, s2[i]);
+                }
+            }
+    }
+    const int64_t at = (q.n * a.chunks + q.chunk) * a.C + (q.c0 - p.cv * VEC);
+    const int width = a.tc * VEC;
+    channel_sums<VEC>(s1, a, p, part, chan);
+    for (int c = threadIdx.x; c < width; c += blockDim.x)
+        if (q.c0 - p.cv * VEC + c < a.C) a.part[at + c] = chan[c];
+    __syncthreads();
+    channel_sums<VEC>(s2, a, p, part, chan);
+    for (int c = threadIdx.x; c < width; c += blockDim.x)
+        if (q.c0 - p.cv * VEC + c < a.C) a.part2[at + c] = chan[c];
+}
+
+// One workgroup per (image, group): s1 / m and s2 / m, after the two sums of
+// the chunks in a.part and a.part2 (N chunks C values each).
+__global__ __launch_bounds__(kSplitThreads) void norm_back_join(NormArgs a, float* shared_terms) {
+    __shared__ float lds[kSplitThreads / 64];
+    const int64_t n = blockIdx.x / (unsigned)a.G;
+    const int g = (int)(blockIdx.x - n * a.G);
+    const int total = a.chunks * a.cpg;
+    const int64_t base = n * a.chunks * a.C + (int64_t)g * a.cpg;
+    const float m = (float)((int64_t)a.S * a.cpg);
+    float s1 = 0.0f, s2 = 0.0f;
+    for (int e = threadIdx.x; e < total; e += blockDim.x) {
+        const int k = e / a.cpg, c = e - k * a.cpg;
+        const float w = a.gamma ? a.gamma[g * a.cpg + c] : 1.0f;
+        s1 += w * a.part[base + (int64_t)k * a.C + c];
+        s2 += w * a.part2[base + (int64_t)k * a.C + c];
+    }
+    s1 = block_sum(s1, lds);
+    s2 = block_sum(s2, lds);
+    if (threadIdx.x == 0) {
+        shared_terms[2 * (n * a.G + g)] = s1 / m;
+        shared_terms[2 * (n * a.G + g) + 1] = s2 / m;
+    }
+}
+
+template <int DT, int VEC>
+__global__ __launch_bounds__(kSplitThreads) void norm_backward_split(NormArgs a, const float* shared_terms) {
+    typedef typename Elem<DT>::T T;
+    typedef Vec<DT, VEC> V;
+    Place p = place(a);
+    const Piece q = piece<VEC>(a, p);
+    if (!p.on) return;
+    const T* px = static_cast<const T*>(a.x) + q.n * a.x_image + q.c0;
+    const T* pd = static_cast<const T*>(a.dy) + q.n * a.dy_image + q.c0;
+    T* po = static_cast<T*>(a.out) + q.n * a.out_image + q.c0;
+    float ga[VEC], be[VEC], mu[VEC], rs[VEC], s1[VEC], s2[VEC];
+    load_params<VEC>(a, q.c0, true, ga, be);
+    load_stats<VEC>(a, q.n, q.c0, true, mu, rs);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+        const int64_t at = 2 * (q.n * a.G + (q.c0 + i) / a.cpg);
+        s1[i] = shared_terms[at];
+        s2[i] = shared_terms[at + 1];
+    }
+    for (int s0 = q.first + p.r; s0 < q.last; s0 += 4 * p.rows) {
+        V xv[4], dv[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (s0 + k * p.rows < q.last) {
+                xv[k] = V::load(px + (int64_t)(s0 + k * p.rows) * a.x_pixel);
+                dv[k] = V::load(pd + (int64_t)(s0 + k * p.rows) * a.dy_pixel);
+            }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (s0 + k * p.rows < q.last) {
+                float f[VEC], d[VEC];
+                xv[k].unpack(f);
+                dv[k].unpack(d);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    const float hat = (f[i] - mu[i]) * rs[i];
+                    const float dz = back_act(d[i], hat * ga[i] + be[i], a.act);
+                    f[i] = rs[i] * (dz * ga[i] - __builtin_fmaf(hat, s2[i], s1[i]));
+                }
+                xv[k].pack(f);
+                xv[k].store(po + (int64_t)(s0 + k * p.rows) * a.out_pixel);
+            }
+    }
+}
+
+// dgamma and dbeta: the sums of `rows` rows of C partial values each.  16
+// channels and 16 row slots a workgroup.
+constexpr int kParamCh = 16;
+__global__ __launch_bounds__(kSplitThreads) void norm_params(const float* part, const float* part2, int64_t rows,
+                                                             int32_t C, float* dgamma, float* dbeta) {
+    __shared__ float lds[2][kSplitThreads];
+    const int c = blockIdx.x * kParamCh + (threadIdx.x & (kParamCh - 1));
+    float s1 = 0.0f, s2 = 0.0f;
+    if (c < C)
+        for (int64_t r = threadIdx.x / kParamCh; r < rows; r += kSplitThreads / kParamCh) {
+            s1 += part[r * C + c];
+            s2 += part2[r * C + c];
+        }
+    lds[0][threadIdx.x] = s1;
+    lds[1][threadIdx.x] = s2;
+    __syncthreads();
+    for (int h = kSplitThreads / 2; h >= kParamCh; h >>= 1) {
+        if (threadIdx.x < h) {
+            lds[0][threadIdx.x] += lds[0][threadIdx.x + h];
+            lds[1][threadIdx.x] += lds[1][threadIdx.x + h];
+        }
+        __syncthreads();
+    }
+    if (threadIdx.x < kParamCh && c < C) {
+        if (dbeta) dbeta[c] = lds[0][threadIdx.x];
+        if (dgamma) dgamma[c] = lds[1][threadIdx.x];
+    }
+}
+
+// -- host ---------------------------------------------------------------------
+
+int log2_up(int64_t n) {
+    int k = 0;
+    while ((int64_t(1) << k) < n) ++k;
+    return k;
+}
+
+struct NormPlan {
+    bool held = false;
+    int vec = 1;      // channels per thread
+    int threads = 0;  // held
+    int kp = 0;
+    size_t lds = 0;
+};
+
+// Chooses the form and fills the geometry of a.
+NormPlan norm_plan(NormArgs& a, int32_t dtype, bool backward) {
+    NormPlan pl;
+    const int full = (int)(16 / type_size(dtype));
+    const int most = backward ? kHeldMostBack : kHeldMost;
+    a.cpg = a.C / a.G;
+    // held: the fewest whole groups whose channels fill a 128-byte line (else a
+    // 64-byte half), with a thread count that leaves at most `most` vectors each
+    for (int line = 128; line >= 64 && !pl.held; line >>= 1)
+        for (int gw = 1; gw <= a.G && !pl.held; ++gw) {
+            if (a.G % gw) continue;
+            const int64_t cb = (int64_t)gw * a.cpg;
+            const bool wide = cb * type_size(dtype) >= line;
+            if (!wide && gw < a.G) continue;
+            const int vec = cb % full == 0 ? full : 1;
+            const int64_t tc = cb / vec;
+            if (tc > kHeldChannels) continue;
+            const int lg = log2_up(tc);
+            int threads = 256;
+            while (threads < kHeldThreads && (((int64_t)a.S << lg) + threads - 1) / threads > 4) threads *= 2;
+            const int rows = threads >> lg;
+            const int64_t kp = (a.S + rows - 1) / rows;
+            if (kp > most) continue;
+            pl.held = true;
+            pl.vec = vec;
+            pl.threads = threads;
+            pl.kp = kp <= 4 ? 4 : most;
+            a.gw = gw;
+            a.cb = (int32_t)cb;
+            a.blocks = a.G / gw;
+            a.tc = (int32_t)tc;
+            a.tp_log2 = lg;
+            const int slots = lg < 6 ? threads / 64 : rows;
+            pl.lds = sizeof(float) * (((size_t)(slots + 1) * vec << lg) + 2 * (size_t)gw);
+        }
+    if (pl.held) return pl;
+    pl.vec = a.C % full == 0 ? full : 1;
+    const int64_t vecs = a.C / pl.vec;
+    a.tc = (int32_t)(vecs < kSplitThreads ? vecs : kSplitThreads);
+    a.tp_log2 = log2_up(a.tc);
+    a.cblocks = (int32_t)((vecs + a.tc - 1) / a.tc);
+    const int rows = kSplitThreads >> a.tp_log2;
+    // pixels per workgroup: enough workgroups for every CU, a few tiles each
+    int64_t chunks = (a.S + (int64_t)rows * kSplitTile - 1) / ((int64_t)rows * kSplitTile);
+    const int64_t want = (4096 + a.N * a.cblocks - 1) / (a.N * a.cblocks);
+    if (chunks > want) chunks = want;
+    a.chunk = (int32_t)((a.S + chunks - 1) / chunks);
+    a.chunks = (a.S + a.chunk - 1) / a.chunk;
+    const int slots = a.tp_log2 < 6 ? kSplitThreads / 64 : rows;
+    pl.threads = kSplitThreads;
+    pl.lds = sizeof(float) * ((size_t)(slots + 1) * pl.vec << a.tp_log2);
+    return pl;
+}
+
+// Scratch in floats: two arrays of per-channel partial values, and for the
+// split backward pass the two shared terms of every group.
+int64_t norm_scratch(const NormArgs& a, const NormPlan& pl, bool backward) {
+    if (pl.held) return backward ? 2 * a.N * a.C : 0;
+    return 2 * a.N * a.chunks * a.C + (backward ? 2 * a.N * a.G : 0);
+}
+
+gmc_status norm_check(const char* me, int32_t dtype, int64_t N, int64_t S, int32_t C, int32_t G, int32_t act) {
+    if (!known_type(dtype)) return op_error(GMC_EINVAL, me, "unknown element type");
+    if (N < 0 || S < 1 || S > 0x7fffffff || C < 1) return op_error(GMC_EINVAL, me, "need N >= 0, 1 <= S < 2^31, C >= 1");
+    if (G < 1 || C % G) return op_error(GMC_EINVAL, me, "C must be a multiple of G >= 1");
+    if (act < GMC_ACT_NONE || act > GMC_ACT_SILU) return op_error(GMC_EINVAL, me, "unknown activation");
+    if ((int64_t)C * S > (int64_t(1) << 40) || N > (int64_t(1) << 40) / ((int64_t)C * S))
+        return op_error(GMC_EINVAL, me, "more than 2^40 elements");
+    return GMC_OK;
+}
+
+bool image_pitch_ok(int64_t N, int64_t S, int64_t C, int64_t image, int64_t pixel) {
+    constexpr int64_t kMost = int64_t(1) << 40;
+    if (pixel < C || pixel > kMost / S) return false;
+    return N <= 1 || (image >= (S - 1) * pixel + C && image <= kMost / N);
+}
+
+int64_t image_span(int64_t N, int64_t S, int64_t C, int64_t image, int64_t pixel, int64_t b) {
+    return ((N - 1) * (N > 1 ? image : 0) + (S - 1) * pixel + C) * b;
+}
+
+}  // namespace
+
+}  // namespace gmc
+
+using namespace gmc;
+
+#define GMC_NORM_VEC(full, ...)                                       \
+    do {                                                              \
+        if (pl.vec == (full)) {                                       \
+            constexpr int VEC = (full);                               \
+            __VA_ARGS__;                                              \
+        } else {                                                      \
+            constexpr int VEC = 1;                                    \
+            __VA_ARGS__;                                              \
+        }                                                             \
+    } while (0)
+
+extern "C" {
+
+int64_t gmc_group_norm_workspace(int32_t dtype, int64_t N, int64_t S, int32_t C, int32_t G, int32_t backward) {
+    if (norm_check("gmc_group_norm_workspace", dtype, N, S, C, G, GMC_ACT_NONE) != GMC_OK) return -1;
+    if (N == 0) return 0;
+    NormArgs a{};
+    a.N = N;
+    a.S = (int32_t)S;
+    a.C = C;
+    a.G = G;
+    const NormPlan pl = norm_plan(a, dtype, backward != 0);
+    return (int64_t)sizeof(float) * norm_scratch(a, pl, backward != 0);
+}
+
+gmc_status gmc_group_norm(void* hip_stream, int32_t dtype, int64_t N, int64_t S, int32_t C, int32_t G,
+                          const void* x_dev, int64_t x_image, int64_t x_pixel, const float* gamma_dev,
+                          const float* beta_dev, double eps, int32_t act, void* y_dev, int64_t y_image,
+                          int64_t y_pixel, float* mean_dev, float* rstd_dev, void* workspace_dev,
+                          int64_t workspace_bytes) {
+    const char* me = "gmc_group_norm";
+    gmc_status ok = norm_check(me, dtype, N, S, C, G, act);
+    if (ok != GMC_OK) return ok;
+    if (!(eps >= 0.0 && eps <= 1.0)) return op_error(GMC_EINVAL, me, "eps must be in [0, 1]");
+    if (N == 0) return GMC_OK;
+    if (!x_dev || !y_dev || !mean_dev || !rstd_dev) return op_error(GMC_EINVAL, me, "NULL argument");
+    if (!image_pitch_ok(N, S, C, x_image, x_pixel) || !image_pitch_ok(N, S, C, y_image, y_pixel))
+        return op_error(GMC_EINVAL, me, "a pitch is shorter than what it steps over");
+    const int64_t b = type_size(dtype);
+    if (overlap(x_dev, image_span(N, S, C, x_image, x_pixel, b), y_dev, image_span(N, S, C, y_image, y_pixel, b)) &&
+        !(x_dev == y_dev && x_pixel == y_pixel && (N == 1 || x_image == y_image)))
+        return op_error(GMC_EINVAL, me, "y overlaps x without being it");
+    NormArgs a{};
+    a.x = x_dev;
+    a.out = y_dev;
+    a.x_image = x_image;
+    a.x_pixel = x_pixel;
+    a.out_image = y_image;
+    a.out_pixel = y_pixel;
+    a.gamma = gamma_dev;
+    a.beta = beta_dev;
+    a.mean = mean_dev;
+    a.rstd = rstd_dev;
+    a.N = N;
+    a.S = (int32_t)S;
+    a.C = C;
+    a.G = G;
+    a.eps = (float)eps;
+    a.act = act;
+    const NormPlan pl = norm_plan(a, dtype, false);
+    const int64_t need = norm_scratch(a, pl, false);
+    if (need && (!workspace_dev || workspace_bytes < need * (int64_t)sizeof(float)))
+        return op_error(GMC_EINVAL, me, "the workspace is too small");
+    hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+    const int64_t blocks = pl.held ? N * a.blocks : N * a.chunks * a.cblocks;
+    if (blocks * pl.threads > 0xffffffffll || (!pl.held && N * G * kSplitThreads > 0xffffffffll))
+        return op_error(GMC_EINVAL, me, "too many images for one launch");
+    const dim3 grid((unsigned)blocks);
+    if (pl.held) {
+        GMC_BY_TYPE(dtype, GMC_NORM_VEC(16 / Elem<DT>::kSize, {
+                        if (pl.kp == 4) norm_forward_held<DT, VEC, 4><<<grid, pl.threads, pl.lds, st>>>(a);
+                        else norm_forward_held<DT, VEC, kHeldMost><<<grid, pl.threads, pl.lds, st>>>(a);
+                    }));
+    } else {
+        a.part = static_cast<float*>(workspace_dev);
+        a.part2 = a.part + N * a.chunks * (int64_t)C;
+        GMC_BY_TYPE(dtype, GMC_NORM_VEC(16 / Elem<DT>::kSize, {
+                        norm_moments<DT, VEC><<<grid, pl.threads, pl.lds, st>>>(a);
+                        norm_join<<<dim3((unsigned)(N * G)), kSplitThreads, 0, st>>>(a);
+                        norm_forward_split<DT, VEC><<<grid, pl.threads, 0, st>>>(a);
+                    }));
+    }
+    return op_launched(me);
+}
+
+gmc_status gmc_group_norm_backward(void* hip_stream, int32_t dtype, int64_t N, int64_t S, int32_t C, int32_t G,
+                                   const void* dy_dev, int64_t dy_image, int64_t dy_pixel, const void* x_dev,
+                                   int64_t x_image, int64_t x_pixel, const float* mean_dev, const float* rstd_dev,
+                                   const float* gamma_dev, const float* beta_dev, int32_t act, void* dx_dev,
+                                   int64_t dx_image, int64_t dx_pixel, float* dgamma_dev, float* dbeta_dev,
+                                   void* workspace_dev, int64_t workspace_bytes) {
+    const char* me = "gmc_group_norm_backward";
+    gmc_status ok = norm_check(me, dtype, N, S, C, G, act);
+    if (ok != GMC_OK) return ok;
+    hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+    const dim3 param_grid((unsigned)((C + kParamCh - 1) / kParamCh));
+    if (N == 0) {
+        if (dgamma_dev || dbeta_dev)
+            norm_params<<<param_grid, kSplitThreads, 0, st>>>(nullptr, nullptr, 0, C, dgamma_dev, dbeta_dev);
+        return op_launched(me);
+    }
+    if (!dy_dev || !x_dev || !dx_dev || !mean_dev || !rstd_dev) return op_error(GMC_EINVAL, me, "NULL argument");
+    if (!image_pitch_ok(N, S, C, x_image, x_pixel) || !image_pitch_ok(N, S, C, dy_image, dy_pixel) ||
+        !image_pitch_ok(N, S, C, dx_image, dx_pixel))
+        return op_error(GMC_EINVAL, me, "a pitch is shorter than what it steps over");
+    const int64_t b = type_size(dtype);
+    const int64_t out_span = image_span(N, S, C, dx_image, dx_pixel, b);
+    if ((overlap(x_dev, image_span(N, S, C, x_image, x_pixel, b), dx_dev, out_span) &&
+         !(x_dev == dx_dev && x_pixel == dx_pixel && (N == 1 || x_image == dx_image))) ||
+        (overlap(dy_dev, image_span(N, S, C, dy_image, dy_pixel, b), dx_dev, out_span) &&
+         !(dy_dev == dx_dev && dy_pixel == dx_pixel && (N == 1 || dy_image == dx_image))))
+        return op_error(GMC_EINVAL, me, "dx overlaps an input without being it");
+    NormArgs a{};
+    a.x = x_dev;
+    a.dy = dy_dev;
+    a.out = dx_dev;
+    a.x_image = x_image;
+    a.x_pixel = x_pixel;
+    a.dy_image = dy_image;
+    a.dy_pixel = dy_pixel;
+    a.out_image = dx_image;
+    a.out_pixel = dx_pixel;
+    a.gamma = gamma_dev;
+    a.beta = beta_dev;
+    a.mean = const_cast<float*>(mean_dev);
+    a.rstd = const_cast<float*>(rstd_dev);
+    a.N = N;
+    a.S = (int32_t)S;
+    a.C = C;
+    a.G = G;
+    a.act = act;
+    const NormPlan pl = norm_plan(a, dtype, true);
+    const int64_t need = norm_scratch(a, pl, true);
+    if (!workspace_dev || workspace_bytes < need * (int64_t)sizeof(float))
+        return op_error(GMC_EINVAL, me, "the workspace is too small");
+    const int64_t rows = pl.held ? N : N * a.chunks;
+    const int64_t blocks = pl.held ? N * a.blocks : rows * a.cblocks;
+    if (blocks * pl.threads > 0xffffffffll || (!pl.held && N * G * kSplitThreads > 0xffffffffll))
+        return op_error(GMC_EINVAL, me, "too many images for one launch");
+    const dim3 grid((unsigned)blocks);
+    a.part = static_cast<float*>(workspace_dev);
+    a.part2 = a.part + rows * (int64_t)C;
+    if (pl.held) {
+        GMC_BY_TYPE(dtype, GMC_NORM_VEC(16 / Elem<DT>::kSize, {
+                        if (pl.kp == 4) norm_backward_held<DT, VEC, 4><<<grid, pl.threads, pl.lds, st>>>(a);
+                        else norm_backward_held<DT, VEC, kHeldMostBack><<<grid, pl.threads, pl.lds, st>>>(a);
+                    }));
+    } else {
+        float* shared_terms = a.part2 + rows * (int64_t)C;
+        GMC_BY_TYPE(dtype, GMC_NORM_VEC(16 / Elem<DT>::kSize, {
+                        norm_back_sums<DT, VEC><<<grid, pl.threads, pl.lds, st>>>(a);
+                        norm_back_join<<<dim3((unsigned)(N * G)), kSplitThreads, 0, st>>>(a, shared_terms);
+                        norm_backward_split<DT, VEC><<<grid, pl.threads, 0, st>>>(a, shared_terms);
+                    }));
+    }
+    if (dgamma_dev || dbeta_dev)
+        norm_params<<<param_grid, kSplitThreads, 0, st>>>(a.part, a.part2, rows, C, dgamma_dev, dbeta_dev);
+    return op_launched(me);
+}
+
+}  // extern "C"

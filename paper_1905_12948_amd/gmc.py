@@ -33,7 +33,9 @@ EXPORTS = ("gmc_init", "gmc_set_segments", "gmc_set_block", "gmc_set_stream", "g
            "gmc_set_option", "gmc_stats", "gmc_profile_read", "gmc_last_error", "gmc_destroy",
            "gmc_calib_copy", "gmc_aggregate_apply", "gmc_set_rule", "gmc_set_eta", "gmc_set_lambda",
            "gmc_step_detach", "gmc_finish", "gmc_detach", "gmc_iteration", "gmc_calib_stream", "gmc_pair_stats",
-           "gmc_count", "gmc_aggregate_static", "gmc_iteration_inplace")
+           "gmc_count", "gmc_aggregate_static", "gmc_iteration_inplace",
+           "gmc_dropout", "gmc_group_norm", "gmc_group_norm_backward", "gmc_group_norm_workspace",
+           "gmc_policy_loss", "gmc_policy_loss_workspace", "gmc_preference_loss", "gmc_preference_loss_workspace")
 
 RULES = {"gmc": 0, "server_momentum": 1, "lr_in_residual": 2}
 
@@ -94,11 +96,27 @@ def load() -> ctypes.CDLL:
     lib.gmc_aggregate_static.restype = ctypes.c_int
     lib.gmc_count.argtypes = [i64, dbl]
     lib.gmc_count.restype = i64
+    lib.gmc_dropout.argtypes = [P, i32, i64, i64, P, i64, P, i64, P, i64, dbl, u64, i64, i32, i32]
+    lib.gmc_group_norm.argtypes = [P, i32, i64, i64, i32, i32, P, i64, i64, P, P, dbl, i32, P, i64, i64, P, P, P, i64]
+    lib.gmc_group_norm_backward.argtypes = [P, i32, i64, i64, i32, i32, P, i64, i64, P, i64, i64, P, P, P, P, i32,
+                                            P, i64, i64, P, P, P, i64]
+    lib.gmc_group_norm_workspace.argtypes = [i32, i64, i64, i32, i32, i32]
+    lib.gmc_group_norm_workspace.restype = i64
+    lib.gmc_policy_loss.argtypes = [P, i32, i64, i64, i64, P, i64, i64, P, i64, i64, P, P, P, i64, i64, dbl, dbl, dbl,
+                                    dbl, i32, dbl, P, P, P, i64, i64, P, i64]
+    lib.gmc_policy_loss_workspace.argtypes = [i64, i64]
+    lib.gmc_policy_loss_workspace.restype = i64
+    lib.gmc_preference_loss.argtypes = [P, i32, i64, i64, i64, P, i64, i64, P, i64, i64, P, dbl, dbl, i32, dbl,
+                                        P, P, P, P, P, i64, i64, P, i64]
+    lib.gmc_preference_loss_workspace.argtypes = [i64, i64]
+    lib.gmc_preference_loss_workspace.restype = i64
     for name in ("gmc_init", "gmc_set_segments", "gmc_set_block", "gmc_set_stream", "gmc_step",
                  "gmc_aggregate", "gmc_apply", "gmc_get_step", "gmc_set_step", "gmc_set_option",
                  "gmc_stats", "gmc_profile_read", "gmc_calib_copy", "gmc_aggregate_apply",
                  "gmc_set_rule", "gmc_set_eta", "gmc_set_lambda", "gmc_step_detach", "gmc_finish",
-                 "gmc_detach", "gmc_iteration", "gmc_calib_stream", "gmc_pair_stats", "gmc_iteration_inplace"):
+                 "gmc_detach", "gmc_iteration", "gmc_calib_stream", "gmc_pair_stats", "gmc_iteration_inplace",
+                 "gmc_dropout", "gmc_group_norm", "gmc_group_norm_backward", "gmc_policy_loss",
+                 "gmc_preference_loss"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
