@@ -31,7 +31,8 @@ constexpr int kHeldMost = 16;      // vectors of x a thread holds (16 bytes each
 constexpr int kHeldMostBack = 8;   // ... of x and of dy
 constexpr int kHeldChannels = 256; // threads across channels, at most
 constexpr int kSplitThreads = 256;
-constexpr int kSplitTile = 8;      // pixels a thread joins at once
+constexpr int kSplitTile = 8;      // pixels whose loads a thread issues together
+constexpr int kSplitBlocks = 1280;  // workgroups, about
 
 struct NormArgs {
     const void* x;
@@ -48,6 +49,7 @@ struct NormArgs {
     int32_t S, C, G, cpg;
     int32_t gw, cb, blocks;  // held: groups and channels per workgroup, workgroups per image
     int32_t tc, tp_log2;     // threads across channels, and the power of two above
+    int32_t cpg_log2;        // -1: cpg is no power of two
     int32_t chunk, chunks;   // split: pixels per workgroup, workgroups per image
     int32_t cblocks;         // split: workgroups across channels
     float eps;
@@ -68,6 +70,10 @@ __device__ __forceinline__ float back_act(float dy, float z, int act) {
         return dy * (gate * (1.0f + z * (1.0f - gate)));
     }
     return dy;
+}
+
+__device__ __forceinline__ int group_of(const NormArgs& a, int c) {
+    return a.cpg_log2 >= 0 ? c >> a.cpg_log2 : c / a.cpg;
 }
 
 // A workgroup's place in its block of channels.
@@ -176,7 +182,7 @@ __global__ __launch_bounds__(kHeldThreads) void norm_forward_held(NormArgs a) {
     int gi[VEC];
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
-        gi[i] = p.on ? (p.cv * VEC + i) / a.cpg : 0;
+        gi[i] = p.on ? group_of(a, p.cv * VEC + i) : 0;
         mu[i] = grp[gi[i]] / m;
         sum[i] = 0.0f;
     }
@@ -216,7 +222,7 @@ __device__ __forceinline__ void load_stats(const NormArgs& a, int64_t n, int c0,
                                            float (&rs)[VEC]) {
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
-        const int64_t at = n * a.G + (on ? (c0 + i) / a.cpg : 0);
+        const int64_t at = n * a.G + (on ? group_of(a, c0 + i) : 0);
         mu[i] = a.mean[at];
         rs[i] = a.rstd[at];
     }
@@ -285,7 +291,7 @@ __global__ __launch_bounds__(kHeldThreads) void norm_backward_held(NormArgs a) {
     const float m = (float)((int64_t)a.S * a.cpg);
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
-        const int g = p.on ? (p.cv * VEC + i) / a.cpg : 0;
+        const int g = p.on ? group_of(a, p.cv * VEC + i) : 0;
         s1[i] = grp1[g] / m;
         s2[i] = grp2[g] / m;
     }
@@ -332,7 +338,11 @@ __device__ __forceinline__ Piece piece(const NormArgs& a, Place& p) {
     return q;
 }
 
-// Per (image, chunk, channel): the mean and the sum of squares about it.
+// Per (image, chunk, channel): the mean and the sum of squares about it.  A
+// thread sums differences from its first pixel's value, one of the n values
+// themselves: n times their variance is at least that value's own square about the
+// mean, so the subtraction below loses at most a factor n, the few dozen pixels a
+// thread has, of the 32-bit resolution, and nothing where levels are far from zero.
 template <int DT, int VEC>
 __global__ __launch_bounds__(kSplitThreads) void norm_moments(NormArgs a) {
     typedef typename Elem<DT>::T T;
@@ -342,54 +352,39 @@ __global__ __launch_bounds__(kSplitThreads) void norm_moments(NormArgs a) {
     float* part = norm_lds;
     float* chan = part + (((a.tp_log2 < 6 ? p.waves : p.rows) * VEC) << a.tp_log2);
     const T* px = static_cast<const T*>(a.x) + q.n * a.x_image + q.c0;
-    float mean[VEC], sq[VEC], f[VEC];
+    float mean[VEC], sq[VEC], f[VEC], first[VEC];
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) mean[i] = sq[i] = 0.0f;
+    for (int i = 0; i < VEC; ++i) mean[i] = sq[i] = first[i] = 0.0f;
     float have = 0.0f;
+    if (p.on && q.first + p.r < q.last) {
+        V::load(px + (int64_t)(q.first + p.r) * a.x_pixel).unpack(first);
+        have = (float)((q.last - q.first - p.r + p.rows - 1) / p.rows);
+    }
     for (int s0 = q.first + p.r; s0 < q.last && p.on; s0 += kSplitTile * p.rows) {
         V xv[kSplitTile];
-        int cnt = 0;
+#pragma unroll
+        for (int k = 0; k < kSplitTile; ++k)
+            if (s0 + k * p.rows < q.last) xv[k] = V::load(px + (int64_t)(s0 + k * p.rows) * a.x_pixel);
 #pragma unroll
         for (int k = 0; k < kSplitTile; ++k)
             if (s0 + k * p.rows < q.last) {
-                xv[k] = V::load(px + (int64_t)(s0 + k * p.rows) * a.x_pixel);
-                ++cnt;
-            }
-        // the tile's own mean and squares about it, then joined with what is there
-        float tm[VEC], ts[VEC];
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) tm[i] = ts[i] = 0.0f;
-#pragma unroll
-        for (int k = 0; k < kSplitTile; ++k)
-            if (k < cnt) {
-                xv[k].unpack(f);
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) tm[i] += f[i];
-            }
-        const float inv = 1.0f / (float)cnt, all = have + (float)cnt;
-        const float share = (float)cnt / all, cross = have * share;
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) tm[i] *= inv;
-#pragma unroll
-        for (int k = 0; k < kSplitTile; ++k)
-            if (k < cnt) {
                 xv[k].unpack(f);
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) {
-                    const float d = f[i] - tm[i];
-                    ts[i] = __builtin_fmaf(d, d, ts[i]);
+                    const float d = f[i] - first[i];
+                    mean[i] += d;
+                    sq[i] = __builtin_fmaf(d, d, sq[i]);
                 }
             }
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            const float d = tm[i] - mean[i];
-            mean[i] = __builtin_fmaf(d, share, mean[i]);
-            sq[i] += ts[i] + d * d * cross;
-        }
-        have = all;
     }
+    const float n1 = have > 0.0f ? 1.0f / have : 0.0f;
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) f[i] = have * mean[i];
+    for (int i = 0; i < VEC; ++i) {
+        const float d = mean[i] * n1;
+        sq[i] = fmaxf(__builtin_fmaf(-mean[i], d, sq[i]), 0.0f);
+        mean[i] = first[i] + d;
+        f[i] = have * mean[i];
+    }
     channel_sums<VEC>(f, a, p, part, chan);
     const float inv = 1.0f / (float)(q.last - q.first);
     const int64_t at = (q.n * a.chunks + q.chunk) * a.C + (q.c0 - p.cv * VEC);
@@ -407,42 +402,33 @@ __global__ __launch_bounds__(kSplitThreads) void norm_moments(NormArgs a) {
         if (q.c0 - p.cv * VEC + c < a.C) a.part2[at + c] = chan[c];
 }
 
-__device__ __forceinline__ float block_sum(float v, float* lds) {
-    v = wave_sum(v);
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-    __syncthreads();
-    float s = 0.0f;
-    for (int w = 0; w < (int)(blockDim.x >> 6); ++w) s += lds[w];
-    __syncthreads();
-    return s;
-}
-
-// One workgroup per (image, group): joins the chunks' channel moments.
+// One wavefront per (image, group): joins the chunks' channel moments.
 __global__ __launch_bounds__(kSplitThreads) void norm_join(NormArgs a) {
-    __shared__ float lds[kSplitThreads / 64];
-    const int64_t n = blockIdx.x / (unsigned)a.G;
-    const int g = (int)(blockIdx.x - n * a.G);
+    const int64_t at = (int64_t)blockIdx.x * (kSplitThreads / 64) + (threadIdx.x >> 6);
+    if (at >= a.N * a.G) return;
+    const int64_t n = at / a.G;
+    const int g = (int)(at - n * a.G), lane = threadIdx.x & 63;
     const int total = a.chunks * a.cpg;
     const float* mean = a.part + n * a.chunks * a.C + (int64_t)g * a.cpg;
     const float* sq = a.part2 + n * a.chunks * a.C + (int64_t)g * a.cpg;
     const float m = (float)((int64_t)a.S * a.cpg);
-    const int short_one = a.S - (a.chunks - 1) * a.chunk;
+    const float full = (float)a.chunk, rest = (float)(a.S - (a.chunks - 1) * a.chunk);
     float s = 0.0f;
-    for (int e = threadIdx.x; e < total; e += blockDim.x) {
-        const int k = e / a.cpg, c = e - k * a.cpg;
-        s += (float)(k == a.chunks - 1 ? short_one : a.chunk) * mean[(int64_t)k * a.C + c];
+    for (int e = lane; e < total; e += 64) {
+        const int k = group_of(a, e), c = e - k * a.cpg;
+        s += (k == a.chunks - 1 ? rest : full) * mean[(int64_t)k * a.C + c];
     }
-    const float mu = block_sum(s, lds) / m;
+    const float mu = wave_sum(s) / m;
     s = 0.0f;
-    for (int e = threadIdx.x; e < total; e += blockDim.x) {
-        const int k = e / a.cpg, c = e - k * a.cpg;
+    for (int e = lane; e < total; e += 64) {
+        const int k = group_of(a, e), c = e - k * a.cpg;
         const float d = mean[(int64_t)k * a.C + c] - mu;
-        s += sq[(int64_t)k * a.C + c] + (float)(k == a.chunks - 1 ? short_one : a.chunk) * d * d;
+        s += sq[(int64_t)k * a.C + c] + (k == a.chunks - 1 ? rest : full) * d * d;
     }
-    const float var = block_sum(s, lds) / m;
-    if (threadIdx.x == 0) {
-        a.mean[n * a.G + g] = mu;
-        a.rstd[n * a.G + g] = 1.0f / sqrtf(var + a.eps);
+    const float var = wave_sum(s) / m;
+    if (lane == 0) {
+        a.mean[at] = mu;
+        a.rstd[at] = 1.0f / sqrtf(var + a.eps);
     }
 }
 
@@ -525,27 +511,44 @@ __global__ __launch_bounds__(kSplitThreads) void norm_back_sums(NormArgs a) {
         if (q.c0 - p.cv * VEC + c < a.C) a.part2[at + c] = chan[c];
 }
 
-// One workgroup per (image, group): s1 / m and s2 / m, after the two sums of
-// the chunks in a.part and a.part2 (N chunks C values each).
+// One wavefront per (image, group): s1 / m and s2 / m from the chunks' sums,
+// and each channel's sums over the image's chunks, left in the first chunk's row.
 __global__ __launch_bounds__(kSplitThreads) void norm_back_join(NormArgs a, float* shared_terms) {
-    __shared__ float lds[kSplitThreads / 64];
-    const int64_t n = blockIdx.x / (unsigned)a.G;
-    const int g = (int)(blockIdx.x - n * a.G);
-    const int total = a.chunks * a.cpg;
+    const int64_t at = (int64_t)blockIdx.x * (kSplitThreads / 64) + (threadIdx.x >> 6);
+    if (at >= a.N * a.G) return;
+    const int64_t n = at / a.G;
+    const int g = (int)(at - n * a.G), lane = threadIdx.x & 63;
     const int64_t base = n * a.chunks * a.C + (int64_t)g * a.cpg;
     const float m = (float)((int64_t)a.S * a.cpg);
+    // `step` channels side by side, the other lanes on other chunks
+    int step = 1;
+    while (step < 64 && step < a.cpg) step *= 2;
     float s1 = 0.0f, s2 = 0.0f;
-    for (int e = threadIdx.x; e < total; e += blockDim.x) {
-        const int k = e / a.cpg, c = e - k * a.cpg;
-        const float w = a.gamma ? a.gamma[g * a.cpg + c] : 1.0f;
-        s1 += w * a.part[base + (int64_t)k * a.C + c];
-        s2 += w * a.part2[base + (int64_t)k * a.C + c];
+    for (int c0 = 0; c0 < a.cpg; c0 += step) {
+        const int c = c0 + (lane & (step - 1));
+        float b = 0.0f, w = 0.0f;
+        if (c < a.cpg)
+            for (int k = lane / step; k < a.chunks; k += 64 / step) {
+                b += a.part[base + (int64_t)k * a.C + c];
+                w += a.part2[base + (int64_t)k * a.C + c];
+            }
+        for (int o = step; o < 64; o <<= 1) {
+            b += __shfl_xor(b, o);
+            w += __shfl_xor(w, o);
+        }
+        if (lane < step && c < a.cpg) {
+            a.part[base + c] = b;
+            a.part2[base + c] = w;
+            const float ga = a.gamma ? a.gamma[g * a.cpg + c] : 1.0f;
+            s1 = __builtin_fmaf(ga, b, s1);
+            s2 = __builtin_fmaf(ga, w, s2);
+        }
     }
-    s1 = block_sum(s1, lds);
-    s2 = block_sum(s2, lds);
-    if (threadIdx.x == 0) {
-        shared_terms[2 * (n * a.G + g)] = s1 / m;
-        shared_terms[2 * (n * a.G + g) + 1] = s2 / m;
+    s1 = wave_sum(s1);
+    s2 = wave_sum(s2);
+    if (lane == 0) {
+        shared_terms[2 * at] = s1 / m;
+        shared_terms[2 * at + 1] = s2 / m;
     }
 }
 
@@ -564,7 +567,7 @@ __global__ __launch_bounds__(kSplitThreads) void norm_backward_split(NormArgs a,
     load_stats<VEC>(a, q.n, q.c0, true, mu, rs);
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
-        const int64_t at = 2 * (q.n * a.G + (q.c0 + i) / a.cpg);
+        const int64_t at = 2 * (q.n * a.G + group_of(a, q.c0 + i));
         s1[i] = shared_terms[at];
         s2[i] = shared_terms[at + 1];
     }
@@ -594,18 +597,19 @@ __global__ __launch_bounds__(kSplitThreads) void norm_backward_split(NormArgs a,
     }
 }
 
-// dgamma and dbeta: the sums of `rows` rows of C partial values each.  16
-// channels and 16 row slots a workgroup.
+// dgamma and dbeta: the sums over the images of rows of C values, `pitch`
+// apart.  16 channels (a 64-byte line of each row) and 16 row slots a workgroup.
 constexpr int kParamCh = 16;
 __global__ __launch_bounds__(kSplitThreads) void norm_params(const float* part, const float* part2, int64_t rows,
-                                                             int32_t C, float* dgamma, float* dbeta) {
+                                                             int64_t pitch, int32_t C, float* dgamma, float* dbeta) {
     __shared__ float lds[2][kSplitThreads];
     const int c = blockIdx.x * kParamCh + (threadIdx.x & (kParamCh - 1));
     float s1 = 0.0f, s2 = 0.0f;
     if (c < C)
+#pragma unroll 4
         for (int64_t r = threadIdx.x / kParamCh; r < rows; r += kSplitThreads / kParamCh) {
-            s1 += part[r * C + c];
-            s2 += part2[r * C + c];
+            s1 += part[r * pitch + c];
+            s2 += part2[r * pitch + c];
         }
     lds[0][threadIdx.x] = s1;
     lds[1][threadIdx.x] = s2;
@@ -645,6 +649,7 @@ NormPlan norm_plan(NormArgs& a, int32_t dtype, bool backward) {
     const int full = (int)(16 / type_size(dtype));
     const int most = backward ? kHeldMostBack : kHeldMost;
     a.cpg = a.C / a.G;
+    a.cpg_log2 = a.cpg & (a.cpg - 1) ? -1 : log2_up(a.cpg);
     // held: the fewest whole groups whose channels fill a 128-byte line (else a
     // 64-byte half), with a thread count that leaves at most `most` vectors each
     for (int line = 128; line >= 64 && !pl.held; line >>= 1)
@@ -683,7 +688,7 @@ NormPlan norm_plan(NormArgs& a, int32_t dtype, bool backward) {
     const int rows = kSplitThreads >> a.tp_log2;
     // pixels per workgroup: enough workgroups for every CU, a few tiles each
     int64_t chunks = (a.S + (int64_t)rows * kSplitTile - 1) / ((int64_t)rows * kSplitTile);
-    const int64_t want = (4096 + a.N * a.cblocks - 1) / (a.N * a.cblocks);
+    const int64_t want = (kSplitBlocks + a.N * a.cblocks - 1) / (a.N * a.cblocks);
     if (chunks > want) chunks = want;
     a.chunk = (int32_t)((a.S + chunks - 1) / chunks);
     a.chunks = (a.S + a.chunk - 1) / a.chunk;
@@ -791,9 +796,9 @@ gmc_status gmc_group_norm(void* hip_stream, int32_t dtype, int64_t N, int64_t S,
         return op_error(GMC_EINVAL, me, "the workspace is too small");
     hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
     const int64_t blocks = pl.held ? N * a.blocks : N * a.chunks * a.cblocks;
-    if (blocks * pl.threads > 0xffffffffll || (!pl.held && N * G * kSplitThreads > 0xffffffffll))
+    if (blocks * pl.threads > 0xffffffffll || (!pl.held && N * G > 0xffffffffll / 64))
         return op_error(GMC_EINVAL, me, "too many images for one launch");
-    const dim3 grid((unsigned)blocks);
+    const dim3 grid((unsigned)blocks), joins((unsigned)((N * G + kSplitThreads / 64 - 1) / (kSplitThreads / 64)));
     if (pl.held) {
         GMC_BY_TYPE(dtype, GMC_NORM_VEC(16 / Elem<DT>::kSize, {
                         if (pl.kp == 4) norm_forward_held<DT, VEC, 4><<<grid, pl.threads, pl.lds, st>>>(a);
@@ -804,7 +809,7 @@ gmc_status gmc_group_norm(void* hip_stream, int32_t dtype, int64_t N, int64_t S,
         a.part2 = a.part + N * a.chunks * (int64_t)C;
         GMC_BY_TYPE(dtype, GMC_NORM_VEC(16 / Elem<DT>::kSize, {
                         norm_moments<DT, VEC><<<grid, pl.threads, pl.lds, st>>>(a);
-                        norm_join<<<dim3((unsigned)(N * G)), kSplitThreads, 0, st>>>(a);
+                        norm_join<<<joins, kSplitThreads, 0, st>>>(a);
                         norm_forward_split<DT, VEC><<<grid, pl.threads, 0, st>>>(a);
                     }));
     }
@@ -824,7 +829,7 @@ gmc_status gmc_group_norm_backward(void* hip_stream, int32_t dtype, int64_t N, i
     const dim3 param_grid((unsigned)((C + kParamCh - 1) / kParamCh));
     if (N == 0) {
         if (dgamma_dev || dbeta_dev)
-            norm_params<<<param_grid, kSplitThreads, 0, st>>>(nullptr, nullptr, 0, C, dgamma_dev, dbeta_dev);
+            norm_params<<<param_grid, kSplitThreads, 0, st>>>(nullptr, nullptr, 0, 0, C, dgamma_dev, dbeta_dev);
         return op_launched(me);
     }
     if (!dy_dev || !x_dev || !dx_dev || !mean_dev || !rstd_dev) return op_error(GMC_EINVAL, me, "NULL argument");
@@ -863,9 +868,9 @@ gmc_status gmc_group_norm_backward(void* hip_stream, int32_t dtype, int64_t N, i
         return op_error(GMC_EINVAL, me, "the workspace is too small");
     const int64_t rows = pl.held ? N : N * a.chunks;
     const int64_t blocks = pl.held ? N * a.blocks : rows * a.cblocks;
-    if (blocks * pl.threads > 0xffffffffll || (!pl.held && N * G * kSplitThreads > 0xffffffffll))
+    if (blocks * pl.threads > 0xffffffffll || (!pl.held && N * G > 0xffffffffll / 64))
         return op_error(GMC_EINVAL, me, "too many images for one launch");
-    const dim3 grid((unsigned)blocks);
+    const dim3 grid((unsigned)blocks), joins((unsigned)((N * G + kSplitThreads / 64 - 1) / (kSplitThreads / 64)));
     a.part = static_cast<float*>(workspace_dev);
     a.part2 = a.part + rows * (int64_t)C;
     if (pl.held) {
@@ -877,12 +882,13 @@ gmc_status gmc_group_norm_backward(void* hip_stream, int32_t dtype, int64_t N, i
         float* shared_terms = a.part2 + rows * (int64_t)C;
         GMC_BY_TYPE(dtype, GMC_NORM_VEC(16 / Elem<DT>::kSize, {
                         norm_back_sums<DT, VEC><<<grid, pl.threads, pl.lds, st>>>(a);
-                        norm_back_join<<<dim3((unsigned)(N * G)), kSplitThreads, 0, st>>>(a, shared_terms);
+                        norm_back_join<<<joins, kSplitThreads, 0, st>>>(a, shared_terms);
                         norm_backward_split<DT, VEC><<<grid, pl.threads, 0, st>>>(a, shared_terms);
                     }));
     }
     if (dgamma_dev || dbeta_dev)
-        norm_params<<<param_grid, kSplitThreads, 0, st>>>(a.part, a.part2, rows, C, dgamma_dev, dbeta_dev);
+        norm_params<<<param_grid, kSplitThreads, 0, st>>>(a.part, a.part2, N, (pl.held ? 1 : a.chunks) * (int64_t)C, C,
+                                                          dgamma_dev, dbeta_dev);
     return op_launched(me);
 }
 
