@@ -27,6 +27,7 @@ namespace gmc {
 namespace {
 
 constexpr int kHeldThreads = 1024;
+constexpr int kHeldBlocks = 512;   // held: workgroups below which narrower blocks are tried
 constexpr int kHeldMost = 16;      // vectors of x a thread holds (16 bytes each)
 constexpr int kHeldMostBack = 8;   // ... of x and of dy
 constexpr int kHeldChannels = 256; // threads across channels, at most
@@ -52,7 +53,7 @@ struct NormArgs {
     int32_t cpg_log2;        // -1: cpg is no power of two
     int32_t chunk, chunks;   // split: pixels per workgroup, workgroups per image
     int32_t cblocks;         // split: workgroups across channels
-    float eps;
+    float eps, inv_m;        // inv_m: 1 / (S cpg)
     int32_t act;
 };
 
@@ -123,13 +124,14 @@ __device__ __forceinline__ void channel_sums(float (&v)[VEC], const NormArgs& a,
     __syncthreads();
 }
 
-// grp[g] = the sum of chan over group g's channels, one wavefront a group.
-__device__ __forceinline__ void group_sums(const float* chan, const NormArgs& a, float* grp) {
+// Gives `take` the sum of chan over each group's channels, one wavefront a group.
+template <class Take>
+__device__ __forceinline__ void group_sums(const float* chan, const NormArgs& a, Take take) {
     for (int g = threadIdx.x >> 6; g < a.gw; g += blockDim.x >> 6) {
         float s = 0.0f;
         for (int c = threadIdx.x & 63; c < a.cpg; c += 64) s += chan[g * a.cpg + c];
         s = wave_sum(s);
-        if ((threadIdx.x & 63) == 0) grp[g] = s;
+        if ((threadIdx.x & 63) == 0) take(g, s);
     }
     __syncthreads();
 }
@@ -166,7 +168,6 @@ __global__ __launch_bounds__(kHeldThreads) void norm_forward_held(NormArgs a) {
     }
     float ga[VEC], be[VEC], mu[VEC], rs[VEC];
     load_params<VEC>(a, c0, p.on, ga, be);
-    const float m = (float)((int64_t)a.S * a.cpg);
     float sum[VEC], f[VEC];
 #pragma unroll
     for (int i = 0; i < VEC; ++i) sum[i] = 0.0f;
@@ -178,16 +179,16 @@ __global__ __launch_bounds__(kHeldThreads) void norm_forward_held(NormArgs a) {
             for (int i = 0; i < VEC; ++i) sum[i] += f[i];
         }
     channel_sums<VEC>(sum, a, p, part, chan);
-    group_sums(chan, a, grp);
+    group_sums(chan, a, [&](int g, float s) {
+        grp[g] = a.mean[n * a.G + blk * a.gw + g] = s * a.inv_m;
+    });
     int gi[VEC];
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
         gi[i] = p.on ? group_of(a, p.cv * VEC + i) : 0;
-        mu[i] = grp[gi[i]] / m;
+        mu[i] = grp[gi[i]];
         sum[i] = 0.0f;
     }
-    __syncthreads();  // grp is read
-    for (int g = threadIdx.x; g < a.gw; g += blockDim.x) a.mean[n * a.G + blk * a.gw + g] = grp[g] / m;
 #pragma unroll
     for (int k = 0; k < KP; ++k)
         if (p.on && p.r + k * p.rows < a.S) {
@@ -199,10 +200,11 @@ __global__ __launch_bounds__(kHeldThreads) void norm_forward_held(NormArgs a) {
             }
         }
     channel_sums<VEC>(sum, a, p, part, chan);
-    group_sums(chan, a, grp);
+    group_sums(chan, a, [&](int g, float s) {
+        grp[g] = a.rstd[n * a.G + blk * a.gw + g] = 1.0f / sqrtf(s * a.inv_m + a.eps);
+    });
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) rs[i] = 1.0f / sqrtf(grp[gi[i]] / m + a.eps);
-    for (int g = threadIdx.x; g < a.gw; g += blockDim.x) a.rstd[n * a.G + blk * a.gw + g] = 1.0f / sqrtf(grp[g] / m + a.eps);
+    for (int i = 0; i < VEC; ++i) rs[i] = grp[gi[i]];
 #pragma unroll
     for (int k = 0; k < KP; ++k) {
         const int s = p.r + k * p.rows;
@@ -279,7 +281,7 @@ __global__ __launch_bounds__(kHeldThreads) void norm_backward_held(NormArgs a) {
         chan[c] = a.gamma ? v * a.gamma[blk * a.cb + c] : v;
     }
     __syncthreads();
-    group_sums(chan, a, grp1);
+    group_sums(chan, a, [&](int g, float s) { grp1[g] = s * a.inv_m; });
     channel_sums<VEC>(s2, a, p, part, chan);
     for (int c = threadIdx.x; c < a.cb; c += blockDim.x) {
         const float v = chan[c];
@@ -287,13 +289,12 @@ __global__ __launch_bounds__(kHeldThreads) void norm_backward_held(NormArgs a) {
         chan[c] = a.gamma ? v * a.gamma[blk * a.cb + c] : v;
     }
     __syncthreads();
-    group_sums(chan, a, grp2);
-    const float m = (float)((int64_t)a.S * a.cpg);
+    group_sums(chan, a, [&](int g, float s) { grp2[g] = s * a.inv_m; });
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
         const int g = p.on ? group_of(a, p.cv * VEC + i) : 0;
-        s1[i] = grp1[g] / m;
-        s2[i] = grp2[g] / m;
+        s1[i] = grp1[g];
+        s2[i] = grp2[g];
     }
 #pragma unroll
     for (int k = 0; k < KP; ++k) {
@@ -307,6 +308,268 @@ __global__ __launch_bounds__(kHeldThreads) void norm_backward_held(NormArgs a) {
                 const float hat = (f[i] - mu[i]) * rs[i];
                 const float dz = back_act(d[i], hat * ga[i] + be[i], a.act);
                 f[i] = rs[i] * (dz * ga[i] - __builtin_fmaf(hat, s2[i], s1[i]));
+            }
+            xv[k].pack(f);
+            xv[k].store(po + s * a.out_pixel);
+        }
+    }
+}
+
+// -- held form, groups of a power of two of channels ---------------------------
+//
+// The same statements with fewer instructions, which bound the general kernels
+// above: values are folded into their groups before any exchange between lanes,
+// statistics are formed once a group, and the unpacked values stay in registers
+// where a thread has at most 8 vectors.
+
+// This workgroup's image and channel block.  Workgroups go to the 8 XCDs in
+// turn; each XCD takes a run of neighbouring blocks, so that blocks narrower
+// than a line share it in one L2.
+__device__ __forceinline__ int64_t xcd_run(unsigned total) {
+    const unsigned x = blockIdx.x & 7u, j = blockIdx.x >> 3, q = total >> 3, r = total & 7u;
+    return (int64_t)x * q + (x < r ? x : r) + j;
+}
+
+// The sums of F values over the lanes that share them: the pixel lanes and,
+// where a group is wider than a vector, its neighbours (`within` lanes).
+template <int F>
+__device__ __forceinline__ void fold_lanes(float (&v)[F], int across, int within) {
+    for (int o = 1; o < within; o <<= 1)
+#pragma unroll
+        for (int i = 0; i < F; ++i) v[i] += __shfl_xor(v[i], o);
+    for (int o = across; o < 64; o <<= 1)
+#pragma unroll
+        for (int i = 0; i < F; ++i) v[i] += __shfl_xor(v[i], o);
+}
+
+// F: groups in a thread's vector (1 where a group has at least as many channels).
+template <int DT, int KP, int F>
+__global__ __launch_bounds__(kHeldThreads) void norm_forward_fold(NormArgs a) {
+    typedef typename Elem<DT>::T T;
+    constexpr int VEC = 16 / Elem<DT>::kSize;
+    constexpr int W = VEC / F;            // channels of the vector in one of its groups
+    constexpr bool kKeep = KP <= 8;
+    typedef Vec<DT, VEC> V;
+    const Place p = place(a);
+    const int64_t id = xcd_run(gridDim.x), n = id / (unsigned)a.blocks;
+    const int blk = (int)(id - n * a.blocks);
+    const int c0 = blk * a.cb + p.cv * VEC;
+    const int within = F == 1 ? a.cpg / VEC : 1;
+    const int g0 = F == 1 ? (p.cv * VEC) >> a.cpg_log2 : p.cv * F;  // the thread's first group
+    float* part = norm_lds;               // [wavefronts][gw]
+    float* stat = part + p.waves * a.gw;  // [2][gw]
+    const T* px = static_cast<const T*>(a.x) + n * a.x_image + c0;
+    T* py = static_cast<T*>(a.out) + n * a.out_image + c0;
+    V xv[KP];
+    float x[kKeep ? KP : 1][VEC], f[VEC];
+#pragma unroll
+    for (int k = 0; k < KP; ++k) {
+        const int s = p.r + k * p.rows;
+        if (p.on && s < a.S) xv[k] = V::load(px + s * a.x_pixel);
+    }
+    float ga[VEC], be[VEC], sum[F], mu[F];
+    load_params<VEC>(a, c0, p.on, ga, be);
+    const int lane = threadIdx.x & 63;
+    const bool writer = lane < (1 << a.tp_log2) && p.on && (p.cv & (within - 1)) == 0;
+    const int64_t at = n * a.G + blk * a.gw;
+
+#pragma unroll
+    for (int i = 0; i < F; ++i) sum[i] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < KP; ++k)
+        if (p.on && p.r + k * p.rows < a.S) {
+            xv[k].unpack(f);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) sum[i / W] += f[i];
+            if constexpr (kKeep)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) x[k][i] = f[i];
+        }
+    fold_lanes<F>(sum, 1 << a.tp_log2, within);
+    if (writer)
+#pragma unroll
+        for (int i = 0; i < F; ++i) part[(threadIdx.x >> 6) * a.gw + g0 + i] = sum[i];
+    __syncthreads();
+    for (int g = threadIdx.x; g < a.gw; g += blockDim.x) {
+        float t = 0.0f;
+        for (int w = 0; w < p.waves; ++w) t += part[w * a.gw + g];
+        stat[g] = a.mean[at + g] = t * a.inv_m;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < F; ++i) {
+        mu[i] = p.on ? stat[g0 + i] : 0.0f;
+        sum[i] = 0.0f;
+    }
+#pragma unroll
+    for (int k = 0; k < KP; ++k)
+        if (p.on && p.r + k * p.rows < a.S) {
+            if constexpr (!kKeep) xv[k].unpack(f);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const float d = (kKeep ? x[kKeep ? k : 0][i] : f[i]) - mu[i / W];
+                if constexpr (kKeep) x[k][i] = d;
+                sum[i / W] = __builtin_fmaf(d, d, sum[i / W]);
+            }
+        }
+    fold_lanes<F>(sum, 1 << a.tp_log2, within);
+    if (writer)
+#pragma unroll
+        for (int i = 0; i < F; ++i) part[(threadIdx.x >> 6) * a.gw + g0 + i] = sum[i];
+    __syncthreads();
+    for (int g = threadIdx.x; g < a.gw; g += blockDim.x) {
+        float t = 0.0f;
+        for (int w = 0; w < p.waves; ++w) t += part[w * a.gw + g];
+        stat[a.gw + g] = a.rstd[at + g] = 1.0f / sqrtf(t * a.inv_m + a.eps);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) ga[i] *= p.on ? stat[a.gw + g0 + i / W] : 0.0f;
+#pragma unroll
+    for (int k = 0; k < KP; ++k) {
+        const int s = p.r + k * p.rows;
+        if (p.on && s < a.S) {
+            if constexpr (!kKeep) xv[k].unpack(f);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const float d = kKeep ? x[kKeep ? k : 0][i] : f[i] - mu[i / W];
+                f[i] = activate(__builtin_fmaf(d, ga[i], be[i]), a.act);
+            }
+            xv[k].pack(f);
+            xv[k].store(py + s * a.out_pixel);
+        }
+    }
+}
+
+// The sums of H values over the lanes o, 2 o, ... < 64 apart, by halves: at each
+// step a lane sends the half of its values that its partner keeps, so H values
+// cost about H exchanges in all.  Value j of the result v[0 .. left) is value
+// first + j of the input; `first` and `left` say which the lane holds.
+template <int H>
+__device__ __forceinline__ void scatter_sums(float* v, int lane, int across, int o, int& first, int& left) {
+    if (o < across) return;
+    if constexpr (H > 1) {
+        const bool up = lane & o;
+#pragma unroll
+        for (int i = 0; i < H / 2; ++i) {
+            const float send = up ? v[i] : v[i + H / 2], keep = up ? v[i + H / 2] : v[i];
+            v[i] = keep + __shfl_xor(send, o);
+        }
+        first += up ? H / 2 : 0;
+        left = H / 2;
+        scatter_sums<H / 2>(v, lane, across, o >> 1, first, left);
+    } else {
+        for (; o >= across; o >>= 1) v[0] += __shfl_xor(v[0], o);
+    }
+}
+
+template <int DT, int KP, int F>
+__global__ __launch_bounds__(kHeldThreads) void norm_backward_fold(NormArgs a) {
+    typedef typename Elem<DT>::T T;
+    constexpr int VEC = 16 / Elem<DT>::kSize;
+    constexpr int W = VEC / F;
+    constexpr bool kKeep = KP <= 4;
+    typedef Vec<DT, VEC> V;
+    const Place p = place(a);
+    const int64_t id = xcd_run(gridDim.x), n = id / (unsigned)a.blocks;
+    const int blk = (int)(id - n * a.blocks);
+    const int c0 = blk * a.cb + p.cv * VEC;
+    const int g0 = F == 1 ? (p.cv * VEC) >> a.cpg_log2 : p.cv * F;
+    float* part = norm_lds;                   // [wavefronts][2][cb]
+    float* stat = part + 2 * p.waves * a.cb;  // [2][gw]
+    const T* px = static_cast<const T*>(a.x) + n * a.x_image + c0;
+    const T* pd = static_cast<const T*>(a.dy) + n * a.dy_image + c0;
+    T* po = static_cast<T*>(a.out) + n * a.out_image + c0;
+    V xv[KP], dv[KP];
+#pragma unroll
+    for (int k = 0; k < KP; ++k) {
+        const int s = p.r + k * p.rows;
+        if (p.on && s < a.S) {
+            xv[k] = V::load(px + s * a.x_pixel);
+            dv[k] = V::load(pd + s * a.dy_pixel);
+        }
+    }
+    float ga[VEC], be[VEC], mu[F], rs[F], v[2 * VEC], f[VEC], d[VEC];
+    float hats[kKeep ? KP : 1][VEC], dzs[kKeep ? KP : 1][VEC];
+    load_params<VEC>(a, c0, p.on, ga, be);
+    const int64_t at = n * a.G + blk * a.gw;
+#pragma unroll
+    for (int i = 0; i < F; ++i) {
+        mu[i] = p.on ? a.mean[at + g0 + i] : 0.0f;
+        rs[i] = p.on ? a.rstd[at + g0 + i] : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < 2 * VEC; ++i) v[i] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < KP; ++k)
+        if (p.on && p.r + k * p.rows < a.S) {
+            xv[k].unpack(f);
+            dv[k].unpack(d);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const float hat = (f[i] - mu[i / W]) * rs[i / W];
+                const float dz = back_act(d[i], hat * ga[i] + be[i], a.act);
+                v[i] += dz;
+                v[VEC + i] = __builtin_fmaf(dz, hat, v[VEC + i]);
+                if constexpr (kKeep) {
+                    hats[k][i] = hat;
+                    dzs[k][i] = dz;
+                }
+            }
+        }
+    int first = 0, left = 2 * VEC;
+    const int lane = threadIdx.x & 63;
+    scatter_sums<2 * VEC>(v, lane, 1 << a.tp_log2, 32, first, left);
+    // lanes that differ only in steps taken with one value left hold the same sum
+    if (p.on)
+#pragma unroll
+        for (int j = 0; j < 2 * VEC; ++j)
+            if (j < left) {
+                const int q = first + j;
+                part[((threadIdx.x >> 6) * 2 + q / VEC) * a.cb + p.cv * VEC + (q & (VEC - 1))] = v[j];
+            }
+    __syncthreads();
+    // a thread per channel and sum; a group's channels are neighbouring lanes
+    for (int e0 = 0; e0 < 2 * a.cb; e0 += blockDim.x) {  // whole wavefronts, for the exchange
+        const int e = e0 + threadIdx.x;
+        const bool some = e < 2 * a.cb;
+        const int which = e >= a.cb, c = e - which * a.cb;
+        float t = 0.0f;
+        if (some) {
+            for (int w = 0; w < p.waves; ++w) t += part[(w * 2 + which) * a.cb + c];
+            (which ? a.part2 : a.part)[n * a.C + blk * a.cb + c] = t;
+            if (a.gamma) t *= a.gamma[blk * a.cb + c];
+        }
+        for (int o = 1; o < a.cpg; o <<= 1) t += __shfl_xor(t, o);
+        if (some && (c & (a.cpg - 1)) == 0) stat[which * a.gw + (c >> a.cpg_log2)] = t * a.inv_m;
+    }
+    __syncthreads();
+    float s1[F], s2[F];
+#pragma unroll
+    for (int i = 0; i < F; ++i) {
+        s1[i] = p.on ? stat[g0 + i] : 0.0f;
+        s2[i] = p.on ? stat[a.gw + g0 + i] : 0.0f;
+    }
+#pragma unroll
+    for (int k = 0; k < KP; ++k) {
+        const int s = p.r + k * p.rows;
+        if (p.on && s < a.S) {
+            if constexpr (!kKeep) {
+                xv[k].unpack(f);
+                dv[k].unpack(d);
+            }
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const int g = i / W;
+                float hat, dz;
+                if constexpr (kKeep) {
+                    hat = hats[k][i];
+                    dz = dzs[k][i];
+                } else {
+                    hat = (f[i] - mu[g]) * rs[g];
+                    dz = back_act(d[i], hat * ga[i] + be[i], a.act);
+                }
+                f[i] = rs[g] * (dz * ga[i] - __builtin_fmaf(hat, s2[g], s1[g]));
             }
             xv[k].pack(f);
             xv[k].store(po + s * a.out_pixel);
@@ -411,21 +674,20 @@ __global__ __launch_bounds__(kSplitThreads) void norm_join(NormArgs a) {
     const int total = a.chunks * a.cpg;
     const float* mean = a.part + n * a.chunks * a.C + (int64_t)g * a.cpg;
     const float* sq = a.part2 + n * a.chunks * a.C + (int64_t)g * a.cpg;
-    const float m = (float)((int64_t)a.S * a.cpg);
     const float full = (float)a.chunk, rest = (float)(a.S - (a.chunks - 1) * a.chunk);
     float s = 0.0f;
     for (int e = lane; e < total; e += 64) {
         const int k = group_of(a, e), c = e - k * a.cpg;
         s += (k == a.chunks - 1 ? rest : full) * mean[(int64_t)k * a.C + c];
     }
-    const float mu = wave_sum(s) / m;
+    const float mu = wave_sum(s) * a.inv_m;
     s = 0.0f;
     for (int e = lane; e < total; e += 64) {
         const int k = group_of(a, e), c = e - k * a.cpg;
         const float d = mean[(int64_t)k * a.C + c] - mu;
         s += sq[(int64_t)k * a.C + c] + (k == a.chunks - 1 ? rest : full) * d * d;
     }
-    const float var = wave_sum(s) / m;
+    const float var = wave_sum(s) * a.inv_m;
     if (lane == 0) {
         a.mean[at] = mu;
         a.rstd[at] = 1.0f / sqrtf(var + a.eps);
@@ -519,7 +781,6 @@ __global__ __launch_bounds__(kSplitThreads) void norm_back_join(NormArgs a, floa
     const int64_t n = at / a.G;
     const int g = (int)(at - n * a.G), lane = threadIdx.x & 63;
     const int64_t base = n * a.chunks * a.C + (int64_t)g * a.cpg;
-    const float m = (float)((int64_t)a.S * a.cpg);
     // `step` channels side by side, the other lanes on other chunks
     int step = 1;
     while (step < 64 && step < a.cpg) step *= 2;
@@ -547,8 +808,8 @@ __global__ __launch_bounds__(kSplitThreads) void norm_back_join(NormArgs a, floa
     s1 = wave_sum(s1);
     s2 = wave_sum(s2);
     if (lane == 0) {
-        shared_terms[2 * at] = s1 / m;
-        shared_terms[2 * at + 1] = s2 / m;
+        shared_terms[2 * at] = s1 * a.inv_m;
+        shared_terms[2 * at + 1] = s2 * a.inv_m;
     }
 }
 
@@ -640,8 +901,43 @@ struct NormPlan {
     int vec = 1;      // channels per thread
     int threads = 0;  // held
     int kp = 0;
+    int fold = 0;     // held: groups in a vector, 0: the general kernels
     size_t lds = 0;
 };
+
+// The held form for groups of a power of two of channels: whole groups in
+// segments of at least `line` bytes, as few threads as leave every thread at
+// most `few` vectors.
+bool plan_fold(NormArgs& a, NormPlan& pl, int64_t size, bool backward, int line, int few, int most) {
+    const int full = (int)(16 / size);
+    for (int gw = 1; gw <= a.G; ++gw) {
+        if (a.G % gw) continue;
+        const int64_t cb = (int64_t)gw * a.cpg;
+        if (cb % full || (cb * size < line && gw < a.G)) continue;
+        const int64_t tc = cb / full;
+        if (tc > 64) return false;
+        const int lg = log2_up(tc);
+        int threads = 64;
+        while (threads < kHeldThreads && a.S > (int64_t)few * (threads >> lg)) threads *= 2;
+        const int rows = threads >> lg;
+        const int64_t kp = (a.S + rows - 1) / rows;
+        if (kp > most) return false;
+        pl.held = true;
+        pl.fold = a.cpg >= full ? 1 : full / a.cpg;
+        pl.vec = full;
+        pl.threads = threads;
+        pl.kp = (int)kp;
+        a.gw = gw;
+        a.cb = (int32_t)cb;
+        a.blocks = a.G / gw;
+        a.tc = (int32_t)tc;
+        a.tp_log2 = lg;
+        const int waves = threads / 64;
+        pl.lds = sizeof(float) * (size_t)(backward ? 2 * waves * (int)cb + 2 * gw : (waves + 2) * gw);
+        return true;
+    }
+    return false;
+}
 
 // Chooses the form and fills the geometry of a.
 NormPlan norm_plan(NormArgs& a, int32_t dtype, bool backward) {
@@ -649,9 +945,17 @@ NormPlan norm_plan(NormArgs& a, int32_t dtype, bool backward) {
     const int full = (int)(16 / type_size(dtype));
     const int most = backward ? kHeldMostBack : kHeldMost;
     a.cpg = a.C / a.G;
+    a.inv_m = (float)(1.0 / ((double)a.S * (double)a.cpg));
     a.cpg_log2 = a.cpg & (a.cpg - 1) ? -1 : log2_up(a.cpg);
-    // held: the fewest whole groups whose channels fill a 128-byte line (else a
-    // 64-byte half), with a thread count that leaves at most `most` vectors each
+    if (a.cpg_log2 >= 0 && a.cpg <= 64) {
+        for (int line = 128; line >= 16; line >>= 1) {
+            if (!plan_fold(a, pl, type_size(dtype), backward, line, backward ? 4 : 8, most)) continue;
+            if (a.N * a.blocks >= kHeldBlocks) break;
+        }
+        if (pl.held) return pl;
+    }
+    // any groups: the fewest whose channels fill a 128-byte line (else a 64-byte
+    // half), with a thread count that leaves at most `most` vectors each
     for (int line = 128; line >= 64 && !pl.held; line >>= 1)
         for (int gw = 1; gw <= a.G && !pl.held; ++gw) {
             if (a.G % gw) continue;
@@ -742,6 +1046,23 @@ using namespace gmc;
         }                                                             \
     } while (0)
 
+#define GMC_NORM_FOLD(...)                                            \
+    do {                                                              \
+        if (pl.fold == 1) {                                           \
+            constexpr int F = 1;                                      \
+            __VA_ARGS__;                                              \
+        } else if (pl.fold == 2) {                                    \
+            constexpr int F = 2;                                      \
+            __VA_ARGS__;                                              \
+        } else if (pl.fold == 4) {                                    \
+            constexpr int F = 4;                                      \
+            __VA_ARGS__;                                              \
+        } else if constexpr (DT != GMC_F32) {                         \
+            constexpr int F = 8;                                      \
+            __VA_ARGS__;                                              \
+        }                                                             \
+    } while (0)
+
 extern "C" {
 
 int64_t gmc_group_norm_workspace(int32_t dtype, int64_t N, int64_t S, int32_t C, int32_t G, int32_t backward) {
@@ -799,7 +1120,13 @@ gmc_status gmc_group_norm(void* hip_stream, int32_t dtype, int64_t N, int64_t S,
     if (blocks * pl.threads > 0xffffffffll || (!pl.held && N * G > 0xffffffffll / 64))
         return op_error(GMC_EINVAL, me, "too many images for one launch");
     const dim3 grid((unsigned)blocks), joins((unsigned)((N * G + kSplitThreads / 64 - 1) / (kSplitThreads / 64)));
-    if (pl.held) {
+    if (pl.fold) {
+        GMC_BY_TYPE(dtype, GMC_NORM_FOLD({
+                        if (pl.kp <= 4) norm_forward_fold<DT, 4, F><<<grid, pl.threads, pl.lds, st>>>(a);
+                        else if (pl.kp <= 8) norm_forward_fold<DT, 8, F><<<grid, pl.threads, pl.lds, st>>>(a);
+                        else norm_forward_fold<DT, kHeldMost, F><<<grid, pl.threads, pl.lds, st>>>(a);
+                    }));
+    } else if (pl.held) {
         GMC_BY_TYPE(dtype, GMC_NORM_VEC(16 / Elem<DT>::kSize, {
                         if (pl.kp == 4) norm_forward_held<DT, VEC, 4><<<grid, pl.threads, pl.lds, st>>>(a);
                         else norm_forward_held<DT, VEC, kHeldMost><<<grid, pl.threads, pl.lds, st>>>(a);
@@ -873,7 +1200,13 @@ gmc_status gmc_group_norm_backward(void* hip_stream, int32_t dtype, int64_t N, i
     const dim3 grid((unsigned)blocks), joins((unsigned)((N * G + kSplitThreads / 64 - 1) / (kSplitThreads / 64)));
     a.part = static_cast<float*>(workspace_dev);
     a.part2 = a.part + rows * (int64_t)C;
-    if (pl.held) {
+    if (pl.fold) {
+        GMC_BY_TYPE(dtype, GMC_NORM_FOLD({
+                        if (pl.kp <= 2) norm_backward_fold<DT, 2, F><<<grid, pl.threads, pl.lds, st>>>(a);
+                        else if (pl.kp <= 4) norm_backward_fold<DT, 4, F><<<grid, pl.threads, pl.lds, st>>>(a);
+                        else norm_backward_fold<DT, kHeldMostBack, F><<<grid, pl.threads, pl.lds, st>>>(a);
+                    }));
+    } else if (pl.held) {
         GMC_BY_TYPE(dtype, GMC_NORM_VEC(16 / Elem<DT>::kSize, {
                         if (pl.kp == 4) norm_backward_held<DT, VEC, 4><<<grid, pl.threads, pl.lds, st>>>(a);
                         else norm_backward_held<DT, VEC, kHeldMostBack><<<grid, pl.threads, pl.lds, st>>>(a);
