@@ -20,6 +20,8 @@
 // the sign the forward pass saw.  All sums are 32-bit, in a fixed order.
 #include <math.h>
 
+#include <type_traits>
+
 #include "gmc_ops.h"
 
 namespace gmc {
@@ -75,6 +77,15 @@ __device__ __forceinline__ float back_act(float dy, float z, int act) {
 
 __device__ __forceinline__ int group_of(const NormArgs& a, int c) {
     return a.cpg_log2 >= 0 ? c >> a.cpg_log2 : c / a.cpg;
+}
+
+// Calls f with the activation as a compile-time constant: one branch around a
+// loop over the values instead of one at each.
+template <class Loop>
+__device__ __forceinline__ void by_act(int act, Loop f) {
+    if (act == GMC_ACT_RELU) f(std::integral_constant<int, GMC_ACT_RELU>{});
+    else if (act == GMC_ACT_SILU) f(std::integral_constant<int, GMC_ACT_SILU>{});
+    else f(std::integral_constant<int, GMC_ACT_NONE>{});
 }
 
 // A workgroup's place in its block of channels.
@@ -320,7 +331,7 @@ __global__ __launch_bounds__(kHeldThreads) void norm_backward_held(NormArgs a) {
 // The same statements with fewer instructions, which bound the general kernels
 // above: values are folded into their groups before any exchange between lanes,
 // statistics are formed once a group, and the unpacked values stay in registers
-// where a thread has at most 8 vectors.
+// where a thread has few vectors.
 
 // This workgroup's image and channel block.  Workgroups go to the 8 XCDs in
 // turn; each XCD takes a run of neighbouring blocks, so that blocks narrower
@@ -425,20 +436,22 @@ __global__ __launch_bounds__(kHeldThreads) void norm_forward_fold(NormArgs a) {
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < VEC; ++i) ga[i] *= p.on ? stat[a.gw + g0 + i / W] : 0.0f;
+    by_act(a.act, [&](auto act) {
 #pragma unroll
-    for (int k = 0; k < KP; ++k) {
-        const int s = p.r + k * p.rows;
-        if (p.on && s < a.S) {
-            if constexpr (!kKeep) xv[k].unpack(f);
+        for (int k = 0; k < KP; ++k) {
+            const int s = p.r + k * p.rows;
+            if (p.on && s < a.S) {
+                if constexpr (!kKeep) xv[k].unpack(f);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const float d = kKeep ? x[kKeep ? k : 0][i] : f[i] - mu[i / W];
-                f[i] = activate(__builtin_fmaf(d, ga[i], be[i]), a.act);
+                for (int i = 0; i < VEC; ++i) {
+                    const float d = kKeep ? x[kKeep ? k : 0][i] : f[i] - mu[i / W];
+                    f[i] = activate(__builtin_fmaf(d, ga[i], be[i]), decltype(act)::value);
+                }
+                xv[k].pack(f);
+                xv[k].store(py + s * a.out_pixel);
             }
-            xv[k].pack(f);
-            xv[k].store(py + s * a.out_pixel);
         }
-    }
+    });
 }
 
 // The sums of H values over the lanes o, 2 o, ... < 64 apart, by halves: at each
@@ -468,7 +481,7 @@ __global__ __launch_bounds__(kHeldThreads) void norm_backward_fold(NormArgs a) {
     typedef typename Elem<DT>::T T;
     constexpr int VEC = 16 / Elem<DT>::kSize;
     constexpr int W = VEC / F;
-    constexpr bool kKeep = KP <= 4;
+    constexpr bool kKeep = KP <= 2;
     typedef Vec<DT, VEC> V;
     const Place p = place(a);
     const int64_t id = xcd_run(gridDim.x), n = id / (unsigned)a.blocks;
@@ -490,7 +503,7 @@ __global__ __launch_bounds__(kHeldThreads) void norm_backward_fold(NormArgs a) {
         }
     }
     float ga[VEC], be[VEC], mu[F], rs[F], v[2 * VEC], f[VEC], d[VEC];
-    float hats[kKeep ? KP : 1][VEC], dzs[kKeep ? KP : 1][VEC];
+    float xs[kKeep ? KP : 1][VEC], dzs[kKeep ? KP : 1][VEC];
     load_params<VEC>(a, c0, p.on, ga, be);
     const int64_t at = n * a.G + blk * a.gw;
 #pragma unroll
@@ -500,23 +513,28 @@ __global__ __launch_bounds__(kHeldThreads) void norm_backward_fold(NormArgs a) {
     }
 #pragma unroll
     for (int i = 0; i < 2 * VEC; ++i) v[i] = 0.0f;
+    // dz as raw bits of dy's type: relu's is dy or zero, exactly
+    by_act(a.act, [&](auto act) {
+        constexpr int kAct = decltype(act)::value;
 #pragma unroll
-    for (int k = 0; k < KP; ++k)
-        if (p.on && p.r + k * p.rows < a.S) {
-            xv[k].unpack(f);
-            dv[k].unpack(d);
+        for (int k = 0; k < KP; ++k)
+            if (p.on && p.r + k * p.rows < a.S) {
+                xv[k].unpack(f);
+                dv[k].unpack(d);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const float hat = (f[i] - mu[i / W]) * rs[i / W];
-                const float dz = back_act(d[i], hat * ga[i] + be[i], a.act);
-                v[i] += dz;
-                v[VEC + i] = __builtin_fmaf(dz, hat, v[VEC + i]);
-                if constexpr (kKeep) {
-                    hats[k][i] = hat;
-                    dzs[k][i] = dz;
+                for (int i = 0; i < VEC; ++i) {
+                    const float c = f[i] - mu[i / W], hat = c * rs[i / W];
+                    if constexpr (kAct != GMC_ACT_NONE) d[i] = back_act(d[i], hat * ga[i] + be[i], kAct);
+                    v[i] += d[i];
+                    v[VEC + i] = __builtin_fmaf(d[i], hat, v[VEC + i]);
+                    if constexpr (kKeep) {
+                        xs[k][i] = c;
+                        dzs[k][i] = d[i];
+                    }
                 }
+                if constexpr (!kKeep && kAct == GMC_ACT_RELU) dv[k].pack(d);
             }
-        }
+    });
     int first = 0, left = 2 * VEC;
     const int lane = threadIdx.x & 63;
     scatter_sums<2 * VEC>(v, lane, 1 << a.tp_log2, 32, first, left);
@@ -544,37 +562,42 @@ __global__ __launch_bounds__(kHeldThreads) void norm_backward_fold(NormArgs a) {
         if (some && (c & (a.cpg - 1)) == 0) stat[which * a.gw + (c >> a.cpg_log2)] = t * a.inv_m;
     }
     __syncthreads();
-    float s1[F], s2[F];
+    // dx = rstd (gamma dz - s1/m - hat s2/m) = (rstd gamma) dz + (x - mean) b + c
+    float gb[F], gc[F];
 #pragma unroll
     for (int i = 0; i < F; ++i) {
-        s1[i] = p.on ? stat[g0 + i] : 0.0f;
-        s2[i] = p.on ? stat[a.gw + g0 + i] : 0.0f;
+        gc[i] = p.on ? -rs[i] * stat[g0 + i] : 0.0f;
+        gb[i] = p.on ? -rs[i] * rs[i] * stat[a.gw + g0 + i] : 0.0f;
     }
+    by_act(a.act, [&](auto act) {
+        constexpr int kAct = decltype(act)::value;
 #pragma unroll
-    for (int k = 0; k < KP; ++k) {
-        const int s = p.r + k * p.rows;
-        if (p.on && s < a.S) {
-            if constexpr (!kKeep) {
-                xv[k].unpack(f);
-                dv[k].unpack(d);
-            }
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const int g = i / W;
-                float hat, dz;
-                if constexpr (kKeep) {
-                    hat = hats[k][i];
-                    dz = dzs[k][i];
-                } else {
-                    hat = (f[i] - mu[g]) * rs[g];
-                    dz = back_act(d[i], hat * ga[i] + be[i], a.act);
+        for (int k = 0; k < KP; ++k) {
+            const int s = p.r + k * p.rows;
+            if (p.on && s < a.S) {
+                if constexpr (!kKeep) {
+                    xv[k].unpack(f);
+                    dv[k].unpack(d);
                 }
-                f[i] = rs[g] * (dz * ga[i] - __builtin_fmaf(hat, s2[g], s1[g]));
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    const int g = i / W;
+                    float c, dz;
+                    if constexpr (kKeep) {
+                        c = xs[k][i];
+                        dz = dzs[k][i];
+                    } else {
+                        c = f[i] - mu[g];
+                        dz = d[i];
+                        if constexpr (kAct == GMC_ACT_SILU) dz = back_act(dz, c * rs[g] * ga[i] + be[i], kAct);
+                    }
+                    f[i] = __builtin_fmaf(dz, rs[g] * ga[i], __builtin_fmaf(c, gb[g], gc[g]));
+                }
+                xv[k].pack(f);
+                xv[k].store(po + s * a.out_pixel);
             }
-            xv[k].pack(f);
-            xv[k].store(po + s * a.out_pixel);
         }
-    }
+    });
 }
 
 // -- split form ---------------------------------------------------------------
