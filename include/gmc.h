@@ -525,7 +525,7 @@ gmc_status gmc_calib_stream(void* hip_stream, float* e_dev, const float* g_dev, 
  *   - Pitches count elements.  Any element alignment is accepted.  The
  *     innermost axis (columns, channels, vocabulary) is contiguous.
  *   - Sums are taken in a fixed order: the same call gives the same bits (the
- *     losses' order follows the logits' alignment to 16 bytes).
+ *     losses' order follows the pitches).
  *   - An output may be an input's own buffer where the call says so, with the
  *     same pitches; overlaps of another kind are refused.
  *   - Invalid arguments return GMC_EINVAL before any device work, reported

@@ -4,10 +4,15 @@
 //
 // Both gradients have the form  dlogits_j = c (delta_jy - p_j)  with p the
 // token's softmax and c a scalar of the token.  A row of logits is a token's
-// vocabulary; with M its maximum, e_j = 2^((x_j - M) L), L = log2(e) / tau, and
-// s = sum e_j:  log p_y = ((x_y - M) L - log2 s) ln 2  and  c p_j = (c / s) e_j.
-// The maximum is subtracted first, so that any finite logits are in range
-// (rows at the type's lowest value among them) and -inf entries give zeros.
+// vocabulary; with e_j = 2^((x_j - b) L), L = log2(e) / tau, and s = sum e_j for
+// any shift b:  log p_y = ((x_y - b) L - log2 s) ln 2  and  c p_j = (c / s) e_j.
+//
+// The shift: b = 0 while s stays within [2^-40, 2^60], where every e_j that
+// counts is a normal number and no value has been lost; this spares a pass for
+// the maximum.  A row outside that range (logits beyond about 40 or all below
+// about -27, infinities, NaN) is taken again with b its maximum, for which any
+// finite logits are in range (rows at the type's lowest value among them); -inf
+// entries give zeros either way.
 //
 // Policy: c depends on the token alone, so a workgroup keeps the row in its
 // registers: the logits are read once and the gradient is written once, the
@@ -16,37 +21,57 @@
 // Ignored tokens' logits are never read, and their gradient is zero.
 #include <math.h>
 
+#include <type_traits>
+
 #include "gmc_ops.h"
 
 namespace gmc {
 
 namespace {
 
-constexpr int kHeldVecs = 8;         // vectors of a row a thread holds ...
-constexpr int kHeldVecsLong = 16;    // ... of a long one
-constexpr int kRowThreads = 1024;
-constexpr int kStatThreads = 1024;
+constexpr int kRowThreads = 1024;    // rows that no workgroup's registers hold
+constexpr int kStatThreads = 256;    // preference rows
+constexpr float kLeast = 0x1p-40f, kGreatest = 0x1p60f;  // a sum of unshifted e_j in range
+
+// The row of a workgroup, or of a wavefront where four share one; the same value
+// in every lane, so that what follows from it stays in scalar registers.  The
+// workgroups go to the 8 XCDs in turn; each XCD takes a run of neighbouring rows
+// (a plain copy of 100 KB rows: 5.9 TB/s, in the launch's order 5.6).
+template <int kThreads>
+__device__ __forceinline__ int64_t row_of() {
+    const int64_t id = xcd_run(gridDim.x);
+    if constexpr (kThreads == 64) return id * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    else return id;
+}
 
 // A row of V elements as a head and a tail of single elements and a body of
-// 16-byte aligned vectors.
-template <int DT>
+// vectors.  The body begins where the row, or where one is written its gradient,
+// `at` elements from the start of its tensor, crosses a line (16 bytes where a wavefront has a row of its own):
+// a wavefront's stores then cover whole lines; with lines split between two of
+// them the copy above takes 5% longer.  It follows the pitches, not the pointers,
+// so that a row's sums have one order wherever the tensors lie.
+template <int DT, int kThreads>
 struct Row {
     typedef typename Elem<DT>::T T;
-    static constexpr int N = 16 / Elem<DT>::kSize;
+    static constexpr int kSize = Elem<DT>::kSize;
+    static constexpr int N = 16 / kSize;
+    static constexpr int kAlign = kThreads == 64 ? 16 : 128;
     const T* p;
     int V, head, nb, tail;
 
-    __device__ __forceinline__ Row(const T* q, int v) : p(q), V(v) {
-        const int off = (int)((reinterpret_cast<uintptr_t>(q) & 15u) / Elem<DT>::kSize);
-        head = off ? N - off : 0;
+    __device__ __forceinline__ Row(const T* q, int v, int64_t at) : p(q), V(v) {
+        constexpr int kStep = kAlign / kSize;
+        const int off = (int)(at & (kStep - 1));
+        head = off ? kStep - off : 0;
         if (head > V) head = V;
         nb = (V - head) / N;
         tail = V - head - nb * N;
     }
     // The index of thread `tid`'s single element, -1 for most threads.
     __device__ __forceinline__ int edge(int tid) const {
+        constexpr int kTail = kThreads == 64 ? 32 : 64;
         if (tid < head) return tid;
-        if (tid >= 32 && tid < 32 + tail) return V - tail + (tid - 32);
+        if (tid >= kTail && tid < kTail + tail) return V - tail + (tid - kTail);
         return -1;
     }
 };
@@ -73,6 +98,28 @@ __device__ __forceinline__ void join_stats(float L, float& m, float& s, float2* 
     s = t;
 }
 
+// The sum over the row's threads, in every thread; one barrier.
+template <int kWaves>
+__device__ __forceinline__ float row_sum(float s, float* lds) {
+    s = wave_sum(s);
+    if (kWaves == 1) return s;
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
+    __syncthreads();
+    s = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) s += lds[w];
+    return s;
+}
+
+__device__ __forceinline__ bool in_range(float s) { return s >= kLeast && s <= kGreatest; }
+
+// Unshifted e_j of a vector.
+template <int N>
+__device__ __forceinline__ void exps(float (&f)[N], float L) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = exp2_fast(f[i] * L);
+}
+
 // e_j of a vector, the maximum subtracted.
 template <int N>
 __device__ __forceinline__ void exps(float (&f)[N], float base, float L) {
@@ -82,8 +129,8 @@ __device__ __forceinline__ void exps(float (&f)[N], float base, float L) {
 
 // (max, sum) over the thread's share of a row, read in passes of four vectors.
 template <int DT, int kThreads>
-__device__ __forceinline__ void stream_stats(const Row<DT>& row, int tid, float L, float& m, float& s) {
-    constexpr int N = Row<DT>::N;
+__device__ __forceinline__ void stream_stats(const Row<DT, kThreads>& row, int tid, float L, float& m, float& s) {
+    constexpr int N = 16 / Elem<DT>::kSize;
     typedef Vec<DT, N> V;
     m = -INFINITY;
     s = 0.0f;
@@ -97,7 +144,7 @@ __device__ __forceinline__ void stream_stats(const Row<DT>& row, int tid, float 
         float f[N];
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-            if (v0 + k * kThreads < row.nb) x[k] = V::load(row.p + row.head + (int64_t)(v0 + k * kThreads) * N);
+            if (v0 + k * kThreads < row.nb) x[k] = V::load_once(row.p + row.head + (int64_t)(v0 + k * kThreads) * N);
         float cm = m;
 #pragma unroll
         for (int k = 0; k < 4; ++k)
@@ -120,11 +167,12 @@ __device__ __forceinline__ void stream_stats(const Row<DT>& row, int tid, float 
     }
 }
 
-// A vector of the gradient: c (delta - p), at = the label's place in it or
-// outside [0, N).
-template <int N>
+// A vector of the gradient: c (delta - p), k = -c / s, at = the label's place
+// in it or outside [0, N).
+template <int N, bool kShift>
 __device__ __forceinline__ void gradient(float (&f)[N], float base, float L, float k, float c, int at) {
-    exps<N>(f, base, L);
+    if constexpr (kShift) exps<N>(f, base, L);
+    else exps<N>(f, L);
 #pragma unroll
     for (int i = 0; i < N; ++i) f[i] = f[i] * k;
     if ((unsigned)at < (unsigned)N)
@@ -133,52 +181,109 @@ __device__ __forceinline__ void gradient(float (&f)[N], float base, float L, flo
             if (i == at) f[i] += c;
 }
 
-template <int DT>
-__device__ __forceinline__ void zero_row(typename Elem<DT>::T* out, int V, int tid, int threads) {
-    constexpr int N = Row<DT>::N;
-    const Row<DT> row(out, V);
+// A vector of -inf.
+template <int DT, int N>
+__device__ __forceinline__ Vec<DT, N> nothing() {
+    Vec<DT, N> v;
+    const uint32_t w = DT == GMC_F32 ? 0xff800000u : DT == GMC_BF16 ? 0xff80ff80u : 0xfc00fc00u;
+#pragma unroll
+    for (int i = 0; i < Vec<DT, N>::kBytes / 4; ++i) v.set_word(i, w);
+    return v;
+}
+
+template <int DT, int kThreads>
+__device__ __forceinline__ void zero_row(typename Elem<DT>::T* out, int V, int64_t at, int tid) {
+    const Row<DT, kThreads> row(out, V, at);
+    constexpr int N = row.N;
     Vec<DT, N> z;
     const float f[N] = {};
     z.pack(f);
-    for (int v = tid; v < row.nb; v += threads) z.store(out + row.head + (int64_t)v * N);
+    for (int v = tid; v < row.nb; v += kThreads) z.store_once(out + row.head + (int64_t)v * N);
     const int e = row.edge(tid);
     if (e >= 0) out[e] = Elem<DT>::down(0.0f);
 }
 
 // The gradient of a row read from memory, element by element in its own thread
 // (so it may be written over the logits).
-template <int DT>
-__device__ __forceinline__ void stream_gradient(const Row<DT>& row, typename Elem<DT>::T* out, int tid, int threads,
+template <int DT, int kThreads, bool kShift>
+__device__ __forceinline__ void stream_gradient(const Row<DT, kThreads>& row, typename Elem<DT>::T* out, int tid,
                                                 float base, float L, float k, float c, int y) {
-    constexpr int N = Row<DT>::N;
+    constexpr int N = 16 / Elem<DT>::kSize;
+    constexpr int threads = kThreads;
     typedef Vec<DT, N> V;
     for (int v0 = tid; v0 < row.nb; v0 += 4 * threads) {
         V x[4];
         float f[N];
 #pragma unroll
         for (int u = 0; u < 4; ++u)
-            if (v0 + u * threads < row.nb) x[u] = V::load(row.p + row.head + (int64_t)(v0 + u * threads) * N);
+            if (v0 + u * threads < row.nb) x[u] = V::load_once(row.p + row.head + (int64_t)(v0 + u * threads) * N);
 #pragma unroll
         for (int u = 0; u < 4; ++u)
             if (v0 + u * threads < row.nb) {
                 const int j = row.head + (v0 + u * threads) * N;
                 x[u].unpack(f);
-                gradient<N>(f, base, L, k, c, y - j);
+                gradient<N, kShift>(f, base, L, k, c, y - j);
                 x[u].pack(f);
-                x[u].store(out + j);
+                x[u].store_once(out + j);
             }
     }
     const int e = row.edge(tid);
     if (e >= 0) {
         float f[1] = {Elem<DT>::up(row.p[e])};
-        gradient<1>(f, base, L, k, c, y - e);
+        gradient<1, kShift>(f, base, L, k, c, y - e);
         out[e] = Elem<DT>::down(f[0]);
     }
 }
 
+// The gradient of the row `in` with shift and sum st, in place or not.
+template <int DT, int kThreads>
+__device__ __forceinline__ void write_gradient(const typename Elem<DT>::T* in, typename Elem<DT>::T* out, int V,
+                                               int64_t at, int tid, float2 st, float L, float c, int y) {
+    const Row<DT, kThreads> row(in, V, at);
+    if (st.x == 0.0f) stream_gradient<DT, kThreads, false>(row, out, tid, 0.0f, L, -c / st.y, c, y);
+    else stream_gradient<DT, kThreads, true>(row, out, tid, st.x == -INFINITY ? 0.0f : st.x, L, -c / st.y, c, y);
+}
+
+// A row's shift and sum, read from memory: (0, s) in range, else with the maximum.
+template <int DT, int kThreads>
+__device__ __forceinline__ float2 stream_row(const Row<DT, kThreads>& row, int tid, float L, float2* lds) {
+    constexpr int N = 16 / Elem<DT>::kSize;
+    constexpr int kWaves = kThreads / 64;
+    constexpr int kBatch = 8;
+    typedef Vec<DT, N> V;
+    const int e = row.edge(tid);
+    float s = e >= 0 ? exp2_fast(Elem<DT>::up(row.p[e]) * L) : 0.0f;
+    for (int v0 = tid; v0 < row.nb; v0 += kBatch * kThreads) {
+        V x[kBatch];
+        float f[N];
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k)
+            if (v0 + k * kThreads < row.nb) x[k] = V::load_once(row.p + row.head + (int64_t)(v0 + k * kThreads) * N);
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k)
+            if (v0 + k * kThreads < row.nb) {
+                x[k].unpack(f);
+                exps<N>(f, L);
+#pragma unroll
+                for (int i = 0; i < N; ++i) s += f[i];
+            }
+    }
+    s = row_sum<kWaves>(s, reinterpret_cast<float*>(lds));
+    if (in_range(s)) return make_float2(0.0f, s);
+    float m;
+    stream_stats<DT, kThreads>(row, tid, L, m, s);
+    if (kWaves > 1) __syncthreads();  // the sums are read
+    join_stats<kWaves>(L, m, s, lds);
+    return make_float2(m, s);
+}
+
+// log p_y of a row with shift M (-inf: all entries are) and sum s.  The power of two
+// of s meets the exponent exactly; only its logarithm's fraction is rounded.
 __device__ __forceinline__ float logp_of(float xy, float M, float L, float s) {
     const float base = M == -INFINITY ? 0.0f : M;
-    return ((xy - base) * L - __log2f(s)) * kLn2;
+    int k;
+    const float f = frexpf(s, &k);
+    return (__builtin_fmaf(xy - base, L, -(float)k) - __log2f(f)) * kLn2;
 }
 
 // -- policy -------------------------------------------------------------------
@@ -233,110 +338,171 @@ __global__ __launch_bounds__(1024) void policy_weight(PolicyArgs a, float* weigh
     }
 }
 
-// What a token adds to the loss, and c.
+// A token's inputs, loaded ahead of the row's sum.
 struct Token {
-    float logp, loss, kl, clipped, c;
+    float w, A, old, ref;
 };
 
-__device__ __forceinline__ Token policy_token(const PolicyArgs& a, int64_t r, int64_t t, float logp) {
+__device__ __forceinline__ Token policy_token(const PolicyArgs& a, int64_t r, int64_t t) {
     Token k;
-    float w = a.weight[0];
-    if (a.by_sequence) w = w / a.weight[1 + r];
-    const float A = a.adv[r * a.adv_seq + t * a.adv_tok];
-    const float ratio = a.old_logp ? expf(logp - a.old_logp[r * a.T + t]) : logp == logp ? 1.0f : NAN;
-    const float unclipped = ratio * A;
-    const float clipped = fminf(fmaxf(ratio, 1.0f - a.lo), 1.0f + a.hi) * A;
-    const bool free = !(unclipped > clipped);  // the smaller one, which the gradient follows
-    float slope = free ? -unclipped : 0.0f;
-    float kl = 0.0f;
-    if (a.ref_logp) {
-        const float d = a.ref_logp[r * a.T + t] - logp;
-        const float e = expm1f(d);
-        kl = e - d;
-        slope = slope - a.kl * e;
-    }
-    k.logp = logp;
-    k.loss = w * (-(free ? unclipped : clipped) + a.kl * kl);
-    k.kl = w * kl;
-    k.clipped = free ? 0.0f : w;
-    k.c = a.scale * a.inv_tau * w * slope;
+    k.w = a.by_sequence ? a.weight[0] / a.weight[1 + r] : a.weight[0];
+    k.A = a.adv[r * a.adv_seq + t * a.adv_tok];
+    k.old = a.old_logp ? a.old_logp[r * a.T + t] : 0.0f;
+    k.ref = a.ref_logp ? a.ref_logp[r * a.T + t] : 0.0f;
     return k;
 }
 
-__device__ __forceinline__ void policy_write(const PolicyArgs& a, int64_t i, const Token& k) {
-    a.logp[i] = k.logp;
-    a.tokens[i] = make_float4(k.loss, k.kl, k.clipped, 0.0f);
+// What the clipped term is: the ratio's product, the smaller of the two, and
+// whether that is the unclipped one, which the gradient follows.
+struct Clip {
+    float unclipped, smaller;
+    bool free;
+};
+
+__device__ __forceinline__ Clip policy_clip(const PolicyArgs& a, const Token& k, float logp) {
+    const float ratio = a.old_logp ? exp2_fast((logp - k.old) * kLog2e) : logp == logp ? 1.0f : NAN;
+    Clip c;
+    c.unclipped = ratio * k.A;
+    const float clipped = fminf(fmaxf(ratio, 1.0f - a.lo), 1.0f + a.hi) * k.A;
+    c.free = !(c.unclipped > clipped);
+    c.smaller = c.free ? c.unclipped : clipped;
+    return c;
+}
+
+// c: the loss's slope in the logits' log-probability, for the gradient.
+__device__ __forceinline__ float policy_slope(const PolicyArgs& a, const Token& k, float logp) {
+    const Clip c = policy_clip(a, k, logp);
+    float slope = c.free ? -c.unclipped : 0.0f;
+    if (a.ref_logp) slope = __builtin_fmaf(a.kl, 1.0f - exp2_fast((k.ref - logp) * kLog2e), slope);
+    return a.scale * a.inv_tau * k.w * slope;
+}
+
+// What the token adds to the loss, by one thread.
+__device__ __forceinline__ void policy_write(const PolicyArgs& a, int64_t i, const Token& k, float logp) {
+    const Clip c = policy_clip(a, k, logp);
+    float kl = 0.0f;
+    if (a.ref_logp) {
+        const float d = k.ref - logp;
+        kl = expm1f(d) - d;
+    }
+    a.logp[i] = logp;
+    a.tokens[i] = make_float4(k.w * (-c.smaller + a.kl * kl), k.w * kl, c.free ? 0.0f : k.w, 0.0f);
+}
+
+// A row's label, its logit (NaN where the label is out of range) and place (-1).
+template <int DT>
+struct Label {
+    int y;
+    float x;
+    __device__ __forceinline__ Label(const typename Elem<DT>::T* row, int V, int64_t label) {
+        const bool known = (uint64_t)label < (uint64_t)V;
+        y = known ? (int)label : -1;
+        x = known ? Elem<DT>::up(row[y]) : NAN;
+    }
+};
+
+template <int DT, int kThreads>
+__device__ __forceinline__ void policy_ignored(const PolicyArgs& a, int64_t i, int64_t at, int tid) {
+    if (tid == 0) {
+        a.logp[i] = 0.0f;
+        a.tokens[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    }
+    if (a.grad) zero_row<DT, kThreads>(static_cast<typename Elem<DT>::T*>(a.grad) + at, a.V, at, tid);
 }
 
 // One row of logits per kThreads threads, held in kHeld vectors a thread.
 template <int DT, int kThreads, int kHeld>
-__global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void policy_held(PolicyArgs a) {
+__global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) __attribute__((amdgpu_waves_per_eu(kHeld <= 13 ? 6 : 4)))
+void policy_held(PolicyArgs a) {
     typedef typename Elem<DT>::T T;
-    constexpr int N = Row<DT>::N;
+    constexpr int N = 16 / Elem<DT>::kSize;
     constexpr int kWaves = kThreads / 64;
     typedef Vec<DT, N> V;
     __shared__ float2 lds[kWaves];
     const int tid = threadIdx.x % kThreads;
-    const int64_t i = (int64_t)blockIdx.x * (blockDim.x / kThreads) + threadIdx.x / kThreads;
+    const int64_t i = row_of<kThreads>();
     if (i >= a.rows) return;
     const int64_t r = i / a.T, t = i - r * a.T;
     const int64_t label = a.labels[r * a.label_pitch + t];
-    T* out = static_cast<T*>(a.grad) + r * a.grad_seq + t * a.grad_tok;
+    const int64_t at = r * a.grad_seq + t * a.grad_tok;
+    T* out = static_cast<T*>(a.grad) + at;
     if (label == a.ignore) {
-        if (tid == 0) policy_write(a, i, Token{0.0f, 0.0f, 0.0f, 0.0f, 0.0f});
-        if (a.grad) zero_row<DT>(out, a.V, tid, kThreads);
+        policy_ignored<DT, kThreads>(a, i, at, tid);
         return;
     }
-    const Row<DT> row(static_cast<const T*>(a.logits) + r * a.seq + t * a.tok, a.V);
+    const T* in = static_cast<const T*>(a.logits) + r * a.seq + t * a.tok;
+    const Row<DT, kThreads> row(in, a.V, at);
+    // past the row's end a vector holds -inf, so that only loads and stores ask for the end
     V x[kHeld];
 #pragma unroll
     for (int k = 0; k < kHeld; ++k)
-        if (tid + k * kThreads < row.nb) x[k] = V::load(row.p + row.head + (int64_t)(tid + k * kThreads) * N);
+        if (k * kThreads < row.nb) {
+            x[k] = nothing<DT, N>();
+            if (tid + k * kThreads < row.nb) x[k] = V::load_once(row.p + row.head + (int64_t)(tid + k * kThreads) * N);
+        }
     const int e = row.edge(tid);
     const float ex = e >= 0 ? Elem<DT>::up(row.p[e]) : -INFINITY;
-    const bool known = (uint64_t)label < (uint64_t)a.V;
-    const int y = known ? (int)label : -1;
-    const float xy = known ? Elem<DT>::up(row.p[y]) : NAN;
-    float m = ex, s, f[N];
+    const Label<DT> lab(in, a.V, label);
+    const Token tk = policy_token(a, r, t);
+    float f[N], s = exp2_fast(ex * a.L), base = 0.0f;
 #pragma unroll
     for (int k = 0; k < kHeld; ++k)
-        if (tid + k * kThreads < row.nb) {
+        if (k * kThreads < row.nb) {
             x[k].unpack(f);
-#pragma unroll
-            for (int q = 0; q < N; ++q) m = fmaxf(m, f[q]);
-        }
-    // the wavefront's maximum first: its exponentials are then final up to a factor
-    m = wave_max(m);
-    const float own = m == -INFINITY ? 0.0f : m;
-    s = e >= 0 ? exp2_fast((ex - own) * a.L) : 0.0f;
-#pragma unroll
-    for (int k = 0; k < kHeld; ++k)
-        if (tid + k * kThreads < row.nb) {
-            x[k].unpack(f);
-            exps<N>(f, own, a.L);
+            exps<N>(f, a.L);
 #pragma unroll
             for (int q = 0; q < N; ++q) s += f[q];
         }
-    join_stats<kWaves>(a.L, m, s, lds);
-    const Token tk = policy_token(a, r, t, logp_of(xy, m, a.L, s));
-    if (tid == 0) policy_write(a, i, tk);
-    if (!a.grad) return;
-    const float base = m == -INFINITY ? 0.0f : m;
-    const float k1 = -tk.c / s;
+    s = row_sum<kWaves>(s, reinterpret_cast<float*>(lds));
+    const bool shifted = !in_range(s);
+    if (shifted) {
+        float m = ex;
 #pragma unroll
-    for (int k = 0; k < kHeld; ++k)
-        if (tid + k * kThreads < row.nb) {
-            const int j = row.head + (tid + k * kThreads) * N;
-            x[k].unpack(f);
-            gradient<N>(f, base, a.L, k1, tk.c, y - j);
-            x[k].pack(f);
-            x[k].store(out + j);
-        }
-    if (e >= 0) {
-        float g[1] = {ex};
-        gradient<1>(g, base, a.L, k1, tk.c, y - e);
-        out[e] = Elem<DT>::down(g[0]);
+        for (int k = 0; k < kHeld; ++k)
+            if (k * kThreads < row.nb) {
+                x[k].unpack(f);
+#pragma unroll
+                for (int q = 0; q < N; ++q) m = fmaxf(m, f[q]);
+            }
+        m = wave_max(m);
+        const float own = m == -INFINITY ? 0.0f : m;
+        s = exp2_fast((ex - own) * a.L);
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k)
+            if (k * kThreads < row.nb) {
+                x[k].unpack(f);
+                exps<N>(f, own, a.L);
+#pragma unroll
+                for (int q = 0; q < N; ++q) s += f[q];
+            }
+        if (kWaves > 1) __syncthreads();  // the sums are read
+        join_stats<kWaves>(a.L, m, s, lds);
+        base = m;
     }
+    const float logp = logp_of(lab.x, base, a.L, s);
+    if (tid == 0) policy_write(a, i, tk, logp);
+    if (!a.grad) return;
+    const float c = policy_slope(a, tk, logp), k1 = -c / s;
+    if (base == -INFINITY) base = 0.0f;
+    const auto write = [&](auto shift) {
+        constexpr bool kShift = decltype(shift)::value;
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k)
+            if (k * kThreads < row.nb) {
+                const int j = row.head + (tid + k * kThreads) * N;
+                x[k].unpack(f);
+                gradient<N, kShift>(f, base, a.L, k1, c, lab.y - j);
+                x[k].pack(f);
+                if (tid + k * kThreads < row.nb) x[k].store_once(out + j);
+            }
+        if (e >= 0) {
+            float g[1] = {ex};
+            gradient<1, kShift>(g, base, a.L, k1, c, lab.y - e);
+            out[e] = Elem<DT>::down(g[0]);
+        }
+    };
+    if (shifted) write(std::true_type{});
+    else write(std::false_type{});
 }
 
 // Rows longer than a workgroup's registers: two reads.
@@ -344,25 +510,22 @@ template <int DT>
 __global__ __launch_bounds__(kRowThreads) void policy_long(PolicyArgs a) {
     typedef typename Elem<DT>::T T;
     __shared__ float2 lds[kRowThreads / 64];
-    const int64_t i = blockIdx.x, r = i / a.T, t = i - r * a.T;
+    const int64_t i = row_of<kRowThreads>(), r = i / a.T, t = i - r * a.T;
     const int64_t label = a.labels[r * a.label_pitch + t];
-    T* out = static_cast<T*>(a.grad) + r * a.grad_seq + t * a.grad_tok;
+    const int64_t at = r * a.grad_seq + t * a.grad_tok;
+    T* out = static_cast<T*>(a.grad) + at;
     if (label == a.ignore) {
-        if (threadIdx.x == 0) policy_write(a, i, Token{0.0f, 0.0f, 0.0f, 0.0f, 0.0f});
-        if (a.grad) zero_row<DT>(out, a.V, threadIdx.x, kRowThreads);
+        policy_ignored<DT, kRowThreads>(a, i, at, threadIdx.x);
         return;
     }
-    const Row<DT> row(static_cast<const T*>(a.logits) + r * a.seq + t * a.tok, a.V);
-    const bool known = (uint64_t)label < (uint64_t)a.V;
-    const int y = known ? (int)label : -1;
-    const float xy = known ? Elem<DT>::up(row.p[y]) : NAN;
-    float m, s;
-    stream_stats<DT, kRowThreads>(row, threadIdx.x, a.L, m, s);
-    join_stats<kRowThreads / 64>(a.L, m, s, lds);
-    const Token tk = policy_token(a, r, t, logp_of(xy, m, a.L, s));
-    if (threadIdx.x == 0) policy_write(a, i, tk);
-    if (a.grad)
-        stream_gradient<DT>(row, out, threadIdx.x, kRowThreads, m == -INFINITY ? 0.0f : m, a.L, -tk.c / s, tk.c, y);
+    const T* in = static_cast<const T*>(a.logits) + r * a.seq + t * a.tok;
+    const Label<DT> lab(in, a.V, label);
+    const Token tk = policy_token(a, r, t);
+    const float2 st = stream_row<DT, kRowThreads>({in, a.V, at}, threadIdx.x, a.L, lds);
+    const float logp = logp_of(lab.x, st.x, a.L, st.y);
+    if (threadIdx.x == 0) policy_write(a, i, tk, logp);
+    if (!a.grad) return;
+    write_gradient<DT, kRowThreads>(in, out, a.V, at, threadIdx.x, st, a.L, policy_slope(a, tk, logp), lab.y);
 }
 
 // The three sums over the tokens, in 64 bits and a fixed order.
@@ -406,7 +569,7 @@ struct PrefArgs {
     float* logp;       // [2P][T]
     float* rewards;    // [2P]
     float* pair_loss;  // [P]
-    float2* stats;     // [2P][T] (max, sum)
+    float2* stats;     // [2P][T] (shift, sum)
     float* coef;       // [2P]
 };
 
@@ -422,7 +585,7 @@ __global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void pref_logp(Pre
     constexpr int kWaves = kThreads / 64;
     __shared__ float2 lds[kWaves];
     const int tid = threadIdx.x % kThreads;
-    const int64_t i = (int64_t)blockIdx.x * (blockDim.x / kThreads) + threadIdx.x / kThreads;
+    const int64_t i = row_of<kThreads>();
     if (i >= 2 * a.pairs * a.T) return;
     const int64_t local = i / a.T, t = i - local * a.T, r = pref_sequence(a, local);
     const int64_t label = a.labels[r * a.label_pitch + t];
@@ -430,15 +593,13 @@ __global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void pref_logp(Pre
         if (tid == 0) a.logp[r * a.T + t] = 0.0f;
         return;
     }
-    const Row<DT> row(static_cast<const T*>(a.logits) + r * a.seq + t * a.tok, a.V);
-    const bool known = (uint64_t)label < (uint64_t)a.V;
-    const float xy = known ? Elem<DT>::up(row.p[label]) : NAN;
-    float m, s;
-    stream_stats<DT, kThreads>(row, tid, kLog2e, m, s);
-    join_stats<kWaves>(kLog2e, m, s, lds);
+    const int64_t at = r * a.seq + t * a.tok;  // nothing is written: whole lines are read
+    const T* in = static_cast<const T*>(a.logits) + at;
+    const Label<DT> lab(in, a.V, label);
+    const float2 st = stream_row<DT, kThreads>({in, a.V, at}, tid, kLog2e, lds);
     if (tid == 0) {
-        a.logp[r * a.T + t] = logp_of(xy, m, kLog2e, s);
-        a.stats[r * a.T + t] = make_float2(m, s);
+        a.logp[r * a.T + t] = logp_of(lab.x, st.x, kLog2e, st.y);
+        a.stats[r * a.T + t] = st;
     }
 }
 
@@ -499,20 +660,19 @@ template <int DT, int kThreads>
 __global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void pref_gradient(PrefArgs a) {
     typedef typename Elem<DT>::T T;
     const int tid = threadIdx.x % kThreads;
-    const int64_t i = (int64_t)blockIdx.x * (blockDim.x / kThreads) + threadIdx.x / kThreads;
+    const int64_t i = row_of<kThreads>();
     if (i >= 2 * a.pairs * a.T) return;
     const int64_t local = i / a.T, t = i - local * a.T, r = pref_sequence(a, local);
     const int64_t label = a.labels[r * a.label_pitch + t];
-    T* out = static_cast<T*>(a.grad) + r * a.grad_seq + t * a.grad_tok;
+    const int64_t at = r * a.grad_seq + t * a.grad_tok;
+    T* out = static_cast<T*>(a.grad) + at;
     if (label == a.ignore) {
-        zero_row<DT>(out, a.V, tid, kThreads);
+        zero_row<DT, kThreads>(out, a.V, at, tid);
         return;
     }
-    const Row<DT> row(static_cast<const T*>(a.logits) + r * a.seq + t * a.tok, a.V);
-    const float2 st = a.stats[r * a.T + t];
-    const float c = a.coef[r];
     const int y = (uint64_t)label < (uint64_t)a.V ? (int)label : -1;
-    stream_gradient<DT>(row, out, tid, kThreads, st.x == -INFINITY ? 0.0f : st.x, kLog2e, -c / st.y, c, y);
+    write_gradient<DT, kThreads>(static_cast<const T*>(a.logits) + r * a.seq + t * a.tok, out, a.V, at, tid,
+                                 a.stats[r * a.T + t], kLog2e, a.coef[r], y);
 }
 
 __global__ __launch_bounds__(1024) void pref_mean(const float* pair_loss, int64_t P, float* loss) {
@@ -608,8 +768,8 @@ gmc_status gmc_policy_loss(void* hip_stream, int32_t dtype, int64_t R, int64_t T
         a.grad = grad_dev;
         a.seq = seq_pitch;
         a.tok = tok_pitch;
-        a.grad_seq = grad_seq;
-        a.grad_tok = grad_tok;
+        a.grad_seq = grad_dev ? grad_seq : T * V;  // no gradient: the order of a contiguous one
+        a.grad_tok = grad_dev ? grad_tok : V;
         a.labels = labels_dev;
         a.label_pitch = label_pitch;
         a.ignore = ignore;
@@ -635,10 +795,12 @@ gmc_status gmc_policy_loss(void* hip_stream, int32_t dtype, int64_t R, int64_t T
         const int64_t vecs = V * type_size(dtype) / 16;  // at most, whatever the alignment
         const dim3 rows((unsigned)a.rows), quads((unsigned)((a.rows + 3) / 4));
         GMC_BY_TYPE(dtype, {
-            if (vecs <= 64 * kHeldVecs) policy_held<DT, 64, kHeldVecs><<<quads, 256, 0, st>>>(a);
-            else if (vecs <= 256 * kHeldVecs) policy_held<DT, 256, kHeldVecs><<<rows, 256, 0, st>>>(a);
-            else if (vecs <= 1024 * kHeldVecs) policy_held<DT, 1024, kHeldVecs><<<rows, 1024, 0, st>>>(a);
-            else if (vecs <= 1024 * kHeldVecsLong) policy_held<DT, 1024, kHeldVecsLong><<<rows, 1024, 0, st>>>(a);
+            if (vecs <= 64 * 8) policy_held<DT, 64, 8><<<quads, 256, 0, st>>>(a);
+            else if (vecs <= 256 * 8) policy_held<DT, 256, 8><<<rows, 256, 0, st>>>(a);
+            else if (vecs <= 512 * 8) policy_held<DT, 512, 8><<<rows, 512, 0, st>>>(a);
+            else if (vecs <= 512 * 13) policy_held<DT, 512, 13><<<rows, 512, 0, st>>>(a);
+            else if (vecs <= 512 * 26) policy_held<DT, 512, 26><<<rows, 512, 0, st>>>(a);
+            else if (vecs <= 1024 * 20) policy_held<DT, 1024, 20><<<rows, 1024, 0, st>>>(a);
             else policy_long<DT><<<rows, kRowThreads, 0, st>>>(a);
         });
     }
@@ -701,12 +863,12 @@ gmc_status gmc_preference_loss(void* hip_stream, int32_t dtype, int64_t P, int64
         const dim3 rows((unsigned)tokens), quads((unsigned)((tokens + 3) / 4));
         GMC_BY_TYPE(dtype, {
             if (tokens) {
-                if (vecs <= 64 * kHeldVecs) pref_logp<DT, 64><<<quads, 256, 0, st>>>(a);
+                if (vecs <= 64 * 8) pref_logp<DT, 64><<<quads, 256, 0, st>>>(a);
                 else pref_logp<DT, kStatThreads><<<rows, kStatThreads, 0, st>>>(a);
             }
             pref_pair<<<dim3((unsigned)P), 256, 0, st>>>(a);
             if (tokens && a.grad) {
-                if (vecs <= 64 * kHeldVecs) pref_gradient<DT, 64><<<quads, 256, 0, st>>>(a);
+                if (vecs <= 64 * 8) pref_gradient<DT, 64><<<quads, 256, 0, st>>>(a);
                 else pref_gradient<DT, kStatThreads><<<rows, kStatThreads, 0, st>>>(a);
             }
         });

@@ -333,14 +333,6 @@ __global__ __launch_bounds__(kHeldThreads) void norm_backward_held(NormArgs a) {
 // statistics are formed once a group, and the unpacked values stay in registers
 // where a thread has few vectors.
 
-// This workgroup's image and channel block.  Workgroups go to the 8 XCDs in
-// turn; each XCD takes a run of neighbouring blocks, so that blocks narrower
-// than a line share it in one L2.
-__device__ __forceinline__ int64_t xcd_run(unsigned total) {
-    const unsigned x = blockIdx.x & 7u, j = blockIdx.x >> 3, q = total >> 3, r = total & 7u;
-    return (int64_t)x * q + (x < r ? x : r) + j;
-}
-
 // The sums of F values over the lanes that share them: the pixel lanes and,
 // where a group is wider than a vector, its neighbours (`within` lanes).
 template <int F>
@@ -362,6 +354,7 @@ __global__ __launch_bounds__(kHeldThreads) void norm_forward_fold(NormArgs a) {
     constexpr bool kKeep = KP <= 8;
     typedef Vec<DT, VEC> V;
     const Place p = place(a);
+    // blocks narrower than a line share it in one XCD's cache
     const int64_t id = xcd_run(gridDim.x), n = id / (unsigned)a.blocks;
     const int blk = (int)(id - n * a.blocks);
     const int c0 = blk * a.cb + p.cv * VEC;
@@ -484,6 +477,7 @@ __global__ __launch_bounds__(kHeldThreads) void norm_backward_fold(NormArgs a) {
     constexpr bool kKeep = KP <= 2;
     typedef Vec<DT, VEC> V;
     const Place p = place(a);
+    // blocks narrower than a line share it in one XCD's cache
     const int64_t id = xcd_run(gridDim.x), n = id / (unsigned)a.blocks;
     const int blk = (int)(id - n * a.blocks);
     const int c0 = blk * a.cb + p.cv * VEC;

@@ -114,6 +114,13 @@ struct Vec {
         return r;
     }
     __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<U*>(p) = raw; }
+    // The same for data that is touched once (nontemporal).
+    static __device__ __forceinline__ Vec load_once(const T* p) {
+        Vec r;
+        r.raw = __builtin_nontemporal_load(reinterpret_cast<const U*>(p));
+        return r;
+    }
+    __device__ __forceinline__ void store_once(T* p) const { __builtin_nontemporal_store(raw, reinterpret_cast<U*>(p)); }
 
     __device__ __forceinline__ uint32_t word(int i) const {
         if constexpr (kBytes <= 4) return (uint32_t)raw;
@@ -160,6 +167,13 @@ __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
     return v;
+}
+
+// This workgroup's number among `total`, so numbered that each XCD has a run of
+// neighbours: workgroups go to the 8 XCDs in turn, each with a cache of its own.
+__device__ __forceinline__ int64_t xcd_run(unsigned total) {
+    const unsigned x = blockIdx.x & 7u, j = blockIdx.x >> 3, q = total >> 3, r = total & 7u;
+    return (int64_t)x * q + (x < r ? x : r) + j;
 }
 
 constexpr float kLog2e = 1.44269504088896341f;
