@@ -29,6 +29,8 @@ namespace gmc {
 
 namespace {
 
+constexpr int kFinishBlocks = 32;     // workgroups that add the tokens' shares of the loss
+constexpr int64_t kFewTokens = 65536, kFewSequences = 256;  // counted by one workgroup
 constexpr int kRowThreads = 1024;    // rows that no workgroup's registers hold
 constexpr int kStatThreads = 256;    // preference rows
 constexpr float kLeast = 0x1p-40f, kGreatest = 0x1p60f;  // a sum of unshifted e_j in range
@@ -305,36 +307,58 @@ struct PolicyArgs {
     float* logp;
     const float* weight;  // [R] one token's weight, or [1]
     float4* tokens;       // per token: weighted loss, KL, clipped
+    double* sums;         // [3][kFinishBlocks]
+    int* done;            // workgroups of the last launch that have added theirs
+    float* stats;
 };
 
-// Weights of the mean over tokens, or of the mean over sequences of their
-// means: how many tokens each sequence keeps (one wavefront a sequence) ...
+// Weights of the mean over tokens, or of the mean over sequences of their means:
+// weight[0] the reciprocal of all tokens that count, or of the sequences with any;
+// weight[1 + r] the tokens of sequence r.  One workgroup, a wavefront a sequence at
+// a time, four loads in flight; with many tokens the sequences are counted first by
+// a launch of their own.
+__device__ __forceinline__ int count_labels(const int64_t* labels, int64_t T, int64_t ignore) {
+    int n = 0;
+#pragma unroll 4
+    for (int64_t t = threadIdx.x & 63; t < T; t += 64) n += labels[t] != ignore;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o);
+    return n;
+}
+
 __global__ __launch_bounds__(256) void policy_counts(PolicyArgs a, float* weight) {
     const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (r >= a.R) return;
-    int n = 0;
-    for (int64_t t = threadIdx.x & 63; t < a.T; t += 64) n += a.labels[r * a.label_pitch + t] != a.ignore;
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o);
+    const int n = count_labels(a.labels + r * a.label_pitch, a.T, a.ignore);
     if ((threadIdx.x & 63) == 0) weight[1 + r] = (float)n;
 }
 
-// ... and the reciprocal of all tokens, or of the sequences that keep any.
+template <bool kCounted>
 __global__ __launch_bounds__(1024) void policy_weight(PolicyArgs a, float* weight) {
     __shared__ double lds[16];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     double n = 0.0;
-    for (int64_t r = threadIdx.x; r < a.R; r += 1024) {
-        const float c = weight[1 + r];
-        n += a.by_sequence ? (c > 0.0f ? 1.0 : 0.0) : (double)c;
-    }
+    if constexpr (kCounted) {
+        for (int64_t r = threadIdx.x; r < a.R; r += 1024) {
+            const float c = weight[1 + r];
+            n += a.by_sequence ? (c > 0.0f ? 1.0 : 0.0) : (double)c;
+        }
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o);
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = n;
+        for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o);
+    } else {
+        for (int64_t r = wave; r < a.R; r += 16) {
+            const int c = count_labels(a.labels + r * a.label_pitch, a.T, a.ignore);
+            if (lane == 0) weight[1 + r] = (float)c;
+            n += a.by_sequence ? (c > 0 ? 1.0 : 0.0) : (double)c;
+        }
+    }
+    if (lane == 0) lds[wave] = n;
     __syncthreads();
     if (threadIdx.x == 0) {
         double t = 0.0;
         for (int w = 0; w < 16; ++w) t += lds[w];
         weight[0] = t > 0.0 ? (float)(1.0 / t) : 0.0f;
+        *a.done = 0;
     }
 }
 
@@ -528,28 +552,50 @@ __global__ __launch_bounds__(kRowThreads) void policy_long(PolicyArgs a) {
     write_gradient<DT, kRowThreads>(in, out, a.V, at, threadIdx.x, st, a.L, policy_slope(a, tk, logp), lab.y);
 }
 
-// The three sums over the tokens, in 64 bits and a fixed order.
-__global__ __launch_bounds__(1024) void policy_finish(const float4* tokens, int64_t rows, float* stats) {
-    __shared__ double lds[3][16];
+// The sum over a workgroup's threads, valid in thread 0.
+template <int kWaves>
+__device__ __forceinline__ double block_sum(double v, double* lds) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    if (threadIdx.x == 0)
+        for (int w = 1; w < kWaves; ++w) v += lds[w];
+    __syncthreads();
+    return v;
+}
+
+// The three sums over the tokens, in 64 bits and a fixed order: each workgroup a
+// share, the last one to finish adds the shares.
+__global__ __launch_bounds__(256) void policy_finish(PolicyArgs a) {
+    __shared__ double lds[4];
+    __shared__ bool last;
     double v[3] = {0.0, 0.0, 0.0};
-    for (int64_t i = threadIdx.x; i < rows; i += 1024) {
-        const float4 k = tokens[i];
+#pragma unroll 4
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < a.rows; i += (int64_t)gridDim.x * 256) {
+        const float4 k = a.tokens[i];
         v[0] += k.x;
         v[1] += k.y;
         v[2] += k.z;
     }
 #pragma unroll
-    for (int q = 0; q < 3; ++q) {
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) v[q] += __shfl_xor(v[q], o);
-        if ((threadIdx.x & 63) == 0) lds[q][threadIdx.x >> 6] = v[q];
+    for (int q = 0; q < 3; ++q) v[q] = block_sum<4>(v[q], lds);
+    if (gridDim.x == 1) {
+        if (threadIdx.x == 0)
+            for (int q = 0; q < 3; ++q) a.stats[q] = (float)v[q];
+        return;
+    }
+    if (threadIdx.x == 0) {
+        for (int q = 0; q < 3; ++q) a.sums[q * kFinishBlocks + blockIdx.x] = v[q];
+        __threadfence();
+        last = atomicAdd(a.done, 1) == (int)gridDim.x - 1;
     }
     __syncthreads();
-    if (threadIdx.x < 3) {
-        double t = 0.0;
-        for (int w = 0; w < 16; ++w) t += lds[threadIdx.x][w];
-        stats[threadIdx.x] = (float)t;
-    }
+    if (!last || threadIdx.x >= 3) return;
+    __threadfence();
+    double t = 0.0;
+    for (unsigned b = 0; b < gridDim.x; ++b) t += __hip_atomic_load(a.sums + threadIdx.x * kFinishBlocks + b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    a.stats[threadIdx.x] = (float)t;
 }
 
 // -- preference -----------------------------------------------------------------
@@ -562,22 +608,17 @@ struct PrefArgs {
     int64_t label_pitch, ignore;
     const float* ref_logp;  // NULL: zero
     int64_t P, T;
-    int64_t first, pairs;  // this launch's pairs
     int32_t V;
     float beta, smoothing, scale;
     int32_t average;
     float* logp;       // [2P][T]
     float* rewards;    // [2P]
     float* pair_loss;  // [P]
+    float* loss;
+    int* done;         // pairs that are done
     float2* stats;     // [2P][T] (shift, sum)
     float* coef;       // [2P]
 };
-
-// The token of row i of a launch: the chosen answers of its pairs, then the
-// rejected ones.
-__device__ __forceinline__ int64_t pref_sequence(const PrefArgs& a, int64_t local) {
-    return local < a.pairs ? a.first + local : a.P + a.first + (local - a.pairs);
-}
 
 template <int DT, int kThreads>
 __global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void pref_logp(PrefArgs a) {
@@ -586,8 +627,9 @@ __global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void pref_logp(Pre
     __shared__ float2 lds[kWaves];
     const int tid = threadIdx.x % kThreads;
     const int64_t i = row_of<kThreads>();
-    if (i >= 2 * a.pairs * a.T) return;
-    const int64_t local = i / a.T, t = i - local * a.T, r = pref_sequence(a, local);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.done = 0;  // the next launch counts there
+    if (i >= 2 * a.P * a.T) return;
+    const int64_t r = i / a.T, t = i - r * a.T;
     const int64_t label = a.labels[r * a.label_pitch + t];
     if (label == a.ignore) {
         if (tid == 0) a.logp[r * a.T + t] = 0.0f;
@@ -603,36 +645,10 @@ __global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void pref_logp(Pre
     }
 }
 
-// One workgroup a pair: the two implicit rewards, the loss and both c.
-__global__ __launch_bounds__(256) void pref_pair(PrefArgs a) {
-    __shared__ double lds[2][4];
-    __shared__ int cnt[2][4];
-    const int64_t p = a.first + blockIdx.x;
-    double sum[2];
-    int n[2];
-#pragma unroll
-    for (int side = 0; side < 2; ++side) {
-        const int64_t r = side ? a.P + p : p;
-        sum[side] = 0.0;
-        n[side] = 0;
-        for (int64_t t = threadIdx.x; t < a.T; t += 256) {
-            if (a.labels[r * a.label_pitch + t] == a.ignore) continue;
-            sum[side] += (double)a.logp[r * a.T + t] - (a.ref_logp ? (double)a.ref_logp[r * a.T + t] : 0.0);
-            ++n[side];
-        }
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) {
-            sum[side] += __shfl_xor(sum[side], o);
-            n[side] += __shfl_xor(n[side], o);
-        }
-        if ((threadIdx.x & 63) == 0) {
-            lds[side][threadIdx.x >> 6] = sum[side];
-            cnt[side][threadIdx.x >> 6] = n[side];
-        }
-    }
-    __syncthreads();
-    if (threadIdx.x) return;
-    double share[2];
+// The pair's rewards, loss and both c, from the wavefronts' sums and counts.
+__device__ __forceinline__ void pref_finish_pair(const PrefArgs& a, int64_t p, const double (&lds)[2][4],
+                                                 const int (&cnt)[2][4]) {
+    double sum[2], share[2];
 #pragma unroll
     for (int side = 0; side < 2; ++side) {
         double s = 0.0;
@@ -656,13 +672,57 @@ __global__ __launch_bounds__(256) void pref_pair(PrefArgs a) {
     a.coef[a.P + p] = (float)(-slope * share[1]);
 }
 
+// One workgroup a pair: the two implicit rewards, the loss and both c.
+__global__ __launch_bounds__(256) void pref_pair(PrefArgs a) {
+    __shared__ double lds[2][4];
+    __shared__ int cnt[2][4];
+    __shared__ bool last;
+    const int64_t p = blockIdx.x;
+    double sum[2];
+    int n[2];
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+        const int64_t r = side ? a.P + p : p;
+        sum[side] = 0.0;
+        n[side] = 0;
+        for (int64_t t = threadIdx.x; t < a.T; t += 256) {
+            if (a.labels[r * a.label_pitch + t] == a.ignore) continue;
+            sum[side] += (double)a.logp[r * a.T + t] - (a.ref_logp ? (double)a.ref_logp[r * a.T + t] : 0.0);
+            ++n[side];
+        }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+            sum[side] += __shfl_xor(sum[side], o);
+            n[side] += __shfl_xor(n[side], o);
+        }
+        if ((threadIdx.x & 63) == 0) {
+            lds[side][threadIdx.x >> 6] = sum[side];
+            cnt[side][threadIdx.x >> 6] = n[side];
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) pref_finish_pair(a, p, lds, cnt);
+    // the last pair to finish takes the mean
+    if (threadIdx.x == 0) {
+        __threadfence();
+        last = a.P == 1 || atomicAdd(a.done, 1) == (int)a.P - 1;
+    }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    double v = 0.0;
+    for (int64_t i = threadIdx.x; i < a.P; i += 256)
+        v += __hip_atomic_load(a.pair_loss + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    v = block_sum<4>(v, lds[0]);
+    if (threadIdx.x == 0) a.loss[0] = (float)(v / (double)a.P);
+}
 template <int DT, int kThreads>
 __global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void pref_gradient(PrefArgs a) {
     typedef typename Elem<DT>::T T;
     const int tid = threadIdx.x % kThreads;
     const int64_t i = row_of<kThreads>();
-    if (i >= 2 * a.pairs * a.T) return;
-    const int64_t local = i / a.T, t = i - local * a.T, r = pref_sequence(a, local);
+    if (i >= 2 * a.P * a.T) return;
+    const int64_t r = i / a.T, t = i - r * a.T;
     const int64_t label = a.labels[r * a.label_pitch + t];
     const int64_t at = r * a.grad_seq + t * a.grad_tok;
     T* out = static_cast<T*>(a.grad) + at;
@@ -675,19 +735,10 @@ __global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void pref_gradient
                                  a.stats[r * a.T + t], kLog2e, a.coef[r], y);
 }
 
-__global__ __launch_bounds__(1024) void pref_mean(const float* pair_loss, int64_t P, float* loss) {
-    __shared__ double lds[16];
-    double v = 0.0;
-    for (int64_t i = threadIdx.x; i < P; i += 1024) v += pair_loss[i];
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        double t = 0.0;
-        for (int w = 0; w < 16; ++w) t += lds[w];
-        loss[0] = P > 0 ? (float)(t / (double)P) : 0.0f;
-    }
+// What there is without pairs, or before the first launch without tokens.
+__global__ void pref_clear(float* loss, int* done) {
+    if (loss) *loss = 0.0f;
+    if (done) *done = 0;
 }
 
 // -- host -----------------------------------------------------------------------
@@ -734,7 +785,7 @@ extern "C" {
 
 int64_t gmc_policy_loss_workspace(int64_t R, int64_t T) {
     if (R < 0 || T < 0 || (T > 0 && R > kMostRows / T)) return -1;
-    return R * T * (int64_t)sizeof(float4) + (1 + R) * (int64_t)sizeof(float);
+    return R * T * (int64_t)sizeof(float4) + kFinishBlocks * 3 * (int64_t)sizeof(double) + (2 + R) * (int64_t)sizeof(float);
 }
 
 gmc_status gmc_policy_loss(void* hip_stream, int32_t dtype, int64_t R, int64_t T, int64_t V, const void* logits_dev,
@@ -763,7 +814,9 @@ gmc_status gmc_policy_loss(void* hip_stream, int32_t dtype, int64_t R, int64_t T
     a.tokens = static_cast<float4*>(workspace_dev);
     if (a.rows) {
         if (!adv_dev || !logp_dev) return op_error(GMC_EINVAL, me, "NULL argument");
-        float* weight = reinterpret_cast<float*>(a.tokens + a.rows);
+        a.sums = reinterpret_cast<double*>(a.tokens + a.rows);
+        a.done = reinterpret_cast<int*>(a.sums + 3 * kFinishBlocks);
+        float* weight = reinterpret_cast<float*>(a.done + 1);
         a.logits = logits_dev;
         a.grad = grad_dev;
         a.seq = seq_pitch;
@@ -790,8 +843,12 @@ gmc_status gmc_policy_loss(void* hip_stream, int32_t dtype, int64_t R, int64_t T
         a.by_sequence = by_sequence != 0;
         a.logp = logp_dev;
         a.weight = weight;
-        policy_counts<<<dim3((unsigned)((R + 3) / 4)), 256, 0, st>>>(a, weight);
-        policy_weight<<<1, 1024, 0, st>>>(a, weight);
+        if (a.rows > kFewTokens || R > kFewSequences) {
+            policy_counts<<<dim3((unsigned)((R + 3) / 4)), 256, 0, st>>>(a, weight);
+            policy_weight<true><<<1, 1024, 0, st>>>(a, weight);
+        } else {
+            policy_weight<false><<<1, 1024, 0, st>>>(a, weight);
+        }
         const int64_t vecs = V * type_size(dtype) / 16;  // at most, whatever the alignment
         const dim3 rows((unsigned)a.rows), quads((unsigned)((a.rows + 3) / 4));
         GMC_BY_TYPE(dtype, {
@@ -804,13 +861,16 @@ gmc_status gmc_policy_loss(void* hip_stream, int32_t dtype, int64_t R, int64_t T
             else policy_long<DT><<<rows, kRowThreads, 0, st>>>(a);
         });
     }
-    policy_finish<<<1, 1024, 0, st>>>(a.tokens, a.rows, stats_dev);
+    a.stats = stats_dev;
+    const int64_t shares = (a.rows + 1023) / 1024;
+    const unsigned finish = shares < 1 ? 1u : shares > kFinishBlocks ? (unsigned)kFinishBlocks : (unsigned)shares;
+    policy_finish<<<dim3(finish), 256, 0, st>>>(a);
     return op_launched(me);
 }
 
 int64_t gmc_preference_loss_workspace(int64_t P, int64_t T) {
     if (P < 0 || T < 0 || (T > 0 && P > kMostRows / 2 / T)) return -1;
-    return 2 * P * T * (int64_t)sizeof(float2) + 2 * P * (int64_t)sizeof(float);
+    return 2 * P * T * (int64_t)sizeof(float2) + (2 * P + 2) * (int64_t)sizeof(float);
 }
 
 gmc_status gmc_preference_loss(void* hip_stream, int32_t dtype, int64_t P, int64_t T, int64_t V,
@@ -847,8 +907,6 @@ gmc_status gmc_preference_loss(void* hip_stream, int32_t dtype, int64_t P, int64
         a.ref_logp = ref_logp_dev;
         a.P = P;
         a.T = T;
-        a.first = 0;
-        a.pairs = P;
         a.V = (int32_t)V;
         a.beta = (float)beta;
         a.smoothing = (float)smoothing;
@@ -859,12 +917,16 @@ gmc_status gmc_preference_loss(void* hip_stream, int32_t dtype, int64_t P, int64
         a.pair_loss = pair_loss_dev;
         a.stats = static_cast<float2*>(workspace_dev);
         a.coef = reinterpret_cast<float*>(a.stats + 2 * P * T);
+        a.done = reinterpret_cast<int*>(a.coef + 2 * P);
+        a.loss = loss_dev;
         const int64_t tokens = 2 * P * T, vecs = V * type_size(dtype) / 16;
         const dim3 rows((unsigned)tokens), quads((unsigned)((tokens + 3) / 4));
         GMC_BY_TYPE(dtype, {
             if (tokens) {
                 if (vecs <= 64 * 8) pref_logp<DT, 64><<<quads, 256, 0, st>>>(a);
                 else pref_logp<DT, kStatThreads><<<rows, kStatThreads, 0, st>>>(a);
+            } else {
+                pref_clear<<<1, 1, 0, st>>>(nullptr, a.done);
             }
             pref_pair<<<dim3((unsigned)P), 256, 0, st>>>(a);
             if (tokens && a.grad) {
@@ -872,8 +934,9 @@ gmc_status gmc_preference_loss(void* hip_stream, int32_t dtype, int64_t P, int64
                 else pref_gradient<DT, kStatThreads><<<rows, kStatThreads, 0, st>>>(a);
             }
         });
+    } else {
+        pref_clear<<<1, 1, 0, st>>>(loss_dev, nullptr);
     }
-    pref_mean<<<1, 1024, 0, st>>>(pair_loss_dev, P, loss_dev);
     return op_launched(me);
 }
 

@@ -10,7 +10,8 @@ here: a backward call is a call, and a loss returns the logits' gradient
 """
 from __future__ import annotations
 
-from typing import Optional, Tuple
+import math
+from typing import Tuple
 
 from .gmc import GMC_OK, GmcError, _raw_stream, _torch, load
 
@@ -19,6 +20,9 @@ REDUCTIONS = {"token": 0, "sequence": 1}
 IGNORE = -100
 
 _codes = None
+
+# As in gmc.py, the checks take the cheapest form of each test: at small sizes a
+# call is bound by this code and its launches.
 
 
 def _code(t, name: str) -> int:
@@ -37,48 +41,50 @@ def _code(t, name: str) -> int:
     return code
 
 
-def _like(t, ref, name: str):
-    """t has ref's type, device and shape."""
-    if not isinstance(t, type(ref)) and not isinstance(t, _torch().Tensor):
+def _is(t, dtype, shape, ref, name: str):
+    """t is a tensor of a type and shape on ref's device."""
+    if not isinstance(t, _torch().Tensor):
         raise TypeError("%s must be a torch.Tensor" % name)
-    if t.dtype != ref.dtype:
-        raise TypeError("%s must be %s, got %s" % (name, ref.dtype, t.dtype))
-    if t.device != ref.device:
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    if t.get_device() != ref.get_device():
         raise ValueError("%s must be on %s" % (name, ref.device))
-    if t.shape != ref.shape:
-        raise ValueError("%s must have the shape %s, has %s" % (name, tuple(ref.shape), tuple(t.shape)))
+    if t.shape != shape:
+        raise ValueError("%s must have the shape %s, has %s" % (name, tuple(shape), tuple(t.shape)))
 
 
 def _f32(t, shape, ref, name: str) -> int:
     """Pointer of a contiguous fp32 tensor of a shape, on ref's device (None: 0)."""
     if t is None:
         return 0
-    torch = _torch()
-    if not isinstance(t, torch.Tensor):
-        raise TypeError("%s must be a torch.Tensor" % name)
-    if t.dtype != torch.float32:
-        raise TypeError("%s must be torch.float32, got %s" % (name, t.dtype))
-    if t.device != ref.device:
-        raise ValueError("%s must be on %s" % (name, ref.device))
-    if tuple(t.shape) != shape:
-        raise ValueError("%s must have the shape %s, has %s" % (name, shape, tuple(t.shape)))
+    _is(t, _torch().float32, shape, ref, name)
     if not t.is_contiguous():
         raise ValueError("%s must be contiguous" % name)
     return t.data_ptr()
 
 
-def _call(t, name: str, *args):
-    """The library's entry point on torch's current stream of t's device."""
+def _new(ref, *shape):
+    """A new fp32 tensor on ref's device."""
+    return ref.new_empty(shape, dtype=_torch().float32)
+
+
+def _new_like(t):
+    """A new contiguous tensor of t's shape and type."""
     torch = _torch()
-    lib = load()
+    return torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
+
+
+def _call(t, entry, *args):
+    """An entry point of the library on torch's current stream of t's device."""
+    torch = _torch()
     dev = t.get_device()
     if dev == torch.cuda.current_device():
-        st = getattr(lib, name)(_raw_stream(t), *args)
+        st = entry(_raw_stream(t), *args)
     else:
         with torch.cuda.device(dev):
-            st = getattr(lib, name)(_raw_stream(t), *args)
+            st = entry(_raw_stream(t), *args)
     if st != GMC_OK:
-        raise GmcError(st, lib.gmc_last_error(None).decode())
+        raise GmcError(st, load().gmc_last_error(None).decode())
 
 
 def _rows(t, name: str) -> Tuple[int, int, int]:
@@ -112,21 +118,20 @@ def dropout(x, p: float, seed: int, t: int = 0, worker: int = 0, site: int = 0, 
     """Dropout of x and, with ``residual``, the sum residual + dropout(x).  The
     mask is a function of (seed, t, worker, site) and the element's number in
     x.  ``out`` may be x or residual."""
-    torch = _torch()
     code = _code(x, "x")
     rows, cols, pitch = _rows(x, "x")
     pr = rp = 0
     if residual is not None:
-        _like(residual, x, "residual")
+        _is(residual, x.dtype, x.shape, x, "residual")
         rp = _rows(residual, "residual")[2]
         pr = residual.data_ptr()
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        out = _new_like(x)
         op = cols
     else:
-        _like(out, x, "out")
+        _is(out, x.dtype, x.shape, x, "out")
         op = _rows(out, "out")[2]
-    _call(x, "gmc_dropout", code, rows, cols, x.data_ptr(), pitch, pr, rp, out.data_ptr(), op, float(p),
+    _call(x, load().gmc_dropout, code, rows, cols, x.data_ptr(), pitch, pr, rp, out.data_ptr(), op, float(p),
           int(seed) & (2 ** 64 - 1), int(t), int(worker), int(site))
     return out
 
@@ -141,10 +146,8 @@ def _images(t, name: str) -> Tuple[int, int, int, int, int]:
     """(N, S, C, image pitch, pixel pitch) of an [N, ..., C] tensor."""
     if t.dim() < 2:
         raise ValueError("%s must be [N, ..., C]" % name)
-    N, C = t.shape[0], t.shape[-1]
-    S = 1
-    for n in t.shape[1:-1]:
-        S *= n
+    N, *pixels, C = t.shape
+    S = math.prod(pixels)
     if t.is_contiguous():
         return N, S, C, S * C, C
     if t.stride(-1) != 1 and C > 1:
@@ -164,31 +167,30 @@ def _images(t, name: str) -> Tuple[int, int, int, int, int]:
 def _workspace(n: int, what: str, ref):
     if n < 0:
         raise GmcError(-1, load().gmc_last_error(None).decode() if what is None else what)
-    return _torch().empty(n, dtype=_torch().uint8, device=ref.device) if n else None
+    return ref.new_empty(n, dtype=_torch().uint8) if n else None
 
 
 def group_norm(x, groups: int, gamma=None, beta=None, eps: float = 1e-5, act: str = "none", out=None):
     """Group norm over channels-last x [N, ..., C] and its activation ("none",
     "relu", "silu"): (y, mean, rstd), the last two [N, groups] for the backward
     call.  gamma and beta are fp32 [C] (or None).  ``out`` may be x."""
-    torch = _torch()
     code = _code(x, "x")
     if act not in ACTS:
         raise ValueError("act must be one of %s" % list(ACTS))
     N, S, C, image, pixel = _images(x, "x")
     pg, pb = _f32(gamma, (C,), x, "gamma"), _f32(beta, (C,), x, "beta")
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        out = _new_like(x)
         oi, op = S * C, C
     else:
-        _like(out, x, "out")
+        _is(out, x.dtype, x.shape, x, "out")
         oi, op = _images(out, "out")[3:]
     G = int(groups)
-    n = load().gmc_group_norm_workspace(code, N, S, C, G, 0)
+    lib = load()
+    n = lib.gmc_group_norm_workspace(code, N, S, C, G, 0)
     ws = _workspace(n, None, x)
-    mean = torch.empty((N, G), dtype=torch.float32, device=x.device)
-    rstd = torch.empty((N, G), dtype=torch.float32, device=x.device)
-    _call(x, "gmc_group_norm", code, N, S, C, G, x.data_ptr(), image, pixel, pg, pb, float(eps), ACTS[act],
+    mean, rstd = _new(x, N, G), _new(x, N, G)
+    _call(x, lib.gmc_group_norm, code, N, S, C, G, x.data_ptr(), image, pixel, pg, pb, float(eps), ACTS[act],
           out.data_ptr(), oi, op, mean.data_ptr(), rstd.data_ptr(), 0 if ws is None else ws.data_ptr(), n)
     return out, mean, rstd
 
@@ -197,9 +199,8 @@ def group_norm_backward(dy, x, mean, rstd, gamma=None, beta=None, act: str = "no
     """(dx, dgamma, dbeta) from dy and the forward call's x, mean, rstd, gamma,
     beta and act.  ``out`` may be dy or x; ``dgamma`` and ``dbeta`` may be fp32
     [C] views of a worker's row of gradients."""
-    torch = _torch()
     code = _code(x, "x")
-    _like(dy, x, "dy")
+    _is(dy, x.dtype, x.shape, x, "dy")
     if act not in ACTS:
         raise ValueError("act must be one of %s" % list(ACTS))
     N, S, C, image, pixel = _images(x, "x")
@@ -210,18 +211,19 @@ def group_norm_backward(dy, x, mean, rstd, gamma=None, beta=None, act: str = "no
     pm, ps = _f32(mean, (N, G), x, "mean"), _f32(rstd, (N, G), x, "rstd")
     pg, pb = _f32(gamma, (C,), x, "gamma"), _f32(beta, (C,), x, "beta")
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        out = _new_like(x)
         oi, op = S * C, C
     else:
-        _like(out, x, "out")
+        _is(out, x.dtype, x.shape, x, "out")
         oi, op = _images(out, "out")[3:]
     if dgamma is None:
-        dgamma = torch.empty((C,), dtype=torch.float32, device=x.device)
+        dgamma = _new(x, C)
     if dbeta is None:
-        dbeta = torch.empty((C,), dtype=torch.float32, device=x.device)
-    n = load().gmc_group_norm_workspace(code, N, S, C, G, 1)
+        dbeta = _new(x, C)
+    lib = load()
+    n = lib.gmc_group_norm_workspace(code, N, S, C, G, 1)
     ws = _workspace(n, None, x)
-    _call(x, "gmc_group_norm_backward", code, N, S, C, G, dy.data_ptr(), di, dp, x.data_ptr(), image, pixel, pm, ps,
+    _call(x, lib.gmc_group_norm_backward, code, N, S, C, G, dy.data_ptr(), di, dp, x.data_ptr(), image, pixel, pm, ps,
           pg, pb, ACTS[act], out.data_ptr(), oi, op, _f32(dgamma, (C,), x, "dgamma"), _f32(dbeta, (C,), x, "dbeta"),
           0 if ws is None else ws.data_ptr(), n)
     return out, dgamma, dbeta
@@ -236,14 +238,7 @@ def _logits(logits, labels) -> Tuple[int, int, int, int, int, int]:
     R, T, V = logits.shape
     if V > 1 and logits.stride(2) != 1:
         raise ValueError("logits need a contiguous vocabulary axis")
-    if not isinstance(labels, torch.Tensor):
-        raise TypeError("labels must be a torch.Tensor")
-    if labels.dtype != torch.int64:
-        raise TypeError("labels must be torch.int64, got %s" % labels.dtype)
-    if labels.device != logits.device:
-        raise ValueError("labels must be on %s" % logits.device)
-    if tuple(labels.shape) != (R, T):
-        raise ValueError("labels must have the shape %s, has %s" % ((R, T), tuple(labels.shape)))
+    _is(labels, torch.int64, (R, T), logits, "labels")
     if T > 1 and labels.stride(1) != 1:
         raise ValueError("labels need contiguous tokens")
     return code, R, T, V, labels.data_ptr(), labels.stride(0)
@@ -256,9 +251,10 @@ def _gradient(logits, grad: bool, out):
             raise ValueError("out is the gradient's: it needs grad=True")
         return None, 0, 0, 0
     if out is None:
-        out = _torch().empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        out = _new_like(logits)
+        return out, out.data_ptr(), logits.shape[1] * logits.shape[2], logits.shape[2]
     else:
-        _like(out, logits, "out")
+        _is(out, logits.dtype, logits.shape, logits, "out")
         if out.shape[2] > 1 and out.stride(2) != 1:
             raise ValueError("out needs a contiguous vocabulary axis")
     return out, out.data_ptr(), out.stride(0), out.stride(1)
@@ -284,11 +280,11 @@ def policy_loss(logits, labels, old_logp, advantages, ref_logp=None, clip: Tuple
     per_token = advantages.dim() == 2
     pa = _f32(advantages, (R, T) if per_token else (R,), logits, "advantages")
     out, pg, gs, gt = _gradient(logits, grad, out)
-    n = load().gmc_policy_loss_workspace(R, T)
+    lib = load()
+    n = lib.gmc_policy_loss_workspace(R, T)
     ws = _workspace(n, "gmc_policy_loss: more than 2^22 - 1 tokens", logits)
-    stats = torch.empty((3,), dtype=torch.float32, device=logits.device)
-    logp = torch.empty((R, T), dtype=torch.float32, device=logits.device)
-    _call(logits, "gmc_policy_loss", code, R, T, V, logits.data_ptr(), logits.stride(0), logits.stride(1), pl, lp,
+    stats, logp = _new(logits, 3), _new(logits, R, T)
+    _call(logits, lib.gmc_policy_loss, code, R, T, V, logits.data_ptr(), logits.stride(0), logits.stride(1), pl, lp,
           int(ignore), po, pr, pa, T if per_token else 1, 1 if per_token else 0, float(clip[0]), float(clip[1]),
           float(kl_coef), float(temperature), REDUCTIONS[reduction], float(grad_scale), stats.data_ptr(),
           logp.data_ptr(), pg, gs, gt, ws.data_ptr(), n)
@@ -302,20 +298,17 @@ def preference_loss(logits, labels, ref_logp=None, beta: float = 0.1, smoothing:
 
     ref_logp: the reference's token log-probabilities, fp32 [2 P, T], as a call
     of its own with grad=False returns them, or None.  ``out`` may be logits."""
-    torch = _torch()
     code, R, T, V, pl, lp = _logits(logits, labels)
     if R % 2:
         raise ValueError("logits must hold pairs: [2 P, T, V]")
     P = R // 2
     pr = _f32(ref_logp, (R, T), logits, "ref_logp")
     out, pg, gs, gt = _gradient(logits, grad, out)
-    n = load().gmc_preference_loss_workspace(P, T)
+    lib = load()
+    n = lib.gmc_preference_loss_workspace(P, T)
     ws = _workspace(n, "gmc_preference_loss: more than 2^22 - 1 tokens", logits)
-    loss = torch.empty((), dtype=torch.float32, device=logits.device)
-    each = torch.empty((P,), dtype=torch.float32, device=logits.device)
-    rewards = torch.empty((R,), dtype=torch.float32, device=logits.device)
-    logp = torch.empty((R, T), dtype=torch.float32, device=logits.device)
-    _call(logits, "gmc_preference_loss", code, P, T, V, logits.data_ptr(), logits.stride(0), logits.stride(1), pl, lp,
+    loss, each, rewards, logp = _new(logits), _new(logits, P), _new(logits, R), _new(logits, R, T)
+    _call(logits, lib.gmc_preference_loss, code, P, T, V, logits.data_ptr(), logits.stride(0), logits.stride(1), pl, lp,
           int(ignore), pr, float(beta), float(smoothing), 1 if average else 0, float(grad_scale), loss.data_ptr(),
           each.data_ptr(), rewards.data_ptr(), logp.data_ptr(), pg, gs, gt, 0 if ws is None else ws.data_ptr(), n)
     return loss, each, rewards, logp, out
