@@ -29,7 +29,8 @@ namespace gmc {
 namespace {
 
 constexpr int kHeldThreads = 1024;
-constexpr int kHeldBlocks = 512;   // held: workgroups below which narrower blocks are tried
+constexpr int kHeldBlocks = 256;   // held: workgroups below which narrower blocks are tried
+constexpr int kManyBlocks = 512;   // held: two workgroups for every CU
 constexpr int kHeldMost = 16;      // vectors of x a thread holds (16 bytes each)
 constexpr int kHeldMostBack = 8;   // ... of x and of dy
 constexpr int kHeldChannels = 256; // threads across channels, at most
@@ -499,6 +500,41 @@ __device__ __forceinline__ void scatter_sums(float* v, int lane, int across, int
     }
 }
 
+// The channels' sums of dz (v[0 .. VEC)) and dz hat (v[VEC ..)) over the
+// workgroup: into a.part and a.part2 for dbeta and dgamma, and weighted with gamma
+// and summed over their groups, s1 / m and s2 / m, into stat[2][gw].
+template <int VEC>
+__device__ __forceinline__ void join_back_sums(const NormArgs& a, const Place& p, int64_t n, int blk,
+                                               float (&v)[2 * VEC], float* part, float* stat) {
+    int first = 0, left = 2 * VEC;
+    const int lane = threadIdx.x & 63;
+    scatter_sums<2 * VEC>(v, lane, 1 << a.tp_log2, 32, first, left);
+    // lanes that differ only in steps taken with one value left hold the same sum
+    if (p.on)
+#pragma unroll
+        for (int j = 0; j < 2 * VEC; ++j)
+            if (j < left) {
+                const int q = first + j;
+                part[((threadIdx.x >> 6) * 2 + q / VEC) * a.cb + p.cv * VEC + (q & (VEC - 1))] = v[j];
+            }
+    __syncthreads();
+    // a thread per channel and sum; a group's channels are neighbouring lanes
+    for (int e0 = 0; e0 < 2 * a.cb; e0 += blockDim.x) {  // whole wavefronts, for the exchange
+        const int e = e0 + threadIdx.x;
+        const bool some = e < 2 * a.cb;
+        const int which = e >= a.cb, c = e - which * a.cb;
+        float t = 0.0f;
+        if (some) {
+            for (int w = 0; w < p.waves; ++w) t += part[(w * 2 + which) * a.cb + c];
+            (which ? a.part2 : a.part)[n * a.C + blk * a.cb + c] = t;
+            if (a.gamma) t *= a.gamma[blk * a.cb + c];
+        }
+        for (int o = 1; o < a.cpg; o <<= 1) t += __shfl_xor(t, o);
+        if (some && (c & (a.cpg - 1)) == 0) stat[which * a.gw + (c >> a.cpg_log2)] = t * a.inv_m;
+    }
+    __syncthreads();
+}
+
 template <int DT, int KP, int F>
 __global__ __launch_bounds__(kHeldThreads) void norm_backward_fold(NormArgs a) {
     typedef typename Elem<DT>::T T;
@@ -559,33 +595,7 @@ __global__ __launch_bounds__(kHeldThreads) void norm_backward_fold(NormArgs a) {
                 if constexpr (!kKeep && kAct == GMC_ACT_RELU) dv[k].pack(d);
             }
     });
-    int first = 0, left = 2 * VEC;
-    const int lane = threadIdx.x & 63;
-    scatter_sums<2 * VEC>(v, lane, 1 << a.tp_log2, 32, first, left);
-    // lanes that differ only in steps taken with one value left hold the same sum
-    if (p.on)
-#pragma unroll
-        for (int j = 0; j < 2 * VEC; ++j)
-            if (j < left) {
-                const int q = first + j;
-                part[((threadIdx.x >> 6) * 2 + q / VEC) * a.cb + p.cv * VEC + (q & (VEC - 1))] = v[j];
-            }
-    __syncthreads();
-    // a thread per channel and sum; a group's channels are neighbouring lanes
-    for (int e0 = 0; e0 < 2 * a.cb; e0 += blockDim.x) {  // whole wavefronts, for the exchange
-        const int e = e0 + threadIdx.x;
-        const bool some = e < 2 * a.cb;
-        const int which = e >= a.cb, c = e - which * a.cb;
-        float t = 0.0f;
-        if (some) {
-            for (int w = 0; w < p.waves; ++w) t += part[(w * 2 + which) * a.cb + c];
-            (which ? a.part2 : a.part)[n * a.C + blk * a.cb + c] = t;
-            if (a.gamma) t *= a.gamma[blk * a.cb + c];
-        }
-        for (int o = 1; o < a.cpg; o <<= 1) t += __shfl_xor(t, o);
-        if (some && (c & (a.cpg - 1)) == 0) stat[which * a.gw + (c >> a.cpg_log2)] = t * a.inv_m;
-    }
-    __syncthreads();
+    join_back_sums<VEC>(a, p, n, blk, v, part, stat);
     // dx = rstd (gamma dz - s1/m - hat s2/m) = (rstd gamma) dz + (x - mean) b + c
     float gb[F], gc[F];
 #pragma unroll
@@ -953,9 +963,14 @@ struct NormPlan {
 };
 
 // The held form for groups of a power of two of channels: whole groups in
-// segments of at least `line` bytes, as few threads as leave every thread at
-// most `few` vectors.
-bool plan_fold(NormArgs& a, NormPlan& pl, int64_t size, bool backward, int line, int few, int most) {
+// segments of at least `line` bytes.  Threads: as few as leave each at most 4
+// vectors (forward of many blocks 8); of many blocks rather 512 threads with up to
+// 16 vectors than 1024 with fewer, and for the backward pass 256 with 8 than 512,
+// so that several workgroups share a CU and one loads while another computes.  64 images of 784 pixels of 512 bf16 channels: forward 18.8 us
+// with 512 threads, 26.6 with 1024; 196 pixels of 1024: backward 19.3 us with 256,
+// 23.5 with 512; one image of 49 pixels of 2048: forward 5.5 us with 4 vectors, 6.0
+// with 8.
+bool plan_fold(NormArgs& a, NormPlan& pl, int64_t size, bool backward, int line) {
     const int full = (int)(16 / size);
     for (int gw = 1; gw <= a.G; ++gw) {
         if (a.G % gw) continue;
@@ -964,10 +979,17 @@ bool plan_fold(NormArgs& a, NormPlan& pl, int64_t size, bool backward, int line,
         const int64_t tc = cb / full;
         if (tc > 64) return false;
         const int lg = log2_up(tc);
+        const auto vectors = [&](int threads) { return ((int64_t)a.S + (threads >> lg) - 1) / (threads >> lg); };
+        const int64_t blocks = a.N * (a.G / gw);
+        const int few = !backward && blocks >= kHeldBlocks ? 8 : 4;
+        const int most = backward ? kHeldMostBack : kHeldMost;
         int threads = 64;
-        while (threads < kHeldThreads && a.S > (int64_t)few * (threads >> lg)) threads *= 2;
-        const int rows = threads >> lg;
-        const int64_t kp = (a.S + rows - 1) / rows;
+        while (threads < kHeldThreads && vectors(threads) > few) threads *= 2;
+        if (blocks >= kManyBlocks) {
+            if (threads == 1024 && vectors(512) <= most) threads = 512;
+            if (backward && threads == 512 && vectors(256) <= most) threads = 256;
+        }
+        const int64_t kp = vectors(threads);
         if (kp > most) return false;
         pl.held = true;
         pl.fold = a.cpg >= full ? 1 : full / a.cpg;
@@ -997,7 +1019,7 @@ NormPlan norm_plan(NormArgs& a, int32_t dtype, bool backward) {
     a.cpg_log2 = a.cpg & (a.cpg - 1) ? -1 : log2_up(a.cpg);
     if (a.cpg_log2 >= 0 && a.cpg <= 64) {
         for (int line = 128; line >= 16; line >>= 1) {
-            if (!plan_fold(a, pl, type_size(dtype), backward, line, backward ? 4 : 8, most)) continue;
+            if (!plan_fold(a, pl, type_size(dtype), backward, line)) continue;
             if (a.N * a.blocks >= kHeldBlocks) break;
         }
         if (pl.held) return pl;
