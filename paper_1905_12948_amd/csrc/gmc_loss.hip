@@ -279,13 +279,15 @@ __device__ __forceinline__ float2 stream_row(const Row<DT, kThreads>& row, int t
     return make_float2(m, s);
 }
 
-// log p_y of a row with shift M (-inf: all entries are) and sum s.  The power of two
-// of s meets the exponent exactly; only its logarithm's fraction is rounded.
-__device__ __forceinline__ float logp_of(float xy, float M, float L, float s) {
+// log p_y of a row with shift M (-inf: all entries are) and sum s.  Of log2 s =
+// k + log2 f only the second part, of size below 1, is rounded to 32 bits; the rest
+// is in 64, so that what is taken from it, such as a ratio to an old log-probability
+// near it, does not lose the bits that cancel.
+__device__ __forceinline__ double logp_of(float xy, float M, float L, float s) {
     const float base = M == -INFINITY ? 0.0f : M;
     int k;
     const float f = frexpf(s, &k);
-    return (__builtin_fmaf(xy - base, L, -(float)k) - __log2f(f)) * kLn2;
+    return (((double)xy - (double)base) * (double)L - (double)k - (double)__log2f(f)) * 0.69314718055994531;
 }
 
 // -- policy -------------------------------------------------------------------
@@ -383,8 +385,8 @@ struct Clip {
     bool free;
 };
 
-__device__ __forceinline__ Clip policy_clip(const PolicyArgs& a, const Token& k, float logp) {
-    const float ratio = a.old_logp ? exp2_fast((logp - k.old) * kLog2e) : logp == logp ? 1.0f : NAN;
+__device__ __forceinline__ Clip policy_clip(const PolicyArgs& a, const Token& k, double logp) {
+    const float ratio = a.old_logp ? exp2_fast((float)(logp - k.old) * kLog2e) : logp == logp ? 1.0f : NAN;
     Clip c;
     c.unclipped = ratio * k.A;
     const float clipped = fminf(fmaxf(ratio, 1.0f - a.lo), 1.0f + a.hi) * k.A;
@@ -394,22 +396,22 @@ __device__ __forceinline__ Clip policy_clip(const PolicyArgs& a, const Token& k,
 }
 
 // c: the loss's slope in the logits' log-probability, for the gradient.
-__device__ __forceinline__ float policy_slope(const PolicyArgs& a, const Token& k, float logp) {
+__device__ __forceinline__ float policy_slope(const PolicyArgs& a, const Token& k, double logp) {
     const Clip c = policy_clip(a, k, logp);
     float slope = c.free ? -c.unclipped : 0.0f;
-    if (a.ref_logp) slope = __builtin_fmaf(a.kl, 1.0f - exp2_fast((k.ref - logp) * kLog2e), slope);
+    if (a.ref_logp) slope = __builtin_fmaf(a.kl, 1.0f - exp2_fast((float)(k.ref - logp) * kLog2e), slope);
     return a.scale * a.inv_tau * k.w * slope;
 }
 
 // What the token adds to the loss, by one thread.
-__device__ __forceinline__ void policy_write(const PolicyArgs& a, int64_t i, const Token& k, float logp) {
+__device__ __forceinline__ void policy_write(const PolicyArgs& a, int64_t i, const Token& k, double logp) {
     const Clip c = policy_clip(a, k, logp);
     float kl = 0.0f;
     if (a.ref_logp) {
-        const float d = k.ref - logp;
+        const float d = (float)(k.ref - logp);
         kl = expm1f(d) - d;
     }
-    a.logp[i] = logp;
+    a.logp[i] = (float)logp;
     a.tokens[i] = make_float4(k.w * (-c.smaller + a.kl * kl), k.w * kl, c.free ? 0.0f : k.w, 0.0f);
 }
 
@@ -436,7 +438,7 @@ __device__ __forceinline__ void policy_ignored(const PolicyArgs& a, int64_t i, i
 
 // One row of logits per kThreads threads, held in kHeld vectors a thread.
 template <int DT, int kThreads, int kHeld>
-__global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) __attribute__((amdgpu_waves_per_eu(kHeld <= 13 ? 6 : 4)))
+__global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) __attribute__((amdgpu_waves_per_eu(kHeld <= 8 ? 6 : 4)))
 void policy_held(PolicyArgs a) {
     typedef typename Elem<DT>::T T;
     constexpr int N = 16 / Elem<DT>::kSize;
@@ -503,7 +505,7 @@ void policy_held(PolicyArgs a) {
         join_stats<kWaves>(a.L, m, s, lds);
         base = m;
     }
-    const float logp = logp_of(lab.x, base, a.L, s);
+    const double logp = logp_of(lab.x, base, a.L, s);
     if (tid == 0) policy_write(a, i, tk, logp);
     if (!a.grad) return;
     const float c = policy_slope(a, tk, logp), k1 = -c / s;
@@ -546,7 +548,7 @@ __global__ __launch_bounds__(kRowThreads) void policy_long(PolicyArgs a) {
     const Label<DT> lab(in, a.V, label);
     const Token tk = policy_token(a, r, t);
     const float2 st = stream_row<DT, kRowThreads>({in, a.V, at}, threadIdx.x, a.L, lds);
-    const float logp = logp_of(lab.x, st.x, a.L, st.y);
+    const double logp = logp_of(lab.x, st.x, a.L, st.y);
     if (threadIdx.x == 0) policy_write(a, i, tk, logp);
     if (!a.grad) return;
     write_gradient<DT, kRowThreads>(in, out, a.V, at, threadIdx.x, st, a.L, policy_slope(a, tk, logp), lab.y);
@@ -640,7 +642,7 @@ __global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void pref_logp(Pre
     const Label<DT> lab(in, a.V, label);
     const float2 st = stream_row<DT, kThreads>({in, a.V, at}, tid, kLog2e, lds);
     if (tid == 0) {
-        a.logp[r * a.T + t] = logp_of(lab.x, st.x, kLog2e, st.y);
+        a.logp[r * a.T + t] = (float)logp_of(lab.x, st.x, kLog2e, st.y);
         a.stats[r * a.T + t] = st;
     }
 }
