@@ -31,6 +31,9 @@ namespace {
 
 constexpr int kFinishBlocks = 32;     // workgroups that add the tokens' shares of the loss
 constexpr int64_t kFewTokens = 65536, kFewSequences = 256;  // counted by one workgroup
+constexpr int64_t kRowPairs = 8, kRowPairTokens = 512;  // pairs worked out with every row
+constexpr int64_t kRowTokens = 2048;  // counted by every row's workgroup
+constexpr int kLongest = 20;         // vectors each of 1024 threads holds of the longest held row
 constexpr int kRowThreads = 1024;    // rows that no workgroup's registers hold
 constexpr int kStatThreads = 256;    // preference rows
 constexpr float kLeast = 0x1p-40f, kGreatest = 0x1p60f;  // a sum of unshifted e_j in range
@@ -100,16 +103,21 @@ __device__ __forceinline__ void join_stats(float L, float& m, float& s, float2* 
     s = t;
 }
 
-// The sum over the row's threads, in every thread; one barrier.
+// The sum over the row's threads, in every thread, and that of a number each
+// wavefront brings; one barrier.
 template <int kWaves>
-__device__ __forceinline__ float row_sum(float s, float* lds) {
+__device__ __forceinline__ float row_sum(float s, int& n, float2* lds) {
     s = wave_sum(s);
     if (kWaves == 1) return s;
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = make_float2(s, __int_as_float(n));
     __syncthreads();
     s = 0.0f;
+    n = 0;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) s += lds[w];
+    for (int w = 0; w < kWaves; ++w) {
+        s += lds[w].x;
+        n += __float_as_int(lds[w].y);
+    }
     return s;
 }
 
@@ -270,7 +278,8 @@ __device__ __forceinline__ float2 stream_row(const Row<DT, kThreads>& row, int t
                 for (int i = 0; i < N; ++i) s += f[i];
             }
     }
-    s = row_sum<kWaves>(s, reinterpret_cast<float*>(lds));
+    int none = 0;
+    s = row_sum<kWaves>(s, none, lds);
     if (in_range(s)) return make_float2(0.0f, s);
     float m;
     stream_stats<DT, kThreads>(row, tid, L, m, s);
@@ -307,7 +316,7 @@ struct PolicyArgs {
     float lo, hi, kl, L, inv_tau, scale;
     int32_t by_sequence;
     float* logp;
-    const float* weight;  // [R] one token's weight, or [1]
+    const float* weight;  // policy_weight's; NULL: the mean over few tokens, counted with each row
     float4* tokens;       // per token: weighted loss, KL, clipped
     double* sums;         // [3][kFinishBlocks]
     int* done;            // workgroups of the last launch that have added theirs
@@ -371,11 +380,26 @@ struct Token {
 
 __device__ __forceinline__ Token policy_token(const PolicyArgs& a, int64_t r, int64_t t) {
     Token k;
-    k.w = a.by_sequence ? a.weight[0] / a.weight[1 + r] : a.weight[0];
+    k.w = !a.weight ? 0.0f : a.by_sequence ? a.weight[0] / a.weight[1 + r] : a.weight[0];
     k.A = a.adv[r * a.adv_seq + t * a.adv_tok];
     k.old = a.old_logp ? a.old_logp[r * a.T + t] : 0.0f;
     k.ref = a.ref_logp ? a.ref_logp[r * a.T + t] : 0.0f;
     return k;
+}
+
+// The tokens that count, of those this wavefront looks at.
+__device__ __forceinline__ int count_tokens(const PolicyArgs& a, int tid, int threads) {
+    int n = 0;
+    for (int i0 = 0; i0 < (int)a.rows; i0 += threads) {
+        const int i = i0 + tid;
+        bool some = false;
+        if (i < (int)a.rows) {
+            const int r = i / (int)a.T;
+            some = a.labels[r * a.label_pitch + (i - r * (int)a.T)] != a.ignore;
+        }
+        n += __popcll(__ballot(some));
+    }
+    return n;
 }
 
 // What the clipped term is: the ratio's product, the smaller of the two, and
@@ -469,7 +493,8 @@ void policy_held(PolicyArgs a) {
     const int e = row.edge(tid);
     const float ex = e >= 0 ? Elem<DT>::up(row.p[e]) : -INFINITY;
     const Label<DT> lab(in, a.V, label);
-    const Token tk = policy_token(a, r, t);
+    Token tk = policy_token(a, r, t);
+    int kept = a.weight ? 0 : count_tokens(a, tid, kThreads);
     float f[N], s = exp2_fast(ex * a.L), base = 0.0f;
 #pragma unroll
     for (int k = 0; k < kHeld; ++k)
@@ -479,7 +504,8 @@ void policy_held(PolicyArgs a) {
 #pragma unroll
             for (int q = 0; q < N; ++q) s += f[q];
         }
-    s = row_sum<kWaves>(s, reinterpret_cast<float*>(lds));
+    s = row_sum<kWaves>(s, kept, lds);
+    if (!a.weight) tk.w = 1.0f / (float)kept;
     const bool shifted = !in_range(s);
     if (shifted) {
         float m = ex;
@@ -647,31 +673,60 @@ __global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void pref_logp(Pre
     }
 }
 
-// The pair's rewards, loss and both c, from the wavefronts' sums and counts.
-__device__ __forceinline__ void pref_finish_pair(const PrefArgs& a, int64_t p, const double (&lds)[2][4],
-                                                 const int (&cnt)[2][4]) {
-    double sum[2], share[2];
+// A pair's rewards, loss and both c, from its answers' sums and numbers of tokens.
+struct Pair {
+    double reward[2], loss, c[2];
+};
+
+__device__ __forceinline__ Pair pref_finish_pair(const PrefArgs& a, const double (&sum)[2], const int (&n)[2]) {
+    Pair q;
+    double share[2];
 #pragma unroll
     for (int side = 0; side < 2; ++side) {
-        double s = 0.0;
-        int k = 0;
-        for (int w = 0; w < 4; ++w) {
-            s += lds[side][w];
-            k += cnt[side][w];
-        }
-        share[side] = a.average ? 1.0 / (k > 0 ? k : 1) : 1.0;
-        sum[side] = (double)a.beta * s * share[side];
-        a.rewards[side ? a.P + p : p] = (float)sum[side];
+        share[side] = a.average ? 1.0 / (n[side] > 0 ? n[side] : 1) : 1.0;
+        q.reward[side] = (double)a.beta * sum[side] * share[side];
     }
-    const double h = sum[0] - sum[1], eps = a.smoothing;
-    const double low = log1p(exp(-fabs(h)));  // -log sigmoid(|h|)
-    a.pair_loss[p] = (float)((1.0 - eps) * (low + fmax(-h, 0.0)) + eps * (low + fmax(h, 0.0)));
+    const double h = q.reward[0] - q.reward[1], eps = a.smoothing;
+    const double z = exp(-fabs(h)), low = log1p(z);  // low: -log sigmoid(|h|)
+    q.loss = (1.0 - eps) * (low + fmax(-h, 0.0)) + eps * (low + fmax(h, 0.0));
     // sigmoid(h) - (1 - eps) = eps sigmoid(h) - (1 - eps) sigmoid(-h)
-    const double z = exp(-fabs(h)), big = 1.0 / (1.0 + z), small = z / (1.0 + z);
+    const double big = 1.0 / (1.0 + z), small = z / (1.0 + z);
     const double up = h >= 0.0 ? big : small, down = h >= 0.0 ? small : big;
     const double slope = (double)a.beta * (eps * up - (1.0 - eps) * down) / (double)a.P * (double)a.scale;
-    a.coef[p] = (float)(slope * share[0]);
-    a.coef[a.P + p] = (float)(-slope * share[1]);
+    q.c[0] = slope * share[0];
+    q.c[1] = -slope * share[1];
+    return q;
+}
+
+// What a thread adds to an answer's sum and number of tokens, `step` tokens apart.
+__device__ __forceinline__ void pref_sum(const PrefArgs& a, int64_t r, int first, int step, double& sum, int& n) {
+    sum = 0.0;
+    n = 0;
+    for (int64_t t = first; t < a.T; t += step) {
+        if (a.labels[r * a.label_pitch + t] == a.ignore) continue;
+        sum += (double)a.logp[r * a.T + t] - (a.ref_logp ? (double)a.ref_logp[r * a.T + t] : 0.0);
+        ++n;
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        sum += __shfl_xor(sum, o);
+        n += __shfl_xor(n, o);
+    }
+}
+
+// A pair by one wavefront, the result in every lane.
+__device__ __forceinline__ Pair pref_wave_pair(const PrefArgs& a, int64_t p) {
+    double sum[2];
+    int n[2];
+#pragma unroll
+    for (int side = 0; side < 2; ++side) pref_sum(a, side ? a.P + p : p, threadIdx.x & 63, 64, sum[side], n[side]);
+    return pref_finish_pair(a, sum, n);
+}
+
+__device__ __forceinline__ void pref_write_pair(const PrefArgs& a, int64_t p, const Pair& q) {
+    a.rewards[p] = (float)q.reward[0];
+    a.rewards[a.P + p] = (float)q.reward[1];
+    a.pair_loss[p] = (float)q.loss;
 }
 
 // One workgroup a pair: the two implicit rewards, the loss and both c.
@@ -684,26 +739,25 @@ __global__ __launch_bounds__(256) void pref_pair(PrefArgs a) {
     int n[2];
 #pragma unroll
     for (int side = 0; side < 2; ++side) {
-        const int64_t r = side ? a.P + p : p;
-        sum[side] = 0.0;
-        n[side] = 0;
-        for (int64_t t = threadIdx.x; t < a.T; t += 256) {
-            if (a.labels[r * a.label_pitch + t] == a.ignore) continue;
-            sum[side] += (double)a.logp[r * a.T + t] - (a.ref_logp ? (double)a.ref_logp[r * a.T + t] : 0.0);
-            ++n[side];
-        }
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) {
-            sum[side] += __shfl_xor(sum[side], o);
-            n[side] += __shfl_xor(n[side], o);
-        }
+        pref_sum(a, side ? a.P + p : p, threadIdx.x, 256, sum[side], n[side]);
         if ((threadIdx.x & 63) == 0) {
             lds[side][threadIdx.x >> 6] = sum[side];
             cnt[side][threadIdx.x >> 6] = n[side];
         }
     }
     __syncthreads();
-    if (threadIdx.x == 0) pref_finish_pair(a, p, lds, cnt);
+    if (threadIdx.x == 0) {
+#pragma unroll
+        for (int side = 0; side < 2; ++side)
+            for (int w = 1; w < 4; ++w) {
+                sum[side] += lds[side][w];
+                n[side] += cnt[side][w];
+            }
+        const Pair q = pref_finish_pair(a, sum, n);
+        pref_write_pair(a, p, q);
+        a.coef[p] = (float)q.c[0];
+        a.coef[a.P + p] = (float)q.c[1];
+    }
     // the last pair to finish takes the mean
     if (threadIdx.x == 0) {
         __threadfence();
@@ -718,11 +772,22 @@ __global__ __launch_bounds__(256) void pref_pair(PrefArgs a) {
     v = block_sum<4>(v, lds[0]);
     if (threadIdx.x == 0) a.loss[0] = (float)(v / (double)a.P);
 }
-template <int DT, int kThreads>
+// kPairs: few tokens; every wavefront works out its row's pair for itself, which
+// spares pref_pair's launch, and the first wavefront of the launch writes the pairs.
+template <int DT, int kThreads, bool kPairs>
 __global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void pref_gradient(PrefArgs a) {
     typedef typename Elem<DT>::T T;
     const int tid = threadIdx.x % kThreads;
     const int64_t i = row_of<kThreads>();
+    if (kPairs && blockIdx.x == 0 && threadIdx.x < 64) {
+        double mean = 0.0;
+        for (int64_t p = 0; p < a.P; ++p) {
+            const Pair q = pref_wave_pair(a, p);
+            mean += (float)q.loss;
+            if (threadIdx.x == 0) pref_write_pair(a, p, q);
+        }
+        if (threadIdx.x == 0) a.loss[0] = (float)(mean / (double)a.P);
+    }
     if (i >= 2 * a.P * a.T) return;
     const int64_t r = i / a.T, t = i - r * a.T;
     const int64_t label = a.labels[r * a.label_pitch + t];
@@ -732,9 +797,16 @@ __global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void pref_gradient
         zero_row<DT, kThreads>(out, a.V, at, tid);
         return;
     }
+    float c;
+    if constexpr (kPairs) {
+        const Pair q = pref_wave_pair(a, r < a.P ? r : r - a.P);
+        c = (float)(r < a.P ? q.c[0] : q.c[1]);
+    } else {
+        c = a.coef[r];
+    }
     const int y = (uint64_t)label < (uint64_t)a.V ? (int)label : -1;
     write_gradient<DT, kThreads>(static_cast<const T*>(a.logits) + r * a.seq + t * a.tok, out, a.V, at, tid,
-                                 a.stats[r * a.T + t], kLog2e, a.coef[r], y);
+                                 a.stats[r * a.T + t], kLog2e, c, y);
 }
 
 // What there is without pairs, or before the first launch without tokens.
@@ -845,13 +917,16 @@ gmc_status gmc_policy_loss(void* hip_stream, int32_t dtype, int64_t R, int64_t T
         a.by_sequence = by_sequence != 0;
         a.logp = logp_dev;
         a.weight = weight;
-        if (a.rows > kFewTokens || R > kFewSequences) {
+        const int64_t vecs = V * type_size(dtype) / 16;  // at most, whatever the alignment
+        const bool held = vecs <= 1024 * kLongest;
+        if (held && !a.by_sequence && a.rows <= kRowTokens) {
+            a.weight = nullptr;
+        } else if (a.rows > kFewTokens || R > kFewSequences) {
             policy_counts<<<dim3((unsigned)((R + 3) / 4)), 256, 0, st>>>(a, weight);
             policy_weight<true><<<1, 1024, 0, st>>>(a, weight);
         } else {
             policy_weight<false><<<1, 1024, 0, st>>>(a, weight);
         }
-        const int64_t vecs = V * type_size(dtype) / 16;  // at most, whatever the alignment
         const dim3 rows((unsigned)a.rows), quads((unsigned)((a.rows + 3) / 4));
         GMC_BY_TYPE(dtype, {
             if (vecs <= 64 * 8) policy_held<DT, 64, 8><<<quads, 256, 0, st>>>(a);
@@ -859,13 +934,13 @@ gmc_status gmc_policy_loss(void* hip_stream, int32_t dtype, int64_t R, int64_t T
             else if (vecs <= 512 * 8) policy_held<DT, 512, 8><<<rows, 512, 0, st>>>(a);
             else if (vecs <= 512 * 13) policy_held<DT, 512, 13><<<rows, 512, 0, st>>>(a);
             else if (vecs <= 512 * 26) policy_held<DT, 512, 26><<<rows, 512, 0, st>>>(a);
-            else if (vecs <= 1024 * 20) policy_held<DT, 1024, 20><<<rows, 1024, 0, st>>>(a);
+            else if (held) policy_held<DT, 1024, kLongest><<<rows, 1024, 0, st>>>(a);
             else policy_long<DT><<<rows, kRowThreads, 0, st>>>(a);
         });
     }
     a.stats = stats_dev;
     const int64_t shares = (a.rows + 1023) / 1024;
-    const unsigned finish = shares < 1 ? 1u : shares > kFinishBlocks ? (unsigned)kFinishBlocks : (unsigned)shares;
+    const unsigned finish = a.rows <= 2 * kRowTokens ? 1u : shares > kFinishBlocks ? (unsigned)kFinishBlocks : (unsigned)shares;
     policy_finish<<<dim3(finish), 256, 0, st>>>(a);
     return op_launched(me);
 }
@@ -930,10 +1005,16 @@ gmc_status gmc_preference_loss(void* hip_stream, int32_t dtype, int64_t P, int64
             } else {
                 pref_clear<<<1, 1, 0, st>>>(nullptr, a.done);
             }
-            pref_pair<<<dim3((unsigned)P), 256, 0, st>>>(a);
+            const bool few = a.grad && tokens && P <= kRowPairs && P * T <= kRowPairTokens;
+            if (!few) pref_pair<<<dim3((unsigned)P), 256, 0, st>>>(a);
             if (tokens && a.grad) {
-                if (vecs <= 64 * 8) pref_gradient<DT, 64><<<quads, 256, 0, st>>>(a);
-                else pref_gradient<DT, kStatThreads><<<rows, kStatThreads, 0, st>>>(a);
+                if (vecs <= 64 * 8) {
+                    if (few) pref_gradient<DT, 64, true><<<quads, 256, 0, st>>>(a);
+                    else pref_gradient<DT, 64, false><<<quads, 256, 0, st>>>(a);
+                } else {
+                    if (few) pref_gradient<DT, kStatThreads, true><<<rows, kStatThreads, 0, st>>>(a);
+                    else pref_gradient<DT, kStatThreads, false><<<rows, kStatThreads, 0, st>>>(a);
+                }
             }
         });
     } else {

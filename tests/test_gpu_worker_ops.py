@@ -545,3 +545,70 @@ def test_same_bits_streams_and_graphs():
         torch.cuda.synchronize()
         for a, b in zip(first, held):
             assert torch.equal(a, b), k
+
+
+# -- many short rows: tokens, sequences and pairs counted by launches of their own ----
+
+
+@pytest.mark.parametrize("R,T", [(2, 1500), (600, 3), (40, 60), (70, 1000)])
+@pytest.mark.parametrize("reduction", ["token", "sequence"])
+def test_policy_loss_many_tokens(R, T, reduction):
+    import paper_1905_12948_amd as gmc
+    V = 20
+    rng = np.random.default_rng(R)
+    x = dev(2 * rng.normal(size=(R, T, V)))
+    labels = rng.integers(0, V, (R, T))
+    labels[rng.random((R, T)) < 0.3] = ref.IGNORE
+    labels[::5] = ref.IGNORE
+    adv = dev(rng.normal(size=R))
+    y = np.maximum(labels, 0)
+    table = ref.log_softmax(host(x))
+    kept = labels != ref.IGNORE
+    logp = np.where(kept, np.take_along_axis(table, y[:, :, None], 2)[:, :, 0], 0)
+    old = dev(logp - rng.choice([-0.5, -0.1, 0.02, 0.4], (R, T)))
+    A = host(adv)[:, None]
+    ratio = np.exp(logp - host(old))
+    free, bounded = ratio * A, np.clip(ratio, 0.8, 1.2) * A
+    count = kept.sum(1, keepdims=True)
+    weight = kept / (kept.sum() if reduction == "token" else np.maximum(count, 1) * (count > 0).sum())
+    want = np.array([(weight * -np.minimum(free, bounded)).sum(), 0, (weight * (free > bounded)).sum()])
+    c = weight * np.where(free <= bounded, -free, 0)
+    grad = -c[:, :, None] * np.exp(table)
+    np.put_along_axis(grad, y[:, :, None], np.take_along_axis(grad, y[:, :, None], 2) + c[:, :, None], 2)
+    stats, lp, g = gmc.policy_loss(x, torch.as_tensor(labels).cuda(), old, adv, reduction=reduction)
+    elp = np.where(kept, LP + 8 * U * np.abs(logp), 0.0)
+    size = (weight * (elp + 16 * U) * ratio * np.abs(A)).sum()
+    check(lp, logp, elp, "f32", "logp")
+    check(stats, want, np.array([size + 8 * U * np.abs(want[0]), 0, 16 * U]), "f32", "stats")
+    ec = weight * (elp + 16 * U) * 2 * ratio * np.abs(A)
+    check(g, grad, logits_gradient_slack(c, ec, grad, labels, V), "f32", "gradient")
+
+
+@pytest.mark.parametrize("P,T", [(2, 700), (9, 5), (400, 3), (3, 170), (3, 171), (8, 64), (8, 65)])
+@pytest.mark.parametrize("average", [False, True])
+def test_preference_loss_many_tokens(P, T, average):
+    import paper_1905_12948_amd as gmc
+    V, beta = 20, 0.1
+    rng = np.random.default_rng(P)
+    x = dev(2 * rng.normal(size=(2 * P, T, V)))
+    labels = rng.integers(0, V, (2 * P, T))
+    labels[rng.random((2 * P, T)) < 0.3] = ref.IGNORE
+    labels[1] = ref.IGNORE
+    loss, each, rewards, logp, c, grad = ref.preference(host(x), labels, None, beta, 0.1, average)
+    got = gmc.preference_loss(x, torch.as_tensor(labels).cuda(), beta=beta, smoothing=0.1, average=average)
+    kept = labels != ref.IGNORE
+    elp = np.where(kept, LP + 8 * U * np.abs(logp), 0.0)
+    share = 1 / np.maximum(kept.sum(1), 1) if average else np.ones(2 * P)
+    er = beta * elp.sum(1) * share + U * np.abs(rewards)
+    eh = er[:P] + er[P:]
+    check(got[3], logp, elp, "f32", "logp")
+    check(got[2], rewards, er, "f32", "rewards")
+    check(got[1], each, eh + 4 * U * np.abs(each), "f32", "pair losses")
+    check(got[0], loss, eh.mean() + 8 * U * abs(loss), "f32", "loss")
+    ec = np.concatenate([eh, eh]) * beta * share / (4 * P) + 8 * U * np.abs(c)
+    rows = np.ones((1, T))
+    check(got[4], grad, logits_gradient_slack(c[:, None] * rows, ec[:, None] * rows, grad, labels, V), "f32", "gradient")
+    alone = gmc.preference_loss(x, torch.as_tensor(labels).cuda(), beta=beta, smoothing=0.1, average=average, grad=False)
+    assert torch.equal(alone[3], got[3])
+    for a, b in zip(alone[:3], got[:3]):  # another order of the same 64-bit sums
+        torch.testing.assert_close(a, b, rtol=4 * U, atol=1e-12)
