@@ -582,7 +582,8 @@ gmc_status gmc_group_norm(void* hip_stream, int32_t dtype, int64_t N, int64_t S,
 
 /*
  * Its backward pass: from dL/dy and the forward pass's x, mean and rstd,
- *   dz = dy act'(z) (z as above, bit for bit; relu's derivative at 0 is 0),
+ *   dz = dy act'(z) (z as written, one rounding an operation; relu's derivative
+ *   at 0 is 0),
  *   dgamma[c] = sum dz hat, dbeta[c] = sum dz over images and pixels,
  *   dx = rstd (gamma dz - (s1 + hat s2) / m), s1 = sum gamma dz and s2 = sum
  *   gamma dz hat over the image's group.

@@ -44,7 +44,7 @@ constexpr float kLeast = 0x1p-40f, kGreatest = 0x1p60f;  // a sum of unshifted e
 // (a plain copy of 100 KB rows: 5.9 TB/s, in the launch's order 5.6).
 template <int kThreads>
 __device__ __forceinline__ int64_t row_of() {
-    const int64_t id = xcd_run(gridDim.x);
+    const int64_t id = xcd_run(blockIdx.x, gridDim.x);
     if constexpr (kThreads == 64) return id * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     else return id;
 }

@@ -10,14 +10,18 @@
 // that a wavefront reads whole lines of the channels-last layout; sums are
 // taken per channel and then folded into groups, so groups may have any width.
 //
-// Held form: one workgroup has all pixels of a block of whole groups in its
-// registers: x (and dy) are read once and the result is written once, which is
-// the floor of the bytes; the variance is the second pass over the registers,
-// about the mean.  Split form, for images whose groups do not fit: per-channel
-// moments of pieces of the image, joined about the common mean, and a second
-// launch that reads the images again.  z is formed in the order written, one
-// rounding each, in both directions: a sign of z that decides the gradient is
-// the sign the forward pass saw.  All sums are 32-bit, in a fixed order.
+// What bounds it is the bytes, then, images being small, the fixed work of a
+// workgroup.  Held form: one workgroup has all pixels of a block of whole groups in
+// its registers: x (and dy) are read once and the result is written once, the floor
+// of the bytes.  Split form, for images whose groups do not fit, or fit in slivers
+// of lines only: per-channel sums of pieces of the image, joined, and a second
+// launch that reads the images again.  bf16, relu: 64 x 28 x 28 x 512 forward 18.8 us
+// (5.5 TB/s of x and y), backward 38; 64 x 56 x 56 x 256 forward 46 (4.4 TB/s: two
+// rounds of workgroups of 1024 threads, one a CU), backward 104 (split: 515 MB at
+// 5.5 TB/s and a join of 5 us).
+//
+// In the backward pass z is formed in the order written, one rounding each.  All
+// sums are 32-bit, in a fixed order.
 #include <math.h>
 
 #include <type_traits>
@@ -30,13 +34,20 @@ namespace {
 
 constexpr int kHeldThreads = 1024;
 constexpr int kHeldBlocks = 256;   // held: workgroups below which narrower blocks are tried
+// backward, bytes of x from which blocks under 64 bytes wide (four and more
+// workgroups read every line) give way to the split form's second read:
+// 64 x 3136 x 256 bf16 with silu 124 us held, 112 split, with relu 104 both;
+// 64 x 3136 x 64 24 held, 39 split
+constexpr int64_t kSplitBytes = int64_t(64) << 20;
 constexpr int kManyBlocks = 512;   // held: two workgroups for every CU
 constexpr int kHeldMost = 16;      // vectors of x a thread holds (16 bytes each)
 constexpr int kHeldMostBack = 8;   // ... of x and of dy
 constexpr int kHeldChannels = 256; // threads across channels, at most
 constexpr int kSplitThreads = 256;
 constexpr int kSplitTile = 8;      // pixels whose loads a thread issues together
-constexpr int kSplitBlocks = 1280;  // workgroups, about
+constexpr int kSplitMost = 64;     // pixels a thread sums, at most
+constexpr int kSplitBlocks = 512;   // split: workgroups, about; long pieces stream better
+                                   // (norm_back_sums at 64 x 3136 x 256: 37 us, with 2048 43)
 
 struct NormArgs {
     const void* x;
@@ -379,7 +390,7 @@ __global__ __launch_bounds__(kHeldThreads) void norm_forward_fold(NormArgs a) {
     typedef Vec<DT, VEC> V;
     const Place p = place(a);
     // blocks narrower than a line share it in one XCD's cache
-    const int64_t id = xcd_run(gridDim.x), n = id / (unsigned)a.blocks;
+    const int64_t id = xcd_run(blockIdx.x, gridDim.x), n = id / (unsigned)a.blocks;
     const int blk = (int)(id - n * a.blocks);
     const int c0 = blk * a.cb + p.cv * VEC;
     const int within = F == 1 ? a.cpg / VEC : 1;
@@ -544,7 +555,7 @@ __global__ __launch_bounds__(kHeldThreads) void norm_backward_fold(NormArgs a) {
     typedef Vec<DT, VEC> V;
     const Place p = place(a);
     // blocks narrower than a line share it in one XCD's cache
-    const int64_t id = xcd_run(gridDim.x), n = id / (unsigned)a.blocks;
+    const int64_t id = xcd_run(blockIdx.x, gridDim.x), n = id / (unsigned)a.blocks;
     const int blk = (int)(id - n * a.blocks);
     const int c0 = blk * a.cb + p.cv * VEC;
     const int g0 = F == 1 ? (p.cv * VEC) >> a.cpg_log2 : p.cv * F;
@@ -643,11 +654,11 @@ struct Piece {
 };
 
 template <int VEC>
-__device__ __forceinline__ Piece piece(const NormArgs& a, Place& p) {
+__device__ __forceinline__ Piece piece(const NormArgs& a, Place& p, unsigned before = 0) {
     Piece q;
-    const unsigned per = (unsigned)(a.chunks * a.cblocks);
-    q.n = blockIdx.x / per;
-    const unsigned rest = blockIdx.x - (unsigned)q.n * per;
+    const unsigned per = (unsigned)(a.chunks * a.cblocks), id = (unsigned)xcd_run(blockIdx.x - before, gridDim.x - before);
+    q.n = id / per;
+    const unsigned rest = id - (unsigned)q.n * per;
     q.chunk = (int)(rest / (unsigned)a.cblocks);
     const int cblk = (int)(rest - (unsigned)q.chunk * a.cblocks);
     const int tv = cblk * a.tc + p.cv;
@@ -763,21 +774,24 @@ __global__ __launch_bounds__(kSplitThreads) void norm_forward_split(NormArgs a) 
     float ga[VEC], be[VEC], mu[VEC], rs[VEC], f[VEC];
     load_params<VEC>(a, q.c0, true, ga, be);
     load_stats<VEC>(a, q.n, q.c0, true, mu, rs);
-    for (int s0 = q.first + p.r; s0 < q.last; s0 += 4 * p.rows) {
-        V xv[4];
+    by_act(a.act, [&](auto act) {
+        for (int s0 = q.first + p.r; s0 < q.last; s0 += 4 * p.rows) {
+            V xv[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (s0 + k * p.rows < q.last) xv[k] = V::load(px + (int64_t)(s0 + k * p.rows) * a.x_pixel);
+            for (int k = 0; k < 4; ++k)
+                if (s0 + k * p.rows < q.last) xv[k] = V::load(px + (int64_t)(s0 + k * p.rows) * a.x_pixel);
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (s0 + k * p.rows < q.last) {
-                xv[k].unpack(f);
+            for (int k = 0; k < 4; ++k)
+                if (s0 + k * p.rows < q.last) {
+                    xv[k].unpack(f);
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) f[i] = activate((f[i] - mu[i]) * rs[i] * ga[i] + be[i], a.act);
-                xv[k].pack(f);
-                xv[k].store(py + (int64_t)(s0 + k * p.rows) * a.out_pixel);
-            }
-    }
+                    for (int i = 0; i < VEC; ++i)
+                        f[i] = activate((f[i] - mu[i]) * rs[i] * ga[i] + be[i], decltype(act)::value);
+                    xv[k].pack(f);
+                    xv[k].store_once(py + (int64_t)(s0 + k * p.rows) * a.out_pixel);
+                }
+        }
+    });
 }
 
 // Per (image, chunk, channel): the sums of dz and of dz hat.
@@ -796,29 +810,32 @@ __global__ __launch_bounds__(kSplitThreads) void norm_back_sums(NormArgs a) {
     load_stats<VEC>(a, q.n, q.c0, p.on, mu, rs);
 #pragma unroll
     for (int i = 0; i < VEC; ++i) s1[i] = s2[i] = 0.0f;
-    for (int s0 = q.first + p.r; s0 < q.last && p.on; s0 += 4 * p.rows) {
-        V xv[4], dv[4];
+    by_act(a.act, [&](auto act) {
+        constexpr int kAct = decltype(act)::value;
+        for (int s0 = q.first + p.r; s0 < q.last && p.on; s0 += 4 * p.rows) {
+            V xv[4], dv[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (s0 + k * p.rows < q.last) {
-                xv[k] = V::load(px + (int64_t)(s0 + k * p.rows) * a.x_pixel);
-                dv[k] = V::load(pd + (int64_t)(s0 + k * p.rows) * a.dy_pixel);
-            }
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (s0 + k * p.rows < q.last) {
-                float f[VEC], d[VEC];
-                xv[k].unpack(f);
-                dv[k].unpack(d);
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    const float hat = (f[i] - mu[i]) * rs[i];
-                    const float dz = back_act(d[i], hat * ga[i] + be[i], a.act);
-                    s1[i] += dz;
-                    s2[i] = __builtin_fmaf(dz, hat, s2[i]);
+            for (int k = 0; k < 4; ++k)
+                if (s0 + k * p.rows < q.last) {
+                    xv[k] = V::load_once(px + (int64_t)(s0 + k * p.rows) * a.x_pixel);
+                    dv[k] = V::load_once(pd + (int64_t)(s0 + k * p.rows) * a.dy_pixel);
                 }
-            }
-    }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (s0 + k * p.rows < q.last) {
+                    float f[VEC], d[VEC];
+                    xv[k].unpack(f);
+                    dv[k].unpack(d);
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) {
+                        const float hat = (f[i] - mu[i]) * rs[i];
+                        if constexpr (kAct != GMC_ACT_NONE) d[i] = back_act(d[i], hat * ga[i] + be[i], kAct);
+                        s1[i] += d[i];
+                        s2[i] = __builtin_fmaf(d[i], hat, s2[i]);
+                    }
+                }
+        }
+    });
     const int64_t at = (q.n * a.chunks + q.chunk) * a.C + (q.c0 - p.cv * VEC);
     const int width = a.tc * VEC;
     channel_sums<VEC>(s1, a, p, part, chan);
@@ -870,58 +887,14 @@ __global__ __launch_bounds__(kSplitThreads) void norm_back_join(NormArgs a, floa
     }
 }
 
-template <int DT, int VEC>
-__global__ __launch_bounds__(kSplitThreads) void norm_backward_split(NormArgs a, const float* shared_terms) {
-    typedef typename Elem<DT>::T T;
-    typedef Vec<DT, VEC> V;
-    Place p = place(a);
-    const Piece q = piece<VEC>(a, p);
-    if (!p.on) return;
-    const T* px = static_cast<const T*>(a.x) + q.n * a.x_image + q.c0;
-    const T* pd = static_cast<const T*>(a.dy) + q.n * a.dy_image + q.c0;
-    T* po = static_cast<T*>(a.out) + q.n * a.out_image + q.c0;
-    float ga[VEC], be[VEC], mu[VEC], rs[VEC], s1[VEC], s2[VEC];
-    load_params<VEC>(a, q.c0, true, ga, be);
-    load_stats<VEC>(a, q.n, q.c0, true, mu, rs);
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-        const int64_t at = 2 * (q.n * a.G + group_of(a, q.c0 + i));
-        s1[i] = shared_terms[at];
-        s2[i] = shared_terms[at + 1];
-    }
-    for (int s0 = q.first + p.r; s0 < q.last; s0 += 4 * p.rows) {
-        V xv[4], dv[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (s0 + k * p.rows < q.last) {
-                xv[k] = V::load(px + (int64_t)(s0 + k * p.rows) * a.x_pixel);
-                dv[k] = V::load(pd + (int64_t)(s0 + k * p.rows) * a.dy_pixel);
-            }
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (s0 + k * p.rows < q.last) {
-                float f[VEC], d[VEC];
-                xv[k].unpack(f);
-                dv[k].unpack(d);
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    const float hat = (f[i] - mu[i]) * rs[i];
-                    const float dz = back_act(d[i], hat * ga[i] + be[i], a.act);
-                    f[i] = rs[i] * (dz * ga[i] - __builtin_fmaf(hat, s2[i], s1[i]));
-                }
-                xv[k].pack(f);
-                xv[k].store(po + (int64_t)(s0 + k * p.rows) * a.out_pixel);
-            }
-    }
-}
-
 // dgamma and dbeta: the sums over the images of rows of C values, `pitch`
 // apart.  16 channels (a 64-byte line of each row) and 16 row slots a workgroup.
 constexpr int kParamCh = 16;
-__global__ __launch_bounds__(kSplitThreads) void norm_params(const float* part, const float* part2, int64_t rows,
-                                                             int64_t pitch, int32_t C, float* dgamma, float* dbeta) {
+
+__device__ __forceinline__ void sum_params(int block, const float* part, const float* part2, int64_t rows, int64_t pitch,
+                                           int32_t C, float* dgamma, float* dbeta) {
     __shared__ float lds[2][kSplitThreads];
-    const int c = blockIdx.x * kParamCh + (threadIdx.x & (kParamCh - 1));
+    const int c = block * kParamCh + (threadIdx.x & (kParamCh - 1));
     float s1 = 0.0f, s2 = 0.0f;
     if (c < C)
 #pragma unroll 4
@@ -943,6 +916,71 @@ __global__ __launch_bounds__(kSplitThreads) void norm_params(const float* part, 
         if (dbeta) dbeta[c] = lds[0][threadIdx.x];
         if (dgamma) dgamma[c] = lds[1][threadIdx.x];
     }
+}
+
+__global__ __launch_bounds__(kSplitThreads) void norm_params(const float* part, const float* part2, int64_t rows,
+                                                             int32_t C, float* dgamma, float* dbeta) {
+    sum_params((int)blockIdx.x, part, part2, rows, C, C, dgamma, dbeta);
+}
+
+// The first `params` workgroups sum the parameters' gradients, the others are pieces.
+template <int DT, int VEC>
+__global__ __launch_bounds__(kSplitThreads) void norm_backward_split(NormArgs a, const float* shared_terms, int params,
+                                                                     float* dgamma, float* dbeta) {
+    typedef typename Elem<DT>::T T;
+    typedef Vec<DT, VEC> V;
+    if ((int)blockIdx.x < params) {
+        sum_params((int)blockIdx.x, a.part, a.part2, a.N, a.chunks * (int64_t)a.C, a.C, dgamma, dbeta);
+        return;
+    }
+    Place p = place(a);
+    const Piece q = piece<VEC>(a, p, (unsigned)params);
+    if (!p.on) return;
+    const T* px = static_cast<const T*>(a.x) + q.n * a.x_image + q.c0;
+    const T* pd = static_cast<const T*>(a.dy) + q.n * a.dy_image + q.c0;
+    T* po = static_cast<T*>(a.out) + q.n * a.out_image + q.c0;
+    float ga[VEC], be[VEC], mu[VEC], rs[VEC], s1[VEC], s2[VEC];
+    load_params<VEC>(a, q.c0, true, ga, be);
+    load_stats<VEC>(a, q.n, q.c0, true, mu, rs);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+        const int64_t at = 2 * (q.n * a.G + group_of(a, q.c0 + i));
+        s1[i] = shared_terms[at];
+        s2[i] = shared_terms[at + 1];
+    }
+    // as in norm_backward_fold
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+        s1[i] = -rs[i] * s1[i];
+        s2[i] = -rs[i] * rs[i] * s2[i];
+    }
+    by_act(a.act, [&](auto act) {
+        constexpr int kAct = decltype(act)::value;
+        for (int s0 = q.first + p.r; s0 < q.last; s0 += 4 * p.rows) {
+            V xv[4], dv[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (s0 + k * p.rows < q.last) {
+                    xv[k] = V::load_once(px + (int64_t)(s0 + k * p.rows) * a.x_pixel);
+                    dv[k] = V::load_once(pd + (int64_t)(s0 + k * p.rows) * a.dy_pixel);
+                }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (s0 + k * p.rows < q.last) {
+                    float f[VEC], d[VEC];
+                    xv[k].unpack(f);
+                    dv[k].unpack(d);
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) {
+                        const float c = f[i] - mu[i];
+                        if constexpr (kAct != GMC_ACT_NONE) d[i] = back_act(d[i], c * rs[i] * ga[i] + be[i], kAct);
+                        f[i] = __builtin_fmaf(d[i], rs[i] * ga[i], __builtin_fmaf(c, s2[i], s1[i]));
+                    }
+                    xv[k].pack(f);
+                    xv[k].store_once(po + (int64_t)(s0 + k * p.rows) * a.out_pixel);
+                }
+        }
+    });
 }
 
 // -- host ---------------------------------------------------------------------
@@ -1009,6 +1047,27 @@ bool plan_fold(NormArgs& a, NormPlan& pl, int64_t size, bool backward, int line)
     return false;
 }
 
+// The split form: every channel, pieces of an image.
+NormPlan norm_plan_split(NormArgs& a, NormPlan pl, int full) {
+    pl.vec = a.C % full == 0 ? full : 1;
+    const int64_t vecs = a.C / pl.vec;
+    a.tc = (int32_t)(vecs < kSplitThreads ? vecs : kSplitThreads);
+    a.tp_log2 = log2_up(a.tc);
+    a.cblocks = (int32_t)((vecs + a.tc - 1) / a.tc);
+    const int rows = kSplitThreads >> a.tp_log2;
+    // pixels per workgroup: enough workgroups for every CU, one to eight tiles each
+    int64_t chunks = (a.S + (int64_t)rows * kSplitTile - 1) / ((int64_t)rows * kSplitTile);
+    const int64_t want = (kSplitBlocks + a.N * a.cblocks - 1) / (a.N * a.cblocks);
+    const int64_t least = (a.S + (int64_t)rows * kSplitMost - 1) / ((int64_t)rows * kSplitMost);
+    if (chunks > want) chunks = want > least ? want : least;
+    a.chunk = (int32_t)((a.S + chunks - 1) / chunks);
+    a.chunks = (a.S + a.chunk - 1) / a.chunk;
+    const int slots = a.tp_log2 < 6 ? kSplitThreads / 64 : rows;
+    pl.threads = kSplitThreads;
+    pl.lds = sizeof(float) * ((size_t)(slots + 1) * pl.vec << a.tp_log2);
+    return pl;
+}
+
 // Chooses the form and fills the geometry of a.
 NormPlan norm_plan(NormArgs& a, int32_t dtype, bool backward) {
     NormPlan pl;
@@ -1022,7 +1081,12 @@ NormPlan norm_plan(NormArgs& a, int32_t dtype, bool backward) {
             if (!plan_fold(a, pl, type_size(dtype), backward, line)) continue;
             if (a.N * a.blocks >= kHeldBlocks) break;
         }
-        if (pl.held) return pl;
+        if (pl.held && !(backward && (int64_t)a.cb * type_size(dtype) < 64 &&
+                         a.N * (int64_t)a.S * a.C * type_size(dtype) >= kSplitBytes)) return pl;
+        if (pl.held) {
+            pl = NormPlan{};
+            return norm_plan_split(a, pl, full);
+        }
     }
     // any groups: the fewest whose channels fill a 128-byte line (else a 64-byte
     // half), with a thread count that leaves at most `most` vectors each
@@ -1054,22 +1118,7 @@ NormPlan norm_plan(NormArgs& a, int32_t dtype, bool backward) {
             pl.lds = sizeof(float) * (((size_t)(slots + 1) * vec << lg) + 2 * (size_t)gw);
         }
     if (pl.held) return pl;
-    pl.vec = a.C % full == 0 ? full : 1;
-    const int64_t vecs = a.C / pl.vec;
-    a.tc = (int32_t)(vecs < kSplitThreads ? vecs : kSplitThreads);
-    a.tp_log2 = log2_up(a.tc);
-    a.cblocks = (int32_t)((vecs + a.tc - 1) / a.tc);
-    const int rows = kSplitThreads >> a.tp_log2;
-    // pixels per workgroup: enough workgroups for every CU, a few tiles each
-    int64_t chunks = (a.S + (int64_t)rows * kSplitTile - 1) / ((int64_t)rows * kSplitTile);
-    const int64_t want = (kSplitBlocks + a.N * a.cblocks - 1) / (a.N * a.cblocks);
-    if (chunks > want) chunks = want;
-    a.chunk = (int32_t)((a.S + chunks - 1) / chunks);
-    a.chunks = (a.S + a.chunk - 1) / a.chunk;
-    const int slots = a.tp_log2 < 6 ? kSplitThreads / 64 : rows;
-    pl.threads = kSplitThreads;
-    pl.lds = sizeof(float) * ((size_t)(slots + 1) * pl.vec << a.tp_log2);
-    return pl;
+    return norm_plan_split(a, pl, full);
 }
 
 // Scratch in floats: two arrays of per-channel partial values, and for the
@@ -1226,7 +1275,7 @@ gmc_status gmc_group_norm_backward(void* hip_stream, int32_t dtype, int64_t N, i
     const dim3 param_grid((unsigned)((C + kParamCh - 1) / kParamCh));
     if (N == 0) {
         if (dgamma_dev || dbeta_dev)
-            norm_params<<<param_grid, kSplitThreads, 0, st>>>(nullptr, nullptr, 0, 0, C, dgamma_dev, dbeta_dev);
+            norm_params<<<param_grid, kSplitThreads, 0, st>>>(nullptr, nullptr, 0, C, dgamma_dev, dbeta_dev);
         return op_launched(me);
     }
     if (!dy_dev || !x_dev || !dx_dev || !mean_dev || !rstd_dev) return op_error(GMC_EINVAL, me, "NULL argument");
@@ -1283,15 +1332,16 @@ gmc_status gmc_group_norm_backward(void* hip_stream, int32_t dtype, int64_t N, i
                     }));
     } else {
         float* shared_terms = a.part2 + rows * (int64_t)C;
+        const unsigned params = dgamma_dev || dbeta_dev ? param_grid.x : 0;
         GMC_BY_TYPE(dtype, GMC_NORM_VEC(16 / Elem<DT>::kSize, {
                         norm_back_sums<DT, VEC><<<grid, pl.threads, pl.lds, st>>>(a);
                         norm_back_join<<<joins, kSplitThreads, 0, st>>>(a, shared_terms);
-                        norm_backward_split<DT, VEC><<<grid, pl.threads, 0, st>>>(a, shared_terms);
+                        norm_backward_split<DT, VEC><<<dim3(grid.x + params), pl.threads, 0, st>>>(
+                            a, shared_terms, (int)params, dgamma_dev, dbeta_dev);
                     }));
     }
-    if (dgamma_dev || dbeta_dev)
-        norm_params<<<param_grid, kSplitThreads, 0, st>>>(a.part, a.part2, N, (pl.held ? 1 : a.chunks) * (int64_t)C, C,
-                                                          dgamma_dev, dbeta_dev);
+    if (pl.held && (dgamma_dev || dbeta_dev))
+        norm_params<<<param_grid, kSplitThreads, 0, st>>>(a.part, a.part2, N, C, dgamma_dev, dbeta_dev);
     return op_launched(me);
 }
 

@@ -169,10 +169,10 @@ __device__ __forceinline__ float wave_max(float v) {
     return v;
 }
 
-// This workgroup's number among `total`, so numbered that each XCD has a run of
+// The work of workgroup `index` of `total`, so dealt that each XCD has a run of
 // neighbours: workgroups go to the 8 XCDs in turn, each with a cache of its own.
-__device__ __forceinline__ int64_t xcd_run(unsigned total) {
-    const unsigned x = blockIdx.x & 7u, j = blockIdx.x >> 3, q = total >> 3, r = total & 7u;
+__device__ __forceinline__ int64_t xcd_run(unsigned index, unsigned total) {
+    const unsigned x = index & 7u, j = index >> 3, q = total >> 3, r = total & 7u;
     return (int64_t)x * q + (x < r ? x : r) + j;
 }
 
