@@ -255,7 +255,8 @@ __device__ __forceinline__ void write_gradient(const typename Elem<DT>::T* in, t
 }
 
 // A row's shift and sum, read from memory: (0, s) in range, else with the maximum.
-template <int DT, int kThreads>
+// kOnce: nothing reads the row again.
+template <int DT, int kThreads, bool kOnce>
 __device__ __forceinline__ float2 stream_row(const Row<DT, kThreads>& row, int tid, float L, float2* lds) {
     constexpr int N = 16 / Elem<DT>::kSize;
     constexpr int kWaves = kThreads / 64;
@@ -268,7 +269,10 @@ __device__ __forceinline__ float2 stream_row(const Row<DT, kThreads>& row, int t
         float f[N];
 #pragma unroll
         for (int k = 0; k < kBatch; ++k)
-            if (v0 + k * kThreads < row.nb) x[k] = V::load_once(row.p + row.head + (int64_t)(v0 + k * kThreads) * N);
+            if (v0 + k * kThreads < row.nb) {
+                const typename Elem<DT>::T* q = row.p + row.head + (int64_t)(v0 + k * kThreads) * N;
+                x[k] = kOnce ? V::load_once(q) : V::load(q);
+            }
 #pragma unroll
         for (int k = 0; k < kBatch; ++k)
             if (v0 + k * kThreads < row.nb) {
@@ -573,7 +577,7 @@ __global__ __launch_bounds__(kRowThreads) void policy_long(PolicyArgs a) {
     const T* in = static_cast<const T*>(a.logits) + r * a.seq + t * a.tok;
     const Label<DT> lab(in, a.V, label);
     const Token tk = policy_token(a, r, t);
-    const float2 st = stream_row<DT, kRowThreads>({in, a.V, at}, threadIdx.x, a.L, lds);
+    const float2 st = stream_row<DT, kRowThreads, false>({in, a.V, at}, threadIdx.x, a.L, lds);
     const double logp = logp_of(lab.x, st.x, a.L, st.y);
     if (threadIdx.x == 0) policy_write(a, i, tk, logp);
     if (!a.grad) return;
@@ -648,7 +652,7 @@ struct PrefArgs {
     float* coef;       // [2P]
 };
 
-template <int DT, int kThreads>
+template <int DT, int kThreads, bool kOnce>
 __global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void pref_logp(PrefArgs a) {
     typedef typename Elem<DT>::T T;
     constexpr int kWaves = kThreads / 64;
@@ -666,7 +670,7 @@ __global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void pref_logp(Pre
     const int64_t at = r * a.seq + t * a.tok;  // nothing is written: whole lines are read
     const T* in = static_cast<const T*>(a.logits) + at;
     const Label<DT> lab(in, a.V, label);
-    const float2 st = stream_row<DT, kThreads>({in, a.V, at}, tid, kLog2e, lds);
+    const float2 st = stream_row<DT, kThreads, kOnce>({in, a.V, at}, tid, kLog2e, lds);
     if (tid == 0) {
         a.logp[r * a.T + t] = (float)logp_of(lab.x, st.x, kLog2e, st.y);
         a.stats[r * a.T + t] = st;
@@ -772,13 +776,18 @@ __global__ __launch_bounds__(256) void pref_pair(PrefArgs a) {
     v = block_sum<4>(v, lds[0]);
     if (threadIdx.x == 0) a.loss[0] = (float)(v / (double)a.P);
 }
+// The rows from the last to the first: of what the first launch read, the 256 MB
+// cache behind the XCDs' has the last rows (16 x 512 x 50257 bf16 both launches:
+// 303 us, in the first launch's order 328).  Rows of over 2048 vectors by 1024
+// threads, so that few rows are under way at once (256 threads: 346 us).
+//
 // kPairs: few tokens; every wavefront works out its row's pair for itself, which
 // spares pref_pair's launch, and the first wavefront of the launch writes the pairs.
 template <int DT, int kThreads, bool kPairs>
 __global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void pref_gradient(PrefArgs a) {
     typedef typename Elem<DT>::T T;
     const int tid = threadIdx.x % kThreads;
-    const int64_t i = row_of<kThreads>();
+    const int64_t i = 2 * a.P * a.T - 1 - row_of<kThreads>();
     if (kPairs && blockIdx.x == 0 && threadIdx.x < 64) {
         double mean = 0.0;
         for (int64_t p = 0; p < a.P; ++p) {
@@ -788,7 +797,7 @@ __global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void pref_gradient
         }
         if (threadIdx.x == 0) a.loss[0] = (float)(mean / (double)a.P);
     }
-    if (i >= 2 * a.P * a.T) return;
+    if (i < 0) return;
     const int64_t r = i / a.T, t = i - r * a.T;
     const int64_t label = a.labels[r * a.label_pitch + t];
     const int64_t at = r * a.grad_seq + t * a.grad_tok;
@@ -1000,8 +1009,9 @@ gmc_status gmc_preference_loss(void* hip_stream, int32_t dtype, int64_t P, int64
         const dim3 rows((unsigned)tokens), quads((unsigned)((tokens + 3) / 4));
         GMC_BY_TYPE(dtype, {
             if (tokens) {
-                if (vecs <= 64 * 8) pref_logp<DT, 64><<<quads, 256, 0, st>>>(a);
-                else pref_logp<DT, kStatThreads><<<rows, kStatThreads, 0, st>>>(a);
+                if (vecs <= 64 * 8) pref_logp<DT, 64, false><<<quads, 256, 0, st>>>(a);
+                else if (a.grad) pref_logp<DT, kStatThreads, false><<<rows, kStatThreads, 0, st>>>(a);
+                else pref_logp<DT, kStatThreads, true><<<rows, kStatThreads, 0, st>>>(a);
             } else {
                 pref_clear<<<1, 1, 0, st>>>(nullptr, a.done);
             }
@@ -1013,7 +1023,8 @@ gmc_status gmc_preference_loss(void* hip_stream, int32_t dtype, int64_t P, int64
                     else pref_gradient<DT, 64, false><<<quads, 256, 0, st>>>(a);
                 } else {
                     if (few) pref_gradient<DT, kStatThreads, true><<<rows, kStatThreads, 0, st>>>(a);
-                    else pref_gradient<DT, kStatThreads, false><<<rows, kStatThreads, 0, st>>>(a);
+                    else if (vecs <= 2048) pref_gradient<DT, 512, false><<<rows, 512, 0, st>>>(a);
+                    else pref_gradient<DT, 1024, false><<<rows, 1024, 0, st>>>(a);
                 }
             }
         });

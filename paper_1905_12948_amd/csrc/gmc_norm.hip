@@ -17,8 +17,8 @@
 // of lines only: per-channel sums of pieces of the image, joined, and a second
 // launch that reads the images again.  bf16, relu: 64 x 28 x 28 x 512 forward 18.8 us
 // (5.5 TB/s of x and y), backward 38; 64 x 56 x 56 x 256 forward 46 (4.4 TB/s: two
-// rounds of workgroups of 1024 threads, one a CU), backward 104 (split: 515 MB at
-// 5.5 TB/s and a join of 5 us).
+// rounds of workgroups of 1024 threads, one a CU), backward 93 (split: 515 MB in two
+// launches, and a join of 5 us).
 //
 // In the backward pass z is formed in the order written, one rounding each.  All
 // sums are 32-bit, in a fixed order.
@@ -36,8 +36,8 @@ constexpr int kHeldThreads = 1024;
 constexpr int kHeldBlocks = 256;   // held: workgroups below which narrower blocks are tried
 // backward, bytes of x from which blocks under 64 bytes wide (four and more
 // workgroups read every line) give way to the split form's second read:
-// 64 x 3136 x 256 bf16 with silu 124 us held, 112 split, with relu 104 both;
-// 64 x 3136 x 64 24 held, 39 split
+// 64 x 3136 x 256 bf16 104 us held (silu 124), 93 split (101); 64 x 3136 x 64 24
+// held, 39 split
 constexpr int64_t kSplitBytes = int64_t(64) << 20;
 constexpr int kManyBlocks = 512;   // held: two workgroups for every CU
 constexpr int kHeldMost = 16;      // vectors of x a thread holds (16 bytes each)
@@ -47,7 +47,7 @@ constexpr int kSplitThreads = 256;
 constexpr int kSplitTile = 8;      // pixels whose loads a thread issues together
 constexpr int kSplitMost = 64;     // pixels a thread sums, at most
 constexpr int kSplitBlocks = 512;   // split: workgroups, about; long pieces stream better
-                                   // (norm_back_sums at 64 x 3136 x 256: 37 us, with 2048 43)
+                                   // (norm_back_sums at 64 x 3136 x 256: 37 us, 43 with 2048)
 
 struct NormArgs {
     const void* x;
@@ -794,7 +794,9 @@ __global__ __launch_bounds__(kSplitThreads) void norm_forward_split(NormArgs a) 
     });
 }
 
-// Per (image, chunk, channel): the sums of dz and of dz hat.
+// Per (image, chunk, channel): the sums of dz and of dz hat.  Ordinary loads: the next
+// launch finds up to 256 MB of what is read here in the cache behind the XCDs'
+// (64 x 3136 x 256 bf16: 93 us in all, with nontemporal loads 106).
 template <int DT, int VEC>
 __global__ __launch_bounds__(kSplitThreads) void norm_back_sums(NormArgs a) {
     typedef typename Elem<DT>::T T;
@@ -817,8 +819,8 @@ __global__ __launch_bounds__(kSplitThreads) void norm_back_sums(NormArgs a) {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
                 if (s0 + k * p.rows < q.last) {
-                    xv[k] = V::load_once(px + (int64_t)(s0 + k * p.rows) * a.x_pixel);
-                    dv[k] = V::load_once(pd + (int64_t)(s0 + k * p.rows) * a.dy_pixel);
+                    xv[k] = V::load(px + (int64_t)(s0 + k * p.rows) * a.x_pixel);
+                    dv[k] = V::load(pd + (int64_t)(s0 + k * p.rows) * a.dy_pixel);
                 }
 #pragma unroll
             for (int k = 0; k < 4; ++k)
