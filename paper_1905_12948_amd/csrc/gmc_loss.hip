@@ -16,8 +16,13 @@
 //
 // Policy: c depends on the token alone, so a workgroup keeps the row in its
 // registers: the logits are read once and the gradient is written once, the
-// floor of the bytes.  Preference: c needs the pair's sums over all its tokens;
-// the rows are read for the statistics and again for the gradient.
+// floor of the bytes.  16 x 1024 x 50257 bf16, three quarters of the tokens counting:
+// 511 us, 5.6 TB/s, where a plain copy of such rows reaches 5.9; 555 us from a view
+// whose rows lie off the gradient's by other than 16 bytes.  Preference: c needs the
+// pair's sums over all its tokens; the rows are read for the statistics and again for
+// the gradient, 16 x 512 tokens of which two thirds count in 300 us.  Both are bound by
+// memory: an exponential and its conversions take about 15 operations an element, 40%
+// of what the vector units give in that time.
 // Ignored tokens' logits are never read, and their gradient is zero.
 #include <math.h>
 
@@ -50,11 +55,12 @@ __device__ __forceinline__ int64_t row_of() {
 }
 
 // A row of V elements as a head and a tail of single elements and a body of
-// vectors.  The body begins where the row, or where one is written its gradient,
-// `at` elements from the start of its tensor, crosses a line (16 bytes where a wavefront has a row of its own):
-// a wavefront's stores then cover whole lines; with lines split between two of
-// them the copy above takes 5% longer.  It follows the pitches, not the pointers,
-// so that a row's sums have one order wherever the tensors lie.
+// vectors.  The body begins where the row that is written (where only the logits
+// are read, that one), `at` elements from the start of its tensor, crosses a line, or
+// 16 bytes where a wavefront has a row of its own: a wavefront's accesses then cover
+// whole lines; with lines split between two of them the copy above takes 5% longer.
+// It follows the pitches, not the pointers, so that a row's sums have one order
+// wherever the tensors lie.
 template <int DT, int kThreads>
 struct Row {
     typedef typename Elem<DT>::T T;
@@ -626,7 +632,8 @@ __global__ __launch_bounds__(256) void policy_finish(PolicyArgs a) {
     if (!last || threadIdx.x >= 3) return;
     __threadfence();
     double t = 0.0;
-    for (unsigned b = 0; b < gridDim.x; ++b) t += __hip_atomic_load(a.sums + threadIdx.x * kFinishBlocks + b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    for (unsigned b = 0; b < gridDim.x; ++b)
+        t += __hip_atomic_load(a.sums + threadIdx.x * kFinishBlocks + b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     a.stats[threadIdx.x] = (float)t;
 }
 

@@ -36,9 +36,9 @@ constexpr int kHeldThreads = 1024;
 constexpr int kHeldBlocks = 256;   // held: workgroups below which narrower blocks are tried
 // backward, bytes of x from which blocks under 64 bytes wide (four and more
 // workgroups read every line) give way to the split form's second read:
-// 64 x 3136 x 256 bf16 104 us held (silu 124), 93 split (101); 64 x 3136 x 64 24
-// held, 39 split
-constexpr int64_t kSplitBytes = int64_t(64) << 20;
+// 64 x 3136 x 256 bf16 104 us held (silu 124), 93 split (101); half as many images
+// 54 (65), 52 (58); a quarter 23, 33
+constexpr int64_t kSplitBytes = int64_t(48) << 20;
 constexpr int kManyBlocks = 512;   // held: two workgroups for every CU
 constexpr int kHeldMost = 16;      // vectors of x a thread holds (16 bytes each)
 constexpr int kHeldMostBack = 8;   // ... of x and of dy
