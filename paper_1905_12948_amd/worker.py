@@ -68,6 +68,12 @@ def _new(ref, *shape):
     return ref.new_empty(shape, dtype=_torch().float32)
 
 
+def _another(t, ref, *shape):
+    """A new fp32 tensor of a shape on ref's device; t, if there, is one such
+    (taking its shape is the faster way)."""
+    return _new(ref, *shape) if t is None else _torch().empty_like(t)
+
+
 def _new_like(t):
     """A new contiguous tensor of t's shape and type."""
     torch = _torch()
@@ -189,7 +195,8 @@ def group_norm(x, groups: int, gamma=None, beta=None, eps: float = 1e-5, act: st
     lib = load()
     n = lib.gmc_group_norm_workspace(code, N, S, C, G, 0)
     ws = _workspace(n, None, x)
-    mean, rstd = _new(x, N, G), _new(x, N, G)
+    mean = _new(x, N, G)
+    rstd = _another(mean, x)
     _call(x, lib.gmc_group_norm, code, N, S, C, G, x.data_ptr(), image, pixel, pg, pb, float(eps), ACTS[act],
           out.data_ptr(), oi, op, mean.data_ptr(), rstd.data_ptr(), 0 if ws is None else ws.data_ptr(), n)
     return out, mean, rstd
@@ -217,9 +224,9 @@ def group_norm_backward(dy, x, mean, rstd, gamma=None, beta=None, act: str = "no
         _is(out, x.dtype, x.shape, x, "out")
         oi, op = _images(out, "out")[3:]
     if dgamma is None:
-        dgamma = _new(x, C)
+        dgamma = _another(gamma, x, C)
     if dbeta is None:
-        dbeta = _new(x, C)
+        dbeta = _another(gamma, x, C)
     lib = load()
     n = lib.gmc_group_norm_workspace(code, N, S, C, G, 1)
     ws = _workspace(n, None, x)
@@ -283,7 +290,7 @@ def policy_loss(logits, labels, old_logp, advantages, ref_logp=None, clip: Tuple
     lib = load()
     n = lib.gmc_policy_loss_workspace(R, T)
     ws = _workspace(n, "gmc_policy_loss: more than 2^22 - 1 tokens", logits)
-    stats, logp = _new(logits, 3), _new(logits, R, T)
+    stats, logp = _new(logits, 3), _another(old_logp, logits, R, T)
     _call(logits, lib.gmc_policy_loss, code, R, T, V, logits.data_ptr(), logits.stride(0), logits.stride(1), pl, lp,
           int(ignore), po, pr, pa, T if per_token else 1, 1 if per_token else 0, float(clip[0]), float(clip[1]),
           float(kl_coef), float(temperature), REDUCTIONS[reduction], float(grad_scale), stats.data_ptr(),
@@ -307,7 +314,7 @@ def preference_loss(logits, labels, ref_logp=None, beta: float = 0.1, smoothing:
     lib = load()
     n = lib.gmc_preference_loss_workspace(P, T)
     ws = _workspace(n, "gmc_preference_loss: more than 2^22 - 1 tokens", logits)
-    loss, each, rewards, logp = _new(logits), _new(logits, P), _new(logits, R), _new(logits, R, T)
+    loss, each, rewards, logp = _new(logits), _new(logits, P), _new(logits, R), _another(ref_logp, logits, R, T)
     _call(logits, lib.gmc_preference_loss, code, P, T, V, logits.data_ptr(), logits.stride(0), logits.stride(1), pl, lp,
           int(ignore), pr, float(beta), float(smoothing), 1 if average else 0, float(grad_scale), loss.data_ptr(),
           each.data_ptr(), rewards.data_ptr(), logp.data_ptr(), pg, gs, gt, 0 if ws is None else ws.data_ptr(), n)
