@@ -612,3 +612,33 @@ def test_preference_loss_many_tokens(P, T, average):
     assert torch.equal(alone[3], got[3])
     for a, b in zip(alone[:3], got[:3]):  # another order of the same 64-bit sums
         torch.testing.assert_close(a, b, rtol=4 * U, atol=1e-12)
+
+
+@pytest.mark.parametrize("dtype,V", [("f32", 81920 + 13), ("f32", 120000), ("bf16", 163840 + 21), ("f16", 200001)])
+def test_policy_loss_rows_read_twice(dtype, V):
+    """Vocabularies that no workgroup's registers hold."""
+    test_policy_loss(V, dtype)
+
+
+@pytest.mark.parametrize("V", [120000, 170001])
+def test_losses_over_logits_read_twice(V):
+    test_losses_over_the_logits(V)
+
+
+def test_rows_within_one_sum_range_or_shifted():
+    """Logits around the ends of the range in which sums are taken unshifted: all
+    near -28, near +41, one far above the others, and large negative levels."""
+    import paper_1905_12948_amd as gmc
+    rng = np.random.default_rng(4)
+    for V in (17, 5000, 50257):
+        rows = np.stack([rng.normal(size=V) + level for level in (-60, -29, -27, 0, 39, 42, 300, -3000)])
+        rows[3, V // 2] = 45.0
+        x = dev(rows[None])
+        labels = torch.as_tensor(rng.integers(0, V, (1, len(rows)))).cuda()
+        stats, logp, grad = gmc.policy_loss(x, labels, None, torch.ones(1, device="cuda:0"))
+        _, _, _, lp, c, g = ref.policy(host(x), labels.cpu().numpy(), None, np.ones((1, len(rows))), None, 0.2, 0.2, 0, 1.0, False)
+        # the exponent's argument is as large as the logits where they are not shifted: 2 u of 60 in
+        # base 2 on top of the bounds above; x itself is exact
+        elp = LP + 8 * U * np.abs(lp) + 120 * U
+        check(logp, lp, elp, "f32", "logp")
+        check(grad, g, logits_gradient_slack(c, np.abs(c) * 120 * U, g, labels.cpu().numpy(), V) * 1.5, "f32", "gradient")
