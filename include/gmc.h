@@ -628,7 +628,9 @@ int64_t gmc_group_norm_workspace(int32_t dtype, int64_t N, int64_t S, int32_t C,
  *   stats_dev    fp32 [3] out: loss, the weighted mean of the KL term (without
  *                kl_coef), the weighted share of clipped tokens
  *   logp_dev     fp32 [R][T] out
- *   grad_dev     out, with pitches of its own, or NULL; may be logits_dev
+ *   grad_dev     out, with pitches of its own, or NULL; may be logits_dev.
+ *                Without it grad_seq and grad_tok > 0 make the sums' order that
+ *                of a call with such a gradient, 0 that of a contiguous one
  *   R T < 2^22, 1 <= V < 2^30
  * workspace_dev is 16-byte aligned.
  */

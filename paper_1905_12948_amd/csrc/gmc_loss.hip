@@ -920,8 +920,9 @@ gmc_status gmc_policy_loss(void* hip_stream, int32_t dtype, int64_t R, int64_t T
         a.grad = grad_dev;
         a.seq = seq_pitch;
         a.tok = tok_pitch;
-        a.grad_seq = grad_dev ? grad_seq : T * V;  // no gradient: the order of a contiguous one
-        a.grad_tok = grad_dev ? grad_tok : V;
+        // without a gradient, the order of one with the pitches given or of a contiguous one
+        a.grad_seq = grad_dev || grad_tok > 0 ? grad_seq : T * V;
+        a.grad_tok = grad_dev || grad_tok > 0 ? grad_tok : V;
         a.labels = labels_dev;
         a.label_pitch = label_pitch;
         a.ignore = ignore;

@@ -2,9 +2,9 @@
 (worker_ref.py).
 
 Tolerances, with u = 2^-24 (one 32-bit rounding): a 16-bit output is the 32-bit
-result rounded once, so it is within half a step of its type (2^-9 of the value
-for bfloat16, 2^-12 or half of 2^-24 for float16; doubled here, for a 32-bit
-result on the other side of a tie) plus the 32-bit error.  The 32-bit bounds are
+result rounded once, so it is within half a step of its type (at most 2^-8 of the
+value for bfloat16's 8 bits, 2^-11 or half of 2^-24 for float16's 11; the latter
+doubled here) plus the 32-bit error.  The 32-bit bounds are
 worst cases of the operations each result goes through, named at each check."""
 import math
 
@@ -642,3 +642,27 @@ def test_rows_within_one_sum_range_or_shifted():
         elp = LP + 8 * U * np.abs(lp) + 120 * U
         check(logp, lp, elp, "f32", "logp")
         check(grad, g, logits_gradient_slack(c, np.abs(c) * 120 * U, g, labels.cpu().numpy(), V) * 1.5, "f32", "gradient")
+
+
+def test_loss_gradients_take_the_logits_strides():
+    """A nearly dense view's gradient has its strides, a sparse one's is contiguous;
+    neither changes the values, and calls without the gradient give the same bits."""
+    import paper_1905_12948_amd as gmc
+    torch.manual_seed(6)
+    full = torch.randn(4, 9, 5008, device="cuda:0").bfloat16()
+    labels = torch.randint(0, 5000, (4, 8), device="cuda:0")
+    labels[1, 3:] = ref.IGNORE
+    adv = torch.randn(4, device="cuda:0")
+    for v, like in ((full[:, :-1, :5000], True), (full[:, 1:, 3:5003], True), (full[:, :-1, :2000], False),
+                    (full[:, ::2, :5000], False), (full[::2, :-1, :5000], False)):
+        y = labels[:v.shape[0], :v.shape[1]].clamp(max=v.shape[2] - 1)
+        a = adv[:v.shape[0]]
+        for f in (lambda x, **k: gmc.policy_loss(x, y, None, a, **k), lambda x, **k: gmc.preference_loss(x, y, **k)):
+            got, dense, alone = f(v), f(v.contiguous()), f(v, grad=False)
+            assert got[-1].stride() == (v.stride() if like else v.contiguous().stride())
+            for p, q in zip(alone[:-1], got[:-1]):
+                assert torch.equal(p, q)
+            # both within half a step, 2^-8, of the truth and 2 LP of c p
+            torch.testing.assert_close(got[-1], dense[-1], rtol=2 * (2.0 ** -8 + 2 * LP), atol=1e-10)
+            for p, q in zip(got[:-1], dense[:-1]):
+                torch.testing.assert_close(p, q, rtol=8 * U, atol=8 * 2 * (LP + 8 * U * 20))
