@@ -344,7 +344,8 @@ __global__ __launch_bounds__(kHeldThreads) void norm_backward_held(NormArgs a) {
 // The same statements with fewer instructions, which bound the general kernels
 // above: values are folded into their groups before any exchange between lanes,
 // statistics are formed once a group, and the unpacked values stay in registers
-// where a thread has few vectors.
+// where a thread has few vectors (128 x 32 x 32 x 64 bf16 in 32 groups: forward 25 us
+// by the general kernel, 11.7 so; backward 54 and 17).
 
 // Stores a vector, nontemporal where a workgroup's blocks of channels are whole
 // lines (64 x 14 x 14 x 1024 bf16: 15.1 -> 12.9 us); partial lines have to meet in

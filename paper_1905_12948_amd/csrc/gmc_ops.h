@@ -33,18 +33,14 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
-// A vector of B bytes that may sit at any element boundary: gfx950 takes
-// global accesses of 4 to 16 bytes at any alignment; a wavefront's then touch
+// A vector of B bytes, 16 or one element's, that may sit at any element boundary:
+// gfx950 takes 16-byte global accesses at any alignment; a wavefront's then touch
 // one cache line more.
 template <int B>
 struct Raw;
 template <>
 struct Raw<16> {
     typedef uint32_t V __attribute__((ext_vector_type(4)));
-};
-template <>
-struct Raw<8> {
-    typedef uint32_t V __attribute__((ext_vector_type(2)));
 };
 template <>
 struct Raw<4> {
@@ -177,7 +173,6 @@ __device__ __forceinline__ int64_t xcd_run(unsigned index, unsigned total) {
 }
 
 constexpr float kLog2e = 1.44269504088896341f;
-constexpr float kLn2 = 0.693147180559945309f;
 
 // 2^x by the hardware instruction (1 ulp; results below 2^-126 are zero).
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
