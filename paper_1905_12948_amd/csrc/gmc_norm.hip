@@ -648,10 +648,11 @@ __global__ __launch_bounds__(kHeldThreads) void norm_backward_fold(NormArgs a) {
 
 // -- split form ---------------------------------------------------------------
 
-// Workgroup (channel block, chunk, image) of the split kernels.
+// Workgroup (channel block, chunk, image) of the split kernels.  Pixels are counted from
+// the chunk's first: an image's own numbers end at 2^31 - 1, where a step past them wraps.
 struct Piece {
-    int64_t n;
-    int c0, first, last, chunk;
+    int64_t n, first;
+    int c0, pixels, chunk;
 };
 
 template <int VEC>
@@ -665,8 +666,8 @@ __device__ __forceinline__ Piece piece(const NormArgs& a, Place& p, unsigned bef
     const int tv = cblk * a.tc + p.cv;
     q.c0 = tv * VEC;
     p.on = p.on && q.c0 < a.C;
-    q.first = q.chunk * a.chunk;
-    q.last = q.first + a.chunk < a.S ? q.first + a.chunk : a.S;
+    q.first = (int64_t)q.chunk * a.chunk;
+    q.pixels = a.S - q.first < a.chunk ? (int)(a.S - q.first) : a.chunk;
     return q;
 }
 
@@ -683,23 +684,23 @@ __global__ __launch_bounds__(kSplitThreads) void norm_moments(NormArgs a) {
     const Piece q = piece<VEC>(a, p);
     float* part = norm_lds;
     float* chan = part + (((a.tp_log2 < 6 ? p.waves : p.rows) * VEC) << a.tp_log2);
-    const T* px = static_cast<const T*>(a.x) + q.n * a.x_image + q.c0;
+    const T* px = static_cast<const T*>(a.x) + q.n * a.x_image + q.first * a.x_pixel + q.c0;
     float mean[VEC], sq[VEC], f[VEC], first[VEC];
 #pragma unroll
     for (int i = 0; i < VEC; ++i) mean[i] = sq[i] = first[i] = 0.0f;
     float have = 0.0f;
-    if (p.on && q.first + p.r < q.last) {
-        V::load(px + (int64_t)(q.first + p.r) * a.x_pixel).unpack(first);
-        have = (float)((q.last - q.first - p.r + p.rows - 1) / p.rows);
+    if (p.on && p.r < q.pixels) {
+        V::load(px + p.r * a.x_pixel).unpack(first);
+        have = (float)((q.pixels - p.r + p.rows - 1) / p.rows);
     }
-    for (int s0 = q.first + p.r; s0 < q.last && p.on; s0 += kSplitTile * p.rows) {
+    for (int s0 = p.r; s0 < q.pixels && p.on; s0 += kSplitTile * p.rows) {
         V xv[kSplitTile];
 #pragma unroll
         for (int k = 0; k < kSplitTile; ++k)
-            if (s0 + k * p.rows < q.last) xv[k] = V::load(px + (int64_t)(s0 + k * p.rows) * a.x_pixel);
+            if (s0 + k * p.rows < q.pixels) xv[k] = V::load(px + (int64_t)(s0 + k * p.rows) * a.x_pixel);
 #pragma unroll
         for (int k = 0; k < kSplitTile; ++k)
-            if (s0 + k * p.rows < q.last) {
+            if (s0 + k * p.rows < q.pixels) {
                 xv[k].unpack(f);
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) {
@@ -718,7 +719,7 @@ __global__ __launch_bounds__(kSplitThreads) void norm_moments(NormArgs a) {
         f[i] = have * mean[i];
     }
     channel_sums<VEC>(f, a, p, part, chan);
-    const float inv = 1.0f / (float)(q.last - q.first);
+    const float inv = 1.0f / (float)q.pixels;
     const int64_t at = (q.n * a.chunks + q.chunk) * a.C + (q.c0 - p.cv * VEC);
     const int width = a.tc * VEC;
 #pragma unroll
@@ -740,19 +741,19 @@ __global__ __launch_bounds__(kSplitThreads) void norm_join(NormArgs a) {
     if (at >= a.N * a.G) return;
     const int64_t n = at / a.G;
     const int g = (int)(at - n * a.G), lane = threadIdx.x & 63;
-    const int total = a.chunks * a.cpg;
+    const unsigned total = (unsigned)(a.chunks * a.cpg);  // below 2^31; e passes it by up to 64
     const float* mean = a.part + n * a.chunks * a.C + (int64_t)g * a.cpg;
     const float* sq = a.part2 + n * a.chunks * a.C + (int64_t)g * a.cpg;
     const float full = (float)a.chunk, rest = (float)(a.S - (a.chunks - 1) * a.chunk);
     float s = 0.0f;
-    for (int e = lane; e < total; e += 64) {
-        const int k = group_of(a, e), c = e - k * a.cpg;
+    for (unsigned e = lane; e < total; e += 64) {
+        const int k = group_of(a, (int)e), c = (int)e - k * a.cpg;
         s += (k == a.chunks - 1 ? rest : full) * mean[(int64_t)k * a.C + c];
     }
     const float mu = wave_sum(s) * a.inv_m;
     s = 0.0f;
-    for (int e = lane; e < total; e += 64) {
-        const int k = group_of(a, e), c = e - k * a.cpg;
+    for (unsigned e = lane; e < total; e += 64) {
+        const int k = group_of(a, (int)e), c = (int)e - k * a.cpg;
         const float d = mean[(int64_t)k * a.C + c] - mu;
         s += sq[(int64_t)k * a.C + c] + (k == a.chunks - 1 ? rest : full) * d * d;
     }
@@ -770,20 +771,20 @@ __global__ __launch_bounds__(kSplitThreads) void norm_forward_split(NormArgs a) 
     Place p = place(a);
     const Piece q = piece<VEC>(a, p);
     if (!p.on) return;
-    const T* px = static_cast<const T*>(a.x) + q.n * a.x_image + q.c0;
-    T* py = static_cast<T*>(a.out) + q.n * a.out_image + q.c0;
+    const T* px = static_cast<const T*>(a.x) + q.n * a.x_image + q.first * a.x_pixel + q.c0;
+    T* py = static_cast<T*>(a.out) + q.n * a.out_image + q.first * a.out_pixel + q.c0;
     float ga[VEC], be[VEC], mu[VEC], rs[VEC], f[VEC];
     load_params<VEC>(a, q.c0, true, ga, be);
     load_stats<VEC>(a, q.n, q.c0, true, mu, rs);
     by_act(a.act, [&](auto act) {
-        for (int s0 = q.first + p.r; s0 < q.last; s0 += 4 * p.rows) {
+        for (int s0 = p.r; s0 < q.pixels; s0 += 4 * p.rows) {
             V xv[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                if (s0 + k * p.rows < q.last) xv[k] = V::load(px + (int64_t)(s0 + k * p.rows) * a.x_pixel);
+                if (s0 + k * p.rows < q.pixels) xv[k] = V::load(px + (int64_t)(s0 + k * p.rows) * a.x_pixel);
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                if (s0 + k * p.rows < q.last) {
+                if (s0 + k * p.rows < q.pixels) {
                     xv[k].unpack(f);
 #pragma unroll
                     for (int i = 0; i < VEC; ++i)
@@ -806,8 +807,8 @@ __global__ __launch_bounds__(kSplitThreads) void norm_back_sums(NormArgs a) {
     const Piece q = piece<VEC>(a, p);
     float* part = norm_lds;
     float* chan = part + (((a.tp_log2 < 6 ? p.waves : p.rows) * VEC) << a.tp_log2);
-    const T* px = static_cast<const T*>(a.x) + q.n * a.x_image + q.c0;
-    const T* pd = static_cast<const T*>(a.dy) + q.n * a.dy_image + q.c0;
+    const T* px = static_cast<const T*>(a.x) + q.n * a.x_image + q.first * a.x_pixel + q.c0;
+    const T* pd = static_cast<const T*>(a.dy) + q.n * a.dy_image + q.first * a.dy_pixel + q.c0;
     float ga[VEC], be[VEC], mu[VEC], rs[VEC], s1[VEC], s2[VEC];
     load_params<VEC>(a, q.c0, p.on, ga, be);
     load_stats<VEC>(a, q.n, q.c0, p.on, mu, rs);
@@ -815,17 +816,17 @@ __global__ __launch_bounds__(kSplitThreads) void norm_back_sums(NormArgs a) {
     for (int i = 0; i < VEC; ++i) s1[i] = s2[i] = 0.0f;
     by_act(a.act, [&](auto act) {
         constexpr int kAct = decltype(act)::value;
-        for (int s0 = q.first + p.r; s0 < q.last && p.on; s0 += 4 * p.rows) {
+        for (int s0 = p.r; s0 < q.pixels && p.on; s0 += 4 * p.rows) {
             V xv[4], dv[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                if (s0 + k * p.rows < q.last) {
+                if (s0 + k * p.rows < q.pixels) {
                     xv[k] = V::load(px + (int64_t)(s0 + k * p.rows) * a.x_pixel);
                     dv[k] = V::load(pd + (int64_t)(s0 + k * p.rows) * a.dy_pixel);
                 }
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                if (s0 + k * p.rows < q.last) {
+                if (s0 + k * p.rows < q.pixels) {
                     float f[VEC], d[VEC];
                     xv[k].unpack(f);
                     dv[k].unpack(d);
@@ -862,10 +863,10 @@ __global__ __launch_bounds__(kSplitThreads) void norm_back_join(NormArgs a, floa
     int step = 1;
     while (step < 64 && step < a.cpg) step *= 2;
     float s1 = 0.0f, s2 = 0.0f;
-    for (int c0 = 0; c0 < a.cpg; c0 += step) {
-        const int c = c0 + (lane & (step - 1));
+    for (unsigned c0 = 0; c0 < (unsigned)a.cpg; c0 += step) {
+        const unsigned c = c0 + (lane & (step - 1));
         float b = 0.0f, w = 0.0f;
-        if (c < a.cpg)
+        if (c < (unsigned)a.cpg)
             for (int k = lane / step; k < a.chunks; k += 64 / step) {
                 b += a.part[base + (int64_t)k * a.C + c];
                 w += a.part2[base + (int64_t)k * a.C + c];
@@ -874,10 +875,10 @@ __global__ __launch_bounds__(kSplitThreads) void norm_back_join(NormArgs a, floa
             b += __shfl_xor(b, o);
             w += __shfl_xor(w, o);
         }
-        if (lane < step && c < a.cpg) {
+        if (lane < step && c < (unsigned)a.cpg) {
             a.part[base + c] = b;
             a.part2[base + c] = w;
-            const float ga = a.gamma ? a.gamma[g * a.cpg + c] : 1.0f;
+            const float ga = a.gamma ? a.gamma[(int64_t)g * a.cpg + c] : 1.0f;
             s1 = __builtin_fmaf(ga, b, s1);
             s2 = __builtin_fmaf(ga, w, s2);
         }
@@ -939,9 +940,9 @@ __global__ __launch_bounds__(kSplitThreads) void norm_backward_split(NormArgs a,
     Place p = place(a);
     const Piece q = piece<VEC>(a, p, (unsigned)params);
     if (!p.on) return;
-    const T* px = static_cast<const T*>(a.x) + q.n * a.x_image + q.c0;
-    const T* pd = static_cast<const T*>(a.dy) + q.n * a.dy_image + q.c0;
-    T* po = static_cast<T*>(a.out) + q.n * a.out_image + q.c0;
+    const T* px = static_cast<const T*>(a.x) + q.n * a.x_image + q.first * a.x_pixel + q.c0;
+    const T* pd = static_cast<const T*>(a.dy) + q.n * a.dy_image + q.first * a.dy_pixel + q.c0;
+    T* po = static_cast<T*>(a.out) + q.n * a.out_image + q.first * a.out_pixel + q.c0;
     float ga[VEC], be[VEC], mu[VEC], rs[VEC], s1[VEC], s2[VEC];
     load_params<VEC>(a, q.c0, true, ga, be);
     load_stats<VEC>(a, q.n, q.c0, true, mu, rs);
@@ -959,17 +960,17 @@ __global__ __launch_bounds__(kSplitThreads) void norm_backward_split(NormArgs a,
     }
     by_act(a.act, [&](auto act) {
         constexpr int kAct = decltype(act)::value;
-        for (int s0 = q.first + p.r; s0 < q.last; s0 += 4 * p.rows) {
+        for (int s0 = p.r; s0 < q.pixels; s0 += 4 * p.rows) {
             V xv[4], dv[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                if (s0 + k * p.rows < q.last) {
+                if (s0 + k * p.rows < q.pixels) {
                     xv[k] = V::load_once(px + (int64_t)(s0 + k * p.rows) * a.x_pixel);
                     dv[k] = V::load_once(pd + (int64_t)(s0 + k * p.rows) * a.dy_pixel);
                 }
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                if (s0 + k * p.rows < q.last) {
+                if (s0 + k * p.rows < q.pixels) {
                     float f[VEC], d[VEC];
                     xv[k].unpack(f);
                     dv[k].unpack(d);
@@ -1063,8 +1064,10 @@ NormPlan norm_plan_split(NormArgs& a, NormPlan pl, int full) {
     const int64_t want = (kSplitBlocks + a.N * a.cblocks - 1) / (a.N * a.cblocks);
     const int64_t least = (a.S + (int64_t)rows * kSplitMost - 1) / ((int64_t)rows * kSplitMost);
     if (chunks > want) chunks = want > least ? want : least;
+    const int64_t most = 0x7fffffff / a.C;  // norm_join counts an image's chunks and channels in 32 bits
+    if (chunks > most) chunks = most;
     a.chunk = (int32_t)((a.S + chunks - 1) / chunks);
-    a.chunks = (a.S + a.chunk - 1) / a.chunk;
+    a.chunks = (int32_t)(((int64_t)a.S + a.chunk - 1) / a.chunk);
     const int slots = a.tp_log2 < 6 ? kSplitThreads / 64 : rows;
     pl.threads = kSplitThreads;
     pl.lds = sizeof(float) * ((size_t)(slots + 1) * pl.vec << a.tp_log2);
@@ -1106,7 +1109,7 @@ NormPlan norm_plan(NormArgs& a, int32_t dtype, bool backward) {
             int threads = 256;
             while (threads < kHeldThreads && (((int64_t)a.S << lg) + threads - 1) / threads > 4) threads *= 2;
             const int rows = threads >> lg;
-            const int64_t kp = (a.S + rows - 1) / rows;
+            const int64_t kp = ((int64_t)a.S + rows - 1) / rows;
             if (kp > most) continue;
             pl.held = true;
             pl.vec = vec;
