@@ -527,7 +527,9 @@ gmc_status gmc_calib_stream(void* hip_stream, float* e_dev, const float* g_dev, 
  *   - Sums are taken in a fixed order: the same call gives the same bits (the
  *     losses' order follows the pitches).
  *   - An output may be an input's own buffer where the call says so, with the
- *     same pitches; overlaps of another kind are refused.
+ *     same pitches.  Overlaps of another kind are refused, of outputs and the
+ *     workspace with each other and with any input (a buffer with pitches
+ *     counts from its first element to its last).
  *   - Invalid arguments return GMC_EINVAL before any device work, reported
  *     through gmc_last_error(NULL).
  */

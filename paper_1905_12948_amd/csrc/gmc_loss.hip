@@ -844,6 +844,11 @@ void policy_long_rows(const PolicyArgs& a, dim3 rows, hipStream_t st) {
 
 constexpr int64_t kMostRows = 0xffffffffll / 1024;
 
+// The bytes of R sequences of T rows of V elements of b bytes.
+int64_t rows_span(int64_t R, int64_t T, int64_t V, int64_t seq, int64_t tok, int64_t b) {
+    return ((R - 1) * (R > 1 ? seq : 0) + (T - 1) * (T > 1 ? tok : 0) + V) * b;
+}
+
 gmc_status logits_check(const char* me, int32_t dtype, int64_t R, int64_t T, int64_t V, const void* logits,
                         int64_t seq, int64_t tok, const void* grad, int64_t grad_seq, int64_t grad_tok,
                         const void* labels, int64_t label_pitch) {
@@ -864,11 +869,8 @@ gmc_status logits_check(const char* me, int32_t dtype, int64_t R, int64_t T, int
         return op_error(GMC_EINVAL, me, "the label pitch is shorter than a row");
     if (grad) {
         const int64_t b = type_size(dtype);
-        const auto span = [&](int64_t s, int64_t k) {
-            return ((R - 1) * (R > 1 ? s : 0) + (T - 1) * (T > 1 ? k : 0) + V) * b;
-        };
         const bool same = logits == grad && (R == 1 || seq == grad_seq) && (T == 1 || tok == grad_tok);
-        if (!same && overlap(logits, span(seq, tok), grad, span(grad_seq, grad_tok)))
+        if (!same && overlap(logits, rows_span(R, T, V, seq, tok, b), grad, rows_span(R, T, V, grad_seq, grad_tok, b)))
             return op_error(GMC_EINVAL, me, "the gradient overlaps the logits without being them");
     }
     return GMC_OK;
@@ -913,6 +915,20 @@ gmc_status gmc_policy_loss(void* hip_stream, int32_t dtype, int64_t R, int64_t T
     a.tokens = static_cast<float4*>(workspace_dev);
     if (a.rows) {
         if (!adv_dev || !logp_dev) return op_error(GMC_EINVAL, me, "NULL argument");
+        constexpr int64_t kFar = int64_t(1) << 50;
+        const auto reach = [](int64_t steps, int64_t pitch) { return steps > 0 ? steps * pitch : 0; };
+        if ((R > 1 && (adv_seq < -kFar / R || adv_seq > kFar / R)) || (T > 1 && (adv_tok < -kFar / T || adv_tok > kFar / T)))
+            return op_error(GMC_EINVAL, me, "a pitch of the advantages is out of range");
+        const int64_t by_seq = reach(R - 1, adv_seq), by_tok = reach(T - 1, adv_tok);
+        const int64_t below = (by_seq < 0 ? by_seq : 0) + (by_tok < 0 ? by_tok : 0);
+        const int64_t above = (by_seq > 0 ? by_seq : 0) + (by_tok > 0 ? by_tok : 0);
+        const int64_t b = type_size(dtype), n = a.rows * 4;
+        const Span stats(stats_dev, 12), logp(logp_dev, n), scratch(workspace_dev, gmc_policy_loss_workspace(R, T));
+        if (!apart({stats, logp, scratch, {grad_dev, rows_span(R, T, V, grad_seq, grad_tok, b)}},
+                   {{labels_dev, rows_span(R, 1, T, label_pitch, 0, 8)}, {old_logp_dev, n}, {ref_logp_dev, n},
+                    {adv_dev + below, (above - below + 1) * 4}}) ||
+            !apart({stats, logp, scratch}, {{logits_dev, rows_span(R, T, V, seq_pitch, tok_pitch, b)}}))
+            return op_error(GMC_EINVAL, me, "an output or the workspace overlaps another buffer");
         a.sums = reinterpret_cast<double*>(a.tokens + a.rows);
         a.done = reinterpret_cast<int*>(a.sums + 3 * kFinishBlocks);
         float* weight = reinterpret_cast<float*>(a.done + 1);
@@ -997,6 +1013,13 @@ gmc_status gmc_preference_loss(void* hip_stream, int32_t dtype, int64_t P, int64
             return op_error(GMC_EINVAL, me, "the workspace is too small");
         if (reinterpret_cast<uintptr_t>(workspace_dev) & 7u)
             return op_error(GMC_EINVAL, me, "the workspace is not 8-byte aligned");
+        const int64_t R = 2 * P, b = type_size(dtype), some = T > 0;
+        const Span loss(loss_dev, 4), each(pair_loss_dev, P * 4), rewards(rewards_dev, R * 4), logp(logp_dev, R * T * 4),
+            scratch(workspace_dev, gmc_preference_loss_workspace(P, T));
+        if (!apart({loss, each, rewards, logp, scratch, {grad_dev, some * rows_span(R, T, V, grad_seq, grad_tok, b)}},
+                   {{labels_dev, some * rows_span(R, 1, T, label_pitch, 0, 8)}, {ref_logp_dev, R * T * 4}}) ||
+            !apart({loss, each, rewards, logp, scratch}, {{logits_dev, some * rows_span(R, T, V, seq_pitch, tok_pitch, b)}}))
+            return op_error(GMC_EINVAL, me, "an output or the workspace overlaps another buffer");
         PrefArgs a{};
         a.logits = logits_dev;
         a.grad = grad_dev;

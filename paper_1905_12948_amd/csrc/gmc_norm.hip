@@ -1240,6 +1240,11 @@ gmc_status gmc_group_norm(void* hip_stream, int32_t dtype, int64_t N, int64_t S,
     const int64_t need = norm_scratch(a, pl, false);
     if (need && (!workspace_dev || workspace_bytes < need * (int64_t)sizeof(float)))
         return op_error(GMC_EINVAL, me, "the workspace is too small");
+    const Span mean(mean_dev, N * G * 4), rstd(rstd_dev, N * G * 4), scratch(workspace_dev, need * 4);
+    if (!apart({mean, rstd, scratch, {y_dev, image_span(N, S, C, y_image, y_pixel, b)}},
+               {{gamma_dev, C * int64_t(4)}, {beta_dev, C * int64_t(4)}}) ||
+        !apart({mean, rstd, scratch}, {{x_dev, image_span(N, S, C, x_image, x_pixel, b)}}))
+        return op_error(GMC_EINVAL, me, "an output or the workspace overlaps another buffer");
     hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
     const int64_t blocks = pl.held ? N * a.blocks : N * a.chunks * a.cblocks;
     if (blocks * pl.threads > 0xffffffffll || (!pl.held && N * G > 0xffffffffll / 64))
@@ -1318,6 +1323,12 @@ gmc_status gmc_group_norm_backward(void* hip_stream, int32_t dtype, int64_t N, i
     const int64_t need = norm_scratch(a, pl, true);
     if (!workspace_dev || workspace_bytes < need * (int64_t)sizeof(float))
         return op_error(GMC_EINVAL, me, "the workspace is too small");
+    const Span dgamma(dgamma_dev, C * int64_t(4)), dbeta(dbeta_dev, C * int64_t(4)), scratch(workspace_dev, need * 4);
+    if (!apart({dgamma, dbeta, scratch, {dx_dev, out_span}}, {{gamma_dev, C * int64_t(4)}, {beta_dev, C * int64_t(4)},
+                                                              {mean_dev, N * G * 4}, {rstd_dev, N * G * 4}}) ||
+        !apart({dgamma, dbeta, scratch}, {{x_dev, image_span(N, S, C, x_image, x_pixel, b)},
+                                          {dy_dev, image_span(N, S, C, dy_image, dy_pixel, b)}}))
+        return op_error(GMC_EINVAL, me, "an output or the workspace overlaps another buffer");
     const int64_t rows = pl.held ? N : N * a.chunks;
     const int64_t blocks = pl.held ? N * a.blocks : rows * a.cblocks;
     if (blocks * pl.threads > 0xffffffffll || (!pl.held && N * G > 0xffffffffll / 64))

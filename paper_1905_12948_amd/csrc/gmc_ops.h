@@ -6,6 +6,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <initializer_list>
+
 #include "../../include/gmc.h"
 
 namespace gmc {
@@ -27,6 +29,24 @@ inline int64_t type_size(int32_t dtype) { return dtype == GMC_F32 ? 4 : 2; }
 inline bool overlap(const void* a, int64_t an, const void* b, int64_t bn) {
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
     return an > 0 && bn > 0 && x < y + (uintptr_t)bn && y < x + (uintptr_t)an;
+}
+
+// A buffer of a call; one that is not there has no bytes.
+struct Span {
+    const void* p;
+    int64_t bytes;
+    Span(const void* q, int64_t n) : p(q), bytes(q ? n : 0) {}
+};
+
+// Whether each output is apart from the other outputs and from the inputs.
+inline bool apart(std::initializer_list<Span> outputs, std::initializer_list<Span> inputs) {
+    for (const Span* o = outputs.begin(); o != outputs.end(); ++o) {
+        for (const Span* q = o + 1; q != outputs.end(); ++q)
+            if (overlap(o->p, o->bytes, q->p, q->bytes)) return false;
+        for (const Span& i : inputs)
+            if (overlap(o->p, o->bytes, i.p, i.bytes)) return false;
+    }
+    return true;
 }
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
