@@ -550,7 +550,8 @@ enum { GMC_F32 = 0, GMC_BF16 = 1, GMC_F16 = 2 };
  *   their number.  scale = fl32(65536 / (65536 - level)), the reciprocal of
  *   the probability the mask really has (p in units of 2^-16); level 65536
  *   keeps nothing.  A dropped x is not looked at: NaN there gives 0.
- *   rows, cols  >= 0, rows * cols <= 2^40 (0: nothing to do)
+ *   rows, cols  >= 0, rows * cols <= 2^40 (0: nothing to do) and fewer than
+ *               2^34 - 1023 vectors of 16 bytes, a row's last one counted whole
  *   p           [0, 1]
  *   t           step, >= 0; worker in [0, GMC_MAX_WORKERS); site >= 0, the
  *               dropout's number in the model
@@ -574,7 +575,9 @@ enum { GMC_ACT_NONE = 0, GMC_ACT_RELU = 1, GMC_ACT_SILU = 2 };
  *   eps         [0, 1]
  *   y_dev       may be x_dev
  *   mean_dev, rstd_dev   [N][G] fp32 out, for the backward pass
- *   N >= 0, 1 <= S < 2^31, N S C <= 2^40
+ *   N >= 0, 1 <= S < 2^31, N S C <= 2^40; an image or a number of channels
+ *   that no launch of 2^32 threads can take is refused (none with C < 2^26 and
+ *   S C < 2^35 is)
  */
 gmc_status gmc_group_norm(void* hip_stream, int32_t dtype, int64_t N, int64_t S, int32_t C, int32_t G,
                           const void* x_dev, int64_t x_image, int64_t x_pixel, const float* gamma_dev,

@@ -181,7 +181,7 @@ extern "C" gmc_status gmc_dropout(void* hip_stream, int32_t dtype, int64_t rows,
     // one vector a thread until that gives every CU several workgroups
     const int64_t unroll = a.total >= int64_t(kDropThreads) * 4 * 2048 ? 4 : 1;
     const int64_t blocks = (a.total + kDropThreads * unroll - 1) / (kDropThreads * unroll);
-    if (blocks > 0x7fffffff) return op_error(GMC_EINVAL, me, "too many vectors for one launch");
+    if (blocks > 0xffffffffll / kDropThreads) return op_error(GMC_EINVAL, me, "too many vectors for one launch");
     const dim3 grid((unsigned)blocks);
     GMC_BY_TYPE(dtype, {
         if (a.r) {

@@ -923,8 +923,8 @@ __device__ __forceinline__ void sum_params(int block, const float* part, const f
 }
 
 __global__ __launch_bounds__(kSplitThreads) void norm_params(const float* part, const float* part2, int64_t rows,
-                                                             int32_t C, float* dgamma, float* dbeta) {
-    sum_params((int)blockIdx.x, part, part2, rows, C, C, dgamma, dbeta);
+                                                             int64_t pitch, int32_t C, float* dgamma, float* dbeta) {
+    sum_params((int)blockIdx.x, part, part2, rows, pitch, C, dgamma, dbeta);
 }
 
 // The first `params` workgroups sum the parameters' gradients, the others are pieces.
@@ -1134,6 +1134,36 @@ int64_t norm_scratch(const NormArgs& a, const NormPlan& pl, bool backward) {
     return 2 * a.N * a.chunks * a.C + (backward ? 2 * a.N * a.G : 0);
 }
 
+constexpr int64_t kMostThreads = 0xffffffffll;  // of one launch
+
+unsigned param_blocks(int32_t C) { return (unsigned)(((int64_t)C + kParamCh - 1) / kParamCh); }
+
+// Images one launch of each kernel may have; a call of more takes several.
+int64_t launch_images(const NormArgs& a, const NormPlan& pl, bool backward) {
+    const int64_t params = backward ? param_blocks(a.C) * (int64_t)kSplitThreads : 0;
+    if (params >= kMostThreads) return 0;
+    if (pl.held) return kMostThreads / (pl.threads * (int64_t)a.blocks);
+    const int64_t pieces = (kMostThreads - params) / (kSplitThreads * (int64_t)a.chunks * a.cblocks);
+    const int64_t joins = kMostThreads / 64 / a.G;
+    return pieces < joins ? pieces : joins;
+}
+
+// Images n0, n0 + 1, ... of a, at most n; b: bytes of an element.
+NormArgs some_images(NormArgs a, int64_t n0, int64_t n, int64_t b) {
+    const int64_t rows = n0 * (a.chunks ? a.chunks : 1) * a.C;
+    a.x = static_cast<const char*>(a.x) + n0 * a.x_image * b;
+    if (a.dy) a.dy = static_cast<const char*>(a.dy) + n0 * a.dy_image * b;
+    a.out = static_cast<char*>(a.out) + n0 * a.out_image * b;
+    a.mean += n0 * a.G;
+    a.rstd += n0 * a.G;
+    if (a.part) {
+        a.part += rows;
+        a.part2 += rows;
+    }
+    a.N = a.N - n0 < n ? a.N - n0 : n;
+    return a;
+}
+
 gmc_status norm_check(const char* me, int32_t dtype, int64_t N, int64_t S, int32_t C, int32_t G, int32_t act) {
     if (!known_type(dtype)) return op_error(GMC_EINVAL, me, "unknown element type");
     if (N < 0 || S < 1 || S > 0x7fffffff || C < 1) return op_error(GMC_EINVAL, me, "need N >= 0, 1 <= S < 2^31, C >= 1");
@@ -1199,6 +1229,10 @@ int64_t gmc_group_norm_workspace(int32_t dtype, int64_t N, int64_t S, int32_t C,
     a.C = C;
     a.G = G;
     const NormPlan pl = norm_plan(a, dtype, backward != 0);
+    if (launch_images(a, pl, backward != 0) < 1) {
+        op_error(GMC_EINVAL, "gmc_group_norm_workspace", "more than a launch can have");
+        return -1;
+    }
     return (int64_t)sizeof(float) * norm_scratch(a, pl, backward != 0);
 }
 
@@ -1237,6 +1271,8 @@ gmc_status gmc_group_norm(void* hip_stream, int32_t dtype, int64_t N, int64_t S,
     a.eps = (float)eps;
     a.act = act;
     const NormPlan pl = norm_plan(a, dtype, false);
+    const int64_t most = launch_images(a, pl, false);
+    if (most < 1) return op_error(GMC_EINVAL, me, "more than a launch can have");
     const int64_t need = norm_scratch(a, pl, false);
     if (need && (!workspace_dev || workspace_bytes < need * (int64_t)sizeof(float)))
         return op_error(GMC_EINVAL, me, "the workspace is too small");
@@ -1246,29 +1282,30 @@ gmc_status gmc_group_norm(void* hip_stream, int32_t dtype, int64_t N, int64_t S,
         !apart({mean, rstd, scratch}, {{x_dev, image_span(N, S, C, x_image, x_pixel, b)}}))
         return op_error(GMC_EINVAL, me, "an output or the workspace overlaps another buffer");
     hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
-    const int64_t blocks = pl.held ? N * a.blocks : N * a.chunks * a.cblocks;
-    if (blocks * pl.threads > 0xffffffffll || (!pl.held && N * G > 0xffffffffll / 64))
-        return op_error(GMC_EINVAL, me, "too many images for one launch");
-    const dim3 grid((unsigned)blocks), joins((unsigned)((N * G + kSplitThreads / 64 - 1) / (kSplitThreads / 64)));
-    if (pl.fold) {
-        GMC_BY_TYPE(dtype, GMC_NORM_FOLD({
-                        if (pl.kp <= 4) norm_forward_fold<DT, 4, F><<<grid, pl.threads, pl.lds, st>>>(a);
-                        else if (pl.kp <= 8) norm_forward_fold<DT, 8, F><<<grid, pl.threads, pl.lds, st>>>(a);
-                        else norm_forward_fold<DT, kHeldMost, F><<<grid, pl.threads, pl.lds, st>>>(a);
-                    }));
-    } else if (pl.held) {
-        GMC_BY_TYPE(dtype, GMC_NORM_VEC(16 / Elem<DT>::kSize, {
-                        if (pl.kp == 4) norm_forward_held<DT, VEC, 4><<<grid, pl.threads, pl.lds, st>>>(a);
-                        else norm_forward_held<DT, VEC, kHeldMost><<<grid, pl.threads, pl.lds, st>>>(a);
-                    }));
-    } else {
-        a.part = static_cast<float*>(workspace_dev);
-        a.part2 = a.part + N * a.chunks * (int64_t)C;
-        GMC_BY_TYPE(dtype, GMC_NORM_VEC(16 / Elem<DT>::kSize, {
-                        norm_moments<DT, VEC><<<grid, pl.threads, pl.lds, st>>>(a);
-                        norm_join<<<joins, kSplitThreads, 0, st>>>(a);
-                        norm_forward_split<DT, VEC><<<grid, pl.threads, 0, st>>>(a);
-                    }));
+    a.part = static_cast<float*>(workspace_dev);
+    a.part2 = a.part ? a.part + N * a.chunks * (int64_t)C : nullptr;
+    for (int64_t n0 = 0; n0 < N; n0 += most) {
+        const NormArgs q = some_images(a, n0, most, b);
+        const dim3 grid((unsigned)(q.N * (pl.held ? (int64_t)q.blocks : (int64_t)q.chunks * q.cblocks)));
+        const dim3 joins((unsigned)((q.N * G + kSplitThreads / 64 - 1) / (kSplitThreads / 64)));
+        if (pl.fold) {
+            GMC_BY_TYPE(dtype, GMC_NORM_FOLD({
+                            if (pl.kp <= 4) norm_forward_fold<DT, 4, F><<<grid, pl.threads, pl.lds, st>>>(q);
+                            else if (pl.kp <= 8) norm_forward_fold<DT, 8, F><<<grid, pl.threads, pl.lds, st>>>(q);
+                            else norm_forward_fold<DT, kHeldMost, F><<<grid, pl.threads, pl.lds, st>>>(q);
+                        }));
+        } else if (pl.held) {
+            GMC_BY_TYPE(dtype, GMC_NORM_VEC(16 / Elem<DT>::kSize, {
+                            if (pl.kp == 4) norm_forward_held<DT, VEC, 4><<<grid, pl.threads, pl.lds, st>>>(q);
+                            else norm_forward_held<DT, VEC, kHeldMost><<<grid, pl.threads, pl.lds, st>>>(q);
+                        }));
+        } else {
+            GMC_BY_TYPE(dtype, GMC_NORM_VEC(16 / Elem<DT>::kSize, {
+                            norm_moments<DT, VEC><<<grid, pl.threads, pl.lds, st>>>(q);
+                            norm_join<<<joins, kSplitThreads, 0, st>>>(q);
+                            norm_forward_split<DT, VEC><<<grid, pl.threads, 0, st>>>(q);
+                        }));
+        }
     }
     return op_launched(me);
 }
@@ -1283,10 +1320,11 @@ gmc_status gmc_group_norm_backward(void* hip_stream, int32_t dtype, int64_t N, i
     gmc_status ok = norm_check(me, dtype, N, S, C, G, act);
     if (ok != GMC_OK) return ok;
     hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
-    const dim3 param_grid((unsigned)((C + kParamCh - 1) / kParamCh));
     if (N == 0) {
+        if (param_blocks(C) * (int64_t)kSplitThreads > kMostThreads)
+            return op_error(GMC_EINVAL, me, "more than a launch can have");
         if (dgamma_dev || dbeta_dev)
-            norm_params<<<param_grid, kSplitThreads, 0, st>>>(nullptr, nullptr, 0, C, dgamma_dev, dbeta_dev);
+            norm_params<<<dim3(param_blocks(C)), kSplitThreads, 0, st>>>(nullptr, nullptr, 0, C, C, dgamma_dev, dbeta_dev);
         return op_launched(me);
     }
     if (!dy_dev || !x_dev || !dx_dev || !mean_dev || !rstd_dev) return op_error(GMC_EINVAL, me, "NULL argument");
@@ -1320,6 +1358,8 @@ gmc_status gmc_group_norm_backward(void* hip_stream, int32_t dtype, int64_t N, i
     a.G = G;
     a.act = act;
     const NormPlan pl = norm_plan(a, dtype, true);
+    const int64_t most = launch_images(a, pl, true);
+    if (most < 1) return op_error(GMC_EINVAL, me, "more than a launch can have");
     const int64_t need = norm_scratch(a, pl, true);
     if (!workspace_dev || workspace_bytes < need * (int64_t)sizeof(float))
         return op_error(GMC_EINVAL, me, "the workspace is too small");
@@ -1329,36 +1369,40 @@ gmc_status gmc_group_norm_backward(void* hip_stream, int32_t dtype, int64_t N, i
         !apart({dgamma, dbeta, scratch}, {{x_dev, image_span(N, S, C, x_image, x_pixel, b)},
                                           {dy_dev, image_span(N, S, C, dy_image, dy_pixel, b)}}))
         return op_error(GMC_EINVAL, me, "an output or the workspace overlaps another buffer");
-    const int64_t rows = pl.held ? N : N * a.chunks;
-    const int64_t blocks = pl.held ? N * a.blocks : rows * a.cblocks;
-    if (blocks * pl.threads > 0xffffffffll || (!pl.held && N * G > 0xffffffffll / 64))
-        return op_error(GMC_EINVAL, me, "too many images for one launch");
-    const dim3 grid((unsigned)blocks), joins((unsigned)((N * G + kSplitThreads / 64 - 1) / (kSplitThreads / 64)));
+    const int64_t rows = pl.held ? 1 : a.chunks;  // of partial sums, an image
     a.part = static_cast<float*>(workspace_dev);
-    a.part2 = a.part + rows * (int64_t)C;
-    if (pl.fold) {
-        GMC_BY_TYPE(dtype, GMC_NORM_FOLD({
-                        if (pl.kp <= 2) norm_backward_fold<DT, 2, F><<<grid, pl.threads, pl.lds, st>>>(a);
-                        else if (pl.kp <= 4) norm_backward_fold<DT, 4, F><<<grid, pl.threads, pl.lds, st>>>(a);
-                        else norm_backward_fold<DT, kHeldMostBack, F><<<grid, pl.threads, pl.lds, st>>>(a);
-                    }));
-    } else if (pl.held) {
-        GMC_BY_TYPE(dtype, GMC_NORM_VEC(16 / Elem<DT>::kSize, {
-                        if (pl.kp == 4) norm_backward_held<DT, VEC, 4><<<grid, pl.threads, pl.lds, st>>>(a);
-                        else norm_backward_held<DT, VEC, kHeldMostBack><<<grid, pl.threads, pl.lds, st>>>(a);
-                    }));
-    } else {
-        float* shared_terms = a.part2 + rows * (int64_t)C;
-        const unsigned params = dgamma_dev || dbeta_dev ? param_grid.x : 0;
-        GMC_BY_TYPE(dtype, GMC_NORM_VEC(16 / Elem<DT>::kSize, {
-                        norm_back_sums<DT, VEC><<<grid, pl.threads, pl.lds, st>>>(a);
-                        norm_back_join<<<joins, kSplitThreads, 0, st>>>(a, shared_terms);
-                        norm_backward_split<DT, VEC><<<dim3(grid.x + params), pl.threads, 0, st>>>(
-                            a, shared_terms, (int)params, dgamma_dev, dbeta_dev);
-                    }));
+    a.part2 = a.part + N * rows * C;
+    float* shared_terms = a.part2 + N * rows * C;
+    // the split form's last launch sums the parameters' gradients too, where it is the only one
+    const bool params = dgamma_dev || dbeta_dev, with = params && !pl.held && N <= most;
+    for (int64_t n0 = 0; n0 < N; n0 += most) {
+        const NormArgs q = some_images(a, n0, most, b);
+        const dim3 grid((unsigned)(q.N * (pl.held ? (int64_t)q.blocks : (int64_t)q.chunks * q.cblocks)));
+        if (pl.fold) {
+            GMC_BY_TYPE(dtype, GMC_NORM_FOLD({
+                            if (pl.kp <= 2) norm_backward_fold<DT, 2, F><<<grid, pl.threads, pl.lds, st>>>(q);
+                            else if (pl.kp <= 4) norm_backward_fold<DT, 4, F><<<grid, pl.threads, pl.lds, st>>>(q);
+                            else norm_backward_fold<DT, kHeldMostBack, F><<<grid, pl.threads, pl.lds, st>>>(q);
+                        }));
+        } else if (pl.held) {
+            GMC_BY_TYPE(dtype, GMC_NORM_VEC(16 / Elem<DT>::kSize, {
+                            if (pl.kp == 4) norm_backward_held<DT, VEC, 4><<<grid, pl.threads, pl.lds, st>>>(q);
+                            else norm_backward_held<DT, VEC, kHeldMostBack><<<grid, pl.threads, pl.lds, st>>>(q);
+                        }));
+        } else {
+            float* terms = shared_terms + 2 * n0 * G;
+            const unsigned first = with ? param_blocks(C) : 0;
+            const dim3 joins((unsigned)((q.N * G + kSplitThreads / 64 - 1) / (kSplitThreads / 64)));
+            GMC_BY_TYPE(dtype, GMC_NORM_VEC(16 / Elem<DT>::kSize, {
+                            norm_back_sums<DT, VEC><<<grid, pl.threads, pl.lds, st>>>(q);
+                            norm_back_join<<<joins, kSplitThreads, 0, st>>>(q, terms);
+                            norm_backward_split<DT, VEC><<<dim3(grid.x + first), pl.threads, 0, st>>>(
+                                q, terms, (int)first, dgamma_dev, dbeta_dev);
+                        }));
+        }
     }
-    if (pl.held && (dgamma_dev || dbeta_dev))
-        norm_params<<<param_grid, kSplitThreads, 0, st>>>(a.part, a.part2, N, C, dgamma_dev, dbeta_dev);
+    if (params && !with)
+        norm_params<<<dim3(param_blocks(C)), kSplitThreads, 0, st>>>(a.part, a.part2, N, rows * C, C, dgamma_dev, dbeta_dev);
     return op_launched(me);
 }
 

@@ -65,3 +65,36 @@ def test_group_norm_of_the_longest_image():
         slack = 8 * U * r * 1.25 * (dz.abs() + hat.abs() + 1) + many * 2 * r * 1.25 * (ab + hat.abs() * ag) / S
         err = (dx.view(-1)[a:b].double() - want).abs()
         assert (err <= HALF * want.abs() + 1.01 * slack).all(), (a, err.max().item())
+
+
+@pytest.mark.parametrize("N,C,G,dtype", [
+    (2 ** 24 + 4099, 12, 4, torch.bfloat16),     # 256 threads an image
+    (2 ** 26 + 4099, 16, 2, torch.bfloat16),     # 64; backward 256, in pieces of an image
+    (2 ** 26 + 4099, 32, 4, torch.bfloat16),     # 64, both ways
+    (2 ** 24 + 4099, 4, 2, torch.float32),       # backward: 256, in pieces
+])
+def test_group_norm_of_more_images_than_a_launch_has(N, C, G, dtype):
+    """As many calls of fewer images give the same bits, at both ends and across 2^32 threads."""
+    import paper_1905_12948_amd as gmc
+    g = torch.Generator(device="cuda:0").manual_seed(C)
+    x = torch.empty(N, 1, C, device="cuda:0", dtype=dtype).normal_(0.5, 1.0, generator=g)
+    dy = torch.randint(0, 2, x.shape, device="cuda:0", generator=g, dtype=torch.uint8).to(dtype)
+    gamma, beta = torch.linspace(0.5, 1.5, C, device="cuda:0"), torch.linspace(-0.2, 0.2, C, device="cuda:0")
+    y, mean, rstd = gmc.group_norm(x, G, gamma, beta)
+    dx, dgamma, dbeta = gmc.group_norm_backward(dy, x, mean, rstd, gamma, beta)
+    # enough for the thresholds on the images' number and bytes (48 MB: pieces) to fall as in the whole call
+    few = 4099 if C in (12, 32) else 2 ** 22
+    for a in (0, 2 ** 24 - few // 2, 2 ** 24 - few + 5, N - few):
+        part = x[a:a + few].contiguous()
+        want = gmc.group_norm(part, G, gamma, beta)
+        for got, w in zip((y, mean, rstd), want):
+            assert torch.equal(got[a:a + few], w), a
+        assert torch.equal(dx[a:a + few], gmc.group_norm_backward(dy[a:a + few].contiguous(), part, *want[1:], gamma, beta)[0]), a
+    # zeros and ones: every slot of 16 has a whole number below 2^24, exactly; then four roundings
+    exact = dy.float().view(N, C).sum(0, dtype=torch.float64)
+    assert ((dbeta.double() - exact).abs() <= 4 * U * exact).all(), (dbeta, exact)
+    # a slot's N / 16 terms and a tree: its worst case, loose as it is, and the sums' own sizes
+    hat = (x.view(N, G, -1).float() - mean[:, :, None]) * rstd[:, :, None]
+    terms = dy.view(N, C).double() * hat.view(N, C)
+    bound = (N / 16 + 8) * U * terms.abs().sum(0)
+    assert ((dgamma.double() - terms.sum(0)).abs() <= bound).all()

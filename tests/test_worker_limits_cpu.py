@@ -1,5 +1,6 @@
 """The worker-side operators' sizes and arguments at the ends of their ranges (no GPU:
 nothing here reaches a launch)."""
+import ctypes
 import os
 
 import pytest
@@ -31,3 +32,36 @@ def test_group_norm_workspace_of_wide_long_images(lib):
     for S, C in [(2 ** 17, 2 ** 20), (2 ** 20, 2 ** 17), (2 ** 25, 2 ** 12)]:
         need = lib.gmc_group_norm_workspace(BF16, 1, S, C, 1, 0)
         assert 0 < need <= 2 * 4 * LAST, (S, C, need)
+
+
+@pytest.mark.parametrize("dtype,N,S,C,G", [(BF16, 2 ** 24, 1, 12, 4), (BF16, 2 ** 26 + 1, 1, 64, 8), (F32, 2 ** 25, 1, 4, 1),
+                                           (BF16, 2000, 1, 46523, 46523), (F16, 2 ** 33, 1, 8, 8)])
+def test_group_norm_of_more_images_than_a_launch_has_is_taken(lib, dtype, N, S, C, G):
+    assert lib.gmc_group_norm_workspace(dtype, N, S, C, G, 0) >= 0
+    assert lib.gmc_group_norm_workspace(dtype, N, S, C, G, 1) >= 8 * N * C
+
+
+P = ctypes.c_void_p(1 << 20)
+
+
+def refused(lib, st, needle):
+    assert st == -1 and needle in lib.gmc_last_error(None).decode(), (st, lib.gmc_last_error(None))
+
+
+def test_group_norm_of_an_image_no_launch_has_is_refused(lib):
+    """By the workspace functions too, and before any other buffer is looked at."""
+    C = 2 ** 30
+    for backward in (0, 1):
+        assert lib.gmc_group_norm_workspace(BF16, 1, 30, C - 1, C - 1, backward) == -1
+    refused(lib, lib.gmc_group_norm(None, BF16, 1, 30, C - 1, C - 1, P, 30 * C, C, None, None, 1e-5, 0, P, 30 * C, C, P, P, P,
+                                    1 << 50), "launch")
+    assert lib.gmc_group_norm_workspace(BF16, 1, 1, C, 1, 1) == -1
+    for N in (0, 1):
+        Q, R = ctypes.c_void_p(1 << 40), ctypes.c_void_p(1 << 50)
+        refused(lib, lib.gmc_group_norm_backward(None, BF16, N, 1, C, 1, R, C, C, P, C, C, P, P, None, None, 0, Q, C, C, P, P, P,
+                                                 1 << 50), "launch")
+
+
+def test_dropout_of_more_vectors_than_a_launch_has_is_refused(lib):
+    Q = ctypes.c_void_p(1 << 50)
+    refused(lib, lib.gmc_dropout(None, BF16, 2 ** 34 - 1023, 1, P, 2, None, 0, Q, 2, 0.1, 1, 0, 0, 0), "one launch")
