@@ -1014,12 +1014,12 @@ struct NormPlan {
 // with 8.
 bool plan_fold(NormArgs& a, NormPlan& pl, int64_t size, bool backward, int line) {
     const int full = (int)(16 / size);
-    for (int gw = 1; gw <= a.G; ++gw) {
+    const int widest = 64 * full / a.cpg;  // groups that a block of channels may have
+    for (int gw = 1; gw <= a.G && gw <= widest; ++gw) {
         if (a.G % gw) continue;
         const int64_t cb = (int64_t)gw * a.cpg;
         if (cb % full || (cb * size < line && gw < a.G)) continue;
         const int64_t tc = cb / full;
-        if (tc > 64) return false;
         const int lg = log2_up(tc);
         const auto vectors = [&](int threads) { return ((int64_t)a.S + (threads >> lg) - 1) / (threads >> lg); };
         const int64_t blocks = a.N * (a.G / gw);
@@ -1096,8 +1096,9 @@ NormPlan norm_plan(NormArgs& a, int32_t dtype, bool backward) {
     }
     // any groups: the fewest whose channels fill a 128-byte line (else a 64-byte
     // half), with a thread count that leaves at most `most` vectors each
+    const int widest = kHeldChannels * full / a.cpg;
     for (int line = 128; line >= 64 && !pl.held; line >>= 1)
-        for (int gw = 1; gw <= a.G && !pl.held; ++gw) {
+        for (int gw = 1; gw <= a.G && gw <= widest && !pl.held; ++gw) {
             if (a.G % gw) continue;
             const int64_t cb = (int64_t)gw * a.cpg;
             const bool wide = cb * type_size(dtype) >= line;

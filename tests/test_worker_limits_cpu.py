@@ -2,6 +2,7 @@
 nothing here reaches a launch)."""
 import ctypes
 import os
+import time
 
 import pytest
 
@@ -65,3 +66,10 @@ def test_group_norm_of_an_image_no_launch_has_is_refused(lib):
 def test_dropout_of_more_vectors_than_a_launch_has_is_refused(lib):
     Q = ctypes.c_void_p(1 << 50)
     refused(lib, lib.gmc_dropout(None, BF16, 2 ** 34 - 1023, 1, P, 2, None, 0, Q, 2, 0.1, 1, 0, 0, 0), "one launch")
+
+
+def test_a_large_prime_number_of_groups_is_planned_without_a_search_through_them(lib):
+    # 2^31 - 1 groups of one channel: 46 s where every number of groups was tried
+    at = time.perf_counter()
+    lib.gmc_group_norm_workspace(BF16, 1, 1, LAST, LAST, 0)
+    assert time.perf_counter() - at < 5
