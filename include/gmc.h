@@ -622,7 +622,8 @@ int64_t gmc_group_norm_workspace(int32_t dtype, int64_t N, int64_t S, int32_t C,
  * A token whose label is `ignore` counts nowhere: its logits, old_logp,
  * ref_logp and advantage are not read, its logp is 0 and its gradient row 0.
  * A label outside [0, V) that is not `ignore` makes the token's logp, the
- * loss and its gradient row NaN.  With no token at all the loss is 0.
+ * loss and its gradient row NaN.  With no token at all the loss is 0.  A zero
+ * kl_coef or advantage takes its term out, be the other factor beyond fp32.
  *   logits_dev   [r * seq_pitch + t * tok_pitch + v]; tok_pitch >= V (any
  *                for T = 1); a view without each sequence's last token is fine
  *   labels_dev   int64 [R][T], rows label_pitch apart
@@ -655,7 +656,8 @@ int64_t gmc_policy_loss_workspace(int64_t R, int64_t T);
  *   reward = beta * sum over the answer's tokens of (logp - ref_logp), divided
  *            by their number with `average` (0 for an empty answer)
  *   h      = reward of the chosen - reward of the rejected answer
- *   l      = -(1 - smoothing) log sigmoid(h) - smoothing log sigmoid(-h)
+ *   l      = -(1 - smoothing) log sigmoid(h) - smoothing log sigmoid(-h),
+ *            without a term of weight 0 (the other answer may be impossible)
  *   loss   = the mean of l over the pairs; grad = grad_scale * dloss / dlogits
  * `ignore`, labels out of range, pitches and grad_dev as in gmc_policy_loss.
  *   ref_logp_dev  fp32 [2 P][T], or NULL: zeros

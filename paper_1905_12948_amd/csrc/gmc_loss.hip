@@ -420,7 +420,9 @@ struct Clip {
 };
 
 __device__ __forceinline__ Clip policy_clip(const PolicyArgs& a, const Token& k, double logp) {
-    const float ratio = a.old_logp ? exp2_fast((float)(logp - k.old) * kLog2e) : logp == logp ? 1.0f : NAN;
+    float ratio = a.old_logp ? exp2_fast((float)(logp - k.old) * kLog2e) : logp == logp ? 1.0f : NAN;
+    // beyond 32 bits, from an old log-probability far below: a token without advantage adds 0 all the same
+    if (k.A == 0.0f && ratio == INFINITY) ratio = 1.0f;
     Clip c;
     c.unclipped = ratio * k.A;
     const float clipped = fminf(fmaxf(ratio, 1.0f - a.lo), 1.0f + a.hi) * k.A;
@@ -433,7 +435,7 @@ __device__ __forceinline__ Clip policy_clip(const PolicyArgs& a, const Token& k,
 __device__ __forceinline__ float policy_slope(const PolicyArgs& a, const Token& k, double logp) {
     const Clip c = policy_clip(a, k, logp);
     float slope = c.free ? -c.unclipped : 0.0f;
-    if (a.ref_logp) slope = __builtin_fmaf(a.kl, 1.0f - exp2_fast((float)(k.ref - logp) * kLog2e), slope);
+    if (a.ref_logp && a.kl != 0.0f) slope = __builtin_fmaf(a.kl, 1.0f - exp2_fast((float)(k.ref - logp) * kLog2e), slope);
     return a.scale * a.inv_tau * k.w * slope;
 }
 
@@ -446,7 +448,8 @@ __device__ __forceinline__ void policy_write(const PolicyArgs& a, int64_t i, con
         kl = expm1f(d) - d;
     }
     a.logp[i] = (float)logp;
-    a.tokens[i] = make_float4(k.w * (-c.smaller + a.kl * kl), k.w * kl, c.free ? 0.0f : k.w, 0.0f);
+    // without a coefficient the term is not in the loss, be it beyond 32 bits
+    a.tokens[i] = make_float4(k.w * (-c.smaller + (a.kl != 0.0f ? a.kl * kl : 0.0f)), k.w * kl, c.free ? 0.0f : k.w, 0.0f);
 }
 
 // A row's label, its logit (NaN where the label is out of range) and place (-1).
@@ -699,7 +702,8 @@ __device__ __forceinline__ Pair pref_finish_pair(const PrefArgs& a, const double
     }
     const double h = q.reward[0] - q.reward[1], eps = a.smoothing;
     const double z = exp(-fabs(h)), low = log1p(z);  // low: -log sigmoid(|h|)
-    q.loss = (1.0 - eps) * (low + fmax(-h, 0.0)) + eps * (low + fmax(h, 0.0));
+    // a side without weight is not in the sum: it is infinite where an answer is impossible
+    q.loss = (eps < 1.0 ? (1.0 - eps) * (low + fmax(-h, 0.0)) : 0.0) + (eps > 0.0 ? eps * (low + fmax(h, 0.0)) : 0.0);
     // sigmoid(h) - (1 - eps) = eps sigmoid(h) - (1 - eps) sigmoid(-h)
     const double big = 1.0 / (1.0 + z), small = z / (1.0 + z);
     const double up = h >= 0.0 ? big : small, down = h >= 0.0 ? small : big;
