@@ -435,7 +435,7 @@ __device__ __forceinline__ Clip policy_clip(const PolicyArgs& a, const Token& k,
 __device__ __forceinline__ float policy_slope(const PolicyArgs& a, const Token& k, double logp) {
     const Clip c = policy_clip(a, k, logp);
     float slope = c.free ? -c.unclipped : 0.0f;
-    if (a.ref_logp && a.kl != 0.0f) slope = __builtin_fmaf(a.kl, 1.0f - exp2_fast((float)(k.ref - logp) * kLog2e), slope);
+    if (a.ref_logp && a.kl != 0.0f) slope = __builtin_fmaf(-a.kl, expm1f((float)(k.ref - logp)), slope);
     return a.scale * a.inv_tau * k.w * slope;
 }
 

@@ -80,3 +80,26 @@ def test_impossible_answers(P, T, average):
     assert gmc.preference_loss(y, labels, average=average)[1][0] == math.inf
     _, each, _, _, grad = gmc.preference_loss(y, labels, average=average, smoothing=1.0)
     assert each[0] == 0 and not grad[0].any() and not grad[P].any() and torch.isfinite(grad).all()
+
+
+@pytest.mark.parametrize("V", [2, 4096, 65536, 2 ** 18])
+@pytest.mark.parametrize("size", [1e-2, 1e-4, 1e-6])
+def test_kl_gradient_of_a_reference_close_by(V, size):
+    """Without an advantage the gradient is the KL term's, whose slope 1 - e^d is as
+    small as the difference d of the log-probabilities.  Rows of equal logits, a power of
+    two of them, have a log-probability of -k log 2 without any rounding, so d is known."""
+    import paper_1905_12948_amd as gmc
+    rng = np.random.default_rng(V)
+    R, T, kl = 2, 3, 0.5
+    lp = -math.log(V)
+    refs = dev(lp + size * rng.choice([-1.0, -0.5, 0.5, 1.0], (R, T)))
+    labels = rng.integers(0, V, (R, T))
+    _, logp, grad = gmc.policy_loss(torch.zeros(R, T, V, device="cuda:0"), torch.as_tensor(labels).cuda(), None,
+                                    torch.zeros(R, device="cuda:0"), ref_logp=refs, kl_coef=kl)
+    assert (logp == np.float32(lp)).all()
+    c = kl / (R * T) * -np.expm1(host(refs) - lp)
+    want = np.repeat(-c[:, :, None] / V, V, 2)
+    np.put_along_axis(want, labels[:, :, None], (c * (1 - 1 / V))[:, :, None], 2)
+    # relatively: d, its exponential (2 u), three products, the quotient, the product with p, and the label's
+    # difference of at least half its larger part: 8 u of at most twice the value
+    assert (np.abs(host(grad) - want) <= 16 * U * np.abs(want)).all(), np.abs(host(grad) / want - 1).max() / U
