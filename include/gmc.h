@@ -637,7 +637,8 @@ int64_t gmc_group_norm_workspace(int32_t dtype, int64_t N, int64_t S, int32_t C,
  *   grad_dev     out, with pitches of its own, or NULL; may be logits_dev.
  *                Without it grad_seq and grad_tok > 0 make the sums' order that
  *                of a call with such a gradient, 0 that of a contiguous one
- *   R T < 2^22, 1 <= V < 2^30
+ *   clip_lo in [0, 1], clip_hi >= 0; kl_coef, grad_scale and 1 / temperature
+ *   (> 0) finite in fp32; R T < 2^22, 1 <= V < 2^30
  * workspace_dev is 16-byte aligned.
  */
 gmc_status gmc_policy_loss(void* hip_stream, int32_t dtype, int64_t R, int64_t T, int64_t V, const void* logits_dev,
@@ -661,7 +662,7 @@ int64_t gmc_policy_loss_workspace(int64_t R, int64_t T);
  *   loss   = the mean of l over the pairs; grad = grad_scale * dloss / dlogits
  * `ignore`, labels out of range, pitches and grad_dev as in gmc_policy_loss.
  *   ref_logp_dev  fp32 [2 P][T], or NULL: zeros
- *   smoothing     [0, 1]
+ *   smoothing     [0, 1]; beta and grad_scale finite in fp32
  *   loss_dev      fp32 [1] out (0 for P = 0); pair_loss_dev fp32 [P] out;
  *   rewards_dev   fp32 [2 P] out; logp_dev fp32 [2 P][T] out
  * workspace_dev is 8-byte aligned.

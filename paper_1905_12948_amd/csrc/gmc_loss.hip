@@ -848,6 +848,8 @@ void policy_long_rows(const PolicyArgs& a, dim3 rows, hipStream_t st) {
 
 constexpr int64_t kMostRows = 0xffffffffll / 1024;
 
+bool finite_f32(double v) { return isfinite((float)v); }
+
 // The bytes of R sequences of T rows of V elements of b bytes.
 int64_t rows_span(int64_t R, int64_t T, int64_t V, int64_t seq, int64_t tok, int64_t b) {
     return ((R - 1) * (R > 1 ? seq : 0) + (T - 1) * (T > 1 ? tok : 0) + V) * b;
@@ -906,8 +908,10 @@ gmc_status gmc_policy_loss(void* hip_stream, int32_t dtype, int64_t R, int64_t T
     if (ok != GMC_OK) return ok;
     if (!(clip_lo >= 0.0 && clip_lo <= 1.0 && clip_hi >= 0.0 && isfinite(clip_hi)))
         return op_error(GMC_EINVAL, me, "need 0 <= clip_lo <= 1 and 0 <= clip_hi");
-    if (!isfinite(kl_coef) || !isfinite(grad_scale)) return op_error(GMC_EINVAL, me, "kl_coef and grad_scale must be finite");
-    if (!(temperature > 0.0 && isfinite(temperature))) return op_error(GMC_EINVAL, me, "temperature must be > 0 and finite");
+    if (!finite_f32(kl_coef) || !finite_f32(grad_scale))
+        return op_error(GMC_EINVAL, me, "kl_coef and grad_scale must be finite in fp32");
+    if (!(temperature > 0.0 && isfinite(temperature) && finite_f32(1.4426950408889634 / temperature)))
+        return op_error(GMC_EINVAL, me, "temperature must be > 0 and finite, log2(e) / temperature finite in fp32");
     if (!stats_dev) return op_error(GMC_EINVAL, me, "NULL argument");
     if (workspace_bytes < gmc_policy_loss_workspace(R, T) || !workspace_dev)
         return op_error(GMC_EINVAL, me, "the workspace is too small");
@@ -1007,7 +1011,8 @@ gmc_status gmc_preference_loss(void* hip_stream, int32_t dtype, int64_t P, int64
     const gmc_status ok = logits_check(me, dtype, 2 * P, T, V, logits_dev, seq_pitch, tok_pitch, grad_dev, grad_seq,
                                        grad_tok, labels_dev, label_pitch);
     if (ok != GMC_OK) return ok;
-    if (!isfinite(beta) || !isfinite(grad_scale)) return op_error(GMC_EINVAL, me, "beta and grad_scale must be finite");
+    if (!finite_f32(beta) || !finite_f32(grad_scale))
+        return op_error(GMC_EINVAL, me, "beta and grad_scale must be finite in fp32");
     if (!(smoothing >= 0.0 && smoothing <= 1.0)) return op_error(GMC_EINVAL, me, "smoothing must be in [0, 1]");
     if (!loss_dev) return op_error(GMC_EINVAL, me, "NULL argument");
     hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);

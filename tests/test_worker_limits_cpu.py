@@ -73,3 +73,17 @@ def test_a_large_prime_number_of_groups_is_planned_without_a_search_through_them
     at = time.perf_counter()
     lib.gmc_group_norm_workspace(BF16, 1, 1, LAST, LAST, 0)
     assert time.perf_counter() - at < 5
+
+
+@pytest.mark.parametrize("change,needle", [(dict(kl=1e39), "finite"), (dict(kl=-4e38), "finite"), (dict(scale=1e300), "finite"),
+                                           (dict(tau=1e-39), "temperature"), (dict(tau=5e-324), "temperature")])
+def test_factors_that_are_infinite_in_32_bits_are_refused(lib, change, needle):
+    Q, R = ctypes.c_void_p(1 << 40), ctypes.c_void_p(1 << 50)
+    a = dict(dict(kl=0.1, scale=1.0, tau=1.0), **change)
+    st = lib.gmc_policy_loss(None, BF16, 4, 3, 10, P, 30, 10, P, 3, -100, None, None, P, 1, 0, 0.2, 0.2, a["kl"], a["tau"], 0,
+                             a["scale"], Q, Q, R, 30, 10, None, 0)
+    refused(lib, st, needle)
+    if "tau" not in change:  # kl is beta here
+        st = lib.gmc_preference_loss(None, BF16, 2, 3, 10, P, 30, 10, P, 3, -100, None, a["kl"], 0.0, 0, a["scale"], Q, Q, Q, Q,
+                                     R, 30, 10, None, 0)
+        refused(lib, st, needle)
