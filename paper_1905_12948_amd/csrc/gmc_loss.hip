@@ -892,6 +892,7 @@ extern "C" {
 
 int64_t gmc_policy_loss_workspace(int64_t R, int64_t T) {
     if (R < 0 || T < 0 || (T > 0 && R > kMostRows / T)) return -1;
+    if (T == 0) R = 0;  // sequences without tokens, any number of them
     return R * T * (int64_t)sizeof(float4) + kFinishBlocks * 3 * (int64_t)sizeof(double) + (2 + R) * (int64_t)sizeof(float);
 }
 
@@ -996,7 +997,7 @@ gmc_status gmc_policy_loss(void* hip_stream, int32_t dtype, int64_t R, int64_t T
 }
 
 int64_t gmc_preference_loss_workspace(int64_t P, int64_t T) {
-    if (P < 0 || T < 0 || (T > 0 && P > kMostRows / 2 / T)) return -1;
+    if (P < 0 || P > kMostRows / 2 || T < 0 || (T > 0 && P > kMostRows / 2 / T)) return -1;
     return 2 * P * T * (int64_t)sizeof(float2) + (2 * P + 2) * (int64_t)sizeof(float);
 }
 

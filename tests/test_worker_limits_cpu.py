@@ -87,3 +87,15 @@ def test_factors_that_are_infinite_in_32_bits_are_refused(lib, change, needle):
         st = lib.gmc_preference_loss(None, BF16, 2, 3, 10, P, 30, 10, P, 3, -100, None, a["kl"], 0.0, 0, a["scale"], Q, Q, Q, Q,
                                      R, 30, 10, None, 0)
         refused(lib, st, needle)
+
+
+def test_loss_workspaces_without_tokens(lib):
+    """Sequences without tokens need no more than the sums; pairs beyond what the call takes are refused."""
+    least = lib.gmc_policy_loss_workspace(0, 0)
+    for R in (1, 2 ** 31, 2 ** 61, 2 ** 63 - 1):
+        assert lib.gmc_policy_loss_workspace(R, 0) == least
+    assert lib.gmc_preference_loss_workspace(2 ** 21 - 1, 0) == 4 * 2 ** 22
+    for pairs in (2 ** 21, 2 ** 31, 2 ** 61, 2 ** 63 - 1):
+        assert lib.gmc_preference_loss_workspace(pairs, 0) == -1
+        refused(lib, lib.gmc_preference_loss(None, BF16, pairs, 0, 10, None, 30, 10, None, 3, -100, None, 0.1, 0.0, 0, 1.0, P, P,
+                                             P, P, None, 30, 10, None, 0), "P < 2^21")
