@@ -26,51 +26,12 @@
 
 #include <type_traits>
 
+#include "gmc_norm_plan.h"
 #include "gmc_ops.h"
 
 namespace gmc {
 
 namespace {
-
-constexpr int kHeldThreads = 1024;
-constexpr int kHeldBlocks = 256;   // held: workgroups below which narrower blocks are tried
-// backward, bytes of x from which blocks under 64 bytes wide (four and more
-// workgroups read every line) give way to the split form's second read:
-// 64 x 3136 x 256 bf16 104 us held (silu 124), 93 split (101); half as many images
-// 54 (65), 52 (58); a quarter 23, 33
-constexpr int64_t kSplitBytes = int64_t(48) << 20;
-constexpr int kManyBlocks = 512;   // held: two workgroups for every CU
-constexpr int kHeldMost = 16;      // vectors of x a thread holds (16 bytes each)
-constexpr int kHeldMostBack = 8;   // ... of x and of dy
-constexpr int kHeldChannels = 256; // threads across channels, at most
-constexpr int kSplitThreads = 256;
-constexpr int kSplitTile = 8;      // pixels whose loads a thread issues together
-constexpr int kSplitMost = 64;     // pixels a thread sums, at most
-constexpr int kSplitBlocks = 512;   // split: workgroups, about; long pieces stream better
-                                   // (norm_back_sums at 64 x 3136 x 256: 37 us, 43 with 2048)
-
-struct NormArgs {
-    const void* x;
-    const void* dy;
-    void* out;  // y, or dx
-    int64_t x_image, x_pixel, dy_image, dy_pixel, out_image, out_pixel;
-    const float* gamma;  // NULL: ones
-    const float* beta;   // NULL: zeros
-    float* mean;         // [N][G]: written forward, read backward
-    float* rstd;
-    float* part;         // scratch
-    float* part2;
-    int64_t N;
-    int32_t S, C, G, cpg;
-    int32_t gw, cb, blocks;  // held: groups and channels per workgroup, workgroups per image
-    int32_t tc, tp_log2;     // threads across channels, and the power of two above
-    int32_t cpg_log2;        // -1: cpg is no power of two
-    int32_t once;            // held: blocks of whole lines
-    int32_t chunk, chunks;   // split: pixels per workgroup, workgroups per image
-    int32_t cblocks;         // split: workgroups across channels
-    float eps, inv_m;        // inv_m: 1 / (S cpg)
-    int32_t act;
-};
 
 __device__ __forceinline__ float activate(float z, int act) {
     if (act == GMC_ACT_RELU) return z > 0.0f ? z : (z != z ? z : 0.0f);
@@ -893,8 +854,6 @@ __global__ __launch_bounds__(kSplitThreads) void norm_back_join(NormArgs a, floa
 
 // dgamma and dbeta: the sums over the images of rows of C values, `pitch`
 // apart.  16 channels (a 64-byte line of each row) and 16 row slots a workgroup.
-constexpr int kParamCh = 16;
-
 __device__ __forceinline__ void sum_params(int block, const float* part, const float* part2, int64_t rows, int64_t pitch,
                                            int32_t C, float* dgamma, float* dbeta) {
     __shared__ float lds[2][kSplitThreads];
@@ -989,166 +948,6 @@ __global__ __launch_bounds__(kSplitThreads) void norm_backward_split(NormArgs a,
 
 // -- host ---------------------------------------------------------------------
 
-int log2_up(int64_t n) {
-    int k = 0;
-    while ((int64_t(1) << k) < n) ++k;
-    return k;
-}
-
-struct NormPlan {
-    bool held = false;
-    int vec = 1;      // channels per thread
-    int threads = 0;  // held
-    int kp = 0;
-    int fold = 0;     // held: groups in a vector, 0: the general kernels
-    size_t lds = 0;
-};
-
-// The held form for groups of a power of two of channels: whole groups in
-// segments of at least `line` bytes.  Threads: as few as leave each at most 4
-// vectors (forward of many blocks 8); of many blocks rather 512 threads with up to
-// 16 vectors than 1024 with fewer, and for the backward pass 256 with 8 than 512,
-// so that several workgroups share a CU and one loads while another computes.  64 images of 784 pixels of 512 bf16 channels: forward 18.8 us
-// with 512 threads, 26.6 with 1024; 196 pixels of 1024: backward 19.3 us with 256,
-// 23.5 with 512; one image of 49 pixels of 2048: forward 5.5 us with 4 vectors, 6.0
-// with 8.
-bool plan_fold(NormArgs& a, NormPlan& pl, int64_t size, bool backward, int line) {
-    const int full = (int)(16 / size);
-    const int widest = 64 * full / a.cpg;  // groups that a block of channels may have
-    for (int gw = 1; gw <= a.G && gw <= widest; ++gw) {
-        if (a.G % gw) continue;
-        const int64_t cb = (int64_t)gw * a.cpg;
-        if (cb % full || (cb * size < line && gw < a.G)) continue;
-        const int64_t tc = cb / full;
-        const int lg = log2_up(tc);
-        const auto vectors = [&](int threads) { return ((int64_t)a.S + (threads >> lg) - 1) / (threads >> lg); };
-        const int64_t blocks = a.N * (a.G / gw);
-        const int few = !backward && blocks >= kHeldBlocks ? 8 : 4;
-        const int most = backward ? kHeldMostBack : kHeldMost;
-        int threads = 64;
-        while (threads < kHeldThreads && vectors(threads) > few) threads *= 2;
-        if (blocks >= kManyBlocks) {
-            if (threads == 1024 && vectors(512) <= most) threads = 512;
-            if (backward && threads == 512 && vectors(256) <= most) threads = 256;
-        }
-        const int64_t kp = vectors(threads);
-        if (kp > most) return false;
-        pl.held = true;
-        pl.fold = a.cpg >= full ? 1 : full / a.cpg;
-        pl.vec = full;
-        pl.threads = threads;
-        pl.kp = (int)kp;
-        a.gw = gw;
-        a.cb = (int32_t)cb;
-        a.blocks = a.G / gw;
-        a.tc = (int32_t)tc;
-        a.tp_log2 = lg;
-        a.once = cb * size % 128 == 0 && (a.out_pixel * size) % 128 == 0;
-        const int waves = threads / 64;
-        pl.lds = sizeof(float) * (size_t)(backward ? 2 * waves * (int)cb + 2 * gw : (waves + 2) * gw);
-        return true;
-    }
-    return false;
-}
-
-// The split form: every channel, pieces of an image.
-NormPlan norm_plan_split(NormArgs& a, NormPlan pl, int full) {
-    pl.vec = a.C % full == 0 ? full : 1;
-    const int64_t vecs = a.C / pl.vec;
-    a.tc = (int32_t)(vecs < kSplitThreads ? vecs : kSplitThreads);
-    a.tp_log2 = log2_up(a.tc);
-    a.cblocks = (int32_t)((vecs + a.tc - 1) / a.tc);
-    const int rows = kSplitThreads >> a.tp_log2;
-    // pixels per workgroup: enough workgroups for every CU, one to eight tiles each
-    int64_t chunks = (a.S + (int64_t)rows * kSplitTile - 1) / ((int64_t)rows * kSplitTile);
-    const int64_t want = (kSplitBlocks + a.N * a.cblocks - 1) / (a.N * a.cblocks);
-    const int64_t least = (a.S + (int64_t)rows * kSplitMost - 1) / ((int64_t)rows * kSplitMost);
-    if (chunks > want) chunks = want > least ? want : least;
-    const int64_t most = 0x7fffffff / a.C;  // norm_join counts an image's chunks and channels in 32 bits
-    if (chunks > most) chunks = most;
-    a.chunk = (int32_t)((a.S + chunks - 1) / chunks);
-    a.chunks = (int32_t)(((int64_t)a.S + a.chunk - 1) / a.chunk);
-    const int slots = a.tp_log2 < 6 ? kSplitThreads / 64 : rows;
-    pl.threads = kSplitThreads;
-    pl.lds = sizeof(float) * ((size_t)(slots + 1) * pl.vec << a.tp_log2);
-    return pl;
-}
-
-// Chooses the form and fills the geometry of a.
-NormPlan norm_plan(NormArgs& a, int32_t dtype, bool backward) {
-    NormPlan pl;
-    const int full = (int)(16 / type_size(dtype));
-    const int most = backward ? kHeldMostBack : kHeldMost;
-    a.cpg = a.C / a.G;
-    a.inv_m = (float)(1.0 / ((double)a.S * (double)a.cpg));
-    a.cpg_log2 = a.cpg & (a.cpg - 1) ? -1 : log2_up(a.cpg);
-    if (a.cpg_log2 >= 0 && a.cpg <= 64) {
-        for (int line = 128; line >= 16; line >>= 1) {
-            if (!plan_fold(a, pl, type_size(dtype), backward, line)) continue;
-            if (a.N * a.blocks >= kHeldBlocks) break;
-        }
-        if (pl.held && !(backward && (int64_t)a.cb * type_size(dtype) < 64 &&
-                         a.N * (int64_t)a.S * a.C * type_size(dtype) >= kSplitBytes)) return pl;
-        if (pl.held) {
-            pl = NormPlan{};
-            return norm_plan_split(a, pl, full);
-        }
-    }
-    // any groups: the fewest whose channels fill a 128-byte line (else a 64-byte
-    // half), with a thread count that leaves at most `most` vectors each
-    const int widest = kHeldChannels * full / a.cpg;
-    for (int line = 128; line >= 64 && !pl.held; line >>= 1)
-        for (int gw = 1; gw <= a.G && gw <= widest && !pl.held; ++gw) {
-            if (a.G % gw) continue;
-            const int64_t cb = (int64_t)gw * a.cpg;
-            const bool wide = cb * type_size(dtype) >= line;
-            if (!wide && gw < a.G) continue;
-            const int vec = cb % full == 0 ? full : 1;
-            const int64_t tc = cb / vec;
-            if (tc > kHeldChannels) continue;
-            const int lg = log2_up(tc);
-            int threads = 256;
-            while (threads < kHeldThreads && (((int64_t)a.S << lg) + threads - 1) / threads > 4) threads *= 2;
-            const int rows = threads >> lg;
-            const int64_t kp = ((int64_t)a.S + rows - 1) / rows;
-            if (kp > most) continue;
-            pl.held = true;
-            pl.vec = vec;
-            pl.threads = threads;
-            pl.kp = kp <= 4 ? 4 : most;
-            a.gw = gw;
-            a.cb = (int32_t)cb;
-            a.blocks = a.G / gw;
-            a.tc = (int32_t)tc;
-            a.tp_log2 = lg;
-            const int slots = lg < 6 ? threads / 64 : rows;
-            pl.lds = sizeof(float) * (((size_t)(slots + 1) * vec << lg) + 2 * (size_t)gw);
-        }
-    if (pl.held) return pl;
-    return norm_plan_split(a, pl, full);
-}
-
-// Scratch in floats: two arrays of per-channel partial values, and for the
-// split backward pass the two shared terms of every group.
-int64_t norm_scratch(const NormArgs& a, const NormPlan& pl, bool backward) {
-    if (pl.held) return backward ? 2 * a.N * a.C : 0;
-    return 2 * a.N * a.chunks * a.C + (backward ? 2 * a.N * a.G : 0);
-}
-
-constexpr int64_t kMostThreads = 0xffffffffll;  // of one launch
-
-unsigned param_blocks(int32_t C) { return (unsigned)(((int64_t)C + kParamCh - 1) / kParamCh); }
-
-// Images one launch of each kernel may have; a call of more takes several.
-int64_t launch_images(const NormArgs& a, const NormPlan& pl, bool backward) {
-    const int64_t params = backward ? param_blocks(a.C) * (int64_t)kSplitThreads : 0;
-    if (params >= kMostThreads) return 0;
-    if (pl.held) return kMostThreads / (pl.threads * (int64_t)a.blocks);
-    const int64_t pieces = (kMostThreads - params) / (kSplitThreads * (int64_t)a.chunks * a.cblocks);
-    const int64_t joins = kMostThreads / 64 / a.G;
-    return pieces < joins ? pieces : joins;
-}
-
 // Images n0, n0 + 1, ... of a, at most n; b: bytes of an element.
 NormArgs some_images(NormArgs a, int64_t n0, int64_t n, int64_t b) {
     const int64_t rows = n0 * (a.chunks ? a.chunks : 1) * a.C;
@@ -1229,7 +1028,7 @@ int64_t gmc_group_norm_workspace(int32_t dtype, int64_t N, int64_t S, int32_t C,
     a.S = (int32_t)S;
     a.C = C;
     a.G = G;
-    const NormPlan pl = norm_plan(a, dtype, backward != 0);
+    const NormPlan pl = norm_plan(a, type_size(dtype), backward != 0);
     if (launch_images(a, pl, backward != 0) < 1) {
         op_error(GMC_EINVAL, "gmc_group_norm_workspace", "more than a launch can have");
         return -1;
@@ -1271,7 +1070,7 @@ gmc_status gmc_group_norm(void* hip_stream, int32_t dtype, int64_t N, int64_t S,
     a.G = G;
     a.eps = (float)eps;
     a.act = act;
-    const NormPlan pl = norm_plan(a, dtype, false);
+    const NormPlan pl = norm_plan(a, type_size(dtype), false);
     const int64_t most = launch_images(a, pl, false);
     if (most < 1) return op_error(GMC_EINVAL, me, "more than a launch can have");
     const int64_t need = norm_scratch(a, pl, false);
@@ -1358,7 +1157,7 @@ gmc_status gmc_group_norm_backward(void* hip_stream, int32_t dtype, int64_t N, i
     a.C = C;
     a.G = G;
     a.act = act;
-    const NormPlan pl = norm_plan(a, dtype, true);
+    const NormPlan pl = norm_plan(a, type_size(dtype), true);
     const int64_t most = launch_images(a, pl, true);
     if (most < 1) return op_error(GMC_EINVAL, me, "more than a launch can have");
     const int64_t need = norm_scratch(a, pl, true);
