@@ -10,11 +10,16 @@ namespace gmc {
 
 constexpr int kHeldThreads = 1024;
 constexpr int kHeldBlocks = 256;   // held: workgroups below which narrower blocks are tried
-// backward, bytes of x from which blocks under 64 bytes wide (four and more
-// workgroups read every line) give way to the split form's second read:
-// 64 x 3136 x 256 bf16 104 us held (silu 124), 93 split (101); half as many images
-// 54 (65), 52 (58); a quarter 23, 33
+// backward, bytes of x from which blocks under 64 bytes wide give way to the split
+// form's second read where four and more of them share a line.  In us, held and split:
+// 64 x 3136 x 256 bf16 in 8-channel groups 106 and 90 (silu 125, 97), half as many
+// images 54, 51, a quarter 23, 33; 16-channel groups of 512 channels (32-byte blocks)
+// 199 and 196, 102 and 92, 56 and 54; f32 64 x 3136 x 128 in 4-channel groups 99 and
+// 84, 32 x 6400 149 and 88.  Narrow images, whose lines few blocks share: 1024 x 3136 x
+// 16 bf16 in one block 82 and 92, 200 x 8192 x 16 in two 47 and 60, 4096 x 1024 x 8
+// 65 and 86, 2^19 x 8 x 8 2817 and 5446; 120 x 8192 x 32 in four 67 and 69.
 constexpr int64_t kSplitBytes = int64_t(48) << 20;
+constexpr int kSplitSharing = 4;
 constexpr int kManyBlocks = 512;   // held: two workgroups for every CU
 constexpr int kHeldMost = 16;      // vectors of x a thread holds (16 bytes each)
 constexpr int kHeldMostBack = 8;   // ... of x and of dy
@@ -148,7 +153,7 @@ inline NormPlan norm_plan(NormArgs& a, int64_t size, bool backward) {
             if (!plan_fold(a, pl, size, backward, line)) continue;
             if (a.N * a.blocks >= kHeldBlocks) break;
         }
-        if (pl.held && !(backward && (int64_t)a.cb * size < 64 &&
+        if (pl.held && !(backward && (int64_t)a.cb * size < 64 && a.blocks >= kSplitSharing &&
                          a.N * (int64_t)a.S * a.C * size >= kSplitBytes)) return pl;
         if (pl.held) {
             pl = NormPlan{};

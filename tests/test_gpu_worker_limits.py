@@ -69,9 +69,9 @@ def test_group_norm_of_the_longest_image():
 
 @pytest.mark.parametrize("N,C,G,dtype", [
     (2 ** 24 + 4099, 12, 4, torch.bfloat16),     # 256 threads an image
-    (2 ** 26 + 4099, 16, 2, torch.bfloat16),     # 64; backward 256, in pieces of an image
-    (2 ** 26 + 4099, 32, 4, torch.bfloat16),     # 64, both ways
-    (2 ** 24 + 4099, 4, 2, torch.float32),       # backward: 256, in pieces
+    (2 ** 26 + 4099, 16, 2, torch.bfloat16),     # 64
+    (2 ** 26 + 4099, 32, 4, torch.bfloat16),     # 64
+    (2 ** 24 + 4099, 4, 2, torch.float32),       # 64, in one launch
 ])
 def test_group_norm_of_more_images_than_a_launch_has(N, C, G, dtype):
     """As many calls of fewer images give the same bits, at both ends and across 2^32 threads."""
@@ -82,7 +82,7 @@ def test_group_norm_of_more_images_than_a_launch_has(N, C, G, dtype):
     gamma, beta = torch.linspace(0.5, 1.5, C, device="cuda:0"), torch.linspace(-0.2, 0.2, C, device="cuda:0")
     y, mean, rstd = gmc.group_norm(x, G, gamma, beta)
     dx, dgamma, dbeta = gmc.group_norm_backward(dy, x, mean, rstd, gamma, beta)
-    # enough for the thresholds on the images' number and bytes (48 MB: pieces) to fall as in the whole call
+    # enough for thresholds on the images' number and bytes to fall as in the whole call
     few = 4099 if C in (12, 32) else 2 ** 22
     for a in (0, 2 ** 24 - few // 2, 2 ** 24 - few + 5, N - few):
         part = x[a:a + few].contiguous()
@@ -98,3 +98,25 @@ def test_group_norm_of_more_images_than_a_launch_has(N, C, G, dtype):
     terms = dy.view(N, C).double() * hat.view(N, C)
     bound = (N / 16 + 8) * U * terms.abs().sum(0)
     assert ((dgamma.double() - terms.sum(0)).abs() <= bound).all()
+
+
+def test_group_norm_in_pieces_of_more_images_than_a_launch_has():
+    """A wavefront a group joins the pieces: 1442 images of 46,523 groups have 2^32 threads."""
+    import paper_1905_12948_amd as gmc
+    N, G, C = 1600, 46523, 3 * 46523
+    g = torch.Generator(device="cuda:0").manual_seed(1)
+    x = torch.empty(N, 1, C, device="cuda:0", dtype=torch.bfloat16).normal_(0.5, 1.0, generator=g)
+    dy = torch.randint(0, 2, x.shape, device="cuda:0", generator=g, dtype=torch.uint8).bfloat16()
+    gamma, beta = torch.linspace(0.5, 1.5, C, device="cuda:0"), torch.linspace(-0.2, 0.2, C, device="cuda:0")
+    y, mean, rstd = gmc.group_norm(x, G, gamma, beta, act="relu")
+    dx, dgamma, dbeta = gmc.group_norm_backward(dy, x, mean, rstd, gamma, beta)
+    for a, b in ((0, 300), (1300, 1600)):
+        want = gmc.group_norm(x[a:b].contiguous(), G, gamma, beta, act="relu")
+        for got, w in zip((y, mean, rstd), want):
+            assert torch.equal(got[a:b], w), a
+        back = gmc.group_norm_backward(dy[a:b].contiguous(), x[a:b].contiguous(), *want[1:], gamma, beta)
+        assert torch.equal(dx[a:b], back[0]), a
+    assert torch.equal(dbeta.double(), dy.double().sum((0, 1)))   # whole numbers, exactly
+    hat = (x.view(N, G, 3).float() - mean[:, :, None]) * rstd[:, :, None]
+    terms = dy.view(N, C).double() * hat.view(N, C)
+    assert ((dgamma.double() - terms.sum(0)).abs() <= (N / 16 + 8) * U * terms.abs().sum(0)).all()

@@ -56,3 +56,12 @@ def test_plans_are_within_limits(plan):
         else:
             assert p["chunks"] * p["chunk"] >= S > (p["chunks"] - 1) * p["chunk"] and p["chunks"] * C < 2 ** 31, shape
             assert p["cblocks"] * p["tc"] * p["vec"] >= C > (p["cblocks"] - 1) * p["tc"] * p["vec"], shape
+
+
+@pytest.mark.parametrize("size,shape,form", [
+    (2, (64, 3136, 256, 32), "split"), (2, (32, 3136, 512, 32), "split"), (4, (64, 3136, 128, 32), "split"),
+    (2, (120, 8192, 32, 4), "split"), (2, (16, 3136, 256, 32), "fold"), (2, (1024, 3136, 16, 4), "fold"), (2, (200, 8192, 16, 2), "fold"),
+    (2, (4096, 1024, 8, 8), "fold"), (2, (2 ** 19, 8, 8, 2), "fold"), (4, (2048, 4096, 4, 4), "fold"), (4, (2 ** 22, 1, 4, 1), "fold")])
+def test_only_blocks_that_share_lines_with_many_give_way_to_a_second_read(plan, size, shape, form):
+    """Large images, backward: a block as wide as the image reads whole lines, however narrow."""
+    assert forms.kernel(plan(size, *shape, 1), size, 1)[0] == form
