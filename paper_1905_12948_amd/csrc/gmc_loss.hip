@@ -17,10 +17,14 @@
 // Policy: c depends on the token alone, so a workgroup keeps the row in its
 // registers: the logits are read once and the gradient is written once, the
 // floor of the bytes.  16 x 1024 x 50257 bf16, three quarters of the tokens counting:
-// 511 us, 5.6 TB/s, where a plain copy of such rows reaches 5.9; 555 us from a view
-// whose rows lie off the gradient's by other than 16 bytes.  Preference: c needs the
+// 504 us, 5.7 TB/s, where a plain copy of such rows reaches 5.9; 555 us from a view
+// whose rows lie off the gradient's by other than 16 bytes.  Beyond 6,656 vectors
+// (53,248 entries of 16 bits) a thread's share of the row leaves too few registers for
+// the rest: 43 of 128 go through scratch memory at 26 vectors of 512 threads, 8 at 20 of
+// 1024, with 5.0 to 5.3 TB/s from 53,256 to 151,936 bf16 entries.  Longer rows than 20,480
+// vectors are read twice (200,000: 4.8 TB/s of one read and the write).  Preference: c needs the
 // pair's sums over all its tokens; the rows are read for the statistics and again for
-// the gradient, 16 x 512 tokens of which two thirds count in 300 us.  Both are bound by
+// the gradient, 16 x 512 tokens of which two thirds count in 301 us.  Both are bound by
 // memory: an exponential and its conversions take about 15 operations an element, 40%
 // of what the vector units give in that time.
 // Ignored tokens' logits are never read, and their gradient is zero.
@@ -837,9 +841,10 @@ __global__ void pref_clear(float* loss, int* done) {
 
 // -- host -----------------------------------------------------------------------
 
-// Rows of 6,657 to 13,312 vectors: by 1024 threads in 32 bits (16 x 256 x 50257: 260 us,
-// by 512 285), by 512 in 16 bits, whose rows have twice the elements to work on and two
-// of which then share a CU (16 x 512 x 65536: 356 us, by 1024 365).
+// Rows of 6,657 to 13,312 vectors: by 1024 threads in 32 bits (16 x 256 tokens of 26,628
+// entries 158 us, by 512 167; of 50,257 287 and 313), by 512 in 16 bits, whose rows have
+// twice the elements to work on and two of which then share a CU (of 53,256 172 us, by 1024
+// 191; of 65,536 212 and 215; only at the long end 1024 would gain: 106,496 336 and 328).
 template <int DT>
 void policy_long_rows(const PolicyArgs& a, dim3 rows, hipStream_t st) {
     if constexpr (DT == GMC_F32) policy_held<DT, 1024, 13><<<rows, 1024, 0, st>>>(a);

@@ -16,9 +16,15 @@
 // of the bytes.  Split form, for images whose groups do not fit, or fit in slivers
 // of lines only: per-channel sums of pieces of the image, joined, and a second
 // launch that reads the images again.  bf16, relu: 64 x 28 x 28 x 512 forward 18.8 us
-// (5.5 TB/s of x and y), backward 38; 64 x 56 x 56 x 256 forward 46 (4.4 TB/s: two
-// rounds of workgroups of 1024 threads, one a CU), backward 93 (split: 515 MB in two
-// launches, and a join of 5 us).
+// (5.5 TB/s of x and y), backward 38; 64 x 56 x 56 x 256 forward 47 (4.4 TB/s: two
+// rounds of workgroups of 1024 threads, one a CU), backward 90 (split: 515 MB in two
+// launches, and a join of 5 us).  Far from the bytes: groups of other widths than a power
+// of two up to 64, by the general kernels (64 x 14 x 14 x 384 in 32 groups forward 17 us,
+// backward 23, for 3.3 and 4.9 us of bytes; 8 x 32 x 32 x 640 29 and 49 for 3.6 and 5.3);
+// images in one wide group (64 x 56 x 56 x 256: split, forward 78 us for 35); images of few
+// pixels, a workgroup each and block of channels (16384 x 1 x 768 in 12 groups forward 178 us
+// for 8.5, backward 303 for 12.8).  Folded kernels of 16-bit groups of one or two channels and
+// the general ones at their most vectors put 8 to 46 registers into scratch memory.
 //
 // In the backward pass z is formed in the order written, one rounding each.  All
 // sums are 32-bit, in a fixed order.
