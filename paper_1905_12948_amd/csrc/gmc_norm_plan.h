@@ -26,7 +26,7 @@ constexpr int kHeldMostBack = 8;   // ... of x and of dy
 constexpr int kHeldChannels = 256; // threads across channels, at most
 constexpr int kSplitThreads = 256;
 constexpr int kSplitTile = 8;      // pixels whose loads a thread issues together
-constexpr int kSplitMost = 64;     // pixels a thread sums, at most
+constexpr int kSplitMost = 64;     // pixels a thread sums, at most (of 2^37 values an image a few more)
 constexpr int kSplitBlocks = 512;   // split: workgroups, about; long pieces stream better
                                    // (norm_back_sums at 64 x 3136 x 256: 37 us, 43 with 2048)
 
