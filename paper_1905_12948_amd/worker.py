@@ -41,9 +41,9 @@ def _code(t, name: str) -> int:
     return code
 
 
-def _int(v, bits: int, name: str) -> int:
-    """v as an integer of the C interface (ctypes would take its low bits)."""
-    v = int(v)
+def _int(v: int, bits: int, name: str) -> int:
+    """v, an integer of the C interface, of which ctypes would take the low bits.  The
+    callers look at its high bits first, which is the cheaper test."""
     if not -1 << (bits - 1) <= v < 1 << (bits - 1):
         raise ValueError("%s must be a %d-bit integer, got %d" % (name, bits, v))
     return v
@@ -145,8 +145,11 @@ def dropout(x, p: float, seed: int, t: int = 0, worker: int = 0, site: int = 0, 
     else:
         _is(out, x.dtype, x.shape, x, "out")
         op = _rows(out, "out")[2]
+    t, worker, site = int(t), int(worker), int(site)
+    if (t | worker | site) >> 31:
+        _int(t, 64, "t"), _int(worker, 32, "worker"), _int(site, 32, "site")
     _call(x, load().gmc_dropout, code, rows, cols, x.data_ptr(), pitch, pr, rp, out.data_ptr(), op, float(p),
-          int(seed) & (2 ** 64 - 1), _int(t, 64, "t"), _int(worker, 32, "worker"), _int(site, 32, "site"))
+          int(seed) & (2 ** 64 - 1), t, worker, site)
     return out
 
 
@@ -162,7 +165,8 @@ def _images(t, name: str) -> Tuple[int, int, int, int, int]:
         raise ValueError("%s must be [N, ..., C]" % name)
     N, *pixels, C = t.shape
     S = math.prod(pixels)
-    _int(C, 32, "the number of channels")
+    if C >> 31:
+        _int(C, 32, "the number of channels")
     if t.is_contiguous():
         return N, S, C, S * C, C
     if t.stride(-1) != 1 and C > 1:
@@ -200,7 +204,9 @@ def group_norm(x, groups: int, gamma=None, beta=None, eps: float = 1e-5, act: st
     else:
         _is(out, x.dtype, x.shape, x, "out")
         oi, op = _images(out, "out")[3:]
-    G = _int(groups, 32, "groups")
+    G = int(groups)
+    if G >> 31:
+        _int(G, 32, "groups")
     lib = load()
     n = lib.gmc_group_norm_workspace(code, N, S, C, G, 0)
     ws = _workspace(n, None, x)
@@ -223,7 +229,9 @@ def group_norm_backward(dy, x, mean, rstd, gamma=None, beta=None, act: str = "no
     _, _, _, di, dp = _images(dy, "dy")
     if mean is None or rstd is None or mean.dim() != 2:
         raise ValueError("mean and rstd must be [N, groups]")
-    G = _int(mean.shape[1], 32, "groups")
+    G = int(mean.shape[1])
+    if G >> 31:
+        _int(G, 32, "groups")
     pm, ps = _f32(mean, (N, G), x, "mean"), _f32(rstd, (N, G), x, "rstd")
     pg, pb = _f32(gamma, (C,), x, "gamma"), _f32(beta, (C,), x, "beta")
     if out is None:
@@ -308,12 +316,14 @@ def policy_loss(logits, labels, old_logp, advantages, ref_logp=None, clip: Tuple
     per_token = advantages.dim() == 2
     pa = _f32(advantages, (R, T) if per_token else (R,), logits, "advantages")
     out, pg, gs, gt = _gradient(logits, grad, out)
-    lib = load()
+    lib, ignore = load(), int(ignore)
+    if ignore >> 63 not in (0, -1):
+        _int(ignore, 64, "ignore")
     n = lib.gmc_policy_loss_workspace(R, T)
     ws = _workspace(n, "gmc_policy_loss: more than 2^22 - 1 tokens", logits)
     stats, logp = _new(logits, 3), _another(old_logp, logits, R, T)
     _call(logits, lib.gmc_policy_loss, code, R, T, V, logits.data_ptr(), logits.stride(0), logits.stride(1), pl, lp,
-          _int(ignore, 64, "ignore"), po, pr, pa, T if per_token else 1, 1 if per_token else 0, float(clip[0]), float(clip[1]),
+          ignore, po, pr, pa, T if per_token else 1, 1 if per_token else 0, float(clip[0]), float(clip[1]),
           float(kl_coef), float(temperature), REDUCTIONS[reduction], float(grad_scale), stats.data_ptr(),
           logp.data_ptr(), pg, gs, gt, ws.data_ptr(), n)
     return stats, logp, out
@@ -332,11 +342,13 @@ def preference_loss(logits, labels, ref_logp=None, beta: float = 0.1, smoothing:
     P = R // 2
     pr = _f32(ref_logp, (R, T), logits, "ref_logp")
     out, pg, gs, gt = _gradient(logits, grad, out)
-    lib = load()
+    lib, ignore = load(), int(ignore)
+    if ignore >> 63 not in (0, -1):
+        _int(ignore, 64, "ignore")
     n = lib.gmc_preference_loss_workspace(P, T)
     ws = _workspace(n, "gmc_preference_loss: more than 2^22 - 1 tokens", logits)
     loss, each, rewards, logp = _new(logits), _new(logits, P), _new(logits, R), _another(ref_logp, logits, R, T)
     _call(logits, lib.gmc_preference_loss, code, P, T, V, logits.data_ptr(), logits.stride(0), logits.stride(1), pl, lp,
-          _int(ignore, 64, "ignore"), pr, float(beta), float(smoothing), 1 if average else 0, float(grad_scale), loss.data_ptr(),
+          ignore, pr, float(beta), float(smoothing), 1 if average else 0, float(grad_scale), loss.data_ptr(),
           each.data_ptr(), rewards.data_ptr(), logp.data_ptr(), pg, gs, gt, 0 if ws is None else ws.data_ptr(), n)
     return loss, each, rewards, logp, out
