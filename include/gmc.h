@@ -675,6 +675,119 @@ gmc_status gmc_preference_loss(void* hip_stream, int32_t dtype, int64_t P, int64
                                int64_t grad_seq, int64_t grad_tok, void* workspace_dev, int64_t workspace_bytes);
 int64_t gmc_preference_loss_workspace(int64_t P, int64_t T);
 
+/*
+ * The scores of R sequences of T tokens, from their logits over a vocabulary of V:
+ * log-probabilities of given tokens, entropies, and the most probable tokens.  With
+ * z_j = (logits_j - max) / temperature and S = sum exp(z_j):
+ *   norm     = (max, log S): what the gradient needs of a row
+ *   logp     = z[label] - log S
+ *   entropy  = log S - (sum exp(z_j) z_j) / S = -sum p log p
+ *   top      = the `top` largest logits, equal ones by their place, the first one
+ *              first, and their log-probabilities
+ * A token whose label is `ignore` is not looked at: its scores are 0 and its top_ids
+ * -1.  A label outside [0, V) that is not `ignore` makes the token's logp NaN.  Logits
+ * of -inf have no probability and take no part; where all are, or where one is NaN
+ * or +inf, the row's scores are NaN (its top_ids are still the largest, a NaN
+ * larger than all).
+ *   logits_dev, pitches  as in gmc_policy_loss
+ *   labels_dev   int64 [R][T], rows label_pitch apart, or NULL: all tokens are
+ *                scored and logp_dev is not written
+ *   top          0 to min(V, 32)
+ *   logp_dev, entropy_dev  fp32 [R][T] out; norm_dev fp32 [R][T][2] out
+ *   top_logp_dev fp32 and top_ids_dev int64 [R][T][top] out
+ *   temperature, R T and V as in gmc_policy_loss
+ * workspace_dev is 16-byte aligned.
+ */
+gmc_status gmc_token_scores(void* hip_stream, int32_t dtype, int64_t R, int64_t T, int64_t V, const void* logits_dev,
+                            int64_t seq_pitch, int64_t tok_pitch, const int64_t* labels_dev, int64_t label_pitch,
+                            int64_t ignore, int32_t top, double temperature, float* logp_dev, float* entropy_dev,
+                            float* top_logp_dev, int64_t* top_ids_dev, float* norm_dev, void* workspace_dev,
+                            int64_t workspace_bytes);
+int64_t gmc_token_scores_workspace(int32_t dtype, int64_t R, int64_t T, int64_t V, int32_t top);
+
+/*
+ * The logits' gradient from the scores': with p = softmax(logits / temperature),
+ *   grad_j = (1 / temperature) (dlogp (delta_j,label - p_j)
+ *            - dentropy p_j (log p_j + entropy)
+ *            + sum_i dtop[i] (delta_j,top_ids[i] - p_j))
+ * An ignored token's row is 0 and its logits and gradients are not read.  With dlogp a
+ * label outside [0, V) that is not `ignore` makes the row NaN.  A top_ids[i] outside
+ * [0, V) takes its term out; one that occurs twice counts twice.
+ *   norm_dev, entropy_dev  as gmc_token_scores gave them; entropy_dev only with dentropy
+ *   labels_dev     as there, or NULL: no token is ignored and there is no dlogp
+ *   dlogp_dev, dentropy_dev  fp32 [R][T] or NULL: zeros
+ *   top_ids_dev, dtop_dev    int64 and fp32 [R][T][top], or top = 0; top <= 32
+ *   grad_dev       out, with pitches of its own; may be logits_dev
+ */
+gmc_status gmc_token_scores_backward(void* hip_stream, int32_t dtype, int64_t R, int64_t T, int64_t V,
+                                     const void* logits_dev, int64_t seq_pitch, int64_t tok_pitch,
+                                     const int64_t* labels_dev, int64_t label_pitch, int64_t ignore, int32_t top,
+                                     double temperature, const float* norm_dev, const float* entropy_dev,
+                                     const float* dlogp_dev, const float* dentropy_dev, const int64_t* top_ids_dev,
+                                     const float* dtop_dev, void* grad_dev, int64_t grad_seq, int64_t grad_tok);
+
+/* ---------------------------------------------------------------------------
+ * Orthogonalised matrices, on the server's side: the update's matrices are taken
+ * towards their nearest orthogonal ones by Newton-Schulz steps, alone (between
+ * gmc_aggregate and gmc_apply) or with a momentum of the server's own in the place
+ * of gmc_apply.  The conventions of the operators above hold, but for the plan.
+ *
+ * A plan says which matrices a vector of d components holds: matrix i has
+ * rows[i] x cols[i] components from offset[i] on, rows pitch[i] apart (NULL: cols),
+ * and scale[i] (NULL: 1) is the factor of what becomes of it.  Host arrays, read
+ * before the call returns.  Matrices may be column slices of one wide array; no two
+ * share a component.  The plan keeps its tables on the current device, which later
+ * calls have to be on, and is not changed by them: calls on several streams may
+ * share it.  Making it waits for the device; it cannot be made while a stream is
+ * captured, and has to live as long as the graphs that were captured with it.
+ *   d <= 2^40; 0 to 8192 matrices of 1 to 2^26 rows and columns, and no more than
+ *   2^22 tiles of 64 x 64 (more than any vector of 2^34 components in dense
+ *   matrices of 64 rows and columns or more)
+ */
+typedef struct gmc_matrices gmc_matrices;
+gmc_status gmc_matrices_init(gmc_matrices** out, int64_t d, int32_t n, const int64_t* offset, const int64_t* rows,
+                             const int64_t* cols, const int64_t* pitch, const double* scale);
+void gmc_matrices_destroy(gmc_matrices* plan); /* waits for the device; NULL is a no-op */
+
+/* Scratch bytes of the two calls below (256-byte aligned). */
+int64_t gmc_matrices_workspace(const gmc_matrices* plan);
+
+/*
+ * out = x with every matrix M of the plan replaced by alpha * scale * X_n, where
+ *   X_0 = M / (|M| + eps), |M| the root of the sum of squares (a zero matrix
+ *         stays zero, also with eps = 0),
+ *   X_{k+1} = a_k X_k + b_k (X_k X_k^T) X_k + c_k (X_k X_k^T)^2 X_k
+ * and the components outside the matrices as they are.  The steps take each singular
+ * value s to s (a + b s^2 + c s^4) and leave the singular vectors.  Products are
+ * taken to 22 bits of each factor and summed in 32 bits; |M| is summed in 64.  A matrix
+ * with a NaN or an infinity becomes NaN, and no other one does.
+ *   x_dev, out_dev  d components of a GMC_F32, GMC_BF16 or GMC_F16 type; out_dev may be x_dev
+ *   steps           1 to 64; coefficients: host array [steps][3], finite, such that no singular
+ *                   value in [0, 1] is taken beyond 2.5 by a step (the last one: 10^6), and
+ *                   b s^2 + c s^4 stays within 60
+ *   eps in [0, 1]; alpha finite in fp32
+ */
+gmc_status gmc_orthogonalize(void* hip_stream, const gmc_matrices* plan, int32_t dtype, const void* x_dev, void* out_dev,
+                             int32_t steps, const double* coefficients, double eps, double alpha, void* workspace_dev,
+                             int64_t workspace_bytes);
+
+/*
+ * The server's step with orthogonalised matrices, from the update that gmc_aggregate
+ * gives (it points downhill; a gradient takes a negative rate):
+ *   inside the matrices   momentum = mu * momentum + update
+ *                         u = update + mu * momentum (nesterov) or momentum
+ *                         w_out = (1 - decay) w + rate * scale * X_n(u)
+ *   outside               w_out = w + update, as gmc_apply; momentum is not touched
+ *   update_dev    d components of a GMC_F32, GMC_BF16 or GMC_F16 type
+ *   momentum_dev  fp32 [d], or NULL: u = update
+ *   w_out_dev     may be w_dev; as another buffer it leaves w_t for gmc_step's w_prev
+ *   mu in [0, 1]; rate and decay finite in fp32; the rest as in gmc_orthogonalize
+ */
+gmc_status gmc_orthogonal_step(void* hip_stream, const gmc_matrices* plan, int32_t dtype, const float* w_dev,
+                               const void* update_dev, float* momentum_dev, float* w_out_dev, double rate, double mu,
+                               int32_t nesterov, double decay, int32_t steps, const double* coefficients, double eps,
+                               void* workspace_dev, int64_t workspace_bytes);
+
 /* Message for the last non-OK status of this context (or of gmc_init and the
  * calls without a context when ctx is NULL); never NULL. */
 const char* gmc_last_error(const gmc_ctx* ctx);

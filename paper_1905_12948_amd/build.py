@@ -8,7 +8,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libgmc.so")
-SOURCES = ["gmc_kernels.hip", "gmc_api.hip", "gmc_dropout.hip", "gmc_norm.hip", "gmc_loss.hip"]
+SOURCES = ["gmc_kernels.hip", "gmc_api.hip", "gmc_dropout.hip", "gmc_norm.hip", "gmc_loss.hip", "gmc_scores.hip",
+           "gmc_matrix.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

@@ -35,7 +35,10 @@ EXPORTS = ("gmc_init", "gmc_set_segments", "gmc_set_block", "gmc_set_stream", "g
            "gmc_step_detach", "gmc_finish", "gmc_detach", "gmc_iteration", "gmc_calib_stream", "gmc_pair_stats",
            "gmc_count", "gmc_aggregate_static", "gmc_iteration_inplace",
            "gmc_dropout", "gmc_group_norm", "gmc_group_norm_backward", "gmc_group_norm_workspace",
-           "gmc_policy_loss", "gmc_policy_loss_workspace", "gmc_preference_loss", "gmc_preference_loss_workspace")
+           "gmc_policy_loss", "gmc_policy_loss_workspace", "gmc_preference_loss", "gmc_preference_loss_workspace",
+           "gmc_token_scores", "gmc_token_scores_workspace", "gmc_token_scores_backward",
+           "gmc_matrices_init", "gmc_matrices_destroy", "gmc_matrices_workspace", "gmc_orthogonalize",
+           "gmc_orthogonal_step")
 
 RULES = {"gmc": 0, "server_momentum": 1, "lr_in_residual": 2}
 
@@ -110,13 +113,26 @@ def load() -> ctypes.CDLL:
                                         P, P, P, P, P, i64, i64, P, i64]
     lib.gmc_preference_loss_workspace.argtypes = [i64, i64]
     lib.gmc_preference_loss_workspace.restype = i64
+    lib.gmc_token_scores.argtypes = [P, i32, i64, i64, i64, P, i64, i64, P, i64, i64, i32, dbl, P, P, P, P, P, P, i64]
+    lib.gmc_token_scores_workspace.argtypes = [i32, i64, i64, i64, i32]
+    lib.gmc_token_scores_workspace.restype = i64
+    lib.gmc_token_scores_backward.argtypes = [P, i32, i64, i64, i64, P, i64, i64, P, i64, i64, i32, dbl, P, P, P, P, P,
+                                              P, P, i64, i64]
+    lib.gmc_matrices_init.argtypes = [ctypes.POINTER(P), i64, i32, P, P, P, P, P]
+    lib.gmc_matrices_destroy.argtypes = [P]
+    lib.gmc_matrices_destroy.restype = None
+    lib.gmc_matrices_workspace.argtypes = [P]
+    lib.gmc_matrices_workspace.restype = i64
+    lib.gmc_orthogonalize.argtypes = [P, P, i32, P, P, i32, P, dbl, dbl, P, i64]
+    lib.gmc_orthogonal_step.argtypes = [P, P, i32, P, P, P, P, dbl, dbl, i32, dbl, i32, P, dbl, P, i64]
     for name in ("gmc_init", "gmc_set_segments", "gmc_set_block", "gmc_set_stream", "gmc_step",
                  "gmc_aggregate", "gmc_apply", "gmc_get_step", "gmc_set_step", "gmc_set_option",
                  "gmc_stats", "gmc_profile_read", "gmc_calib_copy", "gmc_aggregate_apply",
                  "gmc_set_rule", "gmc_set_eta", "gmc_set_lambda", "gmc_step_detach", "gmc_finish",
                  "gmc_detach", "gmc_iteration", "gmc_calib_stream", "gmc_pair_stats", "gmc_iteration_inplace",
                  "gmc_dropout", "gmc_group_norm", "gmc_group_norm_backward", "gmc_policy_loss",
-                 "gmc_preference_loss"):
+                 "gmc_preference_loss", "gmc_token_scores", "gmc_token_scores_backward", "gmc_matrices_init",
+                 "gmc_orthogonalize", "gmc_orthogonal_step"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib

@@ -1,6 +1,7 @@
 """The operators of a worker's own pass (include/gmc.h), on torch tensors:
-dropout, group norm with its activation, and the policy and preference losses
-with their gradients.
+dropout, group norm with its activation, the policy and preference losses
+with their gradients, and tokens' scores (log-probabilities, entropies, the most
+probable tokens) with theirs.
 
 Like the rest of the binding this only marshals arguments: it checks types,
 devices, shapes and strides, allocates outputs and scratch, and calls the
@@ -254,7 +255,7 @@ def group_norm_backward(dy, x, mean, rstd, gamma=None, beta=None, act: str = "no
 
 
 def _logits(logits, labels) -> Tuple[int, int, int, int, int, int]:
-    """(code, R, T, V, label pointer, label pitch)."""
+    """(code, R, T, V, label pointer, label pitch); without labels the last two are 0."""
     torch = _torch()
     code = _code(logits, "logits")
     if logits.dim() != 3:
@@ -262,10 +263,18 @@ def _logits(logits, labels) -> Tuple[int, int, int, int, int, int]:
     R, T, V = logits.shape
     if V > 1 and logits.stride(2) != 1:
         raise ValueError("logits need a contiguous vocabulary axis")
+    if labels is None:
+        return code, R, T, V, 0, 0
     _is(labels, torch.int64, (R, T), logits, "labels")
     if T > 1 and labels.stride(1) != 1:
         raise ValueError("labels need contiguous tokens")
     return code, R, T, V, labels.data_ptr(), labels.stride(0)
+
+
+def _labels(labels):
+    if labels is None:
+        raise TypeError("labels must be a torch.Tensor")
+    return labels
 
 
 def _gradient(logits, grad: bool, out):
@@ -307,7 +316,7 @@ def policy_loss(logits, labels, old_logp, advantages, ref_logp=None, clip: Tuple
     grad_scale times the loss's, with strides like the logits' where those are
     nearly dense; ``out`` may be logits."""
     torch = _torch()
-    code, R, T, V, pl, lp = _logits(logits, labels)
+    code, R, T, V, pl, lp = _logits(logits, _labels(labels))
     if reduction not in REDUCTIONS:
         raise ValueError("reduction must be one of %s" % list(REDUCTIONS))
     po, pr = _f32(old_logp, (R, T), logits, "old_logp"), _f32(ref_logp, (R, T), logits, "ref_logp")
@@ -336,7 +345,7 @@ def preference_loss(logits, labels, ref_logp=None, beta: float = 0.1, smoothing:
 
     ref_logp: the reference's token log-probabilities, fp32 [2 P, T], as a call
     of its own with grad=False returns them, or None.  ``out`` may be logits."""
-    code, R, T, V, pl, lp = _logits(logits, labels)
+    code, R, T, V, pl, lp = _logits(logits, _labels(labels))
     if R % 2:
         raise ValueError("logits must hold pairs: [2 P, T, V]")
     P = R // 2
@@ -352,3 +361,72 @@ def preference_loss(logits, labels, ref_logp=None, beta: float = 0.1, smoothing:
           ignore, pr, float(beta), float(smoothing), 1 if average else 0, float(grad_scale), loss.data_ptr(),
           each.data_ptr(), rewards.data_ptr(), logp.data_ptr(), pg, gs, gt, 0 if ws is None else ws.data_ptr(), n)
     return loss, each, rewards, logp, out
+
+
+def token_scores(logits, labels=None, top: int = 0, temperature: float = 1.0, ignore: int = IGNORE):
+    """The scores of tokens with logits [R, T, V]: (logp, entropy, top_logp, top_ids,
+    norm).
+
+    logp: fp32 [R, T], the log-probabilities of ``labels`` (int64 [R, T], ``ignore``
+    marks tokens that are not looked at; None: all are, and logp is None); entropy:
+    fp32 [R, T]; top_logp, top_ids: fp32 and int64 [R, T, top], the ``top`` (up to 32)
+    most probable tokens, equal ones by their place (None without ``top``); norm:
+    fp32 [R, T, 2], the largest logit and the log of the sum, for the backward call."""
+    torch = _torch()
+    code, R, T, V, pl, lp = _logits(logits, labels)
+    lib, ignore, top = load(), int(ignore), int(top)
+    if ignore >> 63 not in (0, -1):
+        _int(ignore, 64, "ignore")
+    if top >> 31:
+        _int(top, 32, "top")
+    n = lib.gmc_token_scores_workspace(code, R, T, V, top)
+    ws = _workspace(n, "gmc_token_scores: top must be in 0 to 32 and no more than the vocabulary, tokens below 2^22",
+                    logits)
+    norm, entropy = _new(logits, R, T, 2), _new(logits, R, T)
+    logp = None if labels is None else _another(entropy, logits, R, T)
+    top_logp = top_ids = None
+    if top:
+        top_logp, top_ids = _new(logits, R, T, top), logits.new_empty((R, T, top), dtype=torch.int64)
+    _call(logits, lib.gmc_token_scores, code, R, T, V, logits.data_ptr(), logits.stride(0), logits.stride(1), pl, lp,
+          ignore, top, float(temperature), 0 if logp is None else logp.data_ptr(), entropy.data_ptr(),
+          0 if top_logp is None else top_logp.data_ptr(), 0 if top_ids is None else top_ids.data_ptr(),
+          norm.data_ptr(), 0 if ws is None else ws.data_ptr(), n)
+    return logp, entropy, top_logp, top_ids, norm
+
+
+def token_scores_backward(logits, norm, labels=None, dlogp=None, entropy=None, dentropy=None, top_ids=None, dtop=None,
+                          temperature: float = 1.0, ignore: int = IGNORE, out=None):
+    """The logits' gradient, with the forward call's logits, norm, labels, temperature
+    and ignore, from the gradients of its results: dlogp and dentropy (fp32 [R, T]; the
+    latter with the forward call's entropy) and dtop (fp32 [R, T, k], of the
+    log-probabilities of top_ids, any k up to 32 tokens; one outside the vocabulary has
+    no part).  The gradient has strides like the logits' where those are nearly dense;
+    ``out`` may be logits."""
+    torch = _torch()
+    code, R, T, V, pl, lp = _logits(logits, labels)
+    out, pg, gs, gt = _gradient(logits, True, out)
+    pn = _f32(norm, (R, T, 2), logits, "norm")
+    pd, ph = _f32(dlogp, (R, T), logits, "dlogp"), _f32(dentropy, (R, T), logits, "dentropy")
+    if dentropy is not None and entropy is None:
+        raise ValueError("dentropy needs entropy")
+    if (top_ids is None) != (dtop is None):
+        raise ValueError("top_ids and dtop come together")
+    pe = _f32(entropy, (R, T), logits, "entropy")
+    top = pi = 0
+    if top_ids is not None:
+        if top_ids.dim() != 3:
+            raise ValueError("top_ids must be [R, T, k]")
+        top = top_ids.shape[2]
+        if top >> 31:
+            _int(top, 32, "the number of top_ids")
+        _is(top_ids, torch.int64, (R, T, top), logits, "top_ids")
+        if not top_ids.is_contiguous():
+            raise ValueError("top_ids must be contiguous")
+        pi = top_ids.data_ptr()
+    pt = _f32(dtop, (R, T, top), logits, "dtop")
+    ignore = int(ignore)
+    if ignore >> 63 not in (0, -1):
+        _int(ignore, 64, "ignore")
+    _call(logits, load().gmc_token_scores_backward, code, R, T, V, logits.data_ptr(), logits.stride(0),
+          logits.stride(1), pl, lp, ignore, top, float(temperature), pn, pe, pd, ph, pi, pt, pg, gs, gt)
+    return out
