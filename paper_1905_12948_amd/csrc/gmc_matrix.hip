@@ -258,6 +258,17 @@ struct ProductArgs {
     float alpha, keep;
 };
 
+// Waits until all but the wavefront's last kLoads loads to shared memory have arrived and its
+// reads of shared memory are done, and then for the workgroup's other wavefronts.
+template <int kLoads>
+__device__ __forceinline__ void wait_stage() {
+    static_assert(kLoads < 64, "the counter has 6 bits");
+    __builtin_amdgcn_s_waitcnt((kLoads & 15) | 7 << 4 | 0 << 8 | (kLoads >> 4) << 14);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
 // One tile of D = P Q^T, both along their contraction, by four wavefronts of kWide x
 // kWide blocks each, and what the mode makes of it:
 //   kGram   P = Q = X            G = D
@@ -268,9 +279,9 @@ struct ProductArgs {
 template <int kWide, int kMode, int DT>
 __global__ __launch_bounds__(256, 2) void matrix_product(ProductArgs a) {
     constexpr int kBlocks = 2 * kWide;                 // of 32 rows, on each side of the tile
-    constexpr int kChunks = 2 * kBlocks * 2 * 2;       // kilobytes a step: sides, blocks, 16 columns, halves
-    constexpr int kStage = kChunks * 512;
-    __shared__ _Float16 lds[2 * kStage];
+    constexpr int kDeep = kWide == 2 ? 1 : 2;          // 16 columns, of a stage
+    constexpr int kChunks = 2 * kBlocks * kDeep * 2;   // kilobytes of a stage: sides, blocks, columns, halves
+    __shared__ _Float16 stage0[kChunks * 512], stage1[kChunks * 512], stage2[kChunks * 512], stage3[kChunks * 512];
     const Tile t = a.tiles[blockIdx.x];
     const Mat m = a.mats[t.mat];
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
@@ -283,25 +294,22 @@ __global__ __launch_bounds__(256, 2) void matrix_product(ProductArgs a) {
                          : flip ? a.B + m.g * 1024 : a.XT + m.x * 1024);
     const int pb = kMode == kGram || kMode == kPoly ? m.mb : flip ? m.nb : m.mb;   // blocks of P's and Q's rows
     const int qb = kMode == kGram || kMode == kPoly ? m.mb : flip ? m.mb : m.nb;
-    const int steps = kMode == kGram ? m.nb : m.mb;    // of 32 columns
-    const int64_t row = (int64_t)steps * 2048;         // halves of a row of blocks
+    const int deep = 2 * (kMode == kGram ? m.nb : m.mb);   // 16 columns
+    const int64_t row = (int64_t)deep * 1024;              // halves of a row of blocks
     const float theta = kMode == kGram ? 1.0f : a.theta[t.mat * (kMostSteps + 1)];
     const float ratio = kMode == kApply ? theta / a.theta[t.mat * (kMostSteps + 1) + 1] : 1.0f;
 
-    // chunk c of a step: side, block, 16 columns, half; a wavefront takes every fourth.
+    // chunk c of a stage: side, block, 16 columns, half; a wavefront takes every fourth.
     // Blocks beyond the matrix are read as its last one and not written.
-    const auto fetch = [&](int s, int buf) {
+    const _Float16* from[kChunks / 4];
 #pragma unroll
-        for (int k = 0; k < kChunks / 4; ++k) {
-            const int c = k * 4 + wave, side = c / (kChunks / 2), b = (c / 4) % kBlocks;
-            int rb = (side ? tj : ti) * kBlocks + b;
-            const int most = (side ? qb : pb) - 1;
-            rb = rb < most ? rb : most;
-            const _Float16* g = (side ? Q : P) + rb * row + (int64_t)s * 2048 + (c & 3) * 512 + lane * 8;
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)g,
-                                             (__attribute__((address_space(3))) void*)(lds + buf * kStage + c * 512), 16, 0, 0);
-        }
-    };
+    for (int k = 0; k < kChunks / 4; ++k) {
+        const int c = k * 4 + wave, side = c / (kChunks / 2), b = c / (2 * kDeep) % kBlocks;
+        int rb = (side ? tj : ti) * kBlocks + b;
+        const int most = (side ? qb : pb) - 1;
+        rb = rb < most ? rb : most;
+        from[k] = (side ? Q : P) + rb * row + (c % (2 * kDeep)) * 512 + lane * 8;
+    }
     f32x16 acc[kWide][kWide];
 #pragma unroll
     for (int i = 0; i < kWide; ++i)
@@ -310,23 +318,32 @@ __global__ __launch_bounds__(256, 2) void matrix_product(ProductArgs a) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
     const int wi = (wave >> 1) * kWide, wj = (wave & 1) * kWide;   // the wavefront's first blocks
-    fetch(0, 0);
-    for (int s = 0; s < steps; ++s) {
-        __syncthreads();   // step s is in shared memory, and step s - 1 has been read
-        const f16x8* at = reinterpret_cast<const f16x8*>(lds + (s & 1) * kStage) + lane;
-        f16x8 p[2][kWide][2], q[2][kWide][2];
+    const int stages = deep / kDeep;
+    const auto fetch = [&](int s, _Float16* to) {
+        s = s < stages ? s : stages - 1;   // the count of loads under way stays what the waits take it for
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
+        for (int k = 0; k < kChunks / 4; ++k)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from[k] + (int64_t)s * (kDeep * 1024)),
+                                             (__attribute__((address_space(3))) void*)(to + (k * 4 + wave) * 512), 16, 0, 0);
+    };
+    // Stage s is in shared memory and stage s - 1 has been read by all, whose place the loads of
+    // s + 3 take; those of s + 1 and s + 2 stay under way.
+    const auto step = [&](int s, const _Float16* here, _Float16* next) {
+        wait_stage<2 * (kChunks / 4)>();
+        const f16x8* at = reinterpret_cast<const f16x8*>(here) + lane;
+        f16x8 p[kDeep][kWide][2], q[kDeep][kWide][2];
+#pragma unroll
+        for (int k = 0; k < kDeep; ++k)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int i = 0; i < kWide; ++i) {
-                    p[k][i][h] = at[(((wi + i) * 2 + k) * 2 + h) * 64];
-                    q[k][i][h] = at[(((kBlocks + wj + i) * 2 + k) * 2 + h) * 64];
+                    p[k][i][h] = at[(((wi + i) * kDeep + k) * 2 + h) * 64];
+                    q[k][i][h] = at[(((kBlocks + wj + i) * kDeep + k) * 2 + h) * 64];
                 }
-        if (s + 1 < steps) fetch(s + 1, (s + 1) & 1);
+        fetch(s + 3, next);
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
+        for (int k = 0; k < kDeep; ++k)
 #pragma unroll
             for (int part = 0; part < 3; ++part)
 #pragma unroll
@@ -334,12 +351,25 @@ __global__ __launch_bounds__(256, 2) void matrix_product(ProductArgs a) {
 #pragma unroll
                     for (int j = 0; j < kWide; ++j)
                         acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[k][i][part == 2], q[k][j][part == 1], acc[i][j], 0, 0, 0);
+    };
+    fetch(0, stage0);
+    fetch(1, stage1);
+    fetch(2, stage2);
+    int s = 0;
+    for (; s + 4 <= stages; s += 4) {
+        step(s, stage0, stage3);
+        step(s + 1, stage1, stage0);
+        step(s + 2, stage2, stage1);
+        step(s + 3, stage3, stage2);
     }
-    __syncthreads();   // shared memory is free
+    if (s < stages) step(s, stage0, stage3);
+    if (s + 1 < stages) step(s + 1, stage1, stage0);
+    if (s + 2 < stages) step(s + 2, stage2, stage1);
+    __syncthreads();   // no load is under way and shared memory is free
 
     // Of a block of D lane l has column l % 32, rows 8 g + 4 (l / 32) + e in entry 4 g + e.
-    float* turn = reinterpret_cast<float*>(lds) + wave * 32 * 33;
-    static_assert(4 * 32 * 33 * 4 <= 2 * kStage * 2, "a wavefront's block fits the stages");
+    static_assert(32 * 33 * 4 <= kChunks * 1024, "a wavefront's block fits a stage");
+    float* turn = reinterpret_cast<float*>(wave == 0 ? stage0 : wave == 1 ? stage1 : wave == 2 ? stage2 : stage3);
     const int col = lane & 31, half = lane >> 5;
 #pragma unroll
     for (int i = 0; i < kWide; ++i)
