@@ -47,7 +47,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr float kScaleX = 0x1p13f, kScaleB = 0x1p10f;   // of X and G, and of b G + c G^2
 constexpr int kSide = 64;                                // side of the pieces the vector is read in
-constexpr int kParts = 256;                              // partial sums of a matrix's squares
+constexpr int kParts = 1024;                             // partial sums of a matrix's squares
 constexpr int64_t kGapChunk = 8192;                      // components outside the matrices, a workgroup
 constexpr int kMostSteps = 64;
 
@@ -61,8 +61,12 @@ struct Mat {
     int32_t part, parts;
 };
 
+// What a workgroup does: of the vector's launches `count` pieces of a matrix from (i, j) on, of a
+// product's one tile (i, j), its contraction from block `first` to `last`; slot: where a part of
+// a tile's sum goes, -1 for a whole tile.  A joining launch adds `count` slots from `slot` on.
 struct Tile {
     int32_t mat, i, j, count;
+    int32_t first, last, slot, unused;
 };
 
 struct Gap {
@@ -89,8 +93,26 @@ struct VectorArgs {
 // What is orthogonalised, from the update and the momentum that holds it already.
 __device__ __forceinline__ float direction(const VectorArgs& a, float u, float v) { return a.nesterov ? u + a.mu * v : v; }
 
+// Four neighbours, of which the matrix has n.
+template <int DT>
+__device__ __forceinline__ void load4(const typename Elem<DT>::T* p, int n, float (&f)[4]) {
+    if (n >= 4) {
+        if constexpr (DT == GMC_F32) {
+            Vec<DT, 4>::load(p).unpack(f);
+        } else {
+            float a[2], b[2];
+            Vec<DT, 2>::load(p).unpack(a);
+            Vec<DT, 2>::load(p + 2).unpack(b);
+            f[0] = a[0], f[1] = a[1], f[2] = b[0], f[3] = b[1];
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f[e] = e < n ? Elem<DT>::up(p[e]) : 0.0f;
+    }
+}
+
 // Sums of squares in 64 bits (no 32-bit value's square leaves their range), and the
-// momentum's update on the way.  A tile of the launch is `count` pieces of a matrix.
+// momentum's update on the way.
 template <int DT, bool kStep>
 __global__ __launch_bounds__(256) void matrix_norm(VectorArgs a) {
     typedef typename Elem<DT>::T T;
@@ -103,56 +125,41 @@ __global__ __launch_bounds__(256) void matrix_norm(VectorArgs a) {
     double sum = 0.0;
     for (int k = 0; k < t.count; ++k) {
         const int piece = t.i + k, pr = piece / wide, pc = piece - pr * wide;
+        const int c = pc * kSide + c0, n = m.cols - c;   // columns from here on
+        // all of a piece's loads before the first is used
+        float u[4][4], w[4][4];
+        const auto place = [&](int q) { return ((int64_t)pr * kSide + r0 + 16 * q) * m.pitch + c; };
+        const auto have = [&](int q) { return (int64_t)pr * kSide + r0 + 16 * q < m.rows ? n : 0; };
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int64_t r = (int64_t)pr * kSide + r0 + 16 * q;
-            const int c = pc * kSide + c0;
-            if (r >= m.rows || c >= m.cols) continue;
-            const int64_t at = r * m.pitch + c;
-            const int n = m.cols - c < 4 ? m.cols - c : 4;
-            float u[4] = {};
-            if (n == 4) {
-                Vec<DT, DT == GMC_F32 ? 4 : 2> v0, v1;
-                if constexpr (DT == GMC_F32) {
-                    v0 = Vec<DT, 4>::load(x + at);
-                    v0.unpack(u);
-                } else {
-                    v0 = Vec<DT, 2>::load(x + at);
-                    v1 = Vec<DT, 2>::load(x + at + 2);
-                    float p[2];
-                    v0.unpack(p);
-                    u[0] = p[0], u[1] = p[1];
-                    v1.unpack(p);
-                    u[2] = p[0], u[3] = p[1];
-                }
-            } else {
-                for (int e = 0; e < n; ++e) u[e] = Elem<DT>::up(x[at + e]);
-            }
-            if constexpr (kStep) {
-                if (a.momentum) {
-                    float* v = a.momentum + m.offset + at;
-                    float w[4] = {};
-                    if (n == 4) Vec<GMC_F32, 4>::load(v).unpack(w);
-                    else
-                        for (int e = 0; e < n; ++e) w[e] = v[e];
+        for (int q = 0; q < 4; ++q) load4<DT>(x + place(q), have(q), u[q]);
+        if constexpr (kStep) {
+            if (a.momentum) {
+                float* v = a.momentum + m.offset;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) load4<GMC_F32>(v + place(q), have(q), w[q]);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        w[e] = a.mu * w[e] + u[e];
-                        u[e] = direction(a, u[e], w[e]);
+                        w[q][e] = a.mu * w[q][e] + u[q][e];
+                        u[q][e] = direction(a, u[q][e], w[q][e]);
                     }
-                    if (n == 4) {
+                    if (have(q) >= 4) {
                         Vec<GMC_F32, 4> o;
-                        o.pack(w);
-                        o.store(v);
+                        o.pack(w[q]);
+                        o.store(v + place(q));
                     } else {
-                        for (int e = 0; e < n; ++e) v[e] = w[e];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (e < have(q)) v[place(q) + e] = w[q][e];
                     }
                 }
             }
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (e < n) sum += (double)u[e] * (double)u[e];
         }
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum = fma((double)u[q][e], (double)u[q][e], sum);
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
@@ -167,6 +174,16 @@ __device__ __forceinline__ void split(float v, _Float16& hi, _Float16& lo) {
     lo = (_Float16)(v - (float)hi);
 }
 
+// What a wavefront's lanes have written to shared memory before is there for what they read after.
+__device__ __forceinline__ void wave_order() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// theta of the steps (see above); NaN stays.
+__device__ __forceinline__ float first_theta(double norm, double eps) { return norm == 0.0 ? 1.0f : (float)(norm / (norm + eps)); }
+__device__ __forceinline__ float next_theta(float theta, float growth) { return fminf(theta * growth, 1.0f) + 0.0f * theta; }
+
 // The matrix over its norm, in halves, along both of its axes.
 template <int DT, bool kStep>
 __global__ __launch_bounds__(256) void matrix_pack(VectorArgs a) {
@@ -176,7 +193,8 @@ __global__ __launch_bounds__(256) void matrix_pack(VectorArgs a) {
     const Tile t = a.tiles[blockIdx.x];
     const Mat m = a.mats[t.mat];
     const T* x = static_cast<const T*>(a.x) + m.offset;
-    double sum = (int)threadIdx.x < m.parts ? a.part[m.part + threadIdx.x] : 0.0;
+    double sum = 0.0;
+    for (int k = threadIdx.x; k < m.parts; k += 256) sum += a.part[m.part + k];
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = sum;
@@ -201,10 +219,10 @@ __global__ __launch_bounds__(256) void matrix_pack(VectorArgs a) {
     const double norm = sqrt(lds[0] + lds[1] + lds[2] + lds[3]);
     const double inv = norm == 0.0 ? 0.0 : (double)kScaleX / norm;
     if (t.i == 0 && t.j == 0 && threadIdx.x == 0) {
-        float v = norm == 0.0 ? 1.0f : (float)(norm / (norm + a.eps));
+        float v = first_theta(norm, a.eps);
         float* theta = a.theta + t.mat * (kMostSteps + 1);
         theta[0] = v;
-        for (int k = 0; k < a.steps; ++k) theta[k + 1] = v = fminf(v * a.growth[k], 1.0f) + 0.0f * v;   // NaN stays
+        for (int k = 0; k < a.steps; ++k) theta[k + 1] = v = next_theta(v, a.growth[k]);
     }
     const int64_t kn = 2 * (int64_t)m.nb, km = 2 * (int64_t)m.mb;
 #pragma unroll
@@ -253,140 +271,53 @@ struct ProductArgs {
     _Float16 *Xo, *XTo, *Go, *Bo;    // and writes
     const float* theta;  // this step's of the first matrix
     float a, b, c;
-    void* out;        // kLast, kLastStep
-    const float* w;   // kLastStep
+    float* slots;        // parts of tiles' sums
+    void* out;           // kLast, kLastStep
+    const float* w;      // kLastStep
     float alpha, keep;
 };
 
-// Waits until all but the wavefront's last kLoads loads to shared memory have arrived and its
-// reads of shared memory are done, and then for the workgroup's other wavefronts.
-template <int kLoads>
-__device__ __forceinline__ void wait_stage() {
-    static_assert(kLoads < 64, "the counter has 6 bits");
-    __builtin_amdgcn_s_waitcnt((kLoads & 15) | 7 << 4 | 0 << 8 | (kLoads >> 4) << 14);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-}
+// The rows and columns of a mode's tiles, in blocks; i and j where a matrix on its side is written last.
+template <int kMode>
+struct Sides {
+    static constexpr bool kEnd = kMode == kLast || kMode == kLastStep, kEven = kMode == kGram || kMode == kPoly;
+    bool flip;
+    int i, j, rows, cols;
+    __device__ __forceinline__ Sides(const Mat& m, const Tile& t) {
+        flip = kEnd && m.flip;
+        i = flip ? t.j : t.i;
+        j = flip ? t.i : t.j;
+        rows = !kEven && flip ? m.nb : m.mb;
+        cols = kEven || flip ? m.mb : m.nb;
+    }
+};
 
-// One tile of D = P Q^T, both along their contraction, by four wavefronts of kWide x
-// kWide blocks each, and what the mode makes of it:
-//   kGram   P = Q = X            G = D
-//   kPoly   P = Q = G            B = b G + c D
-//   kApply  P = B, Q = X^T       X <- a X + D, along both axes
-//   kLast   the same, or P = X^T and Q = B for a matrix on its side, into the vector
-// G and B are symmetric: tiles with j <= i, written to both places.
+// What the mode makes of a wavefront's blocks of D, from (ib, jb) on.  turn: 32 x 33 words of shared memory
+// of the wavefront's own.  Of a block lane l has column l % 32, rows 8 g + 4 (l / 32) + e in
+// entry 4 g + e.
 template <int kWide, int kMode, int DT>
-__global__ __launch_bounds__(256, 2) void matrix_product(ProductArgs a) {
-    constexpr int kBlocks = 2 * kWide;                 // of 32 rows, on each side of the tile
-    constexpr int kDeep = kWide == 2 ? 1 : 2;          // 16 columns, of a stage
-    constexpr int kChunks = 2 * kBlocks * kDeep * 2;   // kilobytes of a stage: sides, blocks, columns, halves
-    __shared__ _Float16 stage0[kChunks * 512], stage1[kChunks * 512], stage2[kChunks * 512], stage3[kChunks * 512];
-    const Tile t = a.tiles[blockIdx.x];
-    const Mat m = a.mats[t.mat];
-    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
-    const bool last = kMode == kLast || kMode == kLastStep;
-    const bool flip = last && m.flip;
-    const int ti = flip ? t.j : t.i, tj = flip ? t.i : t.j;
-    const _Float16* P = (kMode == kGram ? a.X + m.x * 1024 : kMode == kPoly ? a.G + m.g * 1024
-                         : flip ? a.XT + m.x * 1024 : a.B + m.g * 1024);
-    const _Float16* Q = (kMode == kGram ? a.X + m.x * 1024 : kMode == kPoly ? a.G + m.g * 1024
-                         : flip ? a.B + m.g * 1024 : a.XT + m.x * 1024);
-    const int pb = kMode == kGram || kMode == kPoly ? m.mb : flip ? m.nb : m.mb;   // blocks of P's and Q's rows
-    const int qb = kMode == kGram || kMode == kPoly ? m.mb : flip ? m.mb : m.nb;
-    const int deep = 2 * (kMode == kGram ? m.nb : m.mb);   // 16 columns
-    const int64_t row = (int64_t)deep * 1024;              // halves of a row of blocks
+__device__ __forceinline__ void finish_blocks(const ProductArgs& a, const Mat& m, const Tile& t, const Sides<kMode>& sides, int ib0,
+                                              int jb0, const f32x16 (&acc)[kWide][kWide], float* turn) {
+    const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+    const bool flip = sides.flip;
     const float theta = kMode == kGram ? 1.0f : a.theta[t.mat * (kMostSteps + 1)];
     const float ratio = kMode == kApply ? theta / a.theta[t.mat * (kMostSteps + 1) + 1] : 1.0f;
-
-    // chunk c of a stage: side, block, 16 columns, half; a wavefront takes every fourth.
-    // Blocks beyond the matrix are read as its last one and not written.
-    const _Float16* from[kChunks / 4];
-#pragma unroll
-    for (int k = 0; k < kChunks / 4; ++k) {
-        const int c = k * 4 + wave, side = c / (kChunks / 2), b = c / (2 * kDeep) % kBlocks;
-        int rb = (side ? tj : ti) * kBlocks + b;
-        const int most = (side ? qb : pb) - 1;
-        rb = rb < most ? rb : most;
-        from[k] = (side ? Q : P) + rb * row + (c % (2 * kDeep)) * 512 + lane * 8;
-    }
-    f32x16 acc[kWide][kWide];
-#pragma unroll
-    for (int i = 0; i < kWide; ++i)
-#pragma unroll
-        for (int j = 0; j < kWide; ++j)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
-    const int wi = (wave >> 1) * kWide, wj = (wave & 1) * kWide;   // the wavefront's first blocks
-    const int stages = deep / kDeep;
-    const auto fetch = [&](int s, _Float16* to) {
-        s = s < stages ? s : stages - 1;   // the count of loads under way stays what the waits take it for
-#pragma unroll
-        for (int k = 0; k < kChunks / 4; ++k)
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from[k] + (int64_t)s * (kDeep * 1024)),
-                                             (__attribute__((address_space(3))) void*)(to + (k * 4 + wave) * 512), 16, 0, 0);
-    };
-    // Stage s is in shared memory and stage s - 1 has been read by all, whose place the loads of
-    // s + 3 take; those of s + 1 and s + 2 stay under way.
-    const auto step = [&](int s, const _Float16* here, _Float16* next) {
-        wait_stage<2 * (kChunks / 4)>();
-        const f16x8* at = reinterpret_cast<const f16x8*>(here) + lane;
-        f16x8 p[kDeep][kWide][2], q[kDeep][kWide][2];
-#pragma unroll
-        for (int k = 0; k < kDeep; ++k)
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int i = 0; i < kWide; ++i) {
-                    p[k][i][h] = at[(((wi + i) * kDeep + k) * 2 + h) * 64];
-                    q[k][i][h] = at[(((kBlocks + wj + i) * kDeep + k) * 2 + h) * 64];
-                }
-        fetch(s + 3, next);
-#pragma unroll
-        for (int k = 0; k < kDeep; ++k)
-#pragma unroll
-            for (int part = 0; part < 3; ++part)
-#pragma unroll
-                for (int i = 0; i < kWide; ++i)
-#pragma unroll
-                    for (int j = 0; j < kWide; ++j)
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[k][i][part == 2], q[k][j][part == 1], acc[i][j], 0, 0, 0);
-    };
-    fetch(0, stage0);
-    fetch(1, stage1);
-    fetch(2, stage2);
-    int s = 0;
-    for (; s + 4 <= stages; s += 4) {
-        step(s, stage0, stage3);
-        step(s + 1, stage1, stage0);
-        step(s + 2, stage2, stage1);
-        step(s + 3, stage3, stage2);
-    }
-    if (s < stages) step(s, stage0, stage3);
-    if (s + 1 < stages) step(s + 1, stage1, stage0);
-    if (s + 2 < stages) step(s + 2, stage2, stage1);
-    __syncthreads();   // no load is under way and shared memory is free
-
-    // Of a block of D lane l has column l % 32, rows 8 g + 4 (l / 32) + e in entry 4 g + e.
-    static_assert(32 * 33 * 4 <= kChunks * 1024, "a wavefront's block fits a stage");
-    float* turn = reinterpret_cast<float*>(wave == 0 ? stage0 : wave == 1 ? stage1 : wave == 2 ? stage2 : stage3);
-    const int col = lane & 31, half = lane >> 5;
+    // d <- u (hi + lo) + v d
+    const float u = kMode == kPoly ? a.b * (theta * theta) * (kScaleB / kScaleX) : a.a * ratio;
+    const float v = kMode == kPoly ? a.c * (theta * theta) * (theta * theta) * (kScaleB / kScaleX / kScaleX) : ratio / kScaleB;
 #pragma unroll
     for (int i = 0; i < kWide; ++i)
 #pragma unroll
         for (int j = 0; j < kWide; ++j) {
-            const int ib = ti * kBlocks + wi + i, jb = tj * kBlocks + wj + j;
-            if (ib >= pb || jb >= qb) continue;
+            const int ib = ib0 + i, jb = jb0 + j;
+            if (ib >= sides.rows || jb >= sides.cols) continue;
             f32x16 d = acc[i][j];
             // entry (i, j) where its row is j: block (jb, 2 ib + g / 2), lane col + 32 (g % 2), halves 4 half + e
-            const int64_t place = ((int64_t)jb * 2 * pb + 2 * ib) * 1024 + col * 8 + 4 * half;
+            const int64_t place = ((int64_t)jb * 2 * sides.rows + 2 * ib) * 1024 + col * 8 + 4 * half;
             if constexpr (kMode == kGram) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) d[e] *= 1.0f / kScaleX;
             } else {
-                // d <- u (hi + lo) + v d
-                const float u = kMode == kPoly ? a.b * (theta * theta) * (kScaleB / kScaleX) : a.a * ratio;
-                const float v = kMode == kPoly ? a.c * (theta * theta) * (theta * theta) * (kScaleB / kScaleX / kScaleX) : ratio / kScaleB;
                 const _Float16* add = (kMode == kPoly ? a.G + m.g * 1024 : flip ? a.X + m.x * 1024 : a.XT + m.x * 1024) + place;
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
@@ -396,17 +327,27 @@ __global__ __launch_bounds__(256, 2) void matrix_product(ProductArgs a) {
                     for (int e = 0; e < 4; ++e) d[4 * g + e] = u * ((float)hi[e] + (float)lo[e]) + v * d[4 * g + e];
                 }
             }
-            if constexpr (last) {
+            if constexpr (kMode == kLast || kMode == kLastStep) {
                 typedef typename Elem<DT>::T T;
                 const float factor = a.alpha * m.scale * theta * (1.0f / kScaleX);
-                const int c = jb * 32 + col;
+                const int r0 = ib * 32 + 4 * half, c = jb * 32 + col;
+                const int64_t at = m.offset + (int64_t)r0 * m.pitch + c;
+                const bool whole = (ib + 1) * 32 <= m.rows && (jb + 1) * 32 <= m.cols;   // the same in all lanes
+                const auto row = [](int e) { return 8 * (e >> 2) + (e & 3); };
+                if constexpr (kMode == kLastStep) {
+                    float w[16];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int r = ib * 32 + 8 * (e >> 2) + 4 * half + (e & 3);
-                    if (r >= m.rows || c >= m.cols) continue;
-                    const int64_t at = m.offset + (int64_t)r * m.pitch + c;
-                    if constexpr (kMode == kLastStep) static_cast<float*>(a.out)[at] = a.keep * a.w[at] + factor * d[e];
-                    else static_cast<T*>(a.out)[at] = Elem<DT>::down(factor * d[e]);
+                    for (int e = 0; e < 16; ++e)
+                        w[e] = whole || (r0 + row(e) < m.rows && c < m.cols) ? a.w[at + row(e) * m.pitch] : 0.0f;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (whole || (r0 + row(e) < m.rows && c < m.cols))
+                            static_cast<float*>(a.out)[at + row(e) * m.pitch] = a.keep * w[e] + factor * d[e];
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (whole || (r0 + row(e) < m.rows && c < m.cols))
+                            static_cast<T*>(a.out)[at + row(e) * m.pitch] = Elem<DT>::down(factor * d[e]);
                 }
                 continue;
             }
@@ -424,13 +365,13 @@ __global__ __launch_bounds__(256, 2) void matrix_product(ProductArgs a) {
                 *reinterpret_cast<f16x4*>(o + (g >> 1) * 1024 + (g & 1) * 256) = hi;
                 *reinterpret_cast<f16x4*>(o + (g >> 1) * 1024 + (g & 1) * 256 + 512) = lo;
             }
-            if (kMode != kApply && ti == tj) continue;
-            // and where its row is i, through shared memory of the wavefront's own
+            if (kMode != kApply && t.i == t.j) continue;
+            // and where its row is i, by way of shared memory
 #pragma unroll
             for (int e = 0; e < 16; ++e) turn[(8 * (e >> 2) + 4 * half + (e & 3)) * 33 + col] = d[e];
-            __builtin_amdgcn_wave_barrier();
+            wave_order();
             o = (kMode == kGram ? a.Go + m.g * 1024 : kMode == kPoly ? a.Bo + m.g * 1024 : a.Xo + m.x * 1024) +
-                ((int64_t)ib * 2 * qb + 2 * jb) * 1024 + lane * 8;
+                ((int64_t)ib * 2 * sides.cols + 2 * jb) * 1024 + lane * 8;
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 f16x8 hi, lo;
@@ -444,8 +385,397 @@ __global__ __launch_bounds__(256, 2) void matrix_product(ProductArgs a) {
                 *reinterpret_cast<f16x8*>(o + k * 1024) = hi;
                 *reinterpret_cast<f16x8*>(o + k * 1024 + 512) = lo;
             }
-            __builtin_amdgcn_wave_barrier();
+            wave_order();
         }
+}
+
+// Waits until all but the wavefront's last kLoads loads to shared memory have arrived and its
+// reads of shared memory are done, and then for the workgroup's other wavefronts.
+template <int kLoads>
+__device__ __forceinline__ void wait_stage() {
+    static_assert(kLoads < 64, "the counter has 6 bits");
+    __builtin_amdgcn_s_waitcnt((kLoads & 15) | 7 << 4 | 0 << 8 | (kLoads >> 4) << 14);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
+// The first of a lane's vectors of a slot.
+template <int kWide>
+__device__ __forceinline__ int64_t slot_of(int slot, int wave, int lane) {
+    return ((int64_t)slot * 4 + wave) * (kWide * kWide * 4 * 64) + lane;
+}
+
+// One tile of D = P Q^T, both along their contraction, by four wavefronts of kWide x
+// kWide blocks each, and what the mode makes of it:
+//   kGram   P = Q = X            G = D
+//   kPoly   P = Q = G            B = b G + c D
+//   kApply  P = B, Q = X^T       X <- a X + D, along both axes
+//   kLast   the same, or P = X^T and Q = B for a matrix on its side, into the vector
+// or, of a tile whose contraction is cut, its part of the sum for matrix_join.  G and B are symmetric: tiles with j <= i, written to both places.
+template <int kWide, int kMode, int DT>
+__global__ __launch_bounds__(256, 2) void matrix_product(ProductArgs a) {
+    constexpr int kBlocks = 2 * kWide;                 // of 32 rows, on each side of the tile
+    constexpr int kDeep = kWide == 2 ? 1 : 2;          // 16 columns, of a stage
+    constexpr int kChunks = 2 * kBlocks * kDeep * 2;   // kilobytes of a stage: sides, blocks, columns, halves
+    __shared__ _Float16 stage0[kChunks * 512], stage1[kChunks * 512], stage2[kChunks * 512], stage3[kChunks * 512];
+    const Tile t = a.tiles[blockIdx.x];
+    if (t.mat < 0) return;   // fills an XCD's list
+    const Mat m = a.mats[t.mat];
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
+    const Sides<kMode> sides(m, t);
+    const _Float16* P = (kMode == kGram ? a.X + m.x * 1024 : kMode == kPoly ? a.G + m.g * 1024
+                         : sides.flip ? a.XT + m.x * 1024 : a.B + m.g * 1024);
+    const _Float16* Q = (kMode == kGram ? a.X + m.x * 1024 : kMode == kPoly ? a.G + m.g * 1024
+                         : sides.flip ? a.B + m.g * 1024 : a.XT + m.x * 1024);
+    const int64_t row = (int64_t)(kMode == kGram ? m.nb : m.mb) * 2048;   // halves of a row of blocks
+
+    // chunk c of a stage: side, block, 16 columns, half; a wavefront takes every fourth.
+    // Blocks beyond the matrix are read as its last one and not written.
+    const _Float16* from[kChunks / 4];
+#pragma unroll
+    for (int k = 0; k < kChunks / 4; ++k) {
+        const int c = k * 4 + wave, side = c / (kChunks / 2), b = c / (2 * kDeep) % kBlocks;
+        int rb = (side ? sides.j : sides.i) * kBlocks + b;
+        const int most = (side ? sides.cols : sides.rows) - 1;
+        rb = rb < most ? rb : most;
+        from[k] = (side ? Q : P) + rb * row + t.first * 2048 + (c % (2 * kDeep)) * 512 + lane * 8;
+    }
+    f32x16 acc[kWide][kWide];
+#pragma unroll
+    for (int i = 0; i < kWide; ++i)
+#pragma unroll
+        for (int j = 0; j < kWide; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+    const int wi = (wave >> 1) * kWide, wj = (wave & 1) * kWide;   // the wavefront's first blocks
+    const int stages = (t.last - t.first) * 2 / kDeep;
+    const auto fetch = [&](int s, int k, _Float16* to) {
+        s = s < stages ? s : stages - 1;   // the count of loads under way stays what the waits take it for
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from[k] + (int64_t)s * (kDeep * 1024)),
+                                         (__attribute__((address_space(3))) void*)(to + (k * 4 + wave) * 512), 16, 0, 0);
+    };
+    // A wavefront's operands of a stage: of each 16 columns kWide blocks of P in their halves, then of Q.
+    constexpr int kReads = kDeep * 4 * kWide, kProducts = kDeep * 3 * kWide * kWide, kLoads = kChunks / 4;
+    const auto read = [&](f16x8 (&o)[kReads], int r, const _Float16* here) {
+        const int k = r / (4 * kWide), q = r / (2 * kWide) % 2, i = r / 2 % kWide, h = r % 2;
+        o[r] = reinterpret_cast<const f16x8*>(here)[(((q ? kBlocks + wj + i : wi + i) * kDeep + k) * 2 + h) * 64 + lane];
+    };
+    // Stage s + 1 is in shared memory and stage s has been read by all, whose place the loads of
+    // stage s + 4 take; those of s + 2 and s + 3 stay under way.  The operands of s + 1 are read and
+    // the loads issued between the products of s, one after each: in front of them they
+    // hold the products up (2048 x 2048, one workgroup a CU: a stage takes 1.9 times as long).
+    const auto step = [&](int s, const f16x8 (&now)[kReads], f16x8 (&then)[kReads], const _Float16* after, _Float16* here) {
+        wait_stage<2 * kLoads>();
+#pragma unroll
+        for (int n = 0; n < kProducts; ++n) {
+            const int k = n / (3 * kWide * kWide), part = n / (kWide * kWide) % 3, i = n / kWide % kWide, j = n % kWide;
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(now[k * 4 * kWide + 2 * i + (part == 2)],
+                                                               now[k * 4 * kWide + 2 * kWide + 2 * j + (part == 1)], acc[i][j], 0, 0, 0);
+#pragma unroll
+            for (int r = n * (kReads + kLoads) / kProducts; r < (n + 1) * (kReads + kLoads) / kProducts; ++r) {
+                if (r < kReads) read(then, r, after);
+                else fetch(s + 4, r - kReads, here);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    f16x8 one[kReads], two[kReads];
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) fetch(0, k, stage0);
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) fetch(1, k, stage1);
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) fetch(2, k, stage2);
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) fetch(3, k, stage3);
+    wait_stage<3 * kLoads>();
+#pragma unroll
+    for (int r = 0; r < kReads; ++r) read(one, r, stage0);
+    int s = 0;
+    for (; s + 4 <= stages; s += 4) {
+        step(s, one, two, stage1, stage0);
+        step(s + 1, two, one, stage2, stage1);
+        step(s + 2, one, two, stage3, stage2);
+        step(s + 3, two, one, stage0, stage3);
+    }
+    if (s < stages) step(s, one, two, stage1, stage0);
+    if (s + 1 < stages) step(s + 1, two, one, stage2, stage1);
+    if (s + 2 < stages) step(s + 2, one, two, stage3, stage2);
+    __syncthreads();   // no load is under way and shared memory is free
+
+    static_assert(32 * 33 * 4 <= kChunks * 1024, "a wavefront's block fits a stage");
+    float* turn = reinterpret_cast<float*>(wave == 0 ? stage0 : wave == 1 ? stage1 : wave == 2 ? stage2 : stage3);
+    if (t.slot >= 0) {
+        f32x4* o = reinterpret_cast<f32x4*>(a.slots) + slot_of<kWide>(t.slot, wave, lane);
+#pragma unroll
+        for (int i = 0; i < kWide; ++i)
+#pragma unroll
+            for (int j = 0; j < kWide; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    f32x4 v;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * g + e];
+                    o[((i * kWide + j) * 4 + g) * 64] = v;
+                }
+        return;
+    }
+    finish_blocks<kWide, kMode, DT>(a, m, t, sides, sides.i * kBlocks + wi, sides.j * kBlocks + wj, acc, turn);
+}
+
+// The tiles whose contraction was cut: their parts added in order, a wavefront a block.
+template <int kWide, int kMode>
+__global__ __launch_bounds__(256) void matrix_join(ProductArgs a) {
+    __shared__ float turn[4][32 * 33];
+    const Tile t = a.tiles[blockIdx.x / (kWide * kWide)];
+    const Mat m = a.mats[t.mat];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int block = blockIdx.x % (kWide * kWide), i = block / kWide, j = block % kWide;   // of each wavefront's
+    f32x16 acc[1][1];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[0][0][e] = 0.0f;
+    constexpr int64_t kSlot = kWide * kWide * 4 * 4 * 64;
+    const f32x4* p = reinterpret_cast<const f32x4*>(a.slots) + slot_of<kWide>(t.slot, wave, lane) + block * 4 * 64;
+#pragma unroll 4
+    for (int k = 0; k < t.count; ++k) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const f32x4 v = p[k * kSlot + g * 64];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[0][0][4 * g + e] += v[e];
+        }
+    }
+    const Sides<kMode> sides(m, t);
+    finish_blocks<1, kMode, GMC_F32>(a, m, t, sides, (sides.i * 2 + (wave >> 1)) * kWide + i, (sides.j * 2 + (wave & 1)) * kWide + j, acc,
+                                     turn[wave]);
+}
+
+// -- small matrices -----------------------------------------------------------------
+
+struct SmallArgs {
+    VectorArgs in;
+    float c[kMostSteps][3];
+    void* out;
+    const float* w;
+    float alpha, keep;
+};
+
+constexpr int kSmallThreads = 512, kSmallBlocks = 39;   // 4 KB each of 160 KB: X, X^T and G of 32 x 32 blocks
+
+// Matrices of which X, X^T and G fit the shared memory of one CU: all steps in one launch, a workgroup a
+// matrix, a wavefront every eighth block (64 x 147: 13 us, by the launches of the others 62).  The polynomial
+// takes G's place, and X its own, once all have read them.
+template <int DT, bool kStep>
+__global__ __launch_bounds__(kSmallThreads) void matrix_small(SmallArgs a) {
+    typedef typename Elem<DT>::T T;
+    constexpr int kWaves = kSmallThreads / 64, kOwn = 3;   // blocks a wavefront has of up to 20
+    __shared__ f16x8 lds[kSmallBlocks * 256];
+    __shared__ double sums[kWaves];
+    const Mat m = a.in.mats[blockIdx.x];
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+    const int mb = m.mb, nb = m.nb;
+    // a block of 32 rows and 32 columns is four times 64 vectors: 16 columns' hi and lo, twice
+    f16x8 *X = lds, *XT = X + mb * nb * 256, *G = XT + mb * nb * 256;
+    const T* x = static_cast<const T*>(a.in.x) + m.offset;
+    float* past = kStep && a.in.momentum ? a.in.momentum + m.offset : nullptr;
+    const auto place = [&](int i, int j) { return m.flip ? (int64_t)j * m.pitch + i : (int64_t)i * m.pitch + j; };
+    // the sum of squares, and the momentum on the way
+    double sum = 0.0;
+    const int units = m.rows * m.cols;
+    for (int k0 = threadIdx.x; k0 < units; k0 += 8 * kSmallThreads) {
+        // all loads before the first is used: past the end the last component, which does not count
+        int64_t at[8];
+        float u[8], v[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const int k = k0 + q * kSmallThreads < units ? k0 + q * kSmallThreads : units - 1, r = k / m.cols;
+            at[q] = (int64_t)r * m.pitch + (k - r * m.cols);
+            u[q] = Elem<DT>::up(x[at[q]]);
+        }
+        if (past) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v[q] = past[at[q]];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                v[q] = a.in.mu * v[q] + u[q];
+                u[q] = direction(a.in, u[q], v[q]);
+                if (k0 + q * kSmallThreads < units) past[at[q]] = v[q];
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            if (k0 + q * kSmallThreads < units) sum = fma((double)u[q], (double)u[q], sum);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+    if (lane == 0) sums[wave] = sum;
+    __syncthreads();
+    sum = 0.0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) sum += sums[w];
+    const double norm = sqrt(sum), inv = norm == 0.0 ? 0.0 : (double)kScaleX / norm;
+    float theta = first_theta(norm, a.in.eps);
+    // eight neighbours at a time, of X's rows and then of its columns
+    for (int k = threadIdx.x; k < 2 * mb * nb * 128; k += kSmallThreads) {
+        const bool along = k < mb * nb * 128;
+        const int q = along ? k : k - mb * nb * 128, l = q & 63, deep = along ? 2 * nb : 2 * mb;
+        const int b = (q >> 6) / deep, c = (q >> 6) - b * deep, row = b * 32 + (l & 31), k0 = c * 16 + (l >> 5) * 8;
+        f16x8 hi, lo;
+        float u[8], v[8];
+        const auto at = [&](int e) {
+            const int i = along ? row : k0 + e, j = along ? k0 + e : row;
+            return place(i < m.m ? i : m.m - 1, j < m.n ? j : m.n - 1);
+        };
+#pragma unroll
+        for (int e = 0; e < 8; ++e) u[e] = Elem<DT>::up(x[at(e)]);
+        if (past) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = past[at(e)];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) u[e] = direction(a.in, u[e], v[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int i = along ? row : k0 + e, j = along ? k0 + e : row;
+            _Float16 h, s;
+            split(i < m.m && j < m.n ? (float)((double)u[e] * inv) : 0.0f, h, s);
+            hi[e] = h;
+            lo[e] = s;
+        }
+        f16x8* o = (along ? X : XT) + (b * deep + c) * 128 + l;
+        o[0] = hi;
+        o[64] = lo;
+    }
+    __syncthreads();
+    // A block of P Q^T, both `deep` times 16 columns; three sums, so that no product waits for another
+    const auto product = [&](const f16x8* P, const f16x8* Q, int deep) {
+        f32x16 d0, d1, d2;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) d0[e] = d1[e] = d2[e] = 0.0f;
+#pragma unroll 2
+        for (int k = 0; k < deep; ++k) {
+            const f16x8 ph = P[k * 128 + lane], pl = P[k * 128 + 64 + lane], qh = Q[k * 128 + lane], ql = Q[k * 128 + 64 + lane];
+            d0 = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, qh, d0, 0, 0, 0);
+            d1 = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, ql, d1, 0, 0, 0);
+            d2 = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl, qh, d2, 0, 0, 0);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) d0[e] = d0[e] + (d1[e] + d2[e]);
+        return d0;
+    };
+    // Entries 4 g to 4 g + 3 of block (ib, jb) where their row is j
+    const auto half4 = [&](f16x8* base, int ib, int jb, int deep, int g, int h) {
+        return reinterpret_cast<f16x4*>(base + (jb * deep + 2 * ib + (g >> 1)) * 128 + h * 64 + col + 32 * (g & 1)) + half;
+    };
+    const auto value4 = [&](f16x8* base, int ib, int jb, int deep, int g) {
+        const f16x4 hi = *half4(base, ib, jb, deep, g, 0), lo = *half4(base, ib, jb, deep, g, 1);
+        f32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = (float)hi[e] + (float)lo[e];
+        return v;
+    };
+    const auto keep4 = [&](f16x8* base, int ib, int jb, int deep, int g, const f32x16& d) {
+        f16x4 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            _Float16 h, l;
+            split(d[4 * g + e], h, l);
+            hi[e] = h;
+            lo[e] = l;
+        }
+        *half4(base, ib, jb, deep, g, 0) = hi;
+        *half4(base, ib, jb, deep, g, 1) = lo;
+    };
+    for (int step = 0; step < a.in.steps; ++step) {
+        const float ca = a.c[step][0], cb = a.c[step][1], cc = a.c[step][2], theta2 = theta * theta;
+        f32x16 d[kOwn];
+        for (int b = wave; b < mb * mb; b += kWaves) {
+            const int ib = b / mb, jb = b - ib * mb;
+            f32x16 v = product(X + ib * nb * 256, X + jb * nb * 256, 2 * nb);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) v[e] *= 1.0f / kScaleX;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) keep4(G, ib, jb, 2 * mb, g, v);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int b = wave + k * kWaves, ib = b / mb, jb = b - ib * mb;
+            if (b >= mb * mb) break;
+            d[k] = product(G + ib * mb * 256, G + jb * mb * 256, 2 * mb);
+            const float u = cb * theta2 * (kScaleB / kScaleX), v = cc * theta2 * theta2 * (kScaleB / kScaleX / kScaleX);
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const f32x4 add = value4(G, ib, jb, 2 * mb, g);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) d[k][4 * g + e] = u * add[e] + v * d[k][4 * g + e];
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int b = wave + k * kWaves, ib = b / mb, jb = b - ib * mb;
+            if (b >= mb * mb) break;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) keep4(G, ib, jb, 2 * mb, g, d[k]);
+        }
+        __syncthreads();
+        const bool last = step + 1 == a.in.steps, turned = last && m.flip;
+        const float next = last ? 0.0f : next_theta(theta, a.in.growth[step]);
+        const float u = last ? ca : ca * (theta / next), v = last ? 1.0f / kScaleB : (theta / next) / kScaleB;
+        const int cols = turned ? mb : nb;   // of D, which is X^T's product where a matrix on its side is written
+#pragma unroll
+        for (int k = 0; k < kOwn; ++k) {
+            const int b = wave + k * kWaves, ib = b / cols, jb = b - ib * cols;
+            if (b >= mb * nb) break;
+            d[k] = turned ? product(XT + ib * mb * 256, G + jb * mb * 256, 2 * mb) : product(G + ib * mb * 256, XT + jb * mb * 256, 2 * mb);
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const f32x4 add = turned ? value4(X, ib, jb, 2 * nb, g) : value4(XT, ib, jb, 2 * mb, g);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) d[k][4 * g + e] = u * add[e] + v * d[k][4 * g + e];
+            }
+        }
+        if (last) {
+            const float factor = a.alpha * m.scale * theta * (1.0f / kScaleX);
+#pragma unroll
+            for (int k = 0; k < kOwn; ++k) {
+                const int b = wave + k * kWaves, ib = b / cols, jb = b - ib * cols;
+                if (b >= mb * nb) break;
+                const int c = jb * 32 + col;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int r = ib * 32 + 8 * (e >> 2) + 4 * half + (e & 3);
+                    if (r >= m.rows || c >= m.cols) continue;
+                    const int64_t at = m.offset + (int64_t)r * m.pitch + c;
+                    if constexpr (kStep) static_cast<float*>(a.out)[at] = a.keep * a.w[at] + factor * d[k][e];
+                    else static_cast<T*>(a.out)[at] = Elem<DT>::down(factor * d[k][e]);
+                }
+            }
+            return;
+        }
+        theta = next;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kOwn; ++k) {
+            const int b = wave + k * kWaves, ib = b / nb, jb = b - ib * nb;
+            if (b >= mb * nb) break;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) keep4(XT, ib, jb, 2 * mb, g, d[k]);
+            // where its row is i: block (ib, 2 jb + col / 16), lane i % 32 + 32 (col / 8 % 2), half col % 8
+            _Float16* o = reinterpret_cast<_Float16*>(X + (ib * 2 * nb + 2 * jb + (col >> 4)) * 128 + 32 * (col >> 3 & 1)) + (col & 7);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                _Float16 h, l;
+                split(d[k][e], h, l);
+                const int row = 8 * (e >> 2) + 4 * half + (e & 3);
+                o[row * 8] = h;
+                o[row * 8 + 512] = l;
+            }
+        }
+        __syncthreads();
+    }
 }
 
 }  // namespace
@@ -461,11 +791,16 @@ struct gmc_matrices {
     int wide = 1;              // blocks a wavefront's side of a tile
     int32_t n = 0;
     int64_t blocks_x = 0, blocks_g = 0, parts = 0;
-    int64_t norms = 0, pieces = 0, grams = 0, applies = 0, gaps = 0;
+    bool small = false;        // every matrix is one workgroup's
+    int64_t slots = 0;         // of parts of tiles' sums
     void* table = nullptr;     // device memory: all of the below
     const Mat* mats = nullptr;
-    const Tile *norm = nullptr, *pack = nullptr, *gram = nullptr, *apply = nullptr;
+    struct List {
+        const Tile* tiles = nullptr;
+        unsigned n = 0;
+    } norm, pack, gram, gram_join, poly, poly_join, apply;
     const Gap* gap = nullptr;
+    int64_t gaps = 0;
 };
 
 namespace gmc {
@@ -473,6 +808,9 @@ namespace gmc {
 namespace {
 
 constexpr int64_t kMostTiles = int64_t(1) << 22;
+constexpr int64_t kLeastCut = 8;     // blocks of 32 columns, of a part of a contraction
+constexpr int64_t kWorthCut = 48;    // by so many a tile is longer than its share for a cut to pay
+constexpr int64_t kTileCost = 4;     // what a tile costs besides, in such blocks
 
 int64_t up_to(int64_t v, int64_t step) { return (v + step - 1) / step; }
 
@@ -539,7 +877,7 @@ Reach reach(double a, double b, double c, double top) {
 struct Scratch {
     _Float16 *X, *T0, *T1, *G, *B;
     double* part;
-    float* theta;
+    float *theta, *slots;
     int64_t bytes;
 };
 
@@ -557,7 +895,8 @@ Scratch layout(const gmc_matrices* p, void* base) {
     s.G = reinterpret_cast<_Float16*>(take(p->blocks_g * 2048));
     s.B = reinterpret_cast<_Float16*>(take(p->blocks_g * 2048));
     s.part = reinterpret_cast<double*>(take(p->parts * 8));
-    s.theta = reinterpret_cast<float*>(take((int64_t)p->n * (kMostSteps + 1) * 4));
+    s.theta = reinterpret_cast<float*>(take(p->small ? 0 : (int64_t)p->n * (kMostSteps + 1) * 4));
+    s.slots = reinterpret_cast<float*>(take(p->slots * p->wide * p->wide * 16384));
     s.bytes = at - static_cast<char*>(base);
     return s;
 }
@@ -582,11 +921,114 @@ gmc_status matrices_check(const char* me, const gmc_matrices* p, int32_t dtype, 
     int device = -1;
     if (hipGetDevice(&device) != hipSuccess) return op_error(GMC_EDEVICE, me, "no current device");
     if (device != p->device) return op_error(GMC_EINVAL, me, "the plan is another device's");
-    if (p->n) {
+    if (gmc_matrices_workspace(p)) {
         if (!workspace || workspace_bytes < gmc_matrices_workspace(p)) return op_error(GMC_EINVAL, me, "the workspace is too small");
         if (reinterpret_cast<uintptr_t>(workspace) & 255u) return op_error(GMC_EINVAL, me, "the workspace is not 256-byte aligned");
     }
     return GMC_OK;
+}
+
+// -- which workgroup does what ------------------------------------------------------
+
+constexpr int64_t kPlaces = 512;    // workgroups of a product under way at once: two on each of 256 CUs
+constexpr int kXcds = 8;
+
+// Tiles of one matrix that share rows and columns of its operands.
+struct Group {
+    std::vector<Tile> tiles;
+    int64_t work = 0;
+};
+
+struct Launch {
+    std::vector<Tile> tiles, joins;
+    int32_t slots = 0;
+};
+
+// A launch's tiles from whole ones in groups: long contractions cut where there are too few
+// tiles for the places, and the groups dealt to the XCDs (workgroup b goes to XCD b % 8), each with a cache
+// of its own, so that each has as much to do.
+Launch deal(std::vector<Group> groups, bool may_cut) {
+    Launch out;
+    int64_t tiles = 0, work = 0;
+    for (const Group& g : groups)
+        for (const Tile& t : g.tiles) {
+            ++tiles;
+            work += t.last - t.first;
+        }
+    // a fair share of the work, and the parts each tile is cut in for it: where the wait for the longest
+    // tile is shorter by more than a joining launch takes.  Equal tiles that fill the places and a few
+    // more: those few are cut.
+    const int64_t fair = std::max<int64_t>(kLeastCut, up_to(work, kPlaces));
+    const int64_t rest = tiles > kPlaces && tiles < 4 * kPlaces ? tiles % kPlaces : 0;
+    bool some = false;   // a joining launch there is then anyway
+    for (const Group& g : groups)
+        for (const Tile& t : g.tiles) some = some || (may_cut && t.last - t.first - fair > kWorthCut);
+    const auto parts_of = [&](const Tile& t, bool late) -> int32_t {
+        const int64_t length = t.last - t.first;
+        if (!may_cut) return 1;
+        if (length - fair > (some ? kWorthCut / 2 : kWorthCut)) return (int32_t)(length / fair);
+        if (late && length > kWorthCut) return (int32_t)std::min(kPlaces / rest, length / kLeastCut);
+        return 1;
+    };
+    std::vector<Group> cut;
+    int64_t seen = 0;
+    for (Group& g : groups) {
+        int32_t most = 1;
+        std::vector<int32_t> count;
+        for (const Tile& t : g.tiles) {
+            const bool late = rest > 0 && 2 * rest <= kPlaces && seen++ >= tiles - rest;
+            count.push_back(parts_of(t, late));
+            most = std::max(most, count.back());
+        }
+        if (most < 2) {
+            cut.push_back(std::move(g));
+            continue;
+        }
+        std::vector<Group> parts(most);
+        for (size_t at = 0; at < g.tiles.size(); ++at) {
+            const Tile t = g.tiles[at];
+            const int32_t length = t.last - t.first, n = count[at];
+            Tile j = t;
+            j.slot = out.slots;
+            j.count = n;
+            if (n > 1) {
+                out.joins.push_back(j);
+                out.slots += n;
+            }
+            for (int32_t k = 0; k < n; ++k) {
+                Tile q = t;
+                q.first = t.first + (int32_t)((int64_t)length * k / n);
+                q.last = t.first + (int32_t)((int64_t)length * (k + 1) / n);
+                q.slot = n > 1 ? j.slot + k : -1;
+                parts[k].tiles.push_back(q);
+            }
+        }
+        for (Group& q : parts)
+            if (!q.tiles.empty()) cut.push_back(std::move(q));
+    }
+    for (Group& g : cut)
+        for (const Tile& t : g.tiles) g.work += t.last - t.first + kTileCost;
+    std::stable_sort(cut.begin(), cut.end(), [](const Group& a, const Group& b) { return a.work > b.work; });
+    std::vector<Tile> lists[kXcds];
+    int64_t load[kXcds] = {};
+    for (const Group& g : cut) {
+        const int x = (int)(std::min_element(load, load + kXcds) - load);
+        load[x] += g.work;
+        lists[x].insert(lists[x].end(), g.tiles.begin(), g.tiles.end());
+    }
+    size_t most = 0;
+    for (auto& l : lists) {
+        std::stable_sort(l.begin(), l.end(), [](const Tile& a, const Tile& b) { return a.last - a.first > b.last - b.first; });
+        most = std::max(most, l.size());
+    }
+    for (size_t k = 0; k < most; ++k)
+        for (auto& l : lists) {
+            Tile none{};
+            none.mat = -1;
+            out.tiles.push_back(k < l.size() ? l[k] : none);
+        }
+    while (!out.tiles.empty() && out.tiles.back().mat < 0) out.tiles.pop_back();
+    return out;
 }
 
 struct Steps {
@@ -597,26 +1039,39 @@ struct Steps {
 
 template <int DT, bool kStep, int kWide>
 void run_products(const gmc_matrices* p, const Scratch& s, const Steps& how, ProductArgs a, hipStream_t st) {
-    const dim3 grams((unsigned)p->grams), applies((unsigned)p->applies);
     _Float16 *from = s.T0, *to = s.T1;
+    a.slots = s.slots;
+    a.X = s.X;
+    a.Xo = s.X;
+    a.G = a.Go = s.G;
+    a.B = a.Bo = s.B;
+    const auto take = [&](const gmc_matrices::List& l) {
+        a.tiles = l.tiles;
+        return dim3(l.n);
+    };
     for (int32_t k = 0; k < how.n; ++k) {
         a.a = (float)how.coefficients[3 * k];
         a.b = (float)how.coefficients[3 * k + 1];
         a.c = (float)how.coefficients[3 * k + 2];
-        a.X = s.X;
-        a.Xo = s.X;
-        a.G = a.Go = s.G;
-        a.B = a.Bo = s.B;
         a.XT = from;
         a.XTo = to;
         a.theta = s.theta + k;
-        a.tiles = p->gram;
-        matrix_product<kWide, kGram, GMC_F32><<<grams, 256, 0, st>>>(a);
-        matrix_product<kWide, kPoly, GMC_F32><<<grams, 256, 0, st>>>(a);
-        a.tiles = p->apply;
-        if (k + 1 < how.n) matrix_product<kWide, kApply, GMC_F32><<<applies, 256, 0, st>>>(a);
-        else if (kStep) matrix_product<kWide, kLastStep, GMC_F32><<<applies, 256, 0, st>>>(a);
-        else matrix_product<kWide, kLast, DT><<<applies, 256, 0, st>>>(a);
+        dim3 grid = take(p->gram);
+        matrix_product<kWide, kGram, GMC_F32><<<grid, 256, 0, st>>>(a);
+        if (p->gram_join.n) {
+            grid = take(p->gram_join);
+            matrix_join<kWide, kGram><<<dim3(grid.x * kWide * kWide), 256, 0, st>>>(a);
+        }
+        grid = take(p->poly);
+        matrix_product<kWide, kPoly, GMC_F32><<<grid, 256, 0, st>>>(a);
+        if (p->poly_join.n) {
+            grid = take(p->poly_join);
+            matrix_join<kWide, kPoly><<<dim3(grid.x * kWide * kWide), 256, 0, st>>>(a);
+        }
+        grid = take(p->apply);
+        if (k + 1 < how.n) matrix_product<kWide, kApply, GMC_F32><<<grid, 256, 0, st>>>(a);
+        else if (kStep) matrix_product<kWide, kLastStep, GMC_F32><<<grid, 256, 0, st>>>(a);
+        else matrix_product<kWide, kLast, DT><<<grid, 256, 0, st>>>(a);
         std::swap(from, to);
     }
 }
@@ -625,11 +1080,12 @@ template <int DT, bool kStep>
 void run_steps(const gmc_matrices* p, const Scratch& s, const Steps& how, const VectorArgs& v, const ProductArgs& a, hipStream_t st) {
     VectorArgs n = v;
     n.mats = p->mats;
-    n.tiles = p->norm;
+    n.tiles = p->norm.tiles;
     n.part = s.part;
     n.eps = how.eps;
     n.theta = s.theta;
     n.steps = how.n;
+    if (p->small) n.theta = nullptr;
     double top = 1.0;
     for (int32_t k = 0; k < how.n; ++k) {
         const Reach r = reach(how.coefficients[3 * k], how.coefficients[3 * k + 1], how.coefficients[3 * k + 2], top);
@@ -638,9 +1094,21 @@ void run_steps(const gmc_matrices* p, const Scratch& s, const Steps& how, const 
     }
     n.X = s.X;
     n.XT = s.T0;
-    matrix_norm<DT, kStep><<<dim3((unsigned)p->norms), 256, 0, st>>>(n);
-    n.tiles = p->pack;
-    matrix_pack<DT, kStep><<<dim3((unsigned)p->pieces), 256, 0, st>>>(n);
+    if (p->small) {
+        SmallArgs q;
+        q.in = n;
+        for (int32_t k = 0; k < how.n; ++k)
+            for (int e = 0; e < 3; ++e) q.c[k][e] = (float)how.coefficients[3 * k + e];
+        q.out = a.out;
+        q.w = a.w;
+        q.alpha = a.alpha;
+        q.keep = a.keep;
+        matrix_small<DT, kStep><<<dim3((unsigned)p->n), kSmallThreads, 0, st>>>(q);
+        return;
+    }
+    matrix_norm<DT, kStep><<<dim3(p->norm.n), 256, 0, st>>>(n);
+    n.tiles = p->pack.tiles;
+    matrix_pack<DT, kStep><<<dim3(p->pack.n), 256, 0, st>>>(n);
     if (p->wide == 2) run_products<DT, kStep, 2>(p, s, how, a, st);
     else run_products<DT, kStep, 1>(p, s, how, a, st);
 }
@@ -700,34 +1168,50 @@ gmc_status gmc_matrices_init(gmc_matrices** out, int64_t d, int32_t n, const int
             mats.push_back(m);
         }
         p->wide = large >= 256 ? 2 : 1;
+        p->small = n > 0;
+        for (const Mat& m : mats) p->small = p->small && 2 * (int64_t)m.mb * m.nb + (int64_t)m.mb * m.mb <= kSmallBlocks;
         const int side = 2 * p->wide;
-        std::vector<Tile> norm, pack, gram, apply;
-        std::vector<int32_t> order(n);
-        for (int32_t k = 0; k < n; ++k) order[k] = k;
-        // the longest contractions first: they end last
-        std::stable_sort(order.begin(), order.end(), [&](int32_t x, int32_t y) { return mats[x].n > mats[y].n; });
+        std::vector<Tile> norm, pack;
+        std::vector<Group> grams, polys, applies;
+        int64_t tiles = 0;
         bool many = false;
-        for (int32_t o = 0; o < n && !many; ++o) {
-            const int32_t k = order[o];
-            Mat& m = mats[k];
+        for (int32_t k = 0; k < n; ++k) {
+            const Mat& m = mats[k];
             const int64_t mt = up_to(m.mb, side), nt = up_to(m.nb, side), mp = up_to(m.m, kSide), np = up_to(m.n, kSide);
-            if (mt > kMostTiles / nt || mp > kMostTiles / np) {
-                many = true;
-                break;
-            }
-            const int64_t each = up_to(mp * np, kParts);
+            if (mt > kMostTiles / nt || mp > kMostTiles / np) many = true;
+            else tiles += std::max(mt * nt, mp * np);
+            many = many || tiles > kMostTiles;
+            if (many) break;
+        }
+        for (int32_t k = 0; k < n && !many; ++k) {
+            Mat& m = mats[k];
+            const int32_t mt = (m.mb + side - 1) / side, nt = (m.nb + side - 1) / side;
+            const int64_t mp = up_to(m.m, kSide), np = up_to(m.n, kSide), each = up_to(mp * np, kParts);
             m.parts = (int32_t)up_to(mp * np, each);
             m.part = (int32_t)p->parts;
             p->parts += m.parts;
             for (int32_t q = 0; q < m.parts; ++q)
-                norm.push_back({k, (int32_t)(q * each), q, (int32_t)std::min(each, mp * np - q * each)});
+                norm.push_back({k, (int32_t)(q * each), q, (int32_t)std::min(each, mp * np - q * each), 0, 0, -1, 0});
             for (int32_t i = 0; i < mp; ++i)
-                for (int32_t j = 0; j < np; ++j) pack.push_back({k, i, j, 0});
-            for (int32_t i = 0; i < mt; ++i)
-                for (int32_t j = 0; j <= i; ++j) gram.push_back({k, i, j, 0});
-            for (int32_t i = 0; i < mt; ++i)
-                for (int32_t j = 0; j < nt; ++j) apply.push_back({k, i, j, 0});
-            many = (int64_t)std::max(pack.size(), apply.size()) > kMostTiles;
+                for (int32_t j = 0; j < np; ++j) pack.push_back({k, i, j, 1, 0, 0, -1, 0});
+            // groups of up to 8 x 8 tiles, smaller ones where there are few tiles to deal out
+            const int32_t high = std::min(mt, tiles > 2048 ? 8 : 4), broad = tiles > 2048 ? 8 : 4;
+            for (int32_t i0 = 0; i0 < mt; i0 += high)
+                for (int32_t j0 = 0; j0 < nt; j0 += broad) {
+                    Group gram, poly, apply;
+                    for (int32_t j = j0; j < std::min(j0 + broad, nt); ++j)
+                        for (int32_t i = i0; i < std::min(i0 + high, mt); ++i) {
+                            apply.tiles.push_back({k, i, j, 1, 0, m.mb, -1, 0});
+                            if (j > i) continue;
+                            gram.tiles.push_back({k, i, j, 1, 0, m.nb, -1, 0});
+                            poly.tiles.push_back({k, i, j, 1, 0, m.mb, -1, 0});
+                        }
+                    if (!gram.tiles.empty()) {
+                        grams.push_back(std::move(gram));
+                        polys.push_back(std::move(poly));
+                    }
+                    applies.push_back(std::move(apply));
+                }
         }
         if (many) {
             delete p;
@@ -755,11 +1239,12 @@ gmc_status gmc_matrices_init(gmc_matrices** out, int64_t d, int32_t n, const int
             delete p;
             return op_error(GMC_EINVAL, me, "too many pieces outside the matrices");
         }
-        p->norms = norm.size();
-        p->pieces = pack.size();
-        p->grams = gram.size();
-        p->applies = apply.size();
-        p->gaps = gap.size();
+        if (p->small) {   // no other launch, and nothing kept in the workspace
+            norm.clear(), pack.clear(), grams.clear(), polys.clear(), applies.clear();
+            p->blocks_x = p->blocks_g = p->parts = 0;
+        }
+        const Launch gram = deal(std::move(grams), true), poly = deal(std::move(polys), true), apply = deal(std::move(applies), false);
+        p->slots = std::max(gram.slots, poly.slots);
         std::vector<char> host;
         const auto add = [&](const void* from, size_t bytes) {
             const size_t here = host.size();
@@ -767,9 +1252,13 @@ gmc_status gmc_matrices_init(gmc_matrices** out, int64_t d, int32_t n, const int
             if (bytes) memcpy(host.data() + here, from, bytes);
             return here;
         };
-        const size_t at_mats = add(mats.data(), mats.size() * sizeof(Mat)), at_norm = add(norm.data(), norm.size() * sizeof(Tile)),
-                     at_pack = add(pack.data(), pack.size() * sizeof(Tile)), at_gram = add(gram.data(), gram.size() * sizeof(Tile)),
-                     at_apply = add(apply.data(), apply.size() * sizeof(Tile)), at_gap = add(gap.data(), gap.size() * sizeof(Gap));
+        const std::vector<Tile>* lists[] = {&norm, &pack, &gram.tiles, &gram.joins, &poly.tiles, &poly.joins, &apply.tiles};
+        gmc_matrices::List* said[] = {&p->norm, &p->pack, &p->gram, &p->gram_join, &p->poly, &p->poly_join, &p->apply};
+        size_t at_list[7];
+        const size_t at_mats = add(mats.data(), mats.size() * sizeof(Mat));
+        for (int k = 0; k < 7; ++k) at_list[k] = add(lists[k]->data(), lists[k]->size() * sizeof(Tile));
+        const size_t at_gap = add(gap.data(), gap.size() * sizeof(Gap));
+        p->gaps = gap.size();
         if (hipGetDevice(&p->device) != hipSuccess) {
             delete p;
             return op_error(GMC_EDEVICE, me, "no current device");
@@ -791,10 +1280,10 @@ gmc_status gmc_matrices_init(gmc_matrices** out, int64_t d, int32_t n, const int
         }
         char* t = static_cast<char*>(p->table);
         p->mats = reinterpret_cast<const Mat*>(t + at_mats);
-        p->norm = reinterpret_cast<const Tile*>(t + at_norm);
-        p->pack = reinterpret_cast<const Tile*>(t + at_pack);
-        p->gram = reinterpret_cast<const Tile*>(t + at_gram);
-        p->apply = reinterpret_cast<const Tile*>(t + at_apply);
+        for (int k = 0; k < 7; ++k) {
+            said[k]->tiles = reinterpret_cast<const Tile*>(t + at_list[k]);
+            said[k]->n = (unsigned)lists[k]->size();
+        }
         p->gap = reinterpret_cast<const Gap*>(t + at_gap);
         *out = p;
         return GMC_OK;
@@ -824,7 +1313,7 @@ gmc_status gmc_orthogonalize(void* hip_stream, const gmc_matrices* plan, int32_t
     if (!x_dev || !out_dev) return op_error(GMC_EINVAL, me, "NULL argument");
     if (!isfinite((float)alpha)) return op_error(GMC_EINVAL, me, "alpha must be finite in fp32");
     const int64_t bytes = plan->d * type_size(dtype);
-    const Span x(x_dev, bytes), out(out_dev, bytes), scratch(workspace_dev, plan->n ? gmc_matrices_workspace(plan) : 0);
+    const Span x(x_dev, bytes), out(out_dev, bytes), scratch(workspace_dev, gmc_matrices_workspace(plan));
     if (!apart({out, scratch}, {}) || !apart({scratch}, {x}) || (x_dev != out_dev && !apart({out}, {x})))
         return op_error(GMC_EINVAL, me, "an output or the workspace overlaps another buffer");
     hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
@@ -855,7 +1344,7 @@ gmc_status gmc_orthogonal_step(void* hip_stream, const gmc_matrices* plan, int32
     if (!isfinite((float)rate) || !isfinite((float)decay)) return op_error(GMC_EINVAL, me, "rate and decay must be finite in fp32");
     if (!(mu >= 0.0 && mu <= 1.0)) return op_error(GMC_EINVAL, me, "mu must be in [0, 1]");
     const Span w(w_dev, plan->d * 4), update(update_dev, plan->d * type_size(dtype)), momentum(momentum_dev, plan->d * 4),
-        out(w_out_dev, plan->d * 4), scratch(workspace_dev, plan->n ? gmc_matrices_workspace(plan) : 0);
+        out(w_out_dev, plan->d * 4), scratch(workspace_dev, gmc_matrices_workspace(plan));
     if (!apart({out, momentum, scratch}, {update}) || !apart({momentum, scratch}, {w}) || (w_dev != w_out_dev && !apart({out}, {w})))
         return op_error(GMC_EINVAL, me, "an output or the workspace overlaps another buffer");
     hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
