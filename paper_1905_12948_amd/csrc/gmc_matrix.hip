@@ -168,10 +168,27 @@ __global__ __launch_bounds__(256) void matrix_norm(VectorArgs a) {
     if (threadIdx.x == 0) a.part[m.part + t.j] = lds[0] + lds[1] + lds[2] + lds[3];
 }
 
-// A value as its two halves.
-__device__ __forceinline__ void split(float v, _Float16& hi, _Float16& lo) {
-    hi = (_Float16)v;
-    lo = (_Float16)(v - (float)hi);
+// Values as their two halves, two at a time (two values are converted in one operation, and what
+// hi leaves is one of the mixed-precision ones).
+template <int N, class H>
+__device__ __forceinline__ void split(const float (&v)[N], H& hi, H& lo) {
+    float minus = -1.0f;   // not known to be: v - hi is a conversion and a difference
+    asm("" : "+s"(minus));
+#pragma unroll
+    for (int e = 0; e < N; e += 2) {
+        f32x2 x;
+        x.x = v[e];
+        x.y = v[e + 1];
+        const f16x2 h = __builtin_convertvector(x, f16x2);
+        f32x2 r;
+        r.x = __builtin_fmaf((float)h.x, minus, v[e]);
+        r.y = __builtin_fmaf((float)h.y, minus, v[e + 1]);
+        const f16x2 l = __builtin_convertvector(r, f16x2);
+        hi[e] = h.x;
+        hi[e + 1] = h.y;
+        lo[e] = l.x;
+        lo[e + 1] = l.y;
+    }
 }
 
 // What a wavefront's lanes have written to shared memory before is there for what they read after.
@@ -231,14 +248,13 @@ __global__ __launch_bounds__(256) void matrix_pack(VectorArgs a) {
         const int unit = threadIdx.x + 256 * (u & 1), row = unit & 63, k8 = unit >> 6;
         const bool along = u < 2;
         f16x8 hi, lo;
+        float f[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int i = along ? row : 8 * k8 + e, j = along ? 8 * k8 + e : row;
-            _Float16 h, l;
-            split((float)((double)(m.flip ? in[j][i] : in[i][j]) * inv), h, l);
-            hi[e] = h;
-            lo[e] = l;
+            f[e] = (float)((double)(m.flip ? in[j][i] : in[i][j]) * inv);
         }
+        split(f, hi, lo);
         const int rb = (along ? t.i : t.j) * 2 + (row >> 5), kb = (along ? t.j : t.i) * 4 + (k8 >> 1);
         if (rb < (along ? m.mb : m.nb) && kb < (along ? kn : km)) {
             _Float16* o = (along ? a.X : a.XT) + (m.x + rb * (along ? kn : km) + kb) * 1024 + ((row & 31) + 32 * (k8 & 1)) * 8;
@@ -324,7 +340,7 @@ __device__ __forceinline__ void finish_blocks(const ProductArgs& a, const Mat& m
                     const f16x4 hi = *reinterpret_cast<const f16x4*>(add + (g >> 1) * 1024 + (g & 1) * 256);
                     const f16x4 lo = *reinterpret_cast<const f16x4*>(add + (g >> 1) * 1024 + (g & 1) * 256 + 512);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) d[4 * g + e] = u * ((float)hi[e] + (float)lo[e]) + v * d[4 * g + e];
+                    for (int e = 0; e < 4; ++e) d[4 * g + e] = __builtin_fmaf((float)hi[e], u, __builtin_fmaf((float)lo[e], u, v * d[4 * g + e]));
                 }
             }
             if constexpr (kMode == kLast || kMode == kLastStep) {
@@ -355,13 +371,10 @@ __device__ __forceinline__ void finish_blocks(const ProductArgs& a, const Mat& m
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 f16x4 hi, lo;
+                float f[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    _Float16 h, l;
-                    split(d[4 * g + e], h, l);
-                    hi[e] = h;
-                    lo[e] = l;
-                }
+                for (int e = 0; e < 4; ++e) f[e] = d[4 * g + e];
+                split(f, hi, lo);
                 *reinterpret_cast<f16x4*>(o + (g >> 1) * 1024 + (g & 1) * 256) = hi;
                 *reinterpret_cast<f16x4*>(o + (g >> 1) * 1024 + (g & 1) * 256 + 512) = lo;
             }
@@ -375,13 +388,10 @@ __device__ __forceinline__ void finish_blocks(const ProductArgs& a, const Mat& m
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 f16x8 hi, lo;
+                float f[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    _Float16 h, l;
-                    split(turn[col * 33 + 16 * k + 8 * half + e], h, l);
-                    hi[e] = h;
-                    lo[e] = l;
-                }
+                for (int e = 0; e < 8; ++e) f[e] = turn[col * 33 + 16 * k + 8 * half + e];
+                split(f, hi, lo);
                 *reinterpret_cast<f16x8*>(o + k * 1024) = hi;
                 *reinterpret_cast<f16x8*>(o + k * 1024 + 512) = lo;
             }
@@ -561,196 +571,235 @@ struct SmallArgs {
     float alpha, keep;
 };
 
-constexpr int kSmallThreads = 512, kSmallBlocks = 39;   // 4 KB each of 160 KB: X, X^T and G of 32 x 32 blocks
+constexpr int kSmallThreads = 1024, kSmallBlocks = 39;   // 4 KB each of 160 KB: X, X^T and G of 32 x 32 blocks
 
 // Matrices of which X, X^T and G fit the shared memory of one CU: all steps in one launch, a workgroup a
-// matrix, a wavefront every eighth block (64 x 147: 13 us, by the launches of the others 62).  The polynomial
-// takes G's place, and X its own, once all have read them.
-template <int DT, bool kStep>
+// matrix, a wavefront every eighth block of what a phase computes.  The polynomial takes G's place, and
+// X its own, once all have read them.  X and X^T are both computed, the second by the products of the first
+// with their sides exchanged: a block's entries then go to either as 8 bytes a lane, where turning it
+// takes 32 writes of 2 bytes, which cost more than the products.  What shared memory is left takes the parts
+// of G that wavefronts without a block of their own sum, and then the polynomial.
+template <int DT, bool kStep, int mb>
 __global__ __launch_bounds__(kSmallThreads) void matrix_small(SmallArgs a) {
     typedef typename Elem<DT>::T T;
-    constexpr int kWaves = kSmallThreads / 64, kOwn = 3;   // blocks a wavefront has of up to 20
+    constexpr int kWaves = kSmallThreads / 64, kMost = mb == 1 ? 19 : mb == 2 ? 16 : 15;   // blocks of X
+    constexpr int kOwn = (2 * kMost + kWaves - 1) / kWaves, kUnits = kMost * 128 / kSmallThreads + 1;
     __shared__ f16x8 lds[kSmallBlocks * 256];
     __shared__ double sums[kWaves];
     const Mat m = a.in.mats[blockIdx.x];
-    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
-    const int mb = m.mb, nb = m.nb;
+    int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
+    const int nb = m.nb;   // mb = m.mb
     // a block of 32 rows and 32 columns is four times 64 vectors: 16 columns' hi and lo, twice
     f16x8 *X = lds, *XT = X + mb * nb * 256, *G = XT + mb * nb * 256;
-    const T* x = static_cast<const T*>(a.in.x) + m.offset;
-    float* past = kStep && a.in.momentum ? a.in.momentum + m.offset : nullptr;
-    const auto place = [&](int i, int j) { return m.flip ? (int64_t)j * m.pitch + i : (int64_t)i * m.pitch + j; };
-    // the sum of squares, and the momentum on the way
-    double sum = 0.0;
-    const int units = m.rows * m.cols;
-    for (int k0 = threadIdx.x; k0 < units; k0 += 8 * kSmallThreads) {
-        // all loads before the first is used: past the end the last component, which does not count
-        int64_t at[8];
-        float u[8], v[8];
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            const int k = k0 + q * kSmallThreads < units ? k0 + q * kSmallThreads : units - 1, r = k / m.cols;
-            at[q] = (int64_t)r * m.pitch + (k - r * m.cols);
-            u[q] = Elem<DT>::up(x[at[q]]);
-        }
-        if (past) {
-#pragma unroll
-            for (int q = 0; q < 8; ++q) v[q] = past[at[q]];
+    // X in 32 bits, where X^T is later: [i][j], four neighbours exchanged with others by the row so that a
+    // column's walk and a row's both meet all banks
+    float* raw = reinterpret_cast<float*>(XT);
+    const auto spot = [&](int i, int j) { return i * 32 * nb + (j ^ (i & 7) << 2); };
+    const int units = 32 * mb * 32 * nb;
+    {
+        const T* x = static_cast<const T*>(a.in.x) + m.offset;
+        float* past = kStep && a.in.momentum ? a.in.momentum + m.offset : nullptr;
+        // along the matrix's own rows, padded as X is
+        const int wide = 32 * (m.flip ? mb : nb);
+        double sum = 0.0;
+        for (int k0 = threadIdx.x; k0 < units; k0 += 8 * kSmallThreads) {
+            int64_t at[8];
+            float u[8], v[8];
+            int r[8], c[8];
+            // all loads before the first is used; outside the matrix that of its last row or column
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
-                v[q] = a.in.mu * v[q] + u[q];
-                u[q] = direction(a.in, u[q], v[q]);
-                if (k0 + q * kSmallThreads < units) past[at[q]] = v[q];
+                const int k = k0 + q * kSmallThreads < units ? k0 + q * kSmallThreads : units - 1;
+                r[q] = k / wide;
+                c[q] = k - r[q] * wide;
+                at[q] = (int64_t)(r[q] < m.rows ? r[q] : m.rows - 1) * m.pitch + (c[q] < m.cols ? c[q] : m.cols - 1);
+                u[q] = Elem<DT>::up(x[at[q]]);
+            }
+            if (past) {
+#pragma unroll
+                for (int q = 0; q < 8; ++q) v[q] = past[at[q]];
+            }
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                const bool real = r[q] < m.rows && c[q] < m.cols && k0 + q * kSmallThreads < units;
+                if (past) {
+                    v[q] = a.in.mu * v[q] + u[q];
+                    u[q] = direction(a.in, u[q], v[q]);
+                    // (a lane that reads this place for another one outside the matrix does not use it)
+                    if (real) past[at[q]] = v[q];
+                }
+                if (!real) u[q] = 0.0f;
+                sum = fma((double)u[q], (double)u[q], sum);
+                if (k0 + q * kSmallThreads < units) raw[m.flip ? spot(c[q], r[q]) : spot(r[q], c[q])] = u[q];
             }
         }
 #pragma unroll
-        for (int q = 0; q < 8; ++q)
-            if (k0 + q * kSmallThreads < units) sum = fma((double)u[q], (double)u[q], sum);
+        for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+        if (lane == 0) sums[wave] = sum;
     }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-    if (lane == 0) sums[wave] = sum;
     __syncthreads();
-    sum = 0.0;
+    double sum = 0.0;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) sum += sums[w];
     const double norm = sqrt(sum), inv = norm == 0.0 ? 0.0 : (double)kScaleX / norm;
     float theta = first_theta(norm, a.in.eps);
-    // eight neighbours at a time, of X's rows and then of its columns
-    for (int k = threadIdx.x; k < 2 * mb * nb * 128; k += kSmallThreads) {
-        const bool along = k < mb * nb * 128;
-        const int q = along ? k : k - mb * nb * 128, l = q & 63, deep = along ? 2 * nb : 2 * mb;
-        const int b = (q >> 6) / deep, c = (q >> 6) - b * deep, row = b * 32 + (l & 31), k0 = c * 16 + (l >> 5) * 8;
-        f16x8 hi, lo;
-        float u[8], v[8];
-        const auto at = [&](int e) {
-            const int i = along ? row : k0 + e, j = along ? k0 + e : row;
-            return place(i < m.m ? i : m.m - 1, j < m.n ? j : m.n - 1);
-        };
+    {
+        // eight neighbours at a time, of X's rows at once and of its columns when all have read theirs
+        f16x8 hi[kUnits], lo[kUnits];
+        const auto place = [&](int k, int deep) { return (k >> 6) * 128 + (k & 63); };
 #pragma unroll
-        for (int e = 0; e < 8; ++e) u[e] = Elem<DT>::up(x[at(e)]);
-        if (past) {
+        for (int side = 0; side < 2; ++side) {
+            const int deep = side ? 2 * mb : 2 * nb;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = past[at(e)];
+            for (int n = 0; n < kUnits; ++n) {
+                const int k = threadIdx.x + n * kSmallThreads;
+                if (k >= mb * nb * 128) break;
+                const int l = k & 63, b = (k >> 6) / deep, row = b * 32 + (l & 31), k0 = ((k >> 6) - b * deep) * 16 + (l >> 5) * 8;
+                float f[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) u[e] = direction(a.in, u[e], v[e]);
+                for (int e = 0; e < 8; ++e) f[e] = (float)((double)raw[side ? spot(k0 + e, row) : spot(row, k0 + e)] * inv);
+                split(f, hi[n], lo[n]);
+                if (side == 0) {
+                    X[place(k, deep)] = hi[n];
+                    X[place(k, deep) + 64] = lo[n];
+                }
+            }
         }
+        __syncthreads();
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int i = along ? row : k0 + e, j = along ? k0 + e : row;
-            _Float16 h, s;
-            split(i < m.m && j < m.n ? (float)((double)u[e] * inv) : 0.0f, h, s);
-            hi[e] = h;
-            lo[e] = s;
+        for (int n = 0; n < kUnits; ++n) {
+            const int k = threadIdx.x + n * kSmallThreads;
+            if (k >= mb * nb * 128) break;
+            XT[place(k, 0)] = hi[n];
+            XT[place(k, 0) + 64] = lo[n];
         }
-        f16x8* o = (along ? X : XT) + (b * deep + c) * 128 + l;
-        o[0] = hi;
-        o[64] = lo;
     }
     __syncthreads();
-    // A block of P Q^T, both `deep` times 16 columns; three sums, so that no product waits for another
-    const auto product = [&](const f16x8* P, const f16x8* Q, int deep) {
-        f32x16 d0, d1, d2;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) d0[e] = d1[e] = d2[e] = 0.0f;
-#pragma unroll 2
-        for (int k = 0; k < deep; ++k) {
-            const f16x8 ph = P[k * 128 + lane], pl = P[k * 128 + 64 + lane], qh = Q[k * 128 + lane], ql = Q[k * 128 + 64 + lane];
-            d0 = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, qh, d0, 0, 0, 0);
-            d1 = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, ql, d1, 0, 0, 0);
-            d2 = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl, qh, d2, 0, 0, 0);
-        }
-#pragma unroll
-        for (int e = 0; e < 16; ++e) d0[e] = d0[e] + (d1[e] + d2[e]);
-        return d0;
+    // Columns 16 k of a block of P Q^T, in two sums, so that a product does not wait for the one before it
+    const auto multiply = [&](const f16x8* P, const f16x8* Q, int k, f32x16& one, f32x16& two) {
+        const f16x8 ph = P[k * 128 + lane], pl = P[k * 128 + 64 + lane], qh = Q[k * 128 + lane], ql = Q[k * 128 + 64 + lane];
+        one = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, qh, one, 0, 0, 0);
+        two = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, ql, two, 0, 0, 0);
+        two = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl, qh, two, 0, 0, 0);
     };
+    // A block of P Q^T, both 32 mb columns wide
+    const auto product = [&](const f16x8* P, const f16x8* Q) {
+        f32x16 one, two;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) one[e] = two[e] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 2 * mb; ++k) multiply(P, Q, k, one, two);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) one[e] += two[e];
+        return one;
+    };
+    // blocks of 4 KB that are left, and so how many wavefronts share a block of G
+    const int spare = kSmallBlocks - 2 * mb * nb - mb * mb;
+    f16x8* left = G + mb * mb * 256;
+    int shares = kWaves / (mb * mb) < 1 + spare / (mb * mb) ? kWaves / (mb * mb) : 1 + spare / (mb * mb);
+    if (shares > nb) shares = nb;
+    f16x8* B = spare >= mb * mb ? left : G;
     // Entries 4 g to 4 g + 3 of block (ib, jb) where their row is j
     const auto half4 = [&](f16x8* base, int ib, int jb, int deep, int g, int h) {
-        return reinterpret_cast<f16x4*>(base + (jb * deep + 2 * ib + (g >> 1)) * 128 + h * 64 + col + 32 * (g & 1)) + half;
+        return reinterpret_cast<f16x4*>(base + (jb * deep + 2 * ib + (g >> 1)) * 128 + h * 64 + (lane & 31) + 32 * (g & 1)) + (lane >> 5);
     };
-    const auto value4 = [&](f16x8* base, int ib, int jb, int deep, int g) {
-        const f16x4 hi = *half4(base, ib, jb, deep, g, 0), lo = *half4(base, ib, jb, deep, g, 1);
-        f32x4 v;
+    // d <- u times what is there + v d
+    const auto mix4 = [&](f16x8* base, int ib, int jb, int deep, float u, float v, f32x16& d) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = (float)hi[e] + (float)lo[e];
-        return v;
-    };
-    const auto keep4 = [&](f16x8* base, int ib, int jb, int deep, int g, const f32x16& d) {
-        f16x4 hi, lo;
+        for (int g = 0; g < 4; ++g) {
+            const f16x4 hi = *half4(base, ib, jb, deep, g, 0), lo = *half4(base, ib, jb, deep, g, 1);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            _Float16 h, l;
-            split(d[4 * g + e], h, l);
-            hi[e] = h;
-            lo[e] = l;
+            for (int e = 0; e < 4; ++e) d[4 * g + e] = __builtin_fmaf((float)hi[e], u, __builtin_fmaf((float)lo[e], u, v * d[4 * g + e]));
         }
-        *half4(base, ib, jb, deep, g, 0) = hi;
-        *half4(base, ib, jb, deep, g, 1) = lo;
+    };
+    const auto keep4 = [&](f16x8* base, int ib, int jb, int deep, const f32x16& d) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            f16x4 hi, lo;
+            float f[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f[e] = d[4 * g + e];
+            split(f, hi, lo);
+            *half4(base, ib, jb, deep, g, 0) = hi;
+            *half4(base, ib, jb, deep, g, 1) = lo;
+        }
     };
     for (int step = 0; step < a.in.steps; ++step) {
+        // places of blocks are worked out where they are needed: kept over the steps they would take all registers
+        asm volatile("" : "+v"(lane), "+s"(wave));
         const float ca = a.c[step][0], cb = a.c[step][1], cc = a.c[step][2], theta2 = theta * theta;
         f32x16 d[kOwn];
-        for (int b = wave; b < mb * mb; b += kWaves) {
-            const int ib = b / mb, jb = b - ib * mb;
-            f32x16 v = product(X + ib * nb * 256, X + jb * nb * 256, 2 * nb);
+        {
+            const int share = wave / (mb * mb), b = wave - share * mb * mb, ib = b / mb, jb = b - ib * mb;
+            f32x16 one, two;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) v[e] *= 1.0f / kScaleX;
+            for (int e = 0; e < 16; ++e) one[e] = two[e] = 0.0f;
+            if (share < shares) {
+                const int end = 2 * nb * (share + 1) / shares;
+                for (int k = 2 * nb * share / shares; k < end; ++k) multiply(X + ib * nb * 256, X + jb * nb * 256, k, one, two);
 #pragma unroll
-            for (int g = 0; g < 4; ++g) keep4(G, ib, jb, 2 * mb, g, v);
-        }
-        __syncthreads();
+                for (int e = 0; e < 16; ++e) one[e] += two[e];
+                if (share > 0)
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int b = wave + k * kWaves, ib = b / mb, jb = b - ib * mb;
-            if (b >= mb * mb) break;
-            d[k] = product(G + ib * mb * 256, G + jb * mb * 256, 2 * mb);
-            const float u = cb * theta2 * (kScaleB / kScaleX), v = cc * theta2 * theta2 * (kScaleB / kScaleX / kScaleX);
+                    for (int e = 0; e < 16; ++e) reinterpret_cast<float*>(left)[((share - 1) * mb * mb + b) * 1024 + e * 64 + lane] = one[e];
+            }
+            __syncthreads();
+            if (share == 0) {
+                for (int k = 0; k < shares - 1; ++k)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const f32x4 add = value4(G, ib, jb, 2 * mb, g);
+                    for (int e = 0; e < 16; ++e) one[e] += reinterpret_cast<const float*>(left)[(k * mb * mb + b) * 1024 + e * 64 + lane];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) d[k][4 * g + e] = u * add[e] + v * d[k][4 * g + e];
+                for (int e = 0; e < 16; ++e) one[e] *= 1.0f / kScaleX;
+                keep4(G, ib, jb, 2 * mb, one);
             }
         }
         __syncthreads();
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int b = wave + k * kWaves, ib = b / mb, jb = b - ib * mb;
-            if (b >= mb * mb) break;
-#pragma unroll
-            for (int g = 0; g < 4; ++g) keep4(G, ib, jb, 2 * mb, g, d[k]);
+        if (wave < mb * mb) {
+            const int ib = wave / mb, jb = wave - ib * mb;
+            d[0] = product(G + ib * mb * 256, G + jb * mb * 256);
+            mix4(G, ib, jb, 2 * mb, cb * theta2 * (kScaleB / kScaleX), cc * theta2 * theta2 * (kScaleB / kScaleX / kScaleX), d[0]);
         }
+        if (B == G) __syncthreads();
+        if (wave < mb * mb) keep4(B, wave / mb, wave % mb, 2 * mb, d[0]);
         __syncthreads();
-        const bool last = step + 1 == a.in.steps, turned = last && m.flip;
+        const bool last = step + 1 == a.in.steps;
         const float next = last ? 0.0f : next_theta(theta, a.in.growth[step]);
-        const float u = last ? ca : ca * (theta / next), v = last ? 1.0f / kScaleB : (theta / next) / kScaleB;
-        const int cols = turned ? mb : nb;   // of D, which is X^T's product where a matrix on its side is written
+        const float ratio = last ? 1.0f : theta / next;
+        // blocks of X, whose entries have their row j in X^T, and of X^T, whose entries have it in X; in
+        // the last step of the one that lies as the matrix does
+        const int first = last && m.flip ? mb * nb : 0, end = last && !m.flip ? mb * nb : 2 * mb * nb;
 #pragma unroll
         for (int k = 0; k < kOwn; ++k) {
-            const int b = wave + k * kWaves, ib = b / cols, jb = b - ib * cols;
-            if (b >= mb * nb) break;
-            d[k] = turned ? product(XT + ib * mb * 256, G + jb * mb * 256, 2 * mb) : product(G + ib * mb * 256, XT + jb * mb * 256, 2 * mb);
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const f32x4 add = turned ? value4(X, ib, jb, 2 * nb, g) : value4(XT, ib, jb, 2 * mb, g);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) d[k][4 * g + e] = u * add[e] + v * d[k][4 * g + e];
-            }
+            const int b = first + wave + k * kWaves;
+            if (b >= end) break;
+            const bool turned = b >= mb * nb;
+            const int cols = turned ? mb : nb, q = turned ? b - mb * nb : b, ib = q / cols, jb = q - ib * cols;
+            const f16x8 *one = XT + (turned ? ib : jb) * mb * 256, *two = B + (turned ? jb : ib) * mb * 256;
+            d[k] = product(turned ? one : two, turned ? two : one);
+            mix4(turned ? X : XT, ib, jb, turned ? 2 * nb : 2 * mb, ca * ratio, ratio / kScaleB, d[k]);
         }
         if (last) {
             const float factor = a.alpha * m.scale * theta * (1.0f / kScaleX);
 #pragma unroll
             for (int k = 0; k < kOwn; ++k) {
-                const int b = wave + k * kWaves, ib = b / cols, jb = b - ib * cols;
+                const int b = wave + k * kWaves, cols = m.flip ? mb : nb, ib = b / cols, jb = b - ib * cols;
                 if (b >= mb * nb) break;
-                const int c = jb * 32 + col;
+                const int r0 = ib * 32 + 4 * (lane >> 5), c = jb * 32 + (lane & 31);
+                const int64_t at = m.offset + (int64_t)r0 * m.pitch + c;
+                float w[16];
+                if constexpr (kStep) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int r = 8 * (e >> 2) + (e & 3);
+                        w[e] = r0 + r < m.rows && c < m.cols ? a.w[at + r * m.pitch] : 0.0f;
+                    }
+                }
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const int r = ib * 32 + 8 * (e >> 2) + 4 * half + (e & 3);
-                    if (r >= m.rows || c >= m.cols) continue;
-                    const int64_t at = m.offset + (int64_t)r * m.pitch + c;
-                    if constexpr (kStep) static_cast<float*>(a.out)[at] = a.keep * a.w[at] + factor * d[k][e];
-                    else static_cast<T*>(a.out)[at] = Elem<DT>::down(factor * d[k][e]);
+                    const int r = 8 * (e >> 2) + (e & 3);
+                    if (r0 + r >= m.rows || c >= m.cols) continue;
+                    if constexpr (kStep) static_cast<float*>(a.out)[at + r * m.pitch] = a.keep * w[e] + factor * d[k][e];
+                    else static_cast<T*>(a.out)[at + r * m.pitch] = Elem<DT>::down(factor * d[k][e]);
                 }
             }
             return;
@@ -759,20 +808,11 @@ __global__ __launch_bounds__(kSmallThreads) void matrix_small(SmallArgs a) {
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < kOwn; ++k) {
-            const int b = wave + k * kWaves, ib = b / nb, jb = b - ib * nb;
-            if (b >= mb * nb) break;
-#pragma unroll
-            for (int g = 0; g < 4; ++g) keep4(XT, ib, jb, 2 * mb, g, d[k]);
-            // where its row is i: block (ib, 2 jb + col / 16), lane i % 32 + 32 (col / 8 % 2), half col % 8
-            _Float16* o = reinterpret_cast<_Float16*>(X + (ib * 2 * nb + 2 * jb + (col >> 4)) * 128 + 32 * (col >> 3 & 1)) + (col & 7);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                _Float16 h, l;
-                split(d[k][e], h, l);
-                const int row = 8 * (e >> 2) + 4 * half + (e & 3);
-                o[row * 8] = h;
-                o[row * 8 + 512] = l;
-            }
+            const int b = wave + k * kWaves;
+            if (b >= 2 * mb * nb) break;
+            const bool turned = b >= mb * nb;
+            const int cols = turned ? mb : nb, q = turned ? b - mb * nb : b, ib = q / cols, jb = q - ib * cols;
+            keep4(turned ? X : XT, ib, jb, turned ? 2 * nb : 2 * mb, d[k]);
         }
         __syncthreads();
     }
@@ -791,7 +831,7 @@ struct gmc_matrices {
     int wide = 1;              // blocks a wavefront's side of a tile
     int32_t n = 0;
     int64_t blocks_x = 0, blocks_g = 0, parts = 0;
-    bool small = false;        // every matrix is one workgroup's
+    int small = 0;             // every matrix is one workgroup's: their shorter sides' blocks
     int64_t slots = 0;         // of parts of tiles' sums
     void* table = nullptr;     // device memory: all of the below
     const Mat* mats = nullptr;
@@ -1103,7 +1143,10 @@ void run_steps(const gmc_matrices* p, const Scratch& s, const Steps& how, const 
         q.w = a.w;
         q.alpha = a.alpha;
         q.keep = a.keep;
-        matrix_small<DT, kStep><<<dim3((unsigned)p->n), kSmallThreads, 0, st>>>(q);
+        const dim3 grid((unsigned)p->n);
+        if (p->small == 1) matrix_small<DT, kStep, 1><<<grid, kSmallThreads, 0, st>>>(q);
+        else if (p->small == 2) matrix_small<DT, kStep, 2><<<grid, kSmallThreads, 0, st>>>(q);
+        else matrix_small<DT, kStep, 3><<<grid, kSmallThreads, 0, st>>>(q);
         return;
     }
     matrix_norm<DT, kStep><<<dim3(p->norm.n), 256, 0, st>>>(n);
@@ -1168,8 +1211,13 @@ gmc_status gmc_matrices_init(gmc_matrices** out, int64_t d, int32_t n, const int
             mats.push_back(m);
         }
         p->wide = large >= 256 ? 2 : 1;
-        p->small = n > 0;
-        for (const Mat& m : mats) p->small = p->small && 2 * (int64_t)m.mb * m.nb + (int64_t)m.mb * m.mb <= kSmallBlocks;
+        // matrices of another number of rows in blocks are padded to the most of them
+        int most = 0, wide = 0;
+        for (const Mat& m : mats) most = std::max(most, m.mb), wide = std::max(wide, m.nb);
+        if (n > 0 && 2 * (int64_t)most * wide + (int64_t)most * most <= kSmallBlocks) {
+            p->small = most;
+            for (Mat& m : mats) m.mb = most, m.nb = std::max(m.nb, most);
+        }
         const int side = 2 * p->wide;
         std::vector<Tile> norm, pack;
         std::vector<Group> grams, polys, applies;

@@ -46,14 +46,23 @@ def scores_gradient(x, tau, labels, dlogp, dentropy, ids, dtop):
     return (down - p * down.sum(-1, keepdims=True)) / tau
 
 
-def polar(x, steps=5, coefficients=QUINTIC, eps=1e-7, dtype=np.float64):
-    """The Newton-Schulz steps on x / (|x| + eps)."""
+def polar(x, steps=5, coefficients=QUINTIC, eps=1e-7, keep=lambda v: v):
+    """The Newton-Schulz steps on x / (|x| + eps); keep: what becomes of each value that is kept."""
     x = np.asarray(x, np.float64)
     norm = np.sqrt((x * x).sum()) + eps
-    x = (x / norm if norm > 0 else x).astype(dtype)
+    x = keep(x / norm if norm > 0 else x)
     for k in range(steps):
-        a, b, c = (dtype(v) for v in (coefficients if np.ndim(coefficients) == 1 else coefficients[k]))
-        gram = x @ x.T if x.shape[0] <= x.shape[1] else x.T @ x
-        poly = b * gram + c * (gram @ gram)
-        x = a * x + (poly @ x if x.shape[0] <= x.shape[1] else x @ poly)
+        a, b, c = coefficients if np.ndim(coefficients) == 1 else coefficients[k]
+        gram = keep(x @ x.T if x.shape[0] <= x.shape[1] else x.T @ x)
+        poly = keep(b * gram + c * (gram @ gram))
+        x = keep(a * x + (poly @ x if x.shape[0] <= x.shape[1] else x @ poly))
     return x
+
+
+def polar_spread(x, error, **how):
+    """The largest of eight distances between the steps' result and theirs with values off by up to
+    `error` of each, at random."""
+    rng = np.random.default_rng(5)
+    exact = polar(x, **how)
+    noisy = [polar(x, keep=lambda v: v * (1 + error * rng.uniform(-1, 1, v.shape)), **how) for _ in range(8)]
+    return max(np.linalg.norm(v - exact) for v in noisy)
