@@ -61,6 +61,32 @@ __device__ __forceinline__ float key_value(uint64_t k) {
 }
 __device__ __forceinline__ int key_place(uint64_t k) { return (int)~(uint32_t)k; }
 
+// A value of the lane that a fixed pattern pairs with this one.
+template <int kPattern>
+__device__ __forceinline__ float paired(float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), kPattern, 15, 15, true));
+}
+__device__ __forceinline__ float of_lane(float v, int lane) {
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
+}
+// The wavefront's values joined, in every lane: within 16 lanes by patterns (neighbours, pairs, halves and
+// rows mirrored), then the four rows' by reading a lane of each.  An exchange by address takes 15
+// times as long as a pattern, and a row's six such joins would be most of a short row's time.
+template <class F>
+__device__ __forceinline__ float wave_join(float v, F&& op) {
+    v = op(v, paired<0xb1>(v));
+    v = op(v, paired<0x4e>(v));
+    v = op(v, paired<0x141>(v));
+    v = op(v, paired<0x140>(v));
+    return op(op(of_lane(v, 0), of_lane(v, 16)), op(of_lane(v, 32), of_lane(v, 48)));
+}
+__device__ __forceinline__ float lanes_sum(float v) {
+    return wave_join(v, [](float a, float b) { return a + b; });
+}
+__device__ __forceinline__ float lanes_max(float v) {
+    return wave_join(v, [](float a, float b) { return larger(a, b); });
+}
+
 __device__ __forceinline__ uint64_t wave_max(uint64_t v) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {
@@ -84,13 +110,15 @@ __device__ __forceinline__ void row_barrier() {
 
 template <int kWaves>
 struct Shared {
-    static constexpr int kKeys = kWaves == 1 ? kRowKeys : kMostKeys;
+    static constexpr int kKeys = kWaves == 1 ? kRowKeys : kMostKeys, kVectors = kKeys / 4;
     float top[kWaves];
     float2 sum[kWaves];
     float reach[kWaves];
     uint64_t best[2][kWaves];
-    int count;
+    int count, vectors;
     uint64_t keys[kKeys];
+    uint4 vector[kVectors];   // with an entry that reaches the threshold
+    int place[kVectors];      // of its first entry
 };
 
 __device__ __forceinline__ float log_sum(float m, float s) { return fabsf(m) < INFINITY ? logf(s) : NAN; }
@@ -137,7 +165,8 @@ __device__ __forceinline__ void again(Vec<DT, N> (&x)[kHeld]) {
 // One row, or a piece of one (kPieces), per kThreads threads, held in kHeld vectors a
 // thread.
 template <int DT, int kThreads, int kHeld, bool kTop, bool kPieces>
-__global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void score_rows(ScoreArgs a) {
+__global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) __attribute__((amdgpu_waves_per_eu(kHeld <= 8 ? 6 : 4)))
+void score_rows(ScoreArgs a) {
     typedef typename Elem<DT>::T T;
     constexpr int N = 16 / Elem<DT>::kSize;
     constexpr int kWaves = kThreads / 64;
@@ -177,9 +206,7 @@ __global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void score_rows(Sc
 #pragma unroll
             for (int q = 0; q < N; ++q) own = larger(own, f[q]);
         }
-    float m = own;
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) m = larger(m, __shfl_xor(m, o));
+    float m = lanes_max(own);
     if constexpr (kWaves > 1) {
         if (lane == 0) sh.top[wave] = m;
         __syncthreads();
@@ -201,20 +228,18 @@ __global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void score_rows(Sc
                 u = __builtin_fmaf(w, v, u);
             }
         }
-    s = wave_sum(s);
-    u = wave_sum(u);
+    s = lanes_sum(s);
+    u = lanes_sum(u);
     if constexpr (kTop) {
         // the wavefront's share of the threshold: its n-th largest of the threads' maxima
         float left = own != own ? INFINITY : own, least = -INFINITY;
         for (int n = (a.top + kWaves - 1) / kWaves; n > 0; --n) {
-            least = left;
-#pragma unroll
-            for (int o = 32; o > 0; o >>= 1) least = fmaxf(least, __shfl_xor(least, o));
+            least = lanes_max(left);
             const uint64_t who = __ballot(left == least);
             if (lane == __ffsll((unsigned long long)who) - 1) left = -INFINITY;
         }
         if (lane == 0) sh.reach[wave] = least;
-        if (tid == 0) sh.count = 0;
+        if (tid == 0) sh.count = sh.vectors = 0;
     }
     if (kWaves > 1 && lane == 0) sh.sum[wave] = make_float2(s, u);
     row_barrier<kWaves>();
@@ -234,48 +259,70 @@ __global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void score_rows(Sc
         float reach = sh.reach[0];
 #pragma unroll
         for (int w = 1; w < kWaves; ++w) reach = fminf(reach, sh.reach[w]);
-        const auto each = [&](auto&& take) {
+        typedef Shared<kWaves> S;
+        const auto take = [&](float v, int j) {
+            if (v >= reach) {
+                const int n = atomicAdd(&sh.count, 1);
+                if (n < S::kKeys) sh.keys[n] = key_of(v, from + j);
+            }
+        };
+        // the vectors with such an entry go to shared memory whole, and their entries are looked at from
+        // there, one a thread
+        again(x);
+        if (own >= reach) {
             if (e >= 0) take(ex, e);
 #pragma unroll
             for (int k = 0; k < kHeld; ++k)
                 if (tid + k * kThreads < row.nb) {
                     x[k].unpack(f);
+                    float most = f[0];
 #pragma unroll
-                    for (int q = 0; q < N; ++q) take(f[q], row.head + (tid + k * kThreads) * N + q);
+                    for (int q = 1; q < N; ++q) most = fmaxf(most, f[q]);
+                    if (most >= reach) {
+                        const int n = atomicAdd(&sh.vectors, 1);
+                        if (n < S::kVectors) {
+                            sh.vector[n] = __builtin_bit_cast(uint4, x[k].raw);
+                            sh.place[n] = row.head + (tid + k * kThreads) * N;
+                        }
+                    }
                 }
-        };
-        again(x);
-        if (own >= reach) {
-            each([&](float v, int j) {
-                if (v >= reach) {
-                    const int n = atomicAdd(&sh.count, 1);
-                    if (n < Shared<kWaves>::kKeys) sh.keys[n] = key_of(v, from + j);
-                }
-            });
         }
+        row_barrier<kWaves>();
+        const int vectors = sh.vectors;
+        if (vectors <= S::kVectors)
+            for (int c = tid; c < vectors * N; c += kThreads)
+                take(Elem<DT>::up(reinterpret_cast<const T*>(sh.vector)[c]), sh.place[c / N] + c % N);
         row_barrier<kWaves>();
         const int n = sh.count, all = len < a.top ? len : a.top;
         const auto give = [&](int rank, uint64_t key) {
             if constexpr (kPieces) a.keys[id * a.top + rank] = key;
             else write_top(a, i, rank, key, m, s);
         };
-        if (m == m && n <= Shared<kWaves>::kKeys) {
+        if (m == m && vectors <= S::kVectors && n <= S::kKeys) {
             for (int c = tid; c < n; c += kThreads) {
                 const uint64_t key = sh.keys[c];
                 int rank = 0;
+#pragma unroll 8
                 for (int o = 0; o < n; ++o) rank += sh.keys[o] > key;
                 if (rank < all) give(rank, key);
             }
         } else {
-            again(x);
             uint64_t last = ~uint64_t(0), best = last;
             for (int rank = 0; rank < all; ++rank) {
                 if (best >= last) {
+                    // read again: such rows are few, and their code would take the others' registers
                     best = 0;
-                    each([&](float v, int j) {
+                    const auto look = [&](float v, int j) {
                         const uint64_t key = key_of(v, from + j);
                         if (key < last && key > best) best = key;
-                    });
+                    };
+                    if (e >= 0) look(ex, e);
+#pragma unroll 1
+                    for (int v = tid; v < row.nb; v += kThreads) {
+                        V::load(row.p + row.head + (int64_t)v * N).unpack(f);
+#pragma unroll
+                        for (int q = 0; q < N; ++q) look(f[q], row.head + v * N + q);
+                    }
                 }
                 uint64_t top = wave_max(best);
                 if constexpr (kWaves > 1) {
@@ -308,8 +355,7 @@ __global__ __launch_bounds__(256) void score_join(ScoreArgs a) {
     const float4* part = a.part + i * a.pieces;
     float m = -INFINITY;
     for (int p = threadIdx.x; p < a.pieces; p += 256) m = larger(m, part[p].x);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) m = larger(m, __shfl_xor(m, o));
+    m = lanes_max(m);
     if (lane == 0) lds[wave] = m;
     __syncthreads();
     m = larger(larger(lds[0], lds[1]), larger(lds[2], lds[3]));
@@ -321,8 +367,8 @@ __global__ __launch_bounds__(256) void score_join(ScoreArgs a) {
         s += w * v.y;
         u += w * __builtin_fmaf(d, v.y, v.z);
     }
-    s = wave_sum(s);
-    u = wave_sum(u);
+    s = lanes_sum(s);
+    u = lanes_sum(u);
     if (lane == 0) sums[wave] = make_float2(s, u);
     __syncthreads();
     s = sums[0].x + sums[1].x + sums[2].x + sums[3].x;
@@ -345,6 +391,7 @@ __global__ __launch_bounds__(256) void score_join(ScoreArgs a) {
         for (int c = threadIdx.x; c < have + n; c += 256) {
             const uint64_t key = keys[c];
             int rank = 0;
+#pragma unroll 8
             for (int o = 0; o < have + n; ++o) rank += keys[o] > key;
             if (key && rank < a.top) kept[rank] = key;
         }
