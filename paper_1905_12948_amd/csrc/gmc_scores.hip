@@ -517,18 +517,18 @@ __global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void score_gradien
 // -- host -----------------------------------------------------------------------------
 
 // How a call's rows are cut.  Held rows: up to 8 vectors by each of 64, 256 or 512
-// threads, or 13 by 512.
+// threads, or 13 by 512 or 1024.
 struct Cut {
     int threads, held, pieces;
     int32_t piece;
 };
 
-constexpr int64_t kHeldLines = 512 * 13 * 16 / 128;
+constexpr int64_t kHeldLines = 1024 * 13 * 16 / 128;
 
 Cut cut_rows(int32_t dtype, int64_t V) {
     const int64_t b = type_size(dtype), vecs = V * b / 16;   // at most, whatever the alignment
-    Cut c = {vecs <= 64 * 8 ? 64 : vecs <= 256 * 8 ? 256 : 512, vecs <= 512 * 8 ? 8 : 13, 1, (int32_t)V};
-    if (vecs > 512 * 13) {
+    Cut c = {vecs <= 64 * 8 ? 64 : vecs <= 256 * 8 ? 256 : vecs <= 512 * 13 ? 512 : 1024, vecs <= 512 * 8 ? 8 : 13, 1, (int32_t)V};
+    if (vecs > 1024 * 13) {
         // whole lines, so that every piece begins where the row's own lines do
         const int64_t lines = (V * b + 127) / 128, pieces = (lines + kHeldLines - 1) / kHeldLines;
         c.piece = (int32_t)((lines + pieces - 1) / pieces * (128 / b));
@@ -544,7 +544,8 @@ void score_launch(const ScoreArgs& a, const Cut& c, hipStream_t st) {
     if (!kPieces && c.threads == 64) score_rows<DT, 64, 8, kTop, false><<<quads, 256, 0, st>>>(a);
     else if (c.threads == 256) score_rows<DT, 256, 8, kTop, kPieces><<<rows, 256, 0, st>>>(a);
     else if (c.held == 8) score_rows<DT, 512, 8, kTop, kPieces><<<rows, 512, 0, st>>>(a);
-    else score_rows<DT, 512, 13, kTop, kPieces><<<rows, 512, 0, st>>>(a);
+    else if (c.threads == 512) score_rows<DT, 512, 13, kTop, kPieces><<<rows, 512, 0, st>>>(a);
+    else score_rows<DT, 1024, 13, kTop, kPieces><<<rows, 1024, 0, st>>>(a);
 }
 
 }  // namespace
