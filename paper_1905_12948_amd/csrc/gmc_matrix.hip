@@ -423,12 +423,13 @@ __device__ __forceinline__ int64_t slot_of(int slot, int wave, int lane) {
 //   kApply  P = B, Q = X^T       X <- a X + D, along both axes
 //   kLast   the same, or P = X^T and Q = B for a matrix on its side, into the vector
 // or, of a tile whose contraction is cut, its part of the sum for matrix_join.  G and B are symmetric: tiles with j <= i, written to both places.
-template <int kWide, int kMode, int DT>
-__global__ __launch_bounds__(256, 2) void matrix_product(ProductArgs a) {
+template <int kWide, int kStages, int kMode, int DT>
+__global__ __launch_bounds__(256, kStages == 4 ? 2 : 3) void matrix_product(ProductArgs a) {
     constexpr int kBlocks = 2 * kWide;                 // of 32 rows, on each side of the tile
     constexpr int kDeep = kWide == 2 ? 1 : 2;          // 16 columns, of a stage
     constexpr int kChunks = 2 * kBlocks * kDeep * 2;   // kilobytes of a stage: sides, blocks, columns, halves
-    __shared__ _Float16 stage0[kChunks * 512], stage1[kChunks * 512], stage2[kChunks * 512], stage3[kChunks * 512];
+    // arrays of their own, so that a wait for one stage's loads is none for the others'
+    __shared__ _Float16 stage0[kChunks * 512], stage1[kChunks * 512], stage2[kChunks * 512], stage3[kStages == 4 ? kChunks * 512 : 8];
     const Tile t = a.tiles[blockIdx.x];
     if (t.mat < 0) return;   // fills an XCD's list
     const Mat m = a.mats[t.mat];
@@ -472,11 +473,11 @@ __global__ __launch_bounds__(256, 2) void matrix_product(ProductArgs a) {
         o[r] = reinterpret_cast<const f16x8*>(here)[(((q ? kBlocks + wj + i : wi + i) * kDeep + k) * 2 + h) * 64 + lane];
     };
     // Stage s + 1 is in shared memory and stage s has been read by all, whose place the loads of
-    // stage s + 4 take; those of s + 2 and s + 3 stay under way.  The operands of s + 1 are read and
-    // the loads issued between the products of s, one after each: in front of them they
-    // hold the products up (2048 x 2048, one workgroup a CU: a stage takes 1.9 times as long).
+    // stage s + kStages take; those of the stages between stay under way.  The operands of s + 1 are read
+    // and the loads issued between the products of s, one after each: in front of them they
+    // hold the products up (2048 x 2048, one workgroup a CU: X's product 59 us, so 53).
     const auto step = [&](int s, const f16x8 (&now)[kReads], f16x8 (&then)[kReads], const _Float16* after, _Float16* here) {
-        wait_stage<2 * kLoads>();
+        wait_stage<(kStages - 2) * kLoads>();
 #pragma unroll
         for (int n = 0; n < kProducts; ++n) {
             const int k = n / (3 * kWide * kWide), part = n / (kWide * kWide) % 3, i = n / kWide % kWide, j = n % kWide;
@@ -485,7 +486,7 @@ __global__ __launch_bounds__(256, 2) void matrix_product(ProductArgs a) {
 #pragma unroll
             for (int r = n * (kReads + kLoads) / kProducts; r < (n + 1) * (kReads + kLoads) / kProducts; ++r) {
                 if (r < kReads) read(then, r, after);
-                else fetch(s + 4, r - kReads, here);
+                else fetch(s + kStages, r - kReads, here);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -497,25 +498,43 @@ __global__ __launch_bounds__(256, 2) void matrix_product(ProductArgs a) {
     for (int k = 0; k < kLoads; ++k) fetch(1, k, stage1);
 #pragma unroll
     for (int k = 0; k < kLoads; ++k) fetch(2, k, stage2);
+    if constexpr (kStages == 4) {
 #pragma unroll
-    for (int k = 0; k < kLoads; ++k) fetch(3, k, stage3);
-    wait_stage<3 * kLoads>();
+        for (int k = 0; k < kLoads; ++k) fetch(3, k, stage3);
+    }
+    wait_stage<(kStages - 1) * kLoads>();
 #pragma unroll
     for (int r = 0; r < kReads; ++r) read(one, r, stage0);
     int s = 0;
-    for (; s + 4 <= stages; s += 4) {
-        step(s, one, two, stage1, stage0);
-        step(s + 1, two, one, stage2, stage1);
-        step(s + 2, one, two, stage3, stage2);
-        step(s + 3, two, one, stage0, stage3);
+    if constexpr (kStages == 4) {
+        for (; s + 4 <= stages; s += 4) {
+            step(s, one, two, stage1, stage0);
+            step(s + 1, two, one, stage2, stage1);
+            step(s + 2, one, two, stage3, stage2);
+            step(s + 3, two, one, stage0, stage3);
+        }
+        if (s < stages) step(s, one, two, stage1, stage0);
+        if (s + 1 < stages) step(s + 1, two, one, stage2, stage1);
+        if (s + 2 < stages) step(s + 2, one, two, stage3, stage2);
+    } else {
+        for (; s + 6 <= stages; s += 6) {
+            step(s, one, two, stage1, stage0);
+            step(s + 1, two, one, stage2, stage1);
+            step(s + 2, one, two, stage0, stage2);
+            step(s + 3, two, one, stage1, stage0);
+            step(s + 4, one, two, stage2, stage1);
+            step(s + 5, two, one, stage0, stage2);
+        }
+        if (s < stages) step(s, one, two, stage1, stage0);
+        if (s + 1 < stages) step(s + 1, two, one, stage2, stage1);
+        if (s + 2 < stages) step(s + 2, one, two, stage0, stage2);
+        if (s + 3 < stages) step(s + 3, two, one, stage1, stage0);
+        if (s + 4 < stages) step(s + 4, one, two, stage2, stage1);
     }
-    if (s < stages) step(s, one, two, stage1, stage0);
-    if (s + 1 < stages) step(s + 1, two, one, stage2, stage1);
-    if (s + 2 < stages) step(s + 2, one, two, stage3, stage2);
     __syncthreads();   // no load is under way and shared memory is free
 
-    static_assert(32 * 33 * 4 <= kChunks * 1024, "a wavefront's block fits a stage");
-    float* turn = reinterpret_cast<float*>(wave == 0 ? stage0 : wave == 1 ? stage1 : wave == 2 ? stage2 : stage3);
+    static_assert(2 * 32 * 33 * 4 <= kChunks * 1024, "two wavefronts' blocks fit a stage");
+    float* turn = reinterpret_cast<float*>(wave < 2 ? stage0 : stage1) + (wave & 1) * 32 * 33;
     if (t.slot >= 0) {
         f32x4* o = reinterpret_cast<f32x4*>(a.slots) + slot_of<kWide>(t.slot, wave, lane);
 #pragma unroll
@@ -1000,13 +1019,20 @@ Launch deal(std::vector<Group> groups, bool may_cut) {
     // more: those few are cut.
     const int64_t fair = std::max<int64_t>(kLeastCut, up_to(work, kPlaces));
     const int64_t rest = tiles > kPlaces && tiles < 4 * kPlaces ? tiles % kPlaces : 0;
-    bool some = false;   // a joining launch there is then anyway
+    // Where most tiles are as long, a cut spares little of what the launch does at its end, and a joining
+    // launch has to be worth it; where a few are long, or there is one anyway, less will do.
+    int64_t long_work = 0;
+    bool some = false;
     for (const Group& g : groups)
-        for (const Tile& t : g.tiles) some = some || (may_cut && t.last - t.first - fair > kWorthCut);
+        for (const Tile& t : g.tiles) {
+            if (t.last - t.first > 2 * fair) long_work += t.last - t.first;
+            some = some || t.last - t.first - fair > kWorthCut;
+        }
+    const int64_t worth = 5 * long_work < 3 * work ? kWorthCut / 4 : some ? kWorthCut / 2 : kWorthCut;
     const auto parts_of = [&](const Tile& t, bool late) -> int32_t {
         const int64_t length = t.last - t.first;
         if (!may_cut) return 1;
-        if (length - fair > (some ? kWorthCut / 2 : kWorthCut)) return (int32_t)(length / fair);
+        if (length - fair > worth && length >= 2 * fair) return (int32_t)(length / fair);
         if (late && length > kWorthCut) return (int32_t)std::min(kPlaces / rest, length / kLeastCut);
         return 1;
     };
@@ -1077,7 +1103,7 @@ struct Steps {
     double eps;
 };
 
-template <int DT, bool kStep, int kWide>
+template <int DT, bool kStep, int kWide, int kStages>
 void run_products(const gmc_matrices* p, const Scratch& s, const Steps& how, ProductArgs a, hipStream_t st) {
     _Float16 *from = s.T0, *to = s.T1;
     a.slots = s.slots;
@@ -1097,21 +1123,21 @@ void run_products(const gmc_matrices* p, const Scratch& s, const Steps& how, Pro
         a.XTo = to;
         a.theta = s.theta + k;
         dim3 grid = take(p->gram);
-        matrix_product<kWide, kGram, GMC_F32><<<grid, 256, 0, st>>>(a);
+        matrix_product<kWide, kStages, kGram, GMC_F32><<<grid, 256, 0, st>>>(a);
         if (p->gram_join.n) {
             grid = take(p->gram_join);
             matrix_join<kWide, kGram><<<dim3(grid.x * kWide * kWide), 256, 0, st>>>(a);
         }
         grid = take(p->poly);
-        matrix_product<kWide, kPoly, GMC_F32><<<grid, 256, 0, st>>>(a);
+        matrix_product<kWide, kStages, kPoly, GMC_F32><<<grid, 256, 0, st>>>(a);
         if (p->poly_join.n) {
             grid = take(p->poly_join);
             matrix_join<kWide, kPoly><<<dim3(grid.x * kWide * kWide), 256, 0, st>>>(a);
         }
         grid = take(p->apply);
-        if (k + 1 < how.n) matrix_product<kWide, kApply, GMC_F32><<<grid, 256, 0, st>>>(a);
-        else if (kStep) matrix_product<kWide, kLastStep, GMC_F32><<<grid, 256, 0, st>>>(a);
-        else matrix_product<kWide, kLast, DT><<<grid, 256, 0, st>>>(a);
+        if (k + 1 < how.n) matrix_product<kWide, kStages, kApply, GMC_F32><<<grid, 256, 0, st>>>(a);
+        else if (kStep) matrix_product<kWide, kStages, kLastStep, GMC_F32><<<grid, 256, 0, st>>>(a);
+        else matrix_product<kWide, kStages, kLast, DT><<<grid, 256, 0, st>>>(a);
         std::swap(from, to);
     }
 }
@@ -1152,8 +1178,8 @@ void run_steps(const gmc_matrices* p, const Scratch& s, const Steps& how, const 
     matrix_norm<DT, kStep><<<dim3(p->norm.n), 256, 0, st>>>(n);
     n.tiles = p->pack.tiles;
     matrix_pack<DT, kStep><<<dim3(p->pack.n), 256, 0, st>>>(n);
-    if (p->wide == 2) run_products<DT, kStep, 2>(p, s, how, a, st);
-    else run_products<DT, kStep, 1>(p, s, how, a, st);
+    if (p->wide == 2) run_products<DT, kStep, 2, 4>(p, s, how, a, st);
+    else run_products<DT, kStep, 1, 3>(p, s, how, a, st);
 }
 
 }  // namespace
