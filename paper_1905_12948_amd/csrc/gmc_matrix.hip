@@ -321,50 +321,68 @@ __device__ __forceinline__ void finish_blocks(const ProductArgs& a, const Mat& m
     // d <- u (hi + lo) + v d
     const float u = kMode == kPoly ? a.b * (theta * theta) * (kScaleB / kScaleX) : a.a * ratio;
     const float v = kMode == kPoly ? a.c * (theta * theta) * (theta * theta) * (kScaleB / kScaleX / kScaleX) : ratio / kScaleB;
+    const auto inside = [&](int i, int j) { return ib0 + i < sides.rows && jb0 + j < sides.cols; };
+    // entry (i, j) where its row is j: block (jb, 2 ib + g / 2), lane col + 32 (g % 2), halves 4 half + e
+    const auto spot = [&](int i, int j) { return ((int64_t)(jb0 + j) * 2 * sides.rows + 2 * (ib0 + i)) * 1024 + col * 8 + 4 * half; };
+    // in the vector
+    const auto row = [](int e) { return 8 * (e >> 2) + (e & 3); };
+    const auto known = [&](int i, int j, int e) {
+        return ((ib0 + i + 1) * 32 <= m.rows || (ib0 + i) * 32 + 4 * half + row(e) < m.rows) &&
+               ((jb0 + j + 1) * 32 <= m.cols || (jb0 + j) * 32 + col < m.cols);
+    };
+    const auto where = [&](int i, int j) {
+        return m.offset + (int64_t)((ib0 + i) * 32 + 4 * half) * m.pitch + (jb0 + j) * 32 + col;
+    };
+    // all that is read before anything is written: a wait for each block's would follow the other's stores
+    constexpr bool kAdds = kMode != kGram, kParts = kMode == kLastStep;
+    f16x4 hi[kAdds ? kWide : 1][kAdds ? kWide : 1][4], lo[kAdds ? kWide : 1][kAdds ? kWide : 1][4];
+    float w[kParts ? kWide : 1][kParts ? kWide : 1][16];
+    if constexpr (kAdds) {
+        const _Float16* add = kMode == kPoly ? a.G + m.g * 1024 : flip ? a.X + m.x * 1024 : a.XT + m.x * 1024;
+#pragma unroll
+        for (int i = 0; i < kWide; ++i)
+#pragma unroll
+            for (int j = 0; j < kWide; ++j)
+                if (inside(i, j)) {
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        hi[i][j][g] = *reinterpret_cast<const f16x4*>(add + spot(i, j) + (g >> 1) * 1024 + (g & 1) * 256);
+                        lo[i][j][g] = *reinterpret_cast<const f16x4*>(add + spot(i, j) + (g >> 1) * 1024 + (g & 1) * 256 + 512);
+                    }
+                    if constexpr (kParts) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) w[i][j][e] = known(i, j, e) ? a.w[where(i, j) + row(e) * m.pitch] : 0.0f;
+                    }
+                }
+    }
 #pragma unroll
     for (int i = 0; i < kWide; ++i)
 #pragma unroll
         for (int j = 0; j < kWide; ++j) {
+            if (!inside(i, j)) continue;
             const int ib = ib0 + i, jb = jb0 + j;
-            if (ib >= sides.rows || jb >= sides.cols) continue;
+            const int64_t place = spot(i, j);
             f32x16 d = acc[i][j];
-            // entry (i, j) where its row is j: block (jb, 2 ib + g / 2), lane col + 32 (g % 2), halves 4 half + e
-            const int64_t place = ((int64_t)jb * 2 * sides.rows + 2 * ib) * 1024 + col * 8 + 4 * half;
             if constexpr (kMode == kGram) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) d[e] *= 1.0f / kScaleX;
             } else {
-                const _Float16* add = (kMode == kPoly ? a.G + m.g * 1024 : flip ? a.X + m.x * 1024 : a.XT + m.x * 1024) + place;
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const f16x4 hi = *reinterpret_cast<const f16x4*>(add + (g >> 1) * 1024 + (g & 1) * 256);
-                    const f16x4 lo = *reinterpret_cast<const f16x4*>(add + (g >> 1) * 1024 + (g & 1) * 256 + 512);
+                for (int g = 0; g < 4; ++g)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) d[4 * g + e] = __builtin_fmaf((float)hi[e], u, __builtin_fmaf((float)lo[e], u, v * d[4 * g + e]));
-                }
+                    for (int e = 0; e < 4; ++e)
+                        d[4 * g + e] = __builtin_fmaf((float)hi[i][j][g][e], u, __builtin_fmaf((float)lo[i][j][g][e], u, v * d[4 * g + e]));
             }
             if constexpr (kMode == kLast || kMode == kLastStep) {
                 typedef typename Elem<DT>::T T;
                 const float factor = a.alpha * m.scale * theta * (1.0f / kScaleX);
-                const int r0 = ib * 32 + 4 * half, c = jb * 32 + col;
-                const int64_t at = m.offset + (int64_t)r0 * m.pitch + c;
-                const bool whole = (ib + 1) * 32 <= m.rows && (jb + 1) * 32 <= m.cols;   // the same in all lanes
-                const auto row = [](int e) { return 8 * (e >> 2) + (e & 3); };
-                if constexpr (kMode == kLastStep) {
-                    float w[16];
 #pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        w[e] = whole || (r0 + row(e) < m.rows && c < m.cols) ? a.w[at + row(e) * m.pitch] : 0.0f;
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (whole || (r0 + row(e) < m.rows && c < m.cols))
-                            static_cast<float*>(a.out)[at + row(e) * m.pitch] = a.keep * w[e] + factor * d[e];
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (whole || (r0 + row(e) < m.rows && c < m.cols))
-                            static_cast<T*>(a.out)[at + row(e) * m.pitch] = Elem<DT>::down(factor * d[e]);
-                }
+                for (int e = 0; e < 16; ++e)
+                    if (known(i, j, e)) {
+                        const int64_t at = where(i, j) + row(e) * m.pitch;
+                        if constexpr (kMode == kLastStep) static_cast<float*>(a.out)[at] = a.keep * w[i][j][e] + factor * d[e];
+                        else static_cast<T*>(a.out)[at] = Elem<DT>::down(factor * d[e]);
+                    }
                 continue;
             }
             _Float16* o = (kMode == kGram ? a.Go + m.g * 1024 : kMode == kPoly ? a.Bo + m.g * 1024 : a.XTo + m.x * 1024) + place;
