@@ -356,6 +356,7 @@ __global__ __launch_bounds__(256) void score_join(ScoreArgs a) {
     __shared__ float lds[4];
     __shared__ float2 sums[4];
     __shared__ uint64_t keys[kJoinKeys], kept[kMostTop];
+    __shared__ int count;
     const int64_t i = blockIdx.x, r = i / a.T, t = i - r * a.T;
     const int64_t label = a.labels ? a.labels[r * a.label_pitch + t] : 0;
     if (a.labels && label == a.ignore) {
@@ -390,25 +391,43 @@ __global__ __launch_bounds__(256) void score_join(ScoreArgs a) {
         write_scores(a, i, m, s, u, xy);
     }
     if (!a.top) return;
-    // the largest so far and as many pieces' as fit beside them, until all have been looked at
+    // A piece's last key has `top` at or above it: of all keys those below the greatest of these are left out.
     const uint64_t* from = a.keys + i * a.pieces * a.top;
+    uint64_t least = 0;
+    for (int p = threadIdx.x; p < a.pieces; p += 256) {
+        const uint64_t key = from[(int64_t)p * a.top + a.top - 1];
+        least = key > least ? key : least;
+    }
+    least = wave_max(least);
+    if (lane == 0) keys[wave] = least;
+    if (threadIdx.x < kMostTop) kept[threadIdx.x] = 0;
+    if (threadIdx.x == 0) count = 0;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 4; ++w) least = keys[w] > least ? keys[w] : least;
+    // the largest so far and as many others as fit beside them, until all have been looked at
     const int64_t all = (int64_t)a.pieces * a.top;
     int have = 0;
-    if (threadIdx.x < kMostTop) kept[threadIdx.x] = 0;
     for (int64_t done = 0; done < all;) {
         const int fit = kJoinKeys - have, n = (int)(all - done < fit ? all - done : fit);
-        for (int c = threadIdx.x; c < have + n; c += 256) keys[c] = c < have ? kept[c] : from[done + c - have];
         __syncthreads();
         for (int c = threadIdx.x; c < have + n; c += 256) {
+            const uint64_t key = c < have ? kept[c] : from[done + c - have];
+            if (key && key >= least) keys[atomicAdd(&count, 1)] = key;
+        }
+        __syncthreads();
+        const int some = count;
+        for (int c = threadIdx.x; c < some; c += 256) {
             const uint64_t key = keys[c];
             int rank = 0;
 #pragma unroll 8
-            for (int o = 0; o < have + n; ++o) rank += keys[o] > key;
-            if (key && rank < a.top) kept[rank] = key;
+            for (int o = 0; o < some; ++o) rank += keys[o] > key;
+            if (rank < a.top) kept[rank] = key;
         }
-        have = have + n < a.top ? have + n : a.top;
-        done += n;
         __syncthreads();
+        if (threadIdx.x == 0) count = 0;
+        have = some < a.top ? some : a.top;
+        done += n;
     }
     if ((int)threadIdx.x < a.top) write_top(a, i, threadIdx.x, kept[threadIdx.x], m, s);
 }
@@ -527,25 +546,38 @@ __global__ __launch_bounds__(kThreads == 64 ? 256 : kThreads) void score_gradien
 
 // -- host -----------------------------------------------------------------------------
 
-// How a call's rows are cut.  Held rows: up to 8 vectors by each of 64, 256 or 512
+// How a call's rows are cut.  Held: up to 8 vectors by each of 64 (four rows a workgroup), 256 or 512
 // threads, or 13 by 512 or 1024.
 struct Cut {
     int threads, held, pieces;
     int32_t piece;
 };
 
-constexpr int64_t kHeldLines = 1024 * 13 * 16 / 128;
+constexpr int64_t kPlaces = 256;       // CUs
+constexpr int64_t kHeldLines = 512 * 13 * 16 / 128;  // of a piece: two such workgroups share a CU
+constexpr int64_t kShortPiece = 2048;  // vectors: of a row of a call with few
 
-Cut cut_rows(int32_t dtype, int64_t V) {
-    const int64_t b = type_size(dtype), vecs = V * b / 16;   // at most, whatever the alignment
-    Cut c = {vecs <= 64 * 8 ? 64 : vecs <= 256 * 8 ? 256 : vecs <= 512 * 13 ? 512 : 1024, vecs <= 512 * 8 ? 8 : 13, 1, (int32_t)V};
-    if (vecs > 1024 * 13) {
-        // whole lines, so that every piece begins where the row's own lines do
-        const int64_t lines = (V * b + 127) / 128, pieces = (lines + kHeldLines - 1) / kHeldLines;
-        c.piece = (int32_t)((lines + pieces - 1) / pieces * (128 / b));
-        c.pieces = (int)((V + c.piece - 1) / c.piece);
-    }
+Cut held_by(int64_t vecs, int pieces, int32_t piece) {
+    return {vecs <= 64 * 8 ? 64 : vecs <= 256 * 8 ? 256 : vecs <= 512 * 13 ? 512 : 1024, vecs <= 512 * 8 ? 8 : 13, pieces, piece};
+}
+
+// `pieces` of whole lines, so that every piece begins where the row's own lines do.
+Cut in_pieces(int64_t V, int64_t b, int64_t pieces) {
+    const int64_t lines = (V * b + 127) / 128, each = (lines + pieces - 1) / pieces;
+    const int32_t piece = (int32_t)(each * (128 / b));
+    Cut c = held_by(each * 8, (int)((V + piece - 1) / piece), piece);
+    if (c.threads == 64) c.threads = 256;
     return c;
+}
+
+// Rows too long to hold are cut, into more pieces where they leave CUs without one.
+Cut cut_rows(int32_t dtype, int64_t rows, int64_t V) {
+    const int64_t b = type_size(dtype), vecs = V * b / 16;   // at most, whatever the alignment
+    if (vecs <= 1024 * 13 || rows == 0) return held_by(vecs, 1, (int32_t)V);
+    int64_t pieces = ((V * b + 127) / 128 + kHeldLines - 1) / kHeldLines;
+    const int64_t more = rows < kPlaces ? kPlaces / rows : 1, most = vecs / kShortPiece;
+    if (pieces < more) pieces = more < most ? more : most;
+    return in_pieces(V, b, pieces);
 }
 
 template <int DT, bool kTop, bool kPieces>
@@ -571,7 +603,7 @@ int64_t gmc_token_scores_workspace(int32_t dtype, int64_t R, int64_t T, int64_t 
     if (!known_type(dtype) || R < 0 || T < 0 || V < 1 || V > 0x3fffffff || top < 0 || top > kMostTop || top > V) return -1;
     if (T > 0 && R > kMostRows / T) return -1;
     const int64_t rows = R * T;
-    const Cut c = cut_rows(dtype, V);
+    const Cut c = cut_rows(dtype, rows, V);
     return c.pieces == 1 ? 0 : rows * c.pieces * ((int64_t)sizeof(float4) + 8 * top);
 }
 
@@ -601,7 +633,7 @@ gmc_status gmc_token_scores(void* hip_stream, int32_t dtype, int64_t R, int64_t 
                {{logits_dev, rows_span(R, T, V, seq_pitch, tok_pitch, b)}, {labels_dev, rows_span(R, 1, T, label_pitch, 0, 8)}}))
         return op_error(GMC_EINVAL, me, "an output or the workspace overlaps another buffer");
     hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
-    const Cut c = cut_rows(dtype, V);
+    const Cut c = cut_rows(dtype, rows, V);
     ScoreArgs a{};
     a.logits = logits_dev;
     a.seq = seq_pitch;
@@ -687,10 +719,17 @@ gmc_status gmc_token_scores_backward(void* hip_stream, int32_t dtype, int64_t R,
     a.top_ids = top_ids_dev;
     a.dtop = dtop_dev;
     const int64_t vecs = V * b / 16;
+    if (rows < kPlaces && vecs > kShortPiece) {
+        const int64_t more = kPlaces / rows, most = vecs / (kShortPiece / 2);
+        const Cut c = in_pieces(V, b, more < most ? more : most);
+        a.piece = c.piece;
+        a.pieces = c.pieces;
+    }
+    const int64_t groups = rows * a.pieces;
     GMC_BY_TYPE(dtype, {
         if (vecs <= 64 * 8) score_gradient<DT, 64><<<dim3((unsigned)((rows + 3) / 4)), 256, 0, st>>>(a);
-        else if (vecs <= 2048) score_gradient<DT, 512><<<dim3((unsigned)rows), 512, 0, st>>>(a);
-        else score_gradient<DT, 1024><<<dim3((unsigned)rows), 1024, 0, st>>>(a);
+        else if (vecs <= 2048 || a.pieces > 1) score_gradient<DT, 512><<<dim3((unsigned)groups), 512, 0, st>>>(a);
+        else score_gradient<DT, 1024><<<dim3((unsigned)groups), 1024, 0, st>>>(a);
     });
     return op_launched(me);
 }
