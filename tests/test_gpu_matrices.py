@@ -92,6 +92,40 @@ def test_larger_matrices():
         assert torch.equal(out[o + r * c:o + r * c + 3], x[o + r * c:o + r * c + 3])
 
 
+@pytest.mark.parametrize("shapes", [
+    [(5, 9), (40, 10), (64, 64), (1, 1), (30, 70), (64, 200)],     # of one workgroup each, by their longest side
+    [(96, 160), (160, 96), (3, 3)], [(1, 600), (600, 1), (32, 32)], [(96, 161), (64, 64)],
+    [(3, 4)] * 300 + [(4, 3)] * 40, [(512, 4608), (512, 2304), (64, 576), (10, 512)],   # long contractions
+    [(1000, 2048), (64, 147), (128, 512)], [(300, 300), (64, 64), (1, 40)]])
+def test_several_matrices(shapes):
+    """Plans that take different ways through the launches, with and without momentum."""
+    import paper_1905_12948_amd as gmc
+    at, table = 1, []
+    for r, c in shapes:
+        table.append((at, r, c))
+        at += r * c + 1
+    g = torch.Generator(device="cuda:0").manual_seed(len(shapes))
+    x, w, v = (torch.randn(at, device="cuda:0", generator=g) for _ in range(3))
+    plan = gmc.Matrices(at, table)
+    out = gmc.orthogonalize(plan, x)
+    past, into = v.clone(), torch.empty_like(w)
+    gmc.orthogonal_step(plan, w, x, past, 0.5, mu=0.5, w_out=into)
+    outside = torch.ones(at, dtype=torch.bool, device="cuda:0")
+    for o, r, c in table:
+        outside[o:o + r * c] = False
+    assert torch.equal(out[outside], x[outside]) and torch.equal(past[outside], v[outside])
+    assert torch.equal(into[outside], w[outside] + x[outside])
+    inside = past - (0.5 * v + x)
+    assert (inside[~outside].abs() <= 4 * U * (v.abs() + x.abs())[~outside]).all()
+    for o, r, c in table[:8] + table[-1:]:
+        near(host(out[o:o + r * c]).reshape(r, c), host(x[o:o + r * c]).reshape(r, c), 1.0, (r, c))
+        u = (x + 0.5 * past)[o:o + r * c]
+        step = host(into[o:o + r * c]) - host(w[o:o + r * c])
+        want = 0.5 * ref.polar(host(u).reshape(r, c)).reshape(-1)
+        tol = 2 * ref.polar_spread(host(u).reshape(r, c), 2.0 ** -21) + 4 * U * np.linalg.norm(host(w[o:o + r * c]))
+        assert np.linalg.norm(step - want) <= tol + 4 * U * np.linalg.norm(want), (r, c)
+
+
 def test_columns_and_single_rows():
     """Column slices of one array, a narrower one between them, rows of the rest in the gaps."""
     import paper_1905_12948_amd as gmc

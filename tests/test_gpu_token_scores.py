@@ -341,6 +341,23 @@ def test_same_bits_streams_and_graphs(V):
         assert all(torch.equal(a, b) for a, b in zip(held, run()))
 
 
+@pytest.mark.parametrize("dtype,V,R", [("f32", 1_000_003, 1), ("bf16", 700_001, 2), ("f32", 200_000, 300)])
+def test_long_vocabularies(dtype, V, R):
+    """Rows in many pieces, whose keys the joining launch looks at in several turns; equal logits among them."""
+    g = torch.Generator(device="cuda:0").manual_seed(V)
+    x = (2 * torch.randn(R, 1, V, device="cuda:0", generator=g)).to(TYPES[dtype])
+    x[0, 0] = (x[0, 0] * 2).round() / 2
+    labels = torch.randint(0, V, (R, 1), device="cuda:0", generator=g)
+    if R > 8:
+        import paper_1905_12948_amd as gmc
+        got = [None if t is None else t[:8] for t in gmc.token_scores(x, labels, top=32)]
+        compare(x[:8], labels[:8], 1.0, 32, got)
+    else:
+        compare(x, labels, 1.0, 32)
+        x[0] = 1.5
+        compare(x, labels, 1.0, 32)
+
+
 def test_no_tokens_and_refusals():
     import paper_1905_12948_amd as gmc
     x = torch.randn(2, 3, 50, device="cuda:0")
