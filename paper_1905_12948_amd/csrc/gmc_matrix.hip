@@ -48,7 +48,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr float kScaleX = 0x1p13f, kScaleB = 0x1p10f;   // of X and G, and of b G + c G^2
 constexpr int kSide = 64;                                // side of the pieces the vector is read in
 constexpr int kParts = 1024;                             // partial sums of a matrix's squares
-constexpr int64_t kGapChunk = 8192;                      // components outside the matrices, a workgroup
+constexpr int64_t kGapChunk = 1024;                      // components outside the matrices, a workgroup
 constexpr int kMostSteps = 64;
 
 // A matrix of the plan.  m <= n are its sides, mb and nb their number in blocks of 32.
@@ -210,27 +210,34 @@ __global__ __launch_bounds__(256) void matrix_pack(VectorArgs a) {
     const Tile t = a.tiles[blockIdx.x];
     const Mat m = a.mats[t.mat];
     const T* x = static_cast<const T*>(a.x) + m.offset;
+    // piece (i, j) of X is piece (j, i) of a matrix on its side
+    const int pr = m.flip ? t.j : t.i, pc = m.flip ? t.i : t.j;
+    const int c0 = threadIdx.x & 63, r0 = threadIdx.x >> 6, c = pc * kSide + c0;
+    const bool there = c < m.cols;
+    float u[16], v[16];
+    // past the last row and column those are read again, and not used
+    const auto at = [&](int q) {
+        const int64_t r = (int64_t)pr * kSide + r0 + 4 * q;
+        return (r < m.rows ? r : (int64_t)m.rows - 1) * m.pitch + (there ? c : m.cols - 1);
+    };
+#pragma unroll
+    for (int q = 0; q < 16; ++q) u[q] = Elem<DT>::up(x[at(q)]);
+    if constexpr (kStep) {
+        if (a.momentum) {
+#pragma unroll
+            for (int q = 0; q < 16; ++q) v[q] = a.momentum[m.offset + at(q)];
+        }
+    }
     double sum = 0.0;
     for (int k = threadIdx.x; k < m.parts; k += 256) sum += a.part[m.part + k];
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = sum;
-    // piece (i, j) of X is piece (j, i) of a matrix on its side
-    const int pr = m.flip ? t.j : t.i, pc = m.flip ? t.i : t.j;
-    const int c0 = threadIdx.x & 63;
 #pragma unroll
     for (int q = 0; q < 16; ++q) {
-        const int r0 = (threadIdx.x >> 6) + 4 * q;
-        const int64_t r = (int64_t)pr * kSide + r0;
-        const int c = pc * kSide + c0;
-        float u = 0.0f;
-        if (r < m.rows && c < m.cols) {
-            const int64_t at = r * m.pitch + c;
-            u = Elem<DT>::up(x[at]);
-            if constexpr (kStep)
-                if (a.momentum) u = direction(a, u, a.momentum[m.offset + at]);
-        }
-        in[r0][c0] = u;
+        if constexpr (kStep)
+            if (a.momentum) u[q] = direction(a, u[q], v[q]);
+        in[r0 + 4 * q][c0] = there && (int64_t)pr * kSide + r0 + 4 * q < m.rows ? u[q] : 0.0f;
     }
     __syncthreads();
     const double norm = sqrt(lds[0] + lds[1] + lds[2] + lds[3]);
@@ -270,7 +277,10 @@ __global__ __launch_bounds__(256) void matrix_gaps(const Gap* gaps, const void* 
     typedef typename Elem<DT>::T T;
     const Gap g = gaps[blockIdx.x];
     const T* x = static_cast<const T*>(in) + g.at;
-    for (int64_t i = threadIdx.x; i < g.len; i += 256) {
+#pragma unroll
+    for (int k = 0; k < kGapChunk / 256; ++k) {
+        const int64_t i = threadIdx.x + 256 * k;
+        if (i >= g.len) return;
         if constexpr (kStep) static_cast<float*>(out)[g.at + i] = w[g.at + i] + Elem<DT>::up(x[i]);
         else static_cast<T*>(out)[g.at + i] = x[i];
     }
@@ -865,7 +875,7 @@ using namespace gmc;
 struct gmc_matrices {
     int64_t d = 0;
     int device = 0;
-    int wide = 1;              // blocks a wavefront's side of a tile
+    int wide = 1, even = 1;    // blocks a wavefront's side of a tile: of X's products, and of G's and its square's
     int32_t n = 0;
     int64_t blocks_x = 0, blocks_g = 0, parts = 0;
     int small = 0;             // every matrix is one workgroup's: their shorter sides' blocks
@@ -885,6 +895,11 @@ namespace gmc {
 namespace {
 
 constexpr int64_t kMostTiles = int64_t(1) << 22;
+// Tiles of 128 x 128 from which on they are taken: smaller ones read twice the bytes for each product, and
+// pay where they bring more CUs to work.  X's products: 2048 x 2048 (256 tiles) 52 us, by 64 x 64 ones more;
+// 3 of 768 x 768 (108) 16 us by 64 x 64.  G's and its square's: 2048 x 2048 (136) 40 us, by 64 x 64 50; ResNet-18's
+// matrices (about 60) 38 us and a join by 128 x 128, 22 by 64 x 64.
+constexpr int64_t kMany = 256, kManyEven = 100;
 constexpr int64_t kLeastCut = 8;     // blocks of 32 columns, of a part of a contraction
 constexpr int64_t kWorthCut = 48;    // by so many a tile is longer than its share for a cut to pay
 constexpr int64_t kTileCost = 4;     // what a tile costs besides, in such blocks
@@ -973,7 +988,7 @@ Scratch layout(const gmc_matrices* p, void* base) {
     s.B = reinterpret_cast<_Float16*>(take(p->blocks_g * 2048));
     s.part = reinterpret_cast<double*>(take(p->parts * 8));
     s.theta = reinterpret_cast<float*>(take(p->small ? 0 : (int64_t)p->n * (kMostSteps + 1) * 4));
-    s.slots = reinterpret_cast<float*>(take(p->slots * p->wide * p->wide * 16384));
+    s.slots = reinterpret_cast<float*>(take(p->slots * p->even * p->even * 16384));
     s.bytes = at - static_cast<char*>(base);
     return s;
 }
@@ -1121,7 +1136,19 @@ struct Steps {
     double eps;
 };
 
-template <int DT, bool kStep, int kWide, int kStages>
+// Two kernels of products: tiles of 128 x 128, and of 64 x 64 where there are few.
+template <int kMode, int DT>
+void run_product(int wide, dim3 grid, const ProductArgs& a, hipStream_t st) {
+    if (wide == 2) matrix_product<2, 4, kMode, DT><<<grid, 256, 0, st>>>(a);
+    else matrix_product<1, 3, kMode, DT><<<grid, 256, 0, st>>>(a);
+}
+template <int kMode>
+void run_join(int wide, dim3 grid, const ProductArgs& a, hipStream_t st) {
+    if (wide == 2) matrix_join<2, kMode><<<dim3(grid.x * 4), 256, 0, st>>>(a);
+    else matrix_join<1, kMode><<<grid, 256, 0, st>>>(a);
+}
+
+template <int DT, bool kStep>
 void run_products(const gmc_matrices* p, const Scratch& s, const Steps& how, ProductArgs a, hipStream_t st) {
     _Float16 *from = s.T0, *to = s.T1;
     a.slots = s.slots;
@@ -1141,21 +1168,21 @@ void run_products(const gmc_matrices* p, const Scratch& s, const Steps& how, Pro
         a.XTo = to;
         a.theta = s.theta + k;
         dim3 grid = take(p->gram);
-        matrix_product<kWide, kStages, kGram, GMC_F32><<<grid, 256, 0, st>>>(a);
+        run_product<kGram, GMC_F32>(p->even, grid, a, st);
         if (p->gram_join.n) {
             grid = take(p->gram_join);
-            matrix_join<kWide, kGram><<<dim3(grid.x * kWide * kWide), 256, 0, st>>>(a);
+            run_join<kGram>(p->even, grid, a, st);
         }
         grid = take(p->poly);
-        matrix_product<kWide, kStages, kPoly, GMC_F32><<<grid, 256, 0, st>>>(a);
+        run_product<kPoly, GMC_F32>(p->even, grid, a, st);
         if (p->poly_join.n) {
             grid = take(p->poly_join);
-            matrix_join<kWide, kPoly><<<dim3(grid.x * kWide * kWide), 256, 0, st>>>(a);
+            run_join<kPoly>(p->even, grid, a, st);
         }
         grid = take(p->apply);
-        if (k + 1 < how.n) matrix_product<kWide, kStages, kApply, GMC_F32><<<grid, 256, 0, st>>>(a);
-        else if (kStep) matrix_product<kWide, kStages, kLastStep, GMC_F32><<<grid, 256, 0, st>>>(a);
-        else matrix_product<kWide, kStages, kLast, DT><<<grid, 256, 0, st>>>(a);
+        if (k + 1 < how.n) run_product<kApply, GMC_F32>(p->wide, grid, a, st);
+        else if constexpr (kStep) run_product<kLastStep, GMC_F32>(p->wide, grid, a, st);
+        else run_product<kLast, DT>(p->wide, grid, a, st);
         std::swap(from, to);
     }
 }
@@ -1196,8 +1223,7 @@ void run_steps(const gmc_matrices* p, const Scratch& s, const Steps& how, const 
     matrix_norm<DT, kStep><<<dim3(p->norm.n), 256, 0, st>>>(n);
     n.tiles = p->pack.tiles;
     matrix_pack<DT, kStep><<<dim3(p->pack.n), 256, 0, st>>>(n);
-    if (p->wide == 2) run_products<DT, kStep, 2, 4>(p, s, how, a, st);
-    else run_products<DT, kStep, 1, 3>(p, s, how, a, st);
+    run_products<DT, kStep>(p, s, how, a, st);
 }
 
 }  // namespace
@@ -1233,7 +1259,7 @@ gmc_status gmc_matrices_init(gmc_matrices** out, int64_t d, int32_t n, const int
         p->d = d;
         p->n = n;
         std::vector<Mat> mats;
-        int64_t large = 0;
+        int64_t large = 0, large_even = 0;   // tiles of 128 x 128
         for (int32_t k = 0; k < n; ++k) {
             const Part& q = parts[k];
             Mat m{};
@@ -1252,9 +1278,11 @@ gmc_status gmc_matrices_init(gmc_matrices** out, int64_t d, int32_t n, const int
             p->blocks_x += (int64_t)m.mb * m.nb * 2;
             p->blocks_g += (int64_t)m.mb * m.mb * 2;
             large += up_to(m.mb, 4) * up_to(m.nb, 4);
+            large_even += up_to(m.mb, 4) * (up_to(m.mb, 4) + 1) / 2;
             mats.push_back(m);
         }
-        p->wide = large >= 256 ? 2 : 1;
+        p->wide = large >= kMany ? 2 : 1;
+        p->even = large_even >= kManyEven ? 2 : 1;
         // matrices of another number of rows in blocks are padded to the most of them
         int most = 0, wide = 0;
         for (const Mat& m : mats) most = std::max(most, m.mb), wide = std::max(wide, m.nb);
@@ -1262,7 +1290,7 @@ gmc_status gmc_matrices_init(gmc_matrices** out, int64_t d, int32_t n, const int
             p->small = most;
             for (Mat& m : mats) m.mb = most, m.nb = std::max(m.nb, most);
         }
-        const int side = 2 * p->wide;
+        const int side = 2 * p->wide, even = 2 * p->even;
         std::vector<Tile> norm, pack;
         std::vector<Group> grams, polys, applies;
         int64_t tiles = 0;
@@ -1287,27 +1315,25 @@ gmc_status gmc_matrices_init(gmc_matrices** out, int64_t d, int32_t n, const int
             for (int32_t i = 0; i < mp; ++i)
                 for (int32_t j = 0; j < np; ++j) pack.push_back({k, i, j, 1, 0, 0, -1, 0});
             // groups of up to 8 x 8 tiles, smaller ones where there are few tiles to deal out
-            const int32_t high = std::min(mt, tiles > 2048 ? 8 : 4), broad = tiles > 2048 ? 8 : 4;
-            for (int32_t i0 = 0; i0 < mt; i0 += high)
-                for (int32_t j0 = 0; j0 < nt; j0 += broad) {
-                    Group gram, poly, apply;
-                    for (int32_t j = j0; j < std::min(j0 + broad, nt); ++j)
-                        for (int32_t i = i0; i < std::min(i0 + high, mt); ++i) {
-                            apply.tiles.push_back({k, i, j, 1, 0, m.mb, -1, 0});
-                            if (j > i) continue;
+            const int32_t most = tiles > 2048 ? 8 : 4, et = (m.mb + even - 1) / even;
+            for (int32_t i0 = 0; i0 < mt; i0 += most)
+                for (int32_t j0 = 0; j0 < nt; j0 += most) {
+                    Group g;
+                    for (int32_t j = j0; j < std::min(j0 + most, nt); ++j)
+                        for (int32_t i = i0; i < std::min(i0 + most, mt); ++i) g.tiles.push_back({k, i, j, 1, 0, m.mb, -1, 0});
+                    applies.push_back(std::move(g));
+                }
+            for (int32_t i0 = 0; i0 < et; i0 += most)
+                for (int32_t j0 = 0; j0 <= i0; j0 += most) {
+                    Group gram, poly;
+                    for (int32_t j = j0; j < std::min(j0 + most, et); ++j)
+                        for (int32_t i = std::max(i0, j); i < std::min(i0 + most, et); ++i) {
                             gram.tiles.push_back({k, i, j, 1, 0, m.nb, -1, 0});
                             poly.tiles.push_back({k, i, j, 1, 0, m.mb, -1, 0});
                         }
-                    if (!gram.tiles.empty()) {
-                        grams.push_back(std::move(gram));
-                        polys.push_back(std::move(poly));
-                    }
-                    applies.push_back(std::move(apply));
+                    grams.push_back(std::move(gram));
+                    polys.push_back(std::move(poly));
                 }
-        }
-        if (many) {
-            delete p;
-            return op_error(GMC_EINVAL, me, "more than 2^22 tiles");
         }
         // components between the matrices' rows
         std::vector<std::pair<int64_t, int64_t>> spans;
