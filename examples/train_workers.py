@@ -2,13 +2,15 @@
 operators of a worker's pass: an encoder of channels-last images (group norm
 with its activation, dropout joined to the residual stream) and a token head,
 first on pairs of captions (preference loss), then on its own rollouts (clipped
-policy loss with a KL term to the model the pairs left).
+policy loss with a KL term to the model the pairs left; the rollouts' log-probabilities
+and entropies are the tokens' scores).
 
 Each worker has images of its own few classes (non-IID) and masks of its own; the
 gradients of all K workers go into gmc_iteration, which compresses them and updates
-the shared parameters.
+the shared parameters.  With --orthogonal the server takes the sum of the messages
+through a momentum of its own and orthogonalises the weight matrices' part of it.
 
-    python examples/train_workers.py
+    python examples/train_workers.py [--orthogonal]
 """
 import math
 import os
@@ -94,25 +96,60 @@ def gradient_row(p):
     return torch.cat([v.grad.reshape(-1) for v in p.values()])
 
 
-def train(pair_steps=40, policy_steps=40, device="cuda:0", log=print):
+class Server:
+    """The server's side: gmc_iteration, or the messages' sum through orthogonal_step."""
+
+    def __init__(self, w, orthogonal):
+        self.w, self.w_prev, self.err = w, w.clone(), torch.zeros(K, len(w), device=w.device)
+        # the server's momentum is the only one where it orthogonalises
+        self.gmc = gmc.Gmc(len(w), K, "topk", ratio=0.05, beta=0.0 if orthogonal else 0.5, eta=1.0 if orthogonal else 0.5)
+        self.message = self.gmc.alloc_messages(w.device)
+        self.plan = None
+        if orthogonal:
+            table, at = [], 0
+            for name, shape in SHAPES.items():
+                if name in ("stem", "mix", "head"):
+                    table.append((at, *shape))
+                at += math.prod(shape)
+            self.plan = gmc.Matrices(len(w), table, device=w.device)
+            self.update, self.momentum = torch.empty_like(w), torch.zeros_like(w)
+
+    def step(self, grads):
+        if self.plan is None:
+            self.gmc.iteration(self.w, self.w_prev, grads, self.err, *self.message)
+        else:
+            self.gmc.step(self.w, self.w_prev, grads, self.err, *self.message)
+            self.gmc.aggregate(*self.message, self.update)
+            gmc.orthogonal_step(self.plan, self.w, self.update, self.momentum, 0.02, mu=0.9, w_out=self.w_prev)
+        self.w, self.w_prev = self.w_prev, self.w
+
+    def close(self):
+        self.gmc.close()
+        if self.plan is not None:
+            self.plan.close()
+
+
+def policy_gradient(logits, tokens, old, advantage, ref, scores, bonus):
+    """The logits' gradient of the clipped policy loss with a KL term, less bonus times the mean
+    entropy; scores: gmc.token_scores of the same logits and tokens, for the bonus."""
+    grad = gmc.policy_loss(logits, tokens, old, advantage, ref_logp=ref, kl_coef=0.01)[2]
+    if bonus:
+        share = torch.full(tokens.shape, -bonus / tokens.numel(), device=logits.device)
+        grad += gmc.token_scores_backward(logits, scores[4], tokens, entropy=scores[1], dentropy=share)
+    return grad
+
+
+def train(pair_steps=40, policy_steps=40, device="cuda:0", log=print, orthogonal=False, bonus=0.0):
     """(first and last preference loss, first and last mean reward of the rollouts)."""
     task = Task(device)
-    d = sum(math.prod(s) for s in SHAPES.values())
     w = torch.cat([(torch.ones(s, device=device) if name == "gamma" else
                     torch.zeros(s, device=device) if name == "beta" else
                     torch.randn(s, device=device, generator=task.g) / math.sqrt(s[0])).reshape(-1)
                    for name, s in SHAPES.items()])
-    w_prev, err = w.clone(), torch.zeros(K, d, device=device)
-    server = gmc.Gmc(d, K, "topk", ratio=0.05, beta=0.5, eta=0.5)
-    message = server.alloc_messages(device)
-
-    def step(grads):
-        nonlocal w, w_prev
-        server.iteration(w, w_prev, grads, err, *message)
-        w, w_prev = w_prev, w
+    server = Server(w, orthogonal)
 
     # 1. pairs: the class's caption is preferred to a random one
-    frozen = parameters(w.clone())
+    frozen = parameters(server.w.clone())
     losses = []
     for t in range(pair_steps):
         rows, total = [], 0.0
@@ -122,24 +159,24 @@ def train(pair_steps=40, policy_steps=40, device="cuda:0", log=print):
             tokens, images = torch.cat([chosen, rejected]), torch.cat([images, images])
             with torch.no_grad():
                 ref = gmc.preference_loss(logits_of(frozen, images, tokens).contiguous(), tokens, grad=False)[3]
-            p = parameters(w)
+            p = parameters(server.w)
             logits = logits_of(p, images, tokens, t, k)
             loss, _, _, _, grad = gmc.preference_loss(logits.detach(), tokens, ref, beta=0.5)
             logits.backward(grad)
             rows.append(gradient_row(p))
             total += loss.item() / K
         losses.append(total)
-        step(torch.stack(rows))
+        server.step(torch.stack(rows))
     log("preference loss %.4f -> %.4f over %d iterations" % (losses[0], losses[-1], pair_steps))
 
     # 2. rollouts: reward for every token of the caption
-    frozen = parameters(w.clone())
-    rewards = []
+    frozen = parameters(server.w.clone())
+    rewards, entropies = [], []
     for t in range(policy_steps):
-        rows, total = [], 0.0
+        rows, total, spread = [], 0.0, 0.0
         for k in range(K):
             images, caption = task.batch(k)
-            p = parameters(w)
+            p = parameters(server.w)
             with torch.no_grad():
                 tokens = torch.zeros_like(caption)
                 for j in range(T):
@@ -148,19 +185,23 @@ def train(pair_steps=40, policy_steps=40, device="cuda:0", log=print):
                 hit = (tokens == caption).float()
                 advantage = (hit - hit.mean()) / (hit.std() + 0.05)
                 # the rollouts' and the frozen model's log-probabilities
-                old = gmc.policy_loss(logits_of(p, images, tokens), tokens, None, advantage, grad=False)[1]
-                ref = gmc.policy_loss(logits_of(frozen, images, tokens), tokens, None, advantage, grad=False)[1]
+                old = gmc.token_scores(logits_of(p, images, tokens), tokens)[0]
+                ref = gmc.token_scores(logits_of(frozen, images, tokens), tokens)[0]
             logits = logits_of(p, images, tokens, pair_steps + t, k)
-            _, _, grad = gmc.policy_loss(logits.detach(), tokens, old, advantage, ref_logp=ref, kl_coef=0.01)
-            logits.backward(grad)
+            seen = logits.detach()
+            scores = gmc.token_scores(seen, tokens)
+            spread += scores[1].mean().item() / K
+            logits.backward(policy_gradient(seen, tokens, old, advantage, ref, scores, bonus))
             rows.append(gradient_row(p))
             total += hit.mean().item() / K
         rewards.append(total)
-        step(torch.stack(rows))
-    log("caption tokens right %.3f -> %.3f over %d iterations" % (rewards[0], rewards[-1], policy_steps))
+        entropies.append(spread)
+        server.step(torch.stack(rows))
+    log("caption tokens right %.3f -> %.3f, entropy %.3f -> %.3f over %d iterations"
+        % (rewards[0], rewards[-1], entropies[0], entropies[-1], policy_steps))
     server.close()
     return losses[0], losses[-1], rewards[0], rewards[-1]
 
 
 if __name__ == "__main__":
-    train()
+    train(orthogonal="--orthogonal" in sys.argv[1:])
