@@ -742,7 +742,7 @@ gmc_status gmc_token_scores_backward(void* hip_stream, int32_t dtype, int64_t R,
  * captured, and has to live as long as the graphs that were captured with it.
  *   d <= 2^40; 0 to 8192 matrices of 1 to 2^26 rows and columns, and no more than
  *   2^22 tiles of 64 x 64 (more than any vector of 2^34 components in dense
- *   matrices of 64 rows and columns or more)
+ *   matrices of 64 rows and columns or more), nor 2^23 rows with a pitch of their own
  */
 typedef struct gmc_matrices gmc_matrices;
 gmc_status gmc_matrices_init(gmc_matrices** out, int64_t d, int32_t n, const int64_t* offset, const int64_t* rows,
@@ -764,7 +764,8 @@ int64_t gmc_matrices_workspace(const gmc_matrices* plan);
  *   x_dev, out_dev  d components of a GMC_F32, GMC_BF16 or GMC_F16 type; out_dev may be x_dev
  *   steps           1 to 64; coefficients: host array [steps][3], finite, such that no singular
  *                   value in [0, 1] is taken beyond 2.5 by a step (the last one: 10^6), and
- *                   b s^2 + c s^4 stays within 60
+ *                   b s^2 + c s^4 stays within 60, and no step before the last takes all of
+ *                   them below 0.25 (what a later step amplified would have lost its bits)
  *   eps in [0, 1]; alpha finite in fp32
  */
 gmc_status gmc_orthogonalize(void* hip_stream, const gmc_matrices* plan, int32_t dtype, const void* x_dev, void* out_dev,

@@ -48,7 +48,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr float kScaleX = 0x1p13f, kScaleB = 0x1p10f;   // of X and G, and of b G + c G^2
 constexpr int kSide = 64;                                // side of the pieces the vector is read in
 constexpr int kParts = 1024;                             // partial sums of a matrix's squares
-constexpr int64_t kGapChunk = 1024;                      // components outside the matrices, a workgroup
+constexpr int64_t kGapChunk = 1024;                      // components outside the matrices, a workgroup (more in long vectors)
 constexpr int kMostSteps = 64;
 
 // A matrix of the plan.  m <= n are its sides, mb and nb their number in blocks of 32.
@@ -277,10 +277,8 @@ __global__ __launch_bounds__(256) void matrix_gaps(const Gap* gaps, const void* 
     typedef typename Elem<DT>::T T;
     const Gap g = gaps[blockIdx.x];
     const T* x = static_cast<const T*>(in) + g.at;
-#pragma unroll
-    for (int k = 0; k < kGapChunk / 256; ++k) {
-        const int64_t i = threadIdx.x + 256 * k;
-        if (i >= g.len) return;
+#pragma unroll 4
+    for (int64_t i = threadIdx.x; i < g.len; i += 256) {
         if constexpr (kStep) static_cast<float*>(out)[g.at + i] = w[g.at + i] + Elem<DT>::up(x[i]);
         else static_cast<T*>(out)[g.at + i] = x[i];
     }
@@ -478,7 +476,7 @@ __global__ __launch_bounds__(256, kStages == 4 ? 2 : 3) void matrix_product(Prod
         int rb = (side ? sides.j : sides.i) * kBlocks + b;
         const int most = (side ? sides.cols : sides.rows) - 1;
         rb = rb < most ? rb : most;
-        from[k] = (side ? Q : P) + rb * row + t.first * 2048 + (c % (2 * kDeep)) * 512 + lane * 8;
+        from[k] = (side ? Q : P) + rb * row + (int64_t)t.first * 2048 + (c % (2 * kDeep)) * 512 + lane * 8;
     }
     f32x16 acc[kWide][kWide];
 #pragma unroll
@@ -621,7 +619,7 @@ struct SmallArgs {
 constexpr int kSmallThreads = 1024, kSmallBlocks = 39;   // 4 KB each of 160 KB: X, X^T and G of 32 x 32 blocks
 
 // Matrices of which X, X^T and G fit the shared memory of one CU: all steps in one launch, a workgroup a
-// matrix, a wavefront every eighth block of what a phase computes.  The polynomial takes G's place, and
+// matrix, a wavefront every sixteenth block of what a phase computes.  The polynomial takes G's place, and
 // X its own, once all have read them.  X and X^T are both computed, the second by the products of the first
 // with their sides exchanged: a block's entries then go to either as 8 bytes a lane, where turning it
 // takes 32 writes of 2 bytes, which cost more than the products.  What shared memory is left takes the parts
@@ -931,10 +929,10 @@ bool disjoint(std::vector<Part> p) {
     return true;
 }
 
-// The largest |x| and |b x^2 + c x^4| that singular values in [0, top] are taken to,
-// or a negative number where one is not finite.
+// Over singular values s in [0, top] the largest they are taken to, and the largest |b s^2 + c s^4| and
+// |a + b s^2 + c s^4|; infinite where one is not finite.
 struct Reach {
-    double x, poly, growth;   // growth: the largest |a + b x^2 + c x^4|
+    double x, poly, growth;
 };
 
 Reach reach(double a, double b, double c, double top) {
@@ -1008,6 +1006,8 @@ gmc_status matrices_check(const char* me, const gmc_matrices* p, int32_t dtype, 
         // X and G by 2^13 and the polynomial by 2^10 have to stay below f16's 65504
         if (!(r.x <= 2.5 && r.poly <= 60.0) && !(k == steps - 1 && r.x <= 1e6 && r.poly <= 60.0))
             return op_error(GMC_EINVAL, me, "the coefficients take a singular value beyond 2.5");
+        // values are kept to 2^-37 of 1, and a later step may not take that for more than it is
+        if (!(r.x >= 0.25) && k < steps - 1) return op_error(GMC_EINVAL, me, "the coefficients take every singular value below 0.25");
         top = r.x;
     }
     int device = -1;
@@ -1303,7 +1303,13 @@ gmc_status gmc_matrices_init(gmc_matrices** out, int64_t d, int32_t n, const int
             many = many || tiles > kMostTiles;
             if (many) break;
         }
-        for (int32_t k = 0; k < n && !many; ++k) {
+        int64_t spread = 0;   // rows that are apart
+        for (const Part& q : parts) spread += q.pitch == q.cols ? 1 : q.rows;
+        if (many || spread > 2 * kMostTiles) {
+            delete p;
+            return op_error(GMC_EINVAL, me, many ? "the matrices have more tiles than a launch takes" : "too many rows that are apart");
+        }
+        for (int32_t k = 0; k < n; ++k) {
             Mat& m = mats[k];
             const int32_t mt = (m.mb + side - 1) / side, nt = (m.nb + side - 1) / side;
             const int64_t mp = up_to(m.m, kSide), np = up_to(m.n, kSide), each = up_to(mp * np, kParts);
@@ -1344,16 +1350,17 @@ gmc_status gmc_matrices_init(gmc_matrices** out, int64_t d, int32_t n, const int
         }
         std::sort(spans.begin(), spans.end());
         std::vector<Gap> gap;
-        int64_t at = 0;
+        int64_t at = 0, chunk = kGapChunk;
+        while (d / chunk > kMostTiles / 4) chunk *= 2;
         const auto between = [&](int64_t to) {
-            for (; at < to; at += kGapChunk) gap.push_back({at, std::min(kGapChunk, to - at)});
+            for (; at < to; at += chunk) gap.push_back({at, std::min(chunk, to - at)});
         };
         for (const auto& q : spans) {
             between(q.first);
             at = q.first + q.second;
         }
         between(d);
-        if ((int64_t)gap.size() > 4 * kMostTiles) {
+        if ((int64_t)gap.size() > 2 * kMostTiles) {
             delete p;
             return op_error(GMC_EINVAL, me, "too many pieces outside the matrices");
         }

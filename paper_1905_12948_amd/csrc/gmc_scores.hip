@@ -604,6 +604,7 @@ int64_t gmc_token_scores_workspace(int32_t dtype, int64_t R, int64_t T, int64_t 
     if (T > 0 && R > kMostRows / T) return -1;
     const int64_t rows = R * T;
     const Cut c = cut_rows(dtype, rows, V);
+    if (rows > kMostRows / c.pieces) return -1;   // more than a launch has (and than any memory holds)
     return c.pieces == 1 ? 0 : rows * c.pieces * ((int64_t)sizeof(float4) + 8 * top);
 }
 
@@ -623,6 +624,7 @@ gmc_status gmc_token_scores(void* hip_stream, int32_t dtype, int64_t R, int64_t 
     if (!entropy_dev || !norm_dev || (labels_dev && !logp_dev) || (top && (!top_logp_dev || !top_ids_dev)))
         return op_error(GMC_EINVAL, me, "NULL argument");
     const int64_t rows = R * T, need = gmc_token_scores_workspace(dtype, R, T, V, top), b = type_size(dtype);
+    if (need < 0) return op_error(GMC_EINVAL, me, "more rows and pieces of rows than a launch has");
     if (need && (!workspace_dev || workspace_bytes < need)) return op_error(GMC_EINVAL, me, "the workspace is too small");
     if (need && (reinterpret_cast<uintptr_t>(workspace_dev) & 15u))
         return op_error(GMC_EINVAL, me, "the workspace is not 16-byte aligned");

@@ -110,13 +110,14 @@ def orthogonalize(plan: Matrices, x, out=None, steps: int = STEPS, coefficients=
     """x (flat, fp32, bf16 or fp16) with every matrix M of the plan replaced by alpha *
     scale * X, X what ``steps`` steps X <- a X + b (X X^T) X + c (X X^T)^2 X make of
     M / (|M| + eps); the other components as they are.  ``coefficients``: (a, b, c), or
-    one such a step.  ``out`` may be x."""
+    one such a step.  ``out`` may be x; a new one has the plan's number of components where x
+    has more."""
     plan = _plan_of(plan)
     torch = _torch()
     code, px = _typed(plan, x, "x")
     steps, c = _steps(steps, coefficients)
     if out is None:
-        out = torch.empty_like(x)
+        out = torch.empty_like(x) if x.numel() == plan.d else x.new_empty(plan.d)
         po = out.data_ptr()
     else:
         co, po = _typed(plan, out, "out")

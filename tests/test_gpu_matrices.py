@@ -260,6 +260,37 @@ def test_step_without_matrices_is_apply():
     assert torch.equal(gmc.orthogonalize(plan, w), w)
 
 
+def test_vectors_longer_than_the_plan():
+    """What lies behind the plan's components stays as it is; a new result has the plan's."""
+    import paper_1905_12948_amd as gmc
+    d = 40 * 30 + 5
+    x, w, m = (torch.randn(d + 100, device="cuda:0") for _ in range(3))
+    plan = gmc.Matrices(d, [(0, 40, 30)])
+    out = gmc.orthogonalize(plan, x)
+    assert out.shape == (d,)
+    into = torch.full((d + 60,), 3.0, device="cuda:0")
+    gmc.orthogonalize(plan, x, out=into)
+    assert torch.equal(into[:d], out) and (into[d:] == 3).all()
+    shaped = gmc.orthogonalize(plan, x[:d].view(5, 241))
+    assert shaped.shape == (5, 241) and torch.equal(shaped.reshape(-1), out)
+    before = m.clone()
+    into.fill_(3.0)
+    gmc.orthogonal_step(plan, w, x, m, 0.1, w_out=into)
+    assert (into[d:] == 3).all() and torch.equal(m[1200:], before[1200:])
+
+
+def test_long_vector_without_matrices_in_most_of_it():
+    import paper_1905_12948_amd as gmc
+    d = (1 << 30) + 12345
+    x = torch.ones(d, device="cuda:0", dtype=torch.float16)
+    x[77:77 + 900] = torch.randn(900, device="cuda:0").half()
+    plan = gmc.Matrices(d, [(77, 30, 30), (d - 5, 1, 5)])
+    out = gmc.orthogonalize(plan, x)
+    near(host(out[77:977]).reshape(30, 30), host(x[77:977]).reshape(30, 30), 1.0, "first", "f16")
+    near(host(out[-5:]).reshape(1, 5), host(x[-5:]).reshape(1, 5), 1.0, "last", "f16")
+    assert (out[:77] == 1).all() and (out[977:-5] == 1).all()
+
+
 def test_same_bits_streams_and_graphs():
     """The same bits twice, on a side stream, and in two graphs that share a plan and are replayed in
     turn with other inputs between eager calls."""
@@ -307,6 +338,23 @@ def test_far_offsets():
     assert (x[:far] == 0).all() and (x[-2:] == 0).all()
 
 
+def test_one_row_of_the_most_columns():
+    """Parts of G's sum lie beyond 32 bits of halves.  With 1.5 - 0.5 s^2 a singular value of
+    1 stays, and an error of G counts half: of 2^26 squares summed in 512 parts, 16 to a step, at most (8192 + 512)
+    2^-24, once a step (the slope at 1 is 0)."""
+    import paper_1905_12948_amd as gmc
+    d = 1 << 26
+    x = torch.randn(d, device="cuda:0", generator=torch.Generator("cuda:0").manual_seed(5)).half()
+    plan = gmc.Matrices(d, [(0, 1, d)])
+    out = gmc.orthogonalize(plan, x, steps=2, coefficients=(1.5, -0.5, 0.0))
+    want = x.double() / x.double().norm()
+    # halves below 2^-14 round to multiples of 2^-24
+    error = (out.double() - want).abs() - want.abs() * (0.5 * 8704 * 2.0 ** -24 * 1.1 + 2.0 ** -11 + 2.0 ** -20) - 2.0 ** -25
+    assert (error <= 0).all(), float(error.max())
+    del plan, out, want, error
+    torch.cuda.empty_cache()
+
+
 def test_refusals():
     import paper_1905_12948_amd as gmc
     d = 64
@@ -320,6 +368,8 @@ def test_refusals():
         (lambda: gmc.orthogonalize(plan, x, steps=65), ValueError), (lambda: gmc.orthogonalize(plan, x, coefficients=(1, 2)), ValueError),
         (lambda: gmc.orthogonalize(plan, x, steps=2, coefficients=[(1.0, 0.0, 0.0)]), ValueError),
         (lambda: gmc.orthogonalize(plan, x, coefficients=(3.0, 0.0, 0.0)), RuntimeError),       # grows beyond 2.5
+        (lambda: gmc.orthogonalize(plan, x, steps=2, coefficients=[(0.2, 0.0, 0.0), (2.0, -1.0, 0.0)]), RuntimeError),   # below 0.25
+        (lambda: gmc.orthogonalize(plan, x, steps=2, coefficients=[(0.0, 0.0, 0.0), (1e300, 0.0, 0.0)]), RuntimeError),
         (lambda: gmc.orthogonalize(plan, x, coefficients=(1.0, -61.0, 0.0)), RuntimeError),
         (lambda: gmc.orthogonalize(plan, x, coefficients=(math.nan, 0.0, 0.0)), RuntimeError),
         (lambda: gmc.orthogonalize(plan, x, eps=-1.0), RuntimeError), (lambda: gmc.orthogonalize(plan, x, eps=math.nan), RuntimeError),

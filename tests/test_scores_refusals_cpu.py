@@ -58,6 +58,7 @@ BOTH = [
 
 @pytest.mark.parametrize("change,needle", BOTH + [
     (dict(V=4, tok=4, seq=16), "top must"), (dict(entropy=None), "NULL"), (dict(logp=None), "NULL"), (dict(top_logp=None), "NULL"),
+    (dict(R=1 << 21, T=1, V=1 << 29, tok=1 << 29, seq=1 << 29), "than a launch has"),
     (dict(ws=None), "workspace"), (dict(n=100), "workspace"), (dict(ws=PLACE["ws"] + 8), "aligned"),
 ])
 def test_forward(lib, change, needle):
@@ -105,7 +106,7 @@ def test_workspaces(lib):
     assert size(F32, 0, 4, 200000, 5) == 0 and size(F32, 1 << 40, 0, 200000, 5) == 0
     assert size(F32, 100, 10, 1000000, 8) > 1000 * 16
     for bad in ((3, 4, 4, 100, 5), (F32, -1, 4, 100, 5), (F32, 4, -1, 100, 5), (F32, 4, 4, 0, 0), (F32, 4, 4, 1 << 30, 0),
-                (F32, 4, 4, 100, 33), (F32, 4, 4, 100, -1), (F32, 4, 4, 4, 5), (F32, 1 << 20, 1 << 20, 100, 5)):
+                (F32, 4, 4, 100, 33), (F32, 1 << 21, 1, 1 << 29, 0), (F32, 4, 4, 100, -1), (F32, 4, 4, 4, 5), (F32, 1 << 20, 1 << 20, 100, 5)):
         assert size(*bad) == -1, bad
 
 
@@ -139,6 +140,8 @@ def plan(lib, d, table, scales=None, n=None, null=()):
     (40, [(0, 4, 5, 10), (24, 1, 3)], "share"),           # one row over another's columns
     (40, [(0, 1, 20), (5, 2, 3, 10)], "share"),
     (1 << 40, [(0, 1 << 20, 1 << 20)], "tiles"),
+    (1 << 40, [(0, 1 << 13, 1 << 13), (1 << 26, 1 << 20, 1 << 19)], "tiles"),
+    (1 << 40, [(0, 1 << 26, 1, 2), (1, 1 << 26, 1, 2)], "rows that are apart"),
 ])
 def test_plan_refusals(lib, d, table, needle):
     refused(lib, plan(lib, d, table), needle)
