@@ -764,8 +764,8 @@ int64_t gmc_matrices_workspace(const gmc_matrices* plan);
  *   x_dev, out_dev  d components of a GMC_F32, GMC_BF16 or GMC_F16 type; out_dev may be x_dev
  *   steps           1 to 64; coefficients: host array [steps][3], finite, such that no singular
  *                   value in [0, 1] is taken beyond 2.5 by a step (the last one: 10^6), and
- *                   b s^2 + c s^4 stays within 60, and no step before the last takes all of
- *                   them below 0.25 (what a later step amplified would have lost its bits)
+ *                   no step before the last takes all of them below 0.25 (what a later step
+ *                   amplified would have lost its bits)
  *   eps in [0, 1]; alpha finite in fp32
  */
 gmc_status gmc_orthogonalize(void* hip_stream, const gmc_matrices* plan, int32_t dtype, const void* x_dev, void* out_dev,

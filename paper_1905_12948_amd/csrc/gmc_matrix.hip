@@ -1,6 +1,6 @@
 // Orthogonalised matrices of a flat vector (gmc_orthogonalize and
 // gmc_orthogonal_step in include/gmc.h): Newton-Schulz steps
-//   X <- a X + (b G + c G G) X,  G = X X^T,
+//   X <- (a I + b G + c G G) X,  G = X X^T,
 // from X = M / (|M| + eps), |.| the Frobenius norm, M taken on its side where it
 // has more rows than columns (the steps commute with transposition): X is m x n,
 // m <= n.
@@ -9,14 +9,14 @@
 // the five usual ones) and with them any rounding of X, so X, G and the polynomial
 // are kept to 22 bits: each value as the sum of two halves, hi = f16(v) and lo =
 // f16(v - hi), v the value times a power of two that keeps lo clear of the smallest
-// f16 (X and G: 2^13, the polynomial: 2^10).  A product is hi hi + hi lo + lo hi on the f16
+// f16 (X and G: 2^13, the polynomial: 2^10 or less).  A product is hi hi + hi lo + lo hi on the f16
 // matrix instructions with sums in 32 bits: what is left out, lo lo, is 2^-22 of it.  The
 // result is as near to the 64-bit one as products in 32 bits are.
 //
 // Where |M| is not far above eps X is small, as small as M, and would leave f16's range: what
 // is held is Y = X / theta, theta <= 1 a number of the matrix and the step: at first
 // |M| / (|M| + eps), so that |Y| = 1, then as much more as the step's polynomial can
-// amplify, up to 1.  In Y a step is Y <- (theta / theta') (a Y + (b theta^2 G + c theta^4 G G) Y).
+// amplify, up to 1.  In Y a step is Y <- (theta / theta') (a I + b theta^2 G + c theta^4 G G) Y.
 //
 // Layout.  X (along n), its transpose (along m), G and the polynomial are stored in
 // the order the matrix instructions read: blocks of 32 rows x 16 columns, lane l's
@@ -45,7 +45,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr float kScaleX = 0x1p13f, kScaleB = 0x1p10f;   // of X and G, and of b G + c G^2
+constexpr float kScaleX = 0x1p13f;                       // of X and G
 constexpr int kSide = 64;                                // side of the pieces the vector is read in
 constexpr int kParts = 1024;                             // partial sums of a matrix's squares
 constexpr int64_t kGapChunk = 1024;                      // components outside the matrices, a workgroup (more in long vectors)
@@ -294,7 +294,7 @@ struct ProductArgs {
     const _Float16 *X, *XT, *G, *B;  // what the mode reads
     _Float16 *Xo, *XTo, *Go, *Bo;    // and writes
     const float* theta;  // this step's of the first matrix
-    float a, b, c;
+    float a, b, c, scale;   // of the step, and what the polynomial is held times
     float* slots;        // parts of tiles' sums
     void* out;           // kLast, kLastStep
     const float* w;      // kLastStep
@@ -323,12 +323,11 @@ template <int kWide, int kMode, int DT>
 __device__ __forceinline__ void finish_blocks(const ProductArgs& a, const Mat& m, const Tile& t, const Sides<kMode>& sides, int ib0,
                                               int jb0, const f32x16 (&acc)[kWide][kWide], float* turn) {
     const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
-    const bool flip = sides.flip;
     const float theta = kMode == kGram ? 1.0f : a.theta[t.mat * (kMostSteps + 1)];
     const float ratio = kMode == kApply ? theta / a.theta[t.mat * (kMostSteps + 1) + 1] : 1.0f;
-    // d <- u (hi + lo) + v d
-    const float u = kMode == kPoly ? a.b * (theta * theta) * (kScaleB / kScaleX) : a.a * ratio;
-    const float v = kMode == kPoly ? a.c * (theta * theta) * (theta * theta) * (kScaleB / kScaleX / kScaleX) : ratio / kScaleB;
+    // d <- v d, of the polynomial a I + u (hi + lo) + v d
+    const float u = a.b * (theta * theta) * (a.scale / kScaleX);
+    const float v = kMode == kPoly ? a.c * (theta * theta) * (theta * theta) * (a.scale / kScaleX / kScaleX) : ratio / a.scale;
     const auto inside = [&](int i, int j) { return ib0 + i < sides.rows && jb0 + j < sides.cols; };
     // entry (i, j) where its row is j: block (jb, 2 ib + g / 2), lane col + 32 (g % 2), halves 4 half + e
     const auto spot = [&](int i, int j) { return ((int64_t)(jb0 + j) * 2 * sides.rows + 2 * (ib0 + i)) * 1024 + col * 8 + 4 * half; };
@@ -342,20 +341,22 @@ __device__ __forceinline__ void finish_blocks(const ProductArgs& a, const Mat& m
         return m.offset + (int64_t)((ib0 + i) * 32 + 4 * half) * m.pitch + (jb0 + j) * 32 + col;
     };
     // all that is read before anything is written: a wait for each block's would follow the other's stores
-    constexpr bool kAdds = kMode != kGram, kParts = kMode == kLastStep;
+    constexpr bool kAdds = kMode == kPoly, kParts = kMode == kLastStep;
     f16x4 hi[kAdds ? kWide : 1][kAdds ? kWide : 1][4], lo[kAdds ? kWide : 1][kAdds ? kWide : 1][4];
     float w[kParts ? kWide : 1][kParts ? kWide : 1][16];
-    if constexpr (kAdds) {
-        const _Float16* add = kMode == kPoly ? a.G + m.g * 1024 : flip ? a.X + m.x * 1024 : a.XT + m.x * 1024;
+    if constexpr (kAdds || kParts) {
+        const _Float16* add = a.G + m.g * 1024;
 #pragma unroll
         for (int i = 0; i < kWide; ++i)
 #pragma unroll
             for (int j = 0; j < kWide; ++j)
                 if (inside(i, j)) {
+                    if constexpr (kAdds) {
 #pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        hi[i][j][g] = *reinterpret_cast<const f16x4*>(add + spot(i, j) + (g >> 1) * 1024 + (g & 1) * 256);
-                        lo[i][j][g] = *reinterpret_cast<const f16x4*>(add + spot(i, j) + (g >> 1) * 1024 + (g & 1) * 256 + 512);
+                        for (int g = 0; g < 4; ++g) {
+                            hi[i][j][g] = *reinterpret_cast<const f16x4*>(add + spot(i, j) + (g >> 1) * 1024 + (g & 1) * 256);
+                            lo[i][j][g] = *reinterpret_cast<const f16x4*>(add + spot(i, j) + (g >> 1) * 1024 + (g & 1) * 256 + 512);
+                        }
                     }
                     if constexpr (kParts) {
 #pragma unroll
@@ -371,15 +372,19 @@ __device__ __forceinline__ void finish_blocks(const ProductArgs& a, const Mat& m
             const int ib = ib0 + i, jb = jb0 + j;
             const int64_t place = spot(i, j);
             f32x16 d = acc[i][j];
-            if constexpr (kMode == kGram) {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) d[e] *= 1.0f / kScaleX;
-            } else {
+            if constexpr (kMode == kPoly) {
 #pragma unroll
                 for (int g = 0; g < 4; ++g)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                         d[4 * g + e] = __builtin_fmaf((float)hi[i][j][g][e], u, __builtin_fmaf((float)lo[i][j][g][e], u, v * d[4 * g + e]));
+                if (ib == jb) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) d[e] += row(e) + 4 * half == col ? a.a * a.scale : 0.0f;
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) d[e] *= kMode == kGram ? 1.0f / kScaleX : v;
             }
             if constexpr (kMode == kLast || kMode == kLastStep) {
                 typedef typename Elem<DT>::T T;
@@ -445,8 +450,8 @@ __device__ __forceinline__ int64_t slot_of(int slot, int wave, int lane) {
 // One tile of D = P Q^T, both along their contraction, by four wavefronts of kWide x
 // kWide blocks each, and what the mode makes of it:
 //   kGram   P = Q = X            G = D
-//   kPoly   P = Q = G            B = b G + c D
-//   kApply  P = B, Q = X^T       X <- a X + D, along both axes
+//   kPoly   P = Q = G            B = a I + b G + c D
+//   kApply  P = B, Q = X^T       X <- D, along both axes
 //   kLast   the same, or P = X^T and Q = B for a matrix on its side, into the vector
 // or, of a tile whose contraction is cut, its part of the sum for matrix_join.  G and B are symmetric: tiles with j <= i, written to both places.
 template <int kWide, int kStages, int kMode, int DT>
@@ -557,7 +562,7 @@ __global__ __launch_bounds__(256, kStages == 4 ? 2 : 3) void matrix_product(Prod
         if (s + 3 < stages) step(s + 3, two, one, stage1, stage0);
         if (s + 4 < stages) step(s + 4, one, two, stage2, stage1);
     }
-    __syncthreads();   // no load is under way and shared memory is free
+    wait_stage<0>();   // no load is under way and shared memory is free
 
     static_assert(2 * 32 * 33 * 4 <= kChunks * 1024, "two wavefronts' blocks fit a stage");
     float* turn = reinterpret_cast<float*>(wave < 2 ? stage0 : stage1) + (wave & 1) * 32 * 33;
@@ -610,7 +615,7 @@ __global__ __launch_bounds__(256) void matrix_join(ProductArgs a) {
 
 struct SmallArgs {
     VectorArgs in;
-    float c[kMostSteps][3];
+    float c[kMostSteps][4];
     void* out;
     const float* w;
     float alpha, keep;
@@ -772,7 +777,8 @@ __global__ __launch_bounds__(kSmallThreads) void matrix_small(SmallArgs a) {
     for (int step = 0; step < a.in.steps; ++step) {
         // places of blocks are worked out where they are needed: kept over the steps they would take all registers
         asm volatile("" : "+v"(lane), "+s"(wave));
-        const float ca = a.c[step][0], cb = a.c[step][1], cc = a.c[step][2], theta2 = theta * theta;
+        const float ca = a.c[step][0], cb = a.c[step][1], cc = a.c[step][2], scale = a.c[step][3];
+        const float theta2 = theta * theta;
         f32x16 d[kOwn];
         {
             const int share = wave / (mb * mb), b = wave - share * mb * mb, ib = b / mb, jb = b - ib * mb;
@@ -802,7 +808,11 @@ __global__ __launch_bounds__(kSmallThreads) void matrix_small(SmallArgs a) {
         if (wave < mb * mb) {
             const int ib = wave / mb, jb = wave - ib * mb;
             d[0] = product(G + ib * mb * 256, G + jb * mb * 256);
-            mix4(G, ib, jb, 2 * mb, cb * theta2 * (kScaleB / kScaleX), cc * theta2 * theta2 * (kScaleB / kScaleX / kScaleX), d[0]);
+            mix4(G, ib, jb, 2 * mb, cb * theta2 * (scale / kScaleX), cc * theta2 * theta2 * (scale / kScaleX / kScaleX), d[0]);
+            if (ib == jb) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) d[0][e] += 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3) == (lane & 31) ? ca * scale : 0.0f;
+            }
         }
         if (B == G) __syncthreads();
         if (wave < mb * mb) keep4(B, wave / mb, wave % mb, 2 * mb, d[0]);
@@ -821,7 +831,8 @@ __global__ __launch_bounds__(kSmallThreads) void matrix_small(SmallArgs a) {
             const int cols = turned ? mb : nb, q = turned ? b - mb * nb : b, ib = q / cols, jb = q - ib * cols;
             const f16x8 *one = XT + (turned ? ib : jb) * mb * 256, *two = B + (turned ? jb : ib) * mb * 256;
             d[k] = product(turned ? one : two, turned ? two : one);
-            mix4(turned ? X : XT, ib, jb, turned ? 2 * nb : 2 * mb, ca * ratio, ratio / kScaleB, d[k]);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) d[k][e] *= ratio / scale;
         }
         if (last) {
             const float factor = a.alpha * m.scale * theta * (1.0f / kScaleX);
@@ -929,15 +940,14 @@ bool disjoint(std::vector<Part> p) {
     return true;
 }
 
-// Over singular values s in [0, top] the largest they are taken to, and the largest |b s^2 + c s^4| and
-// |a + b s^2 + c s^4|; infinite where one is not finite.
+// Over singular values s in [0, top] the largest they are taken to, and the largest |a + b s^2 + c s^4|;
+// infinite where one is not finite.
 struct Reach {
-    double x, poly, growth;
+    double x, growth;
 };
 
 Reach reach(double a, double b, double c, double top) {
     const auto p = [&](double s) { return fabs(s * (a + s * s * (b + s * s * c))); };
-    const auto q = [&](double s) { return fabs(s * s * (b + s * s * c)); };
     // extrema inside: 5 c y^2 + 3 b y + a = 0 and 2 c y + b = 0 in y = s^2
     double y[3] = {-1.0, -1.0, -1.0};
     if (c != 0.0) {
@@ -951,17 +961,23 @@ Reach reach(double a, double b, double c, double top) {
         y[0] = -a / (3.0 * b);
     }
     const auto slope = [&](double s) { return fabs(a + s * s * (b + s * s * c)); };
-    Reach m = {p(top), q(top), fmax(fabs(a), slope(top))};
+    Reach m = {p(top), fmax(fabs(a), slope(top))};
     for (double v : y) {
         const double s = v > 0.0 ? sqrt(v) : 0.0;
         if (s < top) {
             m.x = fmax(m.x, p(s));
-            m.poly = fmax(m.poly, q(s));
             m.growth = fmax(m.growth, slope(s));
         }
     }
-    if (!isfinite(m.x) || !isfinite(m.poly)) m.x = m.poly = INFINITY;
+    if (!isfinite(m.x) || !isfinite(m.growth)) m.x = m.growth = INFINITY;
     return m;
+}
+
+// What the polynomial is held times: 2^10 (its values then stay below 61440), less where a last step takes it beyond 60.
+float scale_of(double growth) {
+    int half = 10;
+    while (growth > 60.0 && half > -20) growth /= 2.0, --half;
+    return (float)ldexp(1.0, half);
 }
 
 struct Scratch {
@@ -1003,8 +1019,8 @@ gmc_status matrices_check(const char* me, const gmc_matrices* p, int32_t dtype, 
         const double *c = coefficients + 3 * k;
         if (!isfinite(c[0]) || !isfinite(c[1]) || !isfinite(c[2])) return op_error(GMC_EINVAL, me, "a coefficient is not finite");
         const Reach r = reach(c[0], c[1], c[2], top);
-        // X and G by 2^13 and the polynomial by 2^10 have to stay below f16's 65504
-        if (!(r.x <= 2.5 && r.poly <= 60.0) && !(k == steps - 1 && r.x <= 1e6 && r.poly <= 60.0))
+        // X and G by 2^13 have to stay below f16's 65504
+        if (!(r.x <= 2.5 || (k == steps - 1 && r.x <= 1e6)))
             return op_error(GMC_EINVAL, me, "the coefficients take a singular value beyond 2.5");
         // values are kept to 2^-37 of 1, and a later step may not take that for more than it is
         if (!(r.x >= 0.25) && k < steps - 1) return op_error(GMC_EINVAL, me, "the coefficients take every singular value below 0.25");
@@ -1149,7 +1165,7 @@ void run_join(int wide, dim3 grid, const ProductArgs& a, hipStream_t st) {
 }
 
 template <int DT, bool kStep>
-void run_products(const gmc_matrices* p, const Scratch& s, const Steps& how, ProductArgs a, hipStream_t st) {
+void run_products(const gmc_matrices* p, const Scratch& s, const Steps& how, const float* scale, ProductArgs a, hipStream_t st) {
     _Float16 *from = s.T0, *to = s.T1;
     a.slots = s.slots;
     a.X = s.X;
@@ -1164,6 +1180,7 @@ void run_products(const gmc_matrices* p, const Scratch& s, const Steps& how, Pro
         a.a = (float)how.coefficients[3 * k];
         a.b = (float)how.coefficients[3 * k + 1];
         a.c = (float)how.coefficients[3 * k + 2];
+        a.scale = scale[k];
         a.XT = from;
         a.XTo = to;
         a.theta = s.theta + k;
@@ -1198,9 +1215,11 @@ void run_steps(const gmc_matrices* p, const Scratch& s, const Steps& how, const 
     n.steps = how.n;
     if (p->small) n.theta = nullptr;
     double top = 1.0;
+    float scale[kMostSteps];
     for (int32_t k = 0; k < how.n; ++k) {
         const Reach r = reach(how.coefficients[3 * k], how.coefficients[3 * k + 1], how.coefficients[3 * k + 2], top);
         n.growth[k] = (float)fmax(r.growth, 1.0);
+        scale[k] = scale_of(r.growth);
         top = r.x;
     }
     n.X = s.X;
@@ -1209,7 +1228,7 @@ void run_steps(const gmc_matrices* p, const Scratch& s, const Steps& how, const 
         SmallArgs q;
         q.in = n;
         for (int32_t k = 0; k < how.n; ++k)
-            for (int e = 0; e < 3; ++e) q.c[k][e] = (float)how.coefficients[3 * k + e];
+            for (int e = 0; e < 4; ++e) q.c[k][e] = e < 3 ? (float)how.coefficients[3 * k + e] : scale[k];
         q.out = a.out;
         q.w = a.w;
         q.alpha = a.alpha;
@@ -1223,7 +1242,7 @@ void run_steps(const gmc_matrices* p, const Scratch& s, const Steps& how, const 
     matrix_norm<DT, kStep><<<dim3(p->norm.n), 256, 0, st>>>(n);
     n.tiles = p->pack.tiles;
     matrix_pack<DT, kStep><<<dim3(p->pack.n), 256, 0, st>>>(n);
-    run_products<DT, kStep>(p, s, how, a, st);
+    run_products<DT, kStep>(p, s, how, scale, a, st);
 }
 
 }  // namespace
