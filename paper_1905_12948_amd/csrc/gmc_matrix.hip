@@ -18,13 +18,22 @@
 // |M| / (|M| + eps), so that |Y| = 1, then as much more as the step's polynomial can
 // amplify, up to 1.  In Y a step is Y <- (theta / theta') (a I + b theta^2 G + c theta^4 G G) Y.
 //
-// Layout.  X (along n), its transpose (along m), G and the polynomial are stored in
-// the order the matrix instructions read: blocks of 32 rows x 16 columns, lane l's
-// eight neighbours of row l % 32 as 16 bytes at l * 16, hi then lo.  Every operand is
-// read along its contraction (X for G; G, which is its own transpose; X^T for the
-// last product), so a tile's blocks go to shared memory and to registers in whole
-// kilobytes, with no bank conflict and no swizzle.  Rows and columns are padded with
-// zeros to 32, which the steps keep.
+// Layout.  X's transpose, G and the polynomial are stored in the order the matrix
+// instructions read: blocks of 32 rows x 16 columns, lane l's eight neighbours of row
+// l % 32 as 16 bytes at l * 16, hi then lo.  X's product and G's square read every operand
+// along its contraction (the polynomial and X^T along m; G is its own transpose), so a
+// tile's blocks go to shared memory and to registers in whole kilobytes, with no bank
+// conflict and no swizzle.  G's product, along n, turns X^T on its way from shared memory to
+// registers: a copy of X along n, written by every step's last launch, costs more there (ResNet-50's
+// matrices 106 us, without it 80; the server's step 1.08 ms and 0.97) than the turning does in G's
+// product (2048 x 2048: 40 us, turned 41).  Rows and columns are padded with zeros to 32, which the
+// steps keep.
+//
+// What bounds it.  Three products of halves for one in 32 bits: 4096 x 4096 at 1160 to 1220 TFLOP/s of
+// them, 85 to 90 % of the 1366 a library's product of f16 matrices of that size reaches (both hold the
+// clock at 1.6 GHz of 2.4: power).  Many matrices of few rows are bound by what a step's last launch
+// reads and writes (ResNet-50: 8 bytes a component and step, 3.5 TB/s with the loads that tiles share), small
+// ones by the launches' chains (3 of 768 x 768: 12 us a launch, of which 2.5 us are the launch's and 2.5 its end's).
 #include <math.h>
 #include <stdlib.h>
 #include <string.h>
@@ -54,7 +63,7 @@ constexpr int kMostSteps = 64;
 // A matrix of the plan.  m <= n are its sides, mb and nb their number in blocks of 32.
 struct Mat {
     int64_t offset, pitch;
-    int64_t x, g;      // first block of X (and of X^T) and of G
+    int64_t x, g;      // first block of X^T and of G
     int32_t rows, cols, m, n, mb, nb;
     int32_t flip;      // rows > cols: X is the transpose
     float scale;
@@ -84,7 +93,7 @@ struct VectorArgs {
     int32_t nesterov;
     double* part;
     double eps;
-    _Float16 *X, *XT;
+    _Float16* XT;
     float* theta;              // [matrices][kMostSteps + 1]
     int32_t steps;
     float growth[kMostSteps];  // by which a step amplifies at most, 1 or more
@@ -201,7 +210,7 @@ __device__ __forceinline__ void wave_order() {
 __device__ __forceinline__ float first_theta(double norm, double eps) { return norm == 0.0 ? 1.0f : (float)(norm / (norm + eps)); }
 __device__ __forceinline__ float next_theta(float theta, float growth) { return fminf(theta * growth, 1.0f) + 0.0f * theta; }
 
-// The matrix over its norm, in halves, along both of its axes.
+// The transpose of X, the matrix over its norm, in halves.
 template <int DT, bool kStep>
 __global__ __launch_bounds__(256) void matrix_pack(VectorArgs a) {
     typedef typename Elem<DT>::T T;
@@ -248,23 +257,22 @@ __global__ __launch_bounds__(256) void matrix_pack(VectorArgs a) {
         theta[0] = v;
         for (int k = 0; k < a.steps; ++k) theta[k + 1] = v = next_theta(v, a.growth[k]);
     }
-    const int64_t kn = 2 * (int64_t)m.nb, km = 2 * (int64_t)m.mb;
+    const int64_t km = 2 * (int64_t)m.mb;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        // eight neighbours: of X's rows (u < 2) or of its columns
-        const int unit = threadIdx.x + 256 * (u & 1), row = unit & 63, k8 = unit >> 6;
-        const bool along = u < 2;
+    for (int u = 0; u < 2; ++u) {
+        // eight neighbours of a column of X
+        const int unit = threadIdx.x + 256 * u, j = unit & 63, k8 = unit >> 6;
         f16x8 hi, lo;
         float f[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const int i = along ? row : 8 * k8 + e, j = along ? 8 * k8 + e : row;
+            const int i = 8 * k8 + e;
             f[e] = (float)((double)(m.flip ? in[j][i] : in[i][j]) * inv);
         }
         split(f, hi, lo);
-        const int rb = (along ? t.i : t.j) * 2 + (row >> 5), kb = (along ? t.j : t.i) * 4 + (k8 >> 1);
-        if (rb < (along ? m.mb : m.nb) && kb < (along ? kn : km)) {
-            _Float16* o = (along ? a.X : a.XT) + (m.x + rb * (along ? kn : km) + kb) * 1024 + ((row & 31) + 32 * (k8 & 1)) * 8;
+        const int rb = t.j * 2 + (j >> 5), kb = t.i * 4 + (k8 >> 1);
+        if (rb < m.nb && kb < km) {
+            _Float16* o = a.XT + (m.x + rb * km + kb) * 1024 + ((j & 31) + 32 * (k8 & 1)) * 8;
             *reinterpret_cast<f16x8*>(o) = hi;
             *reinterpret_cast<f16x8*>(o + 512) = lo;
         }
@@ -291,8 +299,8 @@ enum { kGram, kPoly, kApply, kLast, kLastStep };
 struct ProductArgs {
     const Mat* mats;
     const Tile* tiles;
-    const _Float16 *X, *XT, *G, *B;  // what the mode reads
-    _Float16 *Xo, *XTo, *Go, *Bo;    // and writes
+    const _Float16 *XT, *G, *B;  // what the mode reads
+    _Float16 *XTo, *Go, *Bo;     // and writes
     const float* theta;  // this step's of the first matrix
     float a, b, c, scale;   // of the step, and what the polynomial is held times
     float* slots;        // parts of tiles' sums
@@ -409,13 +417,12 @@ __device__ __forceinline__ void finish_blocks(const ProductArgs& a, const Mat& m
                 *reinterpret_cast<f16x4*>(o + (g >> 1) * 1024 + (g & 1) * 256) = hi;
                 *reinterpret_cast<f16x4*>(o + (g >> 1) * 1024 + (g & 1) * 256 + 512) = lo;
             }
-            if (kMode != kApply && t.i == t.j) continue;
+            if (kMode == kApply || t.i == t.j) continue;
             // and where its row is i, by way of shared memory
 #pragma unroll
             for (int e = 0; e < 16; ++e) turn[(8 * (e >> 2) + 4 * half + (e & 3)) * 33 + col] = d[e];
             wave_order();
-            o = (kMode == kGram ? a.Go + m.g * 1024 : kMode == kPoly ? a.Bo + m.g * 1024 : a.Xo + m.x * 1024) +
-                ((int64_t)ib * 2 * sides.cols + 2 * jb) * 1024 + lane * 8;
+            o = (kMode == kGram ? a.Go + m.g * 1024 : a.Bo + m.g * 1024) + ((int64_t)ib * 2 * sides.cols + 2 * jb) * 1024 + lane * 8;
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 f16x8 hi, lo;
@@ -441,6 +448,12 @@ __device__ __forceinline__ void wait_stage() {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
+// Four neighbours of each of 16 lanes, turned: lane l of them gets entry l % 4 of lanes l / 4, l / 4 + 4, + 8 and + 12.
+__device__ __forceinline__ f16x4 turned(const _Float16* p) {
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(f16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p));
+}
+
 // The first of a lane's vectors of a slot.
 template <int kWide>
 __device__ __forceinline__ int64_t slot_of(int slot, int wave, int lane) {
@@ -449,9 +462,9 @@ __device__ __forceinline__ int64_t slot_of(int slot, int wave, int lane) {
 
 // One tile of D = P Q^T, both along their contraction, by four wavefronts of kWide x
 // kWide blocks each, and what the mode makes of it:
-//   kGram   P = Q = X            G = D
+//   kGram   P = Q = X            G = D, X read as X^T
 //   kPoly   P = Q = G            B = a I + b G + c D
-//   kApply  P = B, Q = X^T       X <- D, along both axes
+//   kApply  P = B, Q = X^T       X^T <- D^T
 //   kLast   the same, or P = X^T and Q = B for a matrix on its side, into the vector
 // or, of a tile whose contraction is cut, its part of the sum for matrix_join.  G and B are symmetric: tiles with j <= i, written to both places.
 template <int kWide, int kStages, int kMode, int DT>
@@ -466,11 +479,9 @@ __global__ __launch_bounds__(256, kStages == 4 ? 2 : 3) void matrix_product(Prod
     const Mat m = a.mats[t.mat];
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
     const Sides<kMode> sides(m, t);
-    const _Float16* P = (kMode == kGram ? a.X + m.x * 1024 : kMode == kPoly ? a.G + m.g * 1024
-                         : sides.flip ? a.XT + m.x * 1024 : a.B + m.g * 1024);
-    const _Float16* Q = (kMode == kGram ? a.X + m.x * 1024 : kMode == kPoly ? a.G + m.g * 1024
-                         : sides.flip ? a.B + m.g * 1024 : a.XT + m.x * 1024);
-    const int64_t row = (int64_t)(kMode == kGram ? m.nb : m.mb) * 2048;   // halves of a row of blocks
+    const _Float16* P = (kMode == kPoly ? a.G + m.g * 1024 : kMode == kGram || sides.flip ? a.XT + m.x * 1024 : a.B + m.g * 1024);
+    const _Float16* Q = (kMode == kPoly ? a.G + m.g * 1024 : kMode == kGram || !sides.flip ? a.XT + m.x * 1024 : a.B + m.g * 1024);
+    const int64_t row = (int64_t)m.mb * 2048;   // halves of a row of blocks
 
     // chunk c of a stage: side, block, 16 columns, half; a wavefront takes every fourth.
     // Blocks beyond the matrix are read as its last one and not written.
@@ -481,8 +492,13 @@ __global__ __launch_bounds__(256, kStages == 4 ? 2 : 3) void matrix_product(Prod
         int rb = (side ? sides.j : sides.i) * kBlocks + b;
         const int most = (side ? sides.cols : sides.rows) - 1;
         rb = rb < most ? rb : most;
-        from[k] = (side ? Q : P) + rb * row + (int64_t)t.first * 2048 + (c % (2 * kDeep)) * 512 + lane * 8;
+        from[k] = kMode == kGram ? P + t.first * row + (int64_t)rb * 2048 + (c & 1) * 512 + c % (2 * kDeep) / 2 * 128
+                                 : (side ? Q : P) + rb * row + (int64_t)t.first * 2048 + (c % (2 * kDeep)) * 512;
     }
+    // A lane's part.  G's product reads of 16 rows of X^T (of a row of blocks the k-th sixteen, or the stage's) 32 columns: lane l
+    // brings eight neighbours, the l / 16-th of a row, so that 16 lanes read 256 bytes; their rows are
+    // exchanged by fours so that what turns them meets all banks.
+    const unsigned part = kMode != kGram ? lane * 8 : (lane >> 5) * 1024 + ((lane >> 4) & 1) * 256 + ((lane & 15) ^ (4 * (lane >> 4))) * 8;
     f32x16 acc[kWide][kWide];
 #pragma unroll
     for (int i = 0; i < kWide; ++i)
@@ -494,14 +510,25 @@ __global__ __launch_bounds__(256, kStages == 4 ? 2 : 3) void matrix_product(Prod
     const int stages = (t.last - t.first) * 2 / kDeep;
     const auto fetch = [&](int s, int k, _Float16* to) {
         s = s < stages ? s : stages - 1;   // the count of loads under way stays what the waits take it for
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from[k] + (int64_t)s * (kDeep * 1024)),
+        const int64_t at = kMode != kGram ? (int64_t)s * (kDeep * 1024) : kDeep == 2 ? s * row : (s >> 1) * row + (s & 1) * 128;
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from[k] + at + part),
                                          (__attribute__((address_space(3))) void*)(to + (k * 4 + wave) * 512), 16, 0, 0);
     };
     // A wavefront's operands of a stage: of each 16 columns kWide blocks of P in their halves, then of Q.
     constexpr int kReads = kDeep * 4 * kWide, kProducts = kDeep * 3 * kWide * kWide, kLoads = kChunks / 4;
+    // (of G's product: lane l reads four neighbours of row 8 (l / 32) + l / 4 % 4, and then of the fourth after it, of
+    // columns 16 (l / 16 % 2) + 4 (l % 4), and gets four rows' of column l % 32)
+    const int eighth = 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+    const int turn_from = 128 * eighth + (((lane >> 2) & 3) + ((8 * (lane >> 5)) ^ (4 * eighth))) * 8 + 4 * (lane & 1);
     const auto read = [&](f16x8 (&o)[kReads], int r, const _Float16* here) {
         const int k = r / (4 * kWide), q = r / (2 * kWide) % 2, i = r / 2 % kWide, h = r % 2;
-        o[r] = reinterpret_cast<const f16x8*>(here)[(((q ? kBlocks + wj + i : wi + i) * kDeep + k) * 2 + h) * 64 + lane];
+        const _Float16* chunk = here + (((q ? kBlocks + wj + i : wi + i) * kDeep + k) * 2 + h) * 512;
+        if constexpr (kMode == kGram) {
+            const f16x4 one = turned(chunk + turn_from), two = turned(chunk + (turn_from ^ 32));
+            o[r] = __builtin_shufflevector(one, two, 0, 1, 2, 3, 4, 5, 6, 7);
+        } else {
+            o[r] = reinterpret_cast<const f16x8*>(chunk)[lane];
+        }
     };
     // Stage s + 1 is in shared memory and stage s has been read by all, whose place the loads of
     // stage s + kStages take; those of the stages between stay under way.  The operands of s + 1 are read
@@ -981,7 +1008,7 @@ float scale_of(double growth) {
 }
 
 struct Scratch {
-    _Float16 *X, *T0, *T1, *G, *B;
+    _Float16 *T0, *T1, *G, *B;
     double* part;
     float *theta, *slots;
     int64_t bytes;
@@ -995,7 +1022,6 @@ Scratch layout(const gmc_matrices* p, void* base) {
         at += up_to(bytes, 256) * 256;
         return here;
     };
-    s.X = reinterpret_cast<_Float16*>(take(p->blocks_x * 2048));
     s.T0 = reinterpret_cast<_Float16*>(take(p->blocks_x * 2048));
     s.T1 = reinterpret_cast<_Float16*>(take(p->blocks_x * 2048));
     s.G = reinterpret_cast<_Float16*>(take(p->blocks_g * 2048));
@@ -1168,8 +1194,6 @@ template <int DT, bool kStep>
 void run_products(const gmc_matrices* p, const Scratch& s, const Steps& how, const float* scale, ProductArgs a, hipStream_t st) {
     _Float16 *from = s.T0, *to = s.T1;
     a.slots = s.slots;
-    a.X = s.X;
-    a.Xo = s.X;
     a.G = a.Go = s.G;
     a.B = a.Bo = s.B;
     const auto take = [&](const gmc_matrices::List& l) {
@@ -1222,7 +1246,6 @@ void run_steps(const gmc_matrices* p, const Scratch& s, const Steps& how, const 
         scale[k] = scale_of(r.growth);
         top = r.x;
     }
-    n.X = s.X;
     n.XT = s.T0;
     if (p->small) {
         SmallArgs q;
