@@ -533,7 +533,7 @@ __global__ __launch_bounds__(256, kStages == 4 ? 2 : 3) void matrix_product(Prod
     // Stage s + 1 is in shared memory and stage s has been read by all, whose place the loads of
     // stage s + kStages take; those of the stages between stay under way.  The operands of s + 1 are read
     // and the loads issued between the products of s, one after each: in front of them they
-    // hold the products up (2048 x 2048, one workgroup a CU: X's product 59 us, so 53).
+    // hold the products up (2048 x 2048, one workgroup a CU: X's product 59 us, so 53; with what else followed 48).
     const auto step = [&](int s, const f16x8 (&now)[kReads], f16x8 (&then)[kReads], const _Float16* after, _Float16* here) {
         wait_stage<(kStages - 2) * kLoads>();
 #pragma unroll
@@ -655,7 +655,9 @@ constexpr int kSmallThreads = 1024, kSmallBlocks = 39;   // 4 KB each of 160 KB:
 // X its own, once all have read them.  X and X^T are both computed, the second by the products of the first
 // with their sides exchanged: a block's entries then go to either as 8 bytes a lane, where turning it
 // takes 32 writes of 2 bytes, which cost more than the products.  What shared memory is left takes the parts
-// of G that wavefronts without a block of their own sum, and then the polynomial.
+// of G that wavefronts without a block of their own sum, and then the polynomial.  64 x 147 in five steps: 32 us
+// a call (by the launches below 62), about 5 a step, what it takes to hand operands on through shared memory
+// seven times.
 template <int DT, bool kStep, int mb>
 __global__ __launch_bounds__(kSmallThreads) void matrix_small(SmallArgs a) {
     typedef typename Elem<DT>::T T;
@@ -932,9 +934,9 @@ namespace {
 
 constexpr int64_t kMostTiles = int64_t(1) << 22;
 // Tiles of 128 x 128 from which on they are taken: smaller ones read twice the bytes for each product, and
-// pay where they bring more CUs to work.  X's products: 2048 x 2048 (256 tiles) 52 us, by 64 x 64 ones more;
-// 3 of 768 x 768 (108) 16 us by 64 x 64.  G's and its square's: 2048 x 2048 (136) 40 us, by 64 x 64 50; ResNet-18's
-// matrices (about 60) 38 us and a join by 128 x 128, 22 by 64 x 64.
+// pay where they bring more CUs to work.  X's products: 2048 x 2048 (256 tiles) 48 us, by 64 x 64 ones 62;
+// 3 of 768 x 768 (108) 16 us, by 64 x 64 14.4.  G's and its square's, with their joins: 2048 x 2048 (136) 43 and
+// 41 us, by 64 x 64 49 each; ResNet-18's matrices (about 60) 39 and 14 us, by 64 x 64 36 and 10.
 constexpr int64_t kMany = 256, kManyEven = 100;
 constexpr int64_t kLeastCut = 8;     // blocks of 32 columns, of a part of a contraction
 constexpr int64_t kWorthCut = 48;    // by so many a tile is longer than its share for a cut to pay

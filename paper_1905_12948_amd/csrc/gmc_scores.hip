@@ -21,6 +21,11 @@
 // Rows beyond a workgroup's registers, and rows of a call with few of them, are cut
 // into pieces, each with its own maximum, sums and largest keys, which a second launch
 // joins.
+//
+// What bounds it.  Batches are memory's: 16 x 1024 x 50257 bf16 170 to 175 us (6.1 to 5.9 TB/s), the gradient of
+// half as many 237 (5.7, reads and writes).  16-bit rows with alternatives and lengths that no line
+// divides: the exponentials and each row's chain (6 x 333 x 32003 f16, 8 of them: 14 us of 22).  Few rows: one row's
+// chain of load, maximum, sums and choice (one 7 us, 20 alternatives of 64 rows 11.7).
 #include "gmc_rows.h"
 
 namespace gmc {
