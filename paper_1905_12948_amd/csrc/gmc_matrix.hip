@@ -648,28 +648,28 @@ struct SmallArgs {
     float alpha, keep;
 };
 
-constexpr int kSmallThreads = 1024, kSmallBlocks = 39;   // 4 KB each of 160 KB: X, X^T and G of 32 x 32 blocks
+constexpr int kSmallThreads = 1024, kSmallBlocks = 40;   // 4 KB each of 160 KB: X^T and G of 32 x 32 blocks
+constexpr int kSmallSide = 4;                            // the most blocks of the shorter side
 
-// Matrices of which X, X^T and G fit the shared memory of one CU: all steps in one launch, a workgroup a
+// Matrices of which X^T and G fit the shared memory of one CU: all steps in one launch, a workgroup a
 // matrix, a wavefront every sixteenth block of what a phase computes.  The polynomial takes G's place, and
-// X its own, once all have read them.  X and X^T are both computed, the second by the products of the first
-// with their sides exchanged: a block's entries then go to either as 8 bytes a lane, where turning it
-// takes 32 writes of 2 bytes, which cost more than the products.  What shared memory is left takes the parts
-// of G that wavefronts without a block of their own sum, and then the polynomial.  64 x 147 in five steps: 32 us
-// a call (by the launches below 62), about 5 a step, what it takes to hand operands on through shared memory
-// seven times.
+// X^T its own, once all have read them.  G's product turns X^T as above; rows of X^T are exchanged by
+// fours within 16 so that this meets all banks.  What shared memory is left takes the parts
+// of G that wavefronts without a block of their own sum, and then the polynomial.  It is bound by that
+// chain, about 4 us a step: 64 x 147 in five steps 30 us (by the launches above 62), 64 x 576 62 (78), 128 x 192 60
+// (66); 600 of 128 x 192, three a CU one after the other, 212 (436).
 template <int DT, bool kStep, int mb>
 __global__ __launch_bounds__(kSmallThreads) void matrix_small(SmallArgs a) {
     typedef typename Elem<DT>::T T;
-    constexpr int kWaves = kSmallThreads / 64, kMost = mb == 1 ? 19 : mb == 2 ? 16 : 15;   // blocks of X
-    constexpr int kOwn = (2 * kMost + kWaves - 1) / kWaves, kUnits = kMost * 128 / kSmallThreads + 1;
+    constexpr int kWaves = kSmallThreads / 64, kMost = (kSmallBlocks - mb * mb) / mb * mb;   // blocks of X
+    constexpr int kOwn = (kMost + kWaves - 1) / kWaves, kUnits = (kMost * 128 + kSmallThreads - 1) / kSmallThreads;
     __shared__ f16x8 lds[kSmallBlocks * 256];
-    __shared__ double sums[kWaves];
     const Mat m = a.in.mats[blockIdx.x];
     int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
     const int nb = m.nb;   // mb = m.mb
     // a block of 32 rows and 32 columns is four times 64 vectors: 16 columns' hi and lo, twice
-    f16x8 *X = lds, *XT = X + mb * nb * 256, *G = XT + mb * nb * 256;
+    f16x8 *XT = lds, *G = XT + mb * nb * 256;
+    double* sums = reinterpret_cast<double*>(G);
     // X in 32 bits, where X^T is later: [i][j], four neighbours exchanged with others by the row so that a
     // column's walk and a row's both meet all banks
     float* raw = reinterpret_cast<float*>(XT);
@@ -723,75 +723,73 @@ __global__ __launch_bounds__(kSmallThreads) void matrix_small(SmallArgs a) {
     const double norm = sqrt(sum), inv = norm == 0.0 ? 0.0 : (double)kScaleX / norm;
     float theta = first_theta(norm, a.in.eps);
     {
-        // eight neighbours at a time, of X's rows at once and of its columns when all have read theirs
+        // eight neighbours of a column of X at a time, written when all have read theirs
         f16x8 hi[kUnits], lo[kUnits];
-        const auto place = [&](int k, int deep) { return (k >> 6) * 128 + (k & 63); };
 #pragma unroll
-        for (int side = 0; side < 2; ++side) {
-            const int deep = side ? 2 * mb : 2 * nb;
+        for (int n = 0; n < kUnits; ++n) {
+            const int k = threadIdx.x + n * kSmallThreads;
+            if (k >= mb * nb * 128) break;
+            const int l = k & 63, b = (k >> 6) / (2 * mb), row = b * 32 + (l & 31), k0 = ((k >> 6) - b * 2 * mb) * 16 + (l >> 5) * 8;
+            float f[8];
 #pragma unroll
-            for (int n = 0; n < kUnits; ++n) {
-                const int k = threadIdx.x + n * kSmallThreads;
-                if (k >= mb * nb * 128) break;
-                const int l = k & 63, b = (k >> 6) / deep, row = b * 32 + (l & 31), k0 = ((k >> 6) - b * deep) * 16 + (l >> 5) * 8;
-                float f[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) f[e] = (float)((double)raw[side ? spot(k0 + e, row) : spot(row, k0 + e)] * inv);
-                split(f, hi[n], lo[n]);
-                if (side == 0) {
-                    X[place(k, deep)] = hi[n];
-                    X[place(k, deep) + 64] = lo[n];
-                }
-            }
+            for (int e = 0; e < 8; ++e) f[e] = (float)((double)raw[spot(k0 + e, row)] * inv);
+            split(f, hi[n], lo[n]);
         }
         __syncthreads();
 #pragma unroll
         for (int n = 0; n < kUnits; ++n) {
             const int k = threadIdx.x + n * kSmallThreads;
             if (k >= mb * nb * 128) break;
-            XT[place(k, 0)] = hi[n];
-            XT[place(k, 0) + 64] = lo[n];
+            const int at = (k >> 6) * 128 + ((k & 63) ^ (8 * ((k >> 6) & 1) + 4 * ((k >> 5) & 1)));
+            XT[at] = hi[n];
+            XT[at + 64] = lo[n];
         }
     }
     __syncthreads();
     // Columns 16 k of a block of P Q^T, in two sums, so that a product does not wait for the one before it
-    const auto multiply = [&](const f16x8* P, const f16x8* Q, int k, f32x16& one, f32x16& two) {
-        const f16x8 ph = P[k * 128 + lane], pl = P[k * 128 + 64 + lane], qh = Q[k * 128 + lane], ql = Q[k * 128 + 64 + lane];
+    const auto multiply = [&](f16x8 ph, f16x8 pl, f16x8 qh, f16x8 ql, f32x16& one, f32x16& two) {
         one = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, qh, one, 0, 0, 0);
         two = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, ql, two, 0, 0, 0);
         two = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl, qh, two, 0, 0, 0);
     };
-    // A block of P Q^T, both 32 mb columns wide
-    const auto product = [&](const f16x8* P, const f16x8* Q) {
+    // Eight neighbours of rows 16 k of a block of columns of X^T, turned (see matrix_product's)
+    const auto turn = [&](int b, int k, int h) {
+        const int eighth = 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+        const int from = ((eighth >> 1) * 128 + (eighth & 1) * 32 + ((lane >> 2) & 3) + ((8 * (lane >> 5)) ^ (4 * eighth))) * 8 + 4 * (lane & 1);
+        const _Float16* chunk = reinterpret_cast<const _Float16*>(XT) + ((k >> 1) * mb + b) * 2048 + (k & 1) * 128 + h * 512;
+        return __builtin_shufflevector(turned(chunk + from), turned(chunk + (from ^ 32)), 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    // Block ib of the polynomial's rows times block jb of X^T's rows, or (turned) the other way round
+    const auto product = [&](const f16x8* B, int ib, int jb, bool turned) {
         f32x16 one, two;
 #pragma unroll
         for (int e = 0; e < 16; ++e) one[e] = two[e] = 0.0f;
 #pragma unroll
-        for (int k = 0; k < 2 * mb; ++k) multiply(P, Q, k, one, two);
+        for (int k = 0; k < 2 * mb; ++k) {
+            const f16x8* b = B + (ib * 2 * mb + k) * 128 + lane;
+            const f16x8* x = XT + (jb * 2 * mb + k) * 128 + (lane ^ (8 * (k & 1) + 4 * (lane >> 5)));
+            // (in one sum where a wavefront has three blocks: registers)
+            if (turned) multiply(x[0], x[64], b[0], b[64], one, kOwn > 2 ? one : two);
+            else multiply(b[0], b[64], x[0], x[64], one, kOwn > 2 ? one : two);
+        }
+        if constexpr (kOwn <= 2) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) one[e] += two[e];
+            for (int e = 0; e < 16; ++e) one[e] += two[e];
+        }
         return one;
     };
     // blocks of 4 KB that are left, and so how many wavefronts share a block of G
-    const int spare = kSmallBlocks - 2 * mb * nb - mb * mb;
+    const int spare = kSmallBlocks - mb * nb - mb * mb;
     f16x8* left = G + mb * mb * 256;
     int shares = kWaves / (mb * mb) < 1 + spare / (mb * mb) ? kWaves / (mb * mb) : 1 + spare / (mb * mb);
     if (shares > nb) shares = nb;
     f16x8* B = spare >= mb * mb ? left : G;
-    // Entries 4 g to 4 g + 3 of block (ib, jb) where their row is j
-    const auto half4 = [&](f16x8* base, int ib, int jb, int deep, int g, int h) {
-        return reinterpret_cast<f16x4*>(base + (jb * deep + 2 * ib + (g >> 1)) * 128 + h * 64 + (lane & 31) + 32 * (g & 1)) + (lane >> 5);
+    // Entries 4 g to 4 g + 3 of block (ib, jb) where their row is j, of G and the polynomial or of X^T
+    const auto half4 = [&](f16x8* base, int ib, int jb, int g, int h, int exchange) {
+        return reinterpret_cast<f16x4*>(base + (jb * 2 * mb + 2 * ib + (g >> 1)) * 128 + h * 64 + ((lane & 31) ^ exchange) + 32 * (g & 1)) +
+               (lane >> 5);
     };
-    // d <- u times what is there + v d
-    const auto mix4 = [&](f16x8* base, int ib, int jb, int deep, float u, float v, f32x16& d) {
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const f16x4 hi = *half4(base, ib, jb, deep, g, 0), lo = *half4(base, ib, jb, deep, g, 1);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) d[4 * g + e] = __builtin_fmaf((float)hi[e], u, __builtin_fmaf((float)lo[e], u, v * d[4 * g + e]));
-        }
-    };
-    const auto keep4 = [&](f16x8* base, int ib, int jb, int deep, const f32x16& d) {
+    const auto keep4 = [&](f16x8* base, int ib, int jb, const f32x16& d, bool exchange) {
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             f16x4 hi, lo;
@@ -799,8 +797,8 @@ __global__ __launch_bounds__(kSmallThreads) void matrix_small(SmallArgs a) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) f[e] = d[4 * g + e];
             split(f, hi, lo);
-            *half4(base, ib, jb, deep, g, 0) = hi;
-            *half4(base, ib, jb, deep, g, 1) = lo;
+            *half4(base, ib, jb, g, 0, exchange ? 4 * g : 0) = hi;
+            *half4(base, ib, jb, g, 1, exchange ? 4 * g : 0) = lo;
         }
     };
     for (int step = 0; step < a.in.steps; ++step) {
@@ -816,7 +814,7 @@ __global__ __launch_bounds__(kSmallThreads) void matrix_small(SmallArgs a) {
             for (int e = 0; e < 16; ++e) one[e] = two[e] = 0.0f;
             if (share < shares) {
                 const int end = 2 * nb * (share + 1) / shares;
-                for (int k = 2 * nb * share / shares; k < end; ++k) multiply(X + ib * nb * 256, X + jb * nb * 256, k, one, two);
+                for (int k = 2 * nb * share / shares; k < end; ++k) multiply(turn(ib, k, 0), turn(ib, k, 1), turn(jb, k, 0), turn(jb, k, 1), one, two);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) one[e] += two[e];
                 if (share > 0)
@@ -830,44 +828,56 @@ __global__ __launch_bounds__(kSmallThreads) void matrix_small(SmallArgs a) {
                     for (int e = 0; e < 16; ++e) one[e] += reinterpret_cast<const float*>(left)[(k * mb * mb + b) * 1024 + e * 64 + lane];
 #pragma unroll
                 for (int e = 0; e < 16; ++e) one[e] *= 1.0f / kScaleX;
-                keep4(G, ib, jb, 2 * mb, one);
+                keep4(G, ib, jb, one, false);
             }
         }
         __syncthreads();
         if (wave < mb * mb) {
             const int ib = wave / mb, jb = wave - ib * mb;
-            d[0] = product(G + ib * mb * 256, G + jb * mb * 256);
-            mix4(G, ib, jb, 2 * mb, cb * theta2 * (scale / kScaleX), cc * theta2 * theta2 * (scale / kScaleX / kScaleX), d[0]);
+            f32x16 two;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) d[0][e] = two[e] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < 2 * mb; ++k) {
+                const f16x8 *p = G + (ib * 2 * mb + k) * 128 + lane, *q = G + (jb * 2 * mb + k) * 128 + lane;
+                multiply(p[0], p[64], q[0], q[64], d[0], two);
+            }
+            const float u = cb * theta2 * (scale / kScaleX), v = cc * theta2 * theta2 * (scale / kScaleX / kScaleX);
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const f16x4 hi = *half4(G, ib, jb, g, 0, 0), lo = *half4(G, ib, jb, g, 1, 0);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    d[0][4 * g + e] = __builtin_fmaf((float)hi[e], u, __builtin_fmaf((float)lo[e], u, v * (d[0][4 * g + e] + two[4 * g + e])));
+            }
             if (ib == jb) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) d[0][e] += 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3) == (lane & 31) ? ca * scale : 0.0f;
             }
         }
         if (B == G) __syncthreads();
-        if (wave < mb * mb) keep4(B, wave / mb, wave % mb, 2 * mb, d[0]);
+        if (wave < mb * mb) keep4(B, wave / mb, wave % mb, d[0], false);
         __syncthreads();
         const bool last = step + 1 == a.in.steps;
         const float next = last ? 0.0f : next_theta(theta, a.in.growth[step]);
         const float ratio = last ? 1.0f : theta / next;
-        // blocks of X, whose entries have their row j in X^T, and of X^T, whose entries have it in X; in
-        // the last step of the one that lies as the matrix does
-        const int first = last && m.flip ? mb * nb : 0, end = last && !m.flip ? mb * nb : 2 * mb * nb;
+        // blocks of X, whose entries have their row j in X^T; in the last step as the matrix lies
+        const bool turned = last && m.flip;
 #pragma unroll
         for (int k = 0; k < kOwn; ++k) {
-            const int b = first + wave + k * kWaves;
-            if (b >= end) break;
-            const bool turned = b >= mb * nb;
-            const int cols = turned ? mb : nb, q = turned ? b - mb * nb : b, ib = q / cols, jb = q - ib * cols;
-            const f16x8 *one = XT + (turned ? ib : jb) * mb * 256, *two = B + (turned ? jb : ib) * mb * 256;
-            d[k] = product(turned ? one : two, turned ? two : one);
+            const int b = wave + k * kWaves;
+            if (b >= mb * nb) break;
+            d[k] = product(B, b % mb, b / mb, turned);
 #pragma unroll
             for (int e = 0; e < 16; ++e) d[k][e] *= ratio / scale;
+            __builtin_amdgcn_sched_barrier(0);
+            asm volatile("" : "+v"(lane), "+s"(wave));
         }
         if (last) {
             const float factor = a.alpha * m.scale * theta * (1.0f / kScaleX);
 #pragma unroll
             for (int k = 0; k < kOwn; ++k) {
-                const int b = wave + k * kWaves, cols = m.flip ? mb : nb, ib = b / cols, jb = b - ib * cols;
+                const int b = wave + k * kWaves, ib = m.flip ? b / mb : b % mb, jb = m.flip ? b % mb : b / mb;
                 if (b >= mb * nb) break;
                 const int r0 = ib * 32 + 4 * (lane >> 5), c = jb * 32 + (lane & 31);
                 const int64_t at = m.offset + (int64_t)r0 * m.pitch + c;
@@ -894,10 +904,10 @@ __global__ __launch_bounds__(kSmallThreads) void matrix_small(SmallArgs a) {
 #pragma unroll
         for (int k = 0; k < kOwn; ++k) {
             const int b = wave + k * kWaves;
-            if (b >= 2 * mb * nb) break;
-            const bool turned = b >= mb * nb;
-            const int cols = turned ? mb : nb, q = turned ? b - mb * nb : b, ib = q / cols, jb = q - ib * cols;
-            keep4(turned ? X : XT, ib, jb, turned ? 2 * nb : 2 * mb, d[k]);
+            if (b >= mb * nb) break;
+            keep4(XT, b % mb, b / mb, d[k], true);
+            __builtin_amdgcn_sched_barrier(0);
+            asm volatile("" : "+v"(lane), "+s"(wave));
         }
         __syncthreads();
     }
@@ -1261,7 +1271,8 @@ void run_steps(const gmc_matrices* p, const Scratch& s, const Steps& how, const 
         const dim3 grid((unsigned)p->n);
         if (p->small == 1) matrix_small<DT, kStep, 1><<<grid, kSmallThreads, 0, st>>>(q);
         else if (p->small == 2) matrix_small<DT, kStep, 2><<<grid, kSmallThreads, 0, st>>>(q);
-        else matrix_small<DT, kStep, 3><<<grid, kSmallThreads, 0, st>>>(q);
+        else if (p->small == 3) matrix_small<DT, kStep, 3><<<grid, kSmallThreads, 0, st>>>(q);
+        else matrix_small<DT, kStep, kSmallSide><<<grid, kSmallThreads, 0, st>>>(q);
         return;
     }
     matrix_norm<DT, kStep><<<dim3(p->norm.n), 256, 0, st>>>(n);
@@ -1330,7 +1341,7 @@ gmc_status gmc_matrices_init(gmc_matrices** out, int64_t d, int32_t n, const int
         // matrices of another number of rows in blocks are padded to the most of them
         int most = 0, wide = 0;
         for (const Mat& m : mats) most = std::max(most, m.mb), wide = std::max(wide, m.nb);
-        if (n > 0 && 2 * (int64_t)most * wide + (int64_t)most * most <= kSmallBlocks) {
+        if (n > 0 && most <= kSmallSide && (int64_t)most * std::max(wide, most) + most * most <= kSmallBlocks) {
             p->small = most;
             for (Mat& m : mats) m.mb = most, m.nb = std::max(m.nb, most);
         }

@@ -96,7 +96,10 @@ def test_larger_matrices():
     [(5, 9), (40, 10), (64, 64), (1, 1), (30, 70), (64, 200)],     # of one workgroup each, by their longest side
     [(96, 160), (160, 96), (3, 3)], [(1, 600), (600, 1), (32, 32)], [(96, 161), (64, 64)],
     [(3, 4)] * 300 + [(4, 3)] * 40, [(512, 4608), (512, 2304), (64, 576), (10, 512)],   # long contractions
-    [(1000, 2048), (64, 147), (128, 512)], [(300, 300), (64, 64), (1, 40)]])
+    [(1000, 2048), (64, 147), (128, 512)], [(300, 300), (64, 64), (1, 40)],
+    # the longest that one workgroup takes, and those beyond
+    [(32, 1248), (1248, 32)], [(64, 576), (576, 64), (50, 60)], [(96, 320), (33, 320)], [(128, 192), (192, 128), (100, 100)],
+    [(32, 1249)], [(64, 577)], [(321, 96)], [(128, 193)], [(129, 129)]])
 def test_several_matrices(shapes):
     """Plans that take different ways through the launches, with and without momentum."""
     import paper_1905_12948_amd as gmc

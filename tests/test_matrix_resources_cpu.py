@@ -4,10 +4,6 @@ import pytest
 
 from test_kernel_resources_cpu import kernels, named  # noqa: F401 (kernels is a fixture)
 
-# scratch bytes a thread, by part of the name: element type, with momentum, blocks of the shorter side
-SPILLS = {"matrix_smallILi0ELb0ELi1E": 160, "matrix_smallILi1ELb0ELi1E": 160, "matrix_smallILi2ELb0ELi1E": 160,
-          "matrix_smallILi0ELb1ELi1E": 160, "matrix_smallILi1ELb1ELi1E": 160, "matrix_smallILi2ELb1ELi1E": 160}
-
 
 def test_scratch(kernels):  # noqa: F811
     seen = 0
@@ -15,8 +11,7 @@ def test_scratch(kernels):  # noqa: F811
         if "score_" not in name and "matrix_" not in name:
             continue
         seen += 1
-        most = max([b for part, b in SPILLS.items() if part in name], default=0)
-        assert k[".private_segment_fixed_size"] <= most, (name, k[".private_segment_fixed_size"])
+        assert k[".private_segment_fixed_size"] == 0, (name, k[".private_segment_fixed_size"])
     assert seen > 80
 
 
