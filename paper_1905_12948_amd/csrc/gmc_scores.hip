@@ -24,7 +24,7 @@
 //
 // What bounds it.  Batches are memory's: 16 x 1024 x 50257 bf16 170 to 175 us (6.1 to 5.9 TB/s), the gradient of
 // half as many 237 (5.7, reads and writes).  16-bit rows with alternatives and lengths that no line
-// divides: the exponentials and each row's chain (6 x 333 x 32003 f16, 8 of them: 14 us of 22).  Few rows: one row's
+// divides: the exponentials and each row's chain (6 x 333 x 32003 f16, 8 of them: 13 us of 21).  Few rows: one row's
 // chain of load, maximum, sums and choice (one 7 us, 20 alternatives of 64 rows 11.7).
 #include "gmc_rows.h"
 
@@ -215,13 +215,30 @@ void score_rows(ScoreArgs a) {
     float xy = NAN;
     if (!kPieces && a.labels && tid == 0) xy = label_logit<DT>(in, a.V, label);
     float f[N], own = ex;
+    if constexpr (DT == GMC_F16) {
+        // two at a time, as they are: unpacked, the largest takes three times as many operations
+        typedef _Float16 Pair __attribute__((ext_vector_type(2)));
+        struct Pairs {
+            Pair p[N / 2];
+        };
+        Pair most = {(_Float16)-INFINITY, (_Float16)-INFINITY};
 #pragma unroll
-    for (int k = 0; k < kHeld; ++k)
-        if (k * kThreads < row.nb) {
-            x[k].unpack(f);
+        for (int k = 0; k < kHeld; ++k)
+            if (k * kThreads < row.nb) {
+                const Pairs h = __builtin_bit_cast(Pairs, x[k].raw);
 #pragma unroll
-            for (int q = 0; q < N; ++q) own = larger(own, f[q]);
-        }
+                for (int q = 0; q < N / 2; ++q) most = __builtin_elementwise_maximum(most, h.p[q]);
+            }
+        own = larger(own, larger((float)most.x, (float)most.y));
+    } else {
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k)
+            if (k * kThreads < row.nb) {
+                x[k].unpack(f);
+#pragma unroll
+                for (int q = 0; q < N; ++q) own = larger(own, f[q]);
+            }
+    }
     float m = lanes_max(own);
     if constexpr (kWaves > 1) {
         if (lane == 0) sh.top[wave] = m;

@@ -113,6 +113,24 @@ def test_orders_and_ties(V, dtype):
 
 
 @pytest.mark.parametrize("V", [30, 3000, 20000, 70000])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_rows_without_scores_16(V, dtype):
+    """The same in 16 bits: NaN of both signs in either place of a pair, alone and beside an infinity."""
+    import paper_1905_12948_amd as gmc
+    x = torch.randn(7, 1, V, device="cuda:0").to(dtype)
+    x[0, 0, 6] = math.nan
+    x[1, 0, 7] = -math.nan
+    x[2, 0, 17], x[2, 0, 16] = math.nan, math.inf
+    x[3, 0, 2] = math.inf
+    x[4] = -math.inf
+    x[5, 0, :V - 1] = -math.inf
+    logp, entropy, top_logp, top_ids, norm = gmc.token_scores(x, torch.full((7, 1), V - 1, device="cuda:0"), top=3)
+    assert torch.isnan(logp[:5]).all() and torch.isnan(entropy[:5]).all() and torch.isnan(top_logp[:5]).all()
+    assert torch.isfinite(logp[5:]).all() and torch.isfinite(entropy[5:]).all() and logp[5, 0] == 0 and entropy[5, 0] == 0
+    assert np.array_equal(top_ids.cpu().numpy()[:, 0], ref.scores(host(x[:, 0]), 1.0, 3)[3])
+
+
+@pytest.mark.parametrize("V", [30, 3000, 20000, 70000])
 def test_rows_without_scores(V):
     """NaN, +inf and nothing but -inf: NaN scores, and places all the same."""
     import paper_1905_12948_amd as gmc
