@@ -923,11 +923,11 @@ using namespace gmc;
 struct gmc_matrices {
     int64_t d = 0;
     int device = 0;
-    int wide = 1, even = 1;    // blocks a wavefront's side of a tile: of X's products, and of G's and its square's
+    int wide = 1, gram_wide = 1, poly_wide = 1;   // blocks a wavefront's side of a tile
     int32_t n = 0;
     int64_t blocks_x = 0, blocks_g = 0, parts = 0;
     int small = 0;             // every matrix is one workgroup's: their shorter sides' blocks
-    int64_t slots = 0;         // of parts of tiles' sums
+    int64_t slots = 0;         // of parts of tiles' sums, of one block a wavefront
     void* table = nullptr;     // device memory: all of the below
     const Mat* mats = nullptr;
     struct List {
@@ -951,6 +951,9 @@ constexpr int64_t kMany = 256, kManyEven = 100;
 constexpr int64_t kLeastCut = 8;     // blocks of 32 columns, of a part of a contraction
 constexpr int64_t kWorthCut = 48;    // by so many a tile is longer than its share for a cut to pay
 constexpr int64_t kTileCost = 4;     // what a tile costs besides, in such blocks
+// So many blocks for each place, cut and joined, take longer by tiles of 128 x 128 than by whole ones of 64 x 64,
+// which read more: the square of ResNet-50's G's (14) 26 us and 7 for the join, by 64 x 64 26; G's own (30) 55 and 9, by 64 x 64 74.
+constexpr int64_t kWorthJoin = 20;
 
 int64_t up_to(int64_t v, int64_t step) { return (v + step - 1) / step; }
 
@@ -1040,7 +1043,7 @@ Scratch layout(const gmc_matrices* p, void* base) {
     s.B = reinterpret_cast<_Float16*>(take(p->blocks_g * 2048));
     s.part = reinterpret_cast<double*>(take(p->parts * 8));
     s.theta = reinterpret_cast<float*>(take(p->small ? 0 : (int64_t)p->n * (kMostSteps + 1) * 4));
-    s.slots = reinterpret_cast<float*>(take(p->slots * p->even * p->even * 16384));
+    s.slots = reinterpret_cast<float*>(take(p->slots * 16384));
     s.bytes = at - static_cast<char*>(base);
     return s;
 }
@@ -1221,16 +1224,16 @@ void run_products(const gmc_matrices* p, const Scratch& s, const Steps& how, con
         a.XTo = to;
         a.theta = s.theta + k;
         dim3 grid = take(p->gram);
-        run_product<kGram, GMC_F32>(p->even, grid, a, st);
+        run_product<kGram, GMC_F32>(p->gram_wide, grid, a, st);
         if (p->gram_join.n) {
             grid = take(p->gram_join);
-            run_join<kGram>(p->even, grid, a, st);
+            run_join<kGram>(p->gram_wide, grid, a, st);
         }
         grid = take(p->poly);
-        run_product<kPoly, GMC_F32>(p->even, grid, a, st);
+        run_product<kPoly, GMC_F32>(p->poly_wide, grid, a, st);
         if (p->poly_join.n) {
             grid = take(p->poly_join);
-            run_join<kPoly>(p->even, grid, a, st);
+            run_join<kPoly>(p->poly_wide, grid, a, st);
         }
         grid = take(p->apply);
         if (k + 1 < how.n) run_product<kApply, GMC_F32>(p->wide, grid, a, st);
@@ -1337,7 +1340,6 @@ gmc_status gmc_matrices_init(gmc_matrices** out, int64_t d, int32_t n, const int
             mats.push_back(m);
         }
         p->wide = large >= kMany ? 2 : 1;
-        p->even = large_even >= kManyEven ? 2 : 1;
         // matrices of another number of rows in blocks are padded to the most of them
         int most = 0, wide = 0;
         for (const Mat& m : mats) most = std::max(most, m.mb), wide = std::max(wide, m.nb);
@@ -1345,9 +1347,9 @@ gmc_status gmc_matrices_init(gmc_matrices** out, int64_t d, int32_t n, const int
             p->small = most;
             for (Mat& m : mats) m.mb = most, m.nb = std::max(m.nb, most);
         }
-        const int side = 2 * p->wide, even = 2 * p->even;
+        const int side = 2 * p->wide;
         std::vector<Tile> norm, pack;
-        std::vector<Group> grams, polys, applies;
+        std::vector<Group> applies;
         int64_t tiles = 0;
         bool many = false;
         for (int32_t k = 0; k < n; ++k) {
@@ -1376,24 +1378,13 @@ gmc_status gmc_matrices_init(gmc_matrices** out, int64_t d, int32_t n, const int
             for (int32_t i = 0; i < mp; ++i)
                 for (int32_t j = 0; j < np; ++j) pack.push_back({k, i, j, 1, 0, 0, -1, 0});
             // groups of up to 8 x 8 tiles, smaller ones where there are few tiles to deal out
-            const int32_t most = tiles > 2048 ? 8 : 4, et = (m.mb + even - 1) / even;
+            const int32_t most = tiles > 2048 ? 8 : 4;
             for (int32_t i0 = 0; i0 < mt; i0 += most)
                 for (int32_t j0 = 0; j0 < nt; j0 += most) {
                     Group g;
                     for (int32_t j = j0; j < std::min(j0 + most, nt); ++j)
                         for (int32_t i = i0; i < std::min(i0 + most, mt); ++i) g.tiles.push_back({k, i, j, 1, 0, m.mb, -1, 0});
                     applies.push_back(std::move(g));
-                }
-            for (int32_t i0 = 0; i0 < et; i0 += most)
-                for (int32_t j0 = 0; j0 <= i0; j0 += most) {
-                    Group gram, poly;
-                    for (int32_t j = j0; j < std::min(j0 + most, et); ++j)
-                        for (int32_t i = std::max(i0, j); i < std::min(i0 + most, et); ++i) {
-                            gram.tiles.push_back({k, i, j, 1, 0, m.nb, -1, 0});
-                            poly.tiles.push_back({k, i, j, 1, 0, m.mb, -1, 0});
-                        }
-                    grams.push_back(std::move(gram));
-                    polys.push_back(std::move(poly));
                 }
         }
         // components between the matrices' rows
@@ -1419,12 +1410,46 @@ gmc_status gmc_matrices_init(gmc_matrices** out, int64_t d, int32_t n, const int
             delete p;
             return op_error(GMC_EINVAL, me, "too many pieces outside the matrices");
         }
+        // G's product or its square's: tiles with j <= i
+        const auto even_groups = [&](int wide, bool square) {
+            std::vector<Group> out;
+            for (int32_t k = 0; k < n; ++k) {
+                const int32_t even = 2 * wide, most = tiles > 2048 ? 8 : 4, et = (mats[k].mb + even - 1) / even;
+                for (int32_t i0 = 0; i0 < et; i0 += most)
+                    for (int32_t j0 = 0; j0 <= i0; j0 += most) {
+                        Group g;
+                        for (int32_t j = j0; j < std::min(j0 + most, et); ++j)
+                            for (int32_t i = std::max(i0, j); i < std::min(i0 + most, et); ++i)
+                                g.tiles.push_back({k, i, j, 1, 0, square ? mats[k].mb : mats[k].nb, -1, 0});
+                        out.push_back(std::move(g));
+                    }
+            }
+            return out;
+        };
+        const auto deal_even = [&](bool square, int& wide) {
+            wide = large_even >= kManyEven ? 2 : 1;
+            Launch l = deal(even_groups(wide, square), true);
+            int64_t work = 0;
+            for (const Tile& t : l.tiles) work += t.mat < 0 ? 0 : t.last - t.first;
+            if (wide == 2 && !l.joins.empty() && work <= kWorthJoin * kPlaces) {
+                Launch whole = deal(even_groups(1, square), true);
+                if (whole.joins.empty()) {
+                    wide = 1;
+                    return whole;
+                }
+            }
+            return l;
+        };
+        Launch gram, poly, apply;
         if (p->small) {   // no other launch, and nothing kept in the workspace
-            norm.clear(), pack.clear(), grams.clear(), polys.clear(), applies.clear();
+            norm.clear(), pack.clear();
             p->blocks_x = p->blocks_g = p->parts = 0;
+        } else {
+            gram = deal_even(false, p->gram_wide);
+            poly = deal_even(true, p->poly_wide);
+            apply = deal(std::move(applies), false);
         }
-        const Launch gram = deal(std::move(grams), true), poly = deal(std::move(polys), true), apply = deal(std::move(applies), false);
-        p->slots = std::max(gram.slots, poly.slots);
+        p->slots = std::max((int64_t)gram.slots * p->gram_wide * p->gram_wide, (int64_t)poly.slots * p->poly_wide * p->poly_wide);
         std::vector<char> host;
         const auto add = [&](const void* from, size_t bytes) {
             const size_t here = host.size();

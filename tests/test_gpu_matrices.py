@@ -99,7 +99,9 @@ def test_larger_matrices():
     [(1000, 2048), (64, 147), (128, 512)], [(300, 300), (64, 64), (1, 40)],
     # the longest that one workgroup takes, and those beyond
     [(32, 1248), (1248, 32)], [(64, 576), (576, 64), (50, 60)], [(96, 320), (33, 320)], [(128, 192), (192, 128), (100, 100)],
-    [(32, 1249)], [(64, 577)], [(321, 96)], [(128, 193)], [(129, 129)]])
+    [(32, 1249)], [(64, 577)], [(321, 96)], [(128, 193)], [(129, 129)],
+    # G's product by large tiles, its square's by small ones
+    [(1000, 1000)] + [(512, 3400)] * 8 + [(600, 512)] * 6])
 def test_several_matrices(shapes):
     """Plans that take different ways through the launches, with and without momentum."""
     import paper_1905_12948_amd as gmc
