@@ -1410,6 +1410,9 @@ gmc_status gmc_matrices_init(gmc_matrices** out, int64_t d, int32_t n, const int
             delete p;
             return op_error(GMC_EINVAL, me, "too many pieces outside the matrices");
         }
+        // the other way round than the norms: what those read last still lies in the 256 MB cache (ResNet-50's
+        // step 923 us, so 916)
+        std::reverse(pack.begin(), pack.end());
         // G's product or its square's: tiles with j <= i
         const auto even_groups = [&](int wide, bool square) {
             std::vector<Group> out;
