@@ -55,14 +55,18 @@ struct ScoreArgs {
 // NaN where one of the two is.
 __device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
+// A NaN is above +inf (0xff800000) and below what no key is: ~0, with which a search for the largest key
+// begins, would be its own at place 0.
+constexpr uint32_t kNanOrder = 0xfffffffeu;
+
 __device__ __forceinline__ uint64_t key_of(float x, int j) {
     const uint32_t b = __float_as_uint(x + 0.0f);   // -0 as 0
-    const uint32_t o = x != x ? 0xffffffffu : b >> 31 ? ~b : b | 0x80000000u;
+    const uint32_t o = x != x ? kNanOrder : b >> 31 ? ~b : b | 0x80000000u;
     return (uint64_t)o << 32 | (uint32_t)~j;
 }
 __device__ __forceinline__ float key_value(uint64_t k) {
     const uint32_t o = (uint32_t)(k >> 32);
-    return o == 0xffffffffu ? NAN : __uint_as_float(o >> 31 ? o & 0x7fffffffu : ~o);
+    return o == kNanOrder ? NAN : __uint_as_float(o >> 31 ? o & 0x7fffffffu : ~o);
 }
 __device__ __forceinline__ int key_place(uint64_t k) { return (int)~(uint32_t)k; }
 
