@@ -382,15 +382,14 @@ def token_scores(logits, labels=None, top: int = 0, temperature: float = 1.0, ig
     n = lib.gmc_token_scores_workspace(code, R, T, V, top)
     ws = _workspace(n, "gmc_token_scores: top must be in 0 to 32 and no more than the vocabulary, tokens below 2^22",
                     logits)
-    # one allocation for all 32-bit results: a view costs half of one
-    rows = R * T
-    room, row = _new(logits, rows * (4 + top)), (T, 1)
-    norm, entropy = room.as_strided((R, T, 2), (2 * T, 2, 1)), room.as_strided((R, T), row, 2 * rows)
+    # each result is a tensor of its own: views of one would share its version, so that an edit of one in place
+    # is an edit of all to a backward pass that kept them
+    norm, entropy = _new(logits, R, T, 2), _new(logits, R, T)
     logp = top_logp = top_ids = None
     if labels is not None:
-        logp = room.as_strided((R, T), row, 3 * rows)
+        logp = torch.empty_like(entropy)
     if top:
-        top_logp = room.as_strided((R, T, top), (T * top, top, 1), 4 * rows)
+        top_logp = _new(logits, R, T, top)
         top_ids = logits.new_empty((R, T, top), dtype=torch.int64)
     _call(logits, lib.gmc_token_scores, code, R, T, V, logits.data_ptr(), logits.stride(0), logits.stride(1), pl, lp,
           ignore, top, float(temperature), 0 if logp is None else logp.data_ptr(), entropy.data_ptr(),
