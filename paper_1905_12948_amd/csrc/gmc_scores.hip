@@ -132,16 +132,19 @@ struct Shared {
 
 __device__ __forceinline__ float log_sum(float m, float s) { return fabsf(m) < INFINITY ? logf(s) : NAN; }
 
+// A logit's distance to the maximum over the temperature; -inf stays, also where 1 / tau is 0 in 32 bits.
+__device__ __forceinline__ float scaled(const ScoreArgs& a, float x, float m) { return x == -INFINITY ? x : (x - m) * a.inv_tau; }
+
 __device__ __forceinline__ void write_scores(const ScoreArgs& a, int64_t i, float m, float s, float u, float xy) {
     const float ls = log_sum(m, s);
     reinterpret_cast<float2*>(a.norm)[i] = make_float2(m, ls);
     a.entropy[i] = ls - 0.69314718055994531f * (u / s);
-    if (a.logp) a.logp[i] = (xy - m) * a.inv_tau - ls;
+    if (a.logp) a.logp[i] = scaled(a, xy, m) - ls;
 }
 
 __device__ __forceinline__ void write_top(const ScoreArgs& a, int64_t i, int rank, uint64_t key, float m, float s) {
     a.top_ids[i * a.top + rank] = key_place(key);
-    a.top_logp[i * a.top + rank] = (key_value(key) - m) * a.inv_tau - log_sum(m, s);
+    a.top_logp[i * a.top + rank] = scaled(a, key_value(key), m) - log_sum(m, s);
 }
 
 // The scores of a token that is ignored.
