@@ -292,6 +292,12 @@ __global__ __launch_bounds__(256) void matrix_gaps(const Gap* gaps, const void* 
     }
 }
 
+// (1 - decay) w + step as keep w - decay w + step, the small terms first: 1 - decay in 32 bits is off by up to
+// 2^-25, the same way in every step, and a decay below that would be none.
+__device__ __forceinline__ float decayed(float w, float keep, float decay, float step) {
+    return __builtin_fmaf(keep, w, fabsf(w) < INFINITY ? __builtin_fmaf(-decay, w, step) : step);
+}
+
 // -- products ---------------------------------------------------------------------
 
 enum { kGram, kPoly, kApply, kLast, kLastStep };
@@ -306,7 +312,7 @@ struct ProductArgs {
     float* slots;        // parts of tiles' sums
     void* out;           // kLast, kLastStep
     const float* w;      // kLastStep
-    float alpha, keep;
+    float alpha, keep, decay;
 };
 
 // The rows and columns of a mode's tiles, in blocks; i and j where a matrix on its side is written last.
@@ -401,7 +407,7 @@ __device__ __forceinline__ void finish_blocks(const ProductArgs& a, const Mat& m
                 for (int e = 0; e < 16; ++e)
                     if (known(i, j, e)) {
                         const int64_t at = where(i, j) + row(e) * m.pitch;
-                        if constexpr (kMode == kLastStep) static_cast<float*>(a.out)[at] = a.keep * w[i][j][e] + factor * d[e];
+                        if constexpr (kMode == kLastStep) static_cast<float*>(a.out)[at] = decayed(w[i][j][e], a.keep, a.decay, factor * d[e]);
                         else static_cast<T*>(a.out)[at] = Elem<DT>::down(factor * d[e]);
                     }
                 continue;
@@ -645,7 +651,7 @@ struct SmallArgs {
     float c[kMostSteps][4];
     void* out;
     const float* w;
-    float alpha, keep;
+    float alpha, keep, decay;
 };
 
 constexpr int kSmallThreads = 1024, kSmallBlocks = 40;   // 4 KB each of 160 KB: X^T and G of 32 x 32 blocks
@@ -893,7 +899,7 @@ __global__ __launch_bounds__(kSmallThreads) void matrix_small(SmallArgs a) {
                 for (int e = 0; e < 16; ++e) {
                     const int r = 8 * (e >> 2) + (e & 3);
                     if (r0 + r >= m.rows || c >= m.cols) continue;
-                    if constexpr (kStep) static_cast<float*>(a.out)[at + r * m.pitch] = a.keep * w[e] + factor * d[k][e];
+                    if constexpr (kStep) static_cast<float*>(a.out)[at + r * m.pitch] = decayed(w[e], a.keep, a.decay, factor * d[k][e]);
                     else static_cast<T*>(a.out)[at + r * m.pitch] = Elem<DT>::down(factor * d[k][e]);
                 }
             }
@@ -1271,6 +1277,7 @@ void run_steps(const gmc_matrices* p, const Scratch& s, const Steps& how, const 
         q.w = a.w;
         q.alpha = a.alpha;
         q.keep = a.keep;
+        q.decay = a.decay;
         const dim3 grid((unsigned)p->n);
         if (p->small == 1) matrix_small<DT, kStep, 1><<<grid, kSmallThreads, 0, st>>>(q);
         else if (p->small == 2) matrix_small<DT, kStep, 2><<<grid, kSmallThreads, 0, st>>>(q);
@@ -1570,7 +1577,10 @@ gmc_status gmc_orthogonal_step(void* hip_stream, const gmc_matrices* plan, int32
             a.out = w_out_dev;
             a.w = w_dev;
             a.alpha = (float)rate;
-            a.keep = (float)(1.0 - decay);
+            // decays beyond a half leave less than they take: 1 - decay is the small one
+            const bool small = fabs(decay) <= 0.5;
+            a.keep = small ? 1.0f : (float)(1.0 - decay);
+            a.decay = small ? (float)decay : 0.0f;
             run_steps<DT, true>(plan, layout(plan, workspace_dev), {steps, coefficients, eps}, v, a, st);
         }
     });
