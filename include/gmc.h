@@ -759,7 +759,9 @@ int64_t gmc_matrices_workspace(const gmc_matrices* plan);
  *   X_{k+1} = a_k X_k + b_k (X_k X_k^T) X_k + c_k (X_k X_k^T)^2 X_k
  * and the components outside the matrices as they are.  The steps take each singular
  * value s to s (a + b s^2 + c s^4) and leave the singular vectors.  Products are
- * taken to 22 bits of each factor and summed in 32 bits; |M| is summed in 64.  A matrix
+ * taken to 22 bits of each factor, but no finer than 2^-48 of 1 (of |M|, in the first), and
+ * summed in 32 bits; |M| is summed in 64.  Rows or columns of components below 2^-27 of |M|
+ * come out less exact than with products in 32 bits.  A matrix
  * with a NaN or an infinity becomes NaN, and no other one does.
  *   x_dev, out_dev  d components of a GMC_F32, GMC_BF16 or GMC_F16 type; out_dev may be x_dev
  *   steps           1 to 64; coefficients: host array [steps][3], finite, such that no singular

@@ -7,11 +7,13 @@
 //
 // Precision.  The steps amplify small singular values by up to prod a_k (485 for
 // the five usual ones) and with them any rounding of X, so X, G and the polynomial
-// are kept to 22 bits: each value as the sum of two halves, hi = f16(v) and lo =
-// f16(v - hi), v the value times a power of two that keeps lo clear of the smallest
-// f16 (X and G: 2^13, the polynomial: 2^10 or less).  A product is hi hi + hi lo + lo hi on the f16
-// matrix instructions with sums in 32 bits: what is left out, lo lo, is 2^-22 of it.  The
-// result is as near to the 64-bit one as products in 32 bits are.
+// are kept to 22 bits: each value as two halves, hi = f16(v) and lo = f16(2^11 (v - hi)), v the value
+// times a power of two (X and G: 2^13, the polynomial: 2^10 or less).  lo has a scale of its own so that it
+// reaches f16's smallest number, 2^-24, no sooner than hi does: what is lost of a value is 2^-22 of it, or 2^-49 of 1
+// (the polynomial: 2^-46) where that is more.  Without it, 2^-38: rows 10^-5 the size of the others came out
+// 6e-4 off in a 1000 x 1100 matrix, so 2e-6, as with products in 32 bits; rows of 10^-7 4e-5 (32 bits 2e-6).  A product is
+// hi hi + 2^-11 (hi lo + lo hi) on the f16 matrix instructions, in two sums of 32 bits: what is left out, lo lo,
+// is 2^-22 of it.  The result is nearer to the 64-bit one than with products in 32 bits (its error 0.5 to 0.75 of theirs).
 //
 // Where |M| is not far above eps X is small, as small as M, and would leave f16's range: what
 // is held is Y = X / theta, theta <= 1 a number of the matrix and the step: at first
@@ -55,6 +57,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr float kScaleX = 0x1p13f;                       // of X and G
+constexpr float kScaleLo = 0x1p11f;                      // of a low half, beside its value's
 constexpr int kSide = 64;                                // side of the pieces the vector is read in
 constexpr int kParts = 1024;                             // partial sums of a matrix's squares
 constexpr int64_t kGapChunk = 1024;                      // components outside the matrices, a workgroup (more in long vectors)
@@ -178,10 +181,10 @@ __global__ __launch_bounds__(256) void matrix_norm(VectorArgs a) {
 }
 
 // Values as their two halves, two at a time (two values are converted in one operation, and what
-// hi leaves is one of the mixed-precision ones).
+// hi leaves, times kScaleLo, is one of the mixed-precision ones).
 template <int N, class H>
 __device__ __forceinline__ void split(const float (&v)[N], H& hi, H& lo) {
-    float minus = -1.0f;   // not known to be: v - hi is a conversion and a difference
+    float minus = -kScaleLo;   // not known to be: what hi leaves would be a conversion, a product and a difference
     asm("" : "+s"(minus));
 #pragma unroll
     for (int e = 0; e < N; e += 2) {
@@ -190,8 +193,8 @@ __device__ __forceinline__ void split(const float (&v)[N], H& hi, H& lo) {
         x.y = v[e + 1];
         const f16x2 h = __builtin_convertvector(x, f16x2);
         f32x2 r;
-        r.x = __builtin_fmaf((float)h.x, minus, v[e]);
-        r.y = __builtin_fmaf((float)h.y, minus, v[e + 1]);
+        r.x = __builtin_fmaf((float)h.x, minus, v[e] * kScaleLo);
+        r.y = __builtin_fmaf((float)h.y, minus, v[e + 1] * kScaleLo);
         const f16x2 l = __builtin_convertvector(r, f16x2);
         hi[e] = h.x;
         hi[e + 1] = h.y;
@@ -339,8 +342,8 @@ __device__ __forceinline__ void finish_blocks(const ProductArgs& a, const Mat& m
     const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
     const float theta = kMode == kGram ? 1.0f : a.theta[t.mat * (kMostSteps + 1)];
     const float ratio = kMode == kApply ? theta / a.theta[t.mat * (kMostSteps + 1) + 1] : 1.0f;
-    // d <- v d, of the polynomial a I + u (hi + lo) + v d
-    const float u = a.b * (theta * theta) * (a.scale / kScaleX);
+    // d <- v d, of the polynomial a I + u hi + ul lo + v d
+    const float u = a.b * (theta * theta) * (a.scale / kScaleX), ul = u * (1.0f / kScaleLo);
     const float v = kMode == kPoly ? a.c * (theta * theta) * (theta * theta) * (a.scale / kScaleX / kScaleX) : ratio / a.scale;
     const auto inside = [&](int i, int j) { return ib0 + i < sides.rows && jb0 + j < sides.cols; };
     // entry (i, j) where its row is j: block (jb, 2 ib + g / 2), lane col + 32 (g % 2), halves 4 half + e
@@ -391,7 +394,7 @@ __device__ __forceinline__ void finish_blocks(const ProductArgs& a, const Mat& m
                 for (int g = 0; g < 4; ++g)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        d[4 * g + e] = __builtin_fmaf((float)hi[i][j][g][e], u, __builtin_fmaf((float)lo[i][j][g][e], u, v * d[4 * g + e]));
+                        d[4 * g + e] = __builtin_fmaf((float)hi[i][j][g][e], u, __builtin_fmaf((float)lo[i][j][g][e], ul, v * d[4 * g + e]));
                 if (ib == jb) {
 #pragma unroll
                     for (int e = 0; e < 16; ++e) d[e] += row(e) + 4 * half == col ? a.a * a.scale : 0.0f;
@@ -505,13 +508,13 @@ __global__ __launch_bounds__(256, kStages == 4 ? 2 : 3) void matrix_product(Prod
     // brings eight neighbours, the l / 16-th of a row, so that 16 lanes read 256 bytes; their rows are
     // exchanged by fours so that what turns them meets all banks.
     const unsigned part = kMode != kGram ? lane * 8 : (lane >> 5) * 1024 + ((lane >> 4) & 1) * 256 + ((lane & 15) ^ (4 * (lane >> 4))) * 8;
-    f32x16 acc[kWide][kWide];
+    f32x16 acc[kWide][kWide], cross[kWide][kWide];   // hi hi; hi lo + lo hi, times kScaleLo
 #pragma unroll
     for (int i = 0; i < kWide; ++i)
 #pragma unroll
         for (int j = 0; j < kWide; ++j)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = cross[i][j][e] = 0.0f;
     const int wi = (wave >> 1) * kWide, wj = (wave & 1) * kWide;   // the wavefront's first blocks
     const int stages = (t.last - t.first) * 2 / kDeep;
     const auto fetch = [&](int s, int k, _Float16* to) {
@@ -545,8 +548,9 @@ __global__ __launch_bounds__(256, kStages == 4 ? 2 : 3) void matrix_product(Prod
 #pragma unroll
         for (int n = 0; n < kProducts; ++n) {
             const int k = n / (3 * kWide * kWide), part = n / (kWide * kWide) % 3, i = n / kWide % kWide, j = n % kWide;
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(now[k * 4 * kWide + 2 * i + (part == 2)],
-                                                               now[k * 4 * kWide + 2 * kWide + 2 * j + (part == 1)], acc[i][j], 0, 0, 0);
+            f32x16& sum = part ? cross[i][j] : acc[i][j];
+            sum = __builtin_amdgcn_mfma_f32_32x32x16_f16(now[k * 4 * kWide + 2 * i + (part == 2)],
+                                                         now[k * 4 * kWide + 2 * kWide + 2 * j + (part == 1)], sum, 0, 0, 0);
 #pragma unroll
             for (int r = n * (kReads + kLoads) / kProducts; r < (n + 1) * (kReads + kLoads) / kProducts; ++r) {
                 if (r < kReads) read(then, r, after);
@@ -596,6 +600,12 @@ __global__ __launch_bounds__(256, kStages == 4 ? 2 : 3) void matrix_product(Prod
         if (s + 4 < stages) step(s + 4, one, two, stage2, stage1);
     }
     wait_stage<0>();   // no load is under way and shared memory is free
+#pragma unroll
+    for (int i = 0; i < kWide; ++i)
+#pragma unroll
+        for (int j = 0; j < kWide; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = __builtin_fmaf(cross[i][j][e], 1.0f / kScaleLo, acc[i][j][e]);
 
     static_assert(2 * 32 * 33 * 4 <= kChunks * 1024, "two wavefronts' blocks fit a stage");
     float* turn = reinterpret_cast<float*>(wave < 2 ? stage0 : stage1) + (wave & 1) * 32 * 33;
@@ -752,7 +762,7 @@ __global__ __launch_bounds__(kSmallThreads) void matrix_small(SmallArgs a) {
         }
     }
     __syncthreads();
-    // Columns 16 k of a block of P Q^T, in two sums, so that a product does not wait for the one before it
+    // Columns 16 k of a block of P Q^T: hi hi, and hi lo + lo hi times kScaleLo
     const auto multiply = [&](f16x8 ph, f16x8 pl, f16x8 qh, f16x8 ql, f32x16& one, f32x16& two) {
         one = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, qh, one, 0, 0, 0);
         two = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, ql, two, 0, 0, 0);
@@ -770,17 +780,31 @@ __global__ __launch_bounds__(kSmallThreads) void matrix_small(SmallArgs a) {
         f32x16 one, two;
 #pragma unroll
         for (int e = 0; e < 16; ++e) one[e] = two[e] = 0.0f;
-#pragma unroll
-        for (int k = 0; k < 2 * mb; ++k) {
-            const f16x8* b = B + (ib * 2 * mb + k) * 128 + lane;
-            const f16x8* x = XT + (jb * 2 * mb + k) * 128 + (lane ^ (8 * (k & 1) + 4 * (lane >> 5)));
-            // (in one sum where a wavefront has three blocks: registers)
-            if (turned) multiply(x[0], x[64], b[0], b[64], one, kOwn > 2 ? one : two);
-            else multiply(b[0], b[64], x[0], x[64], one, kOwn > 2 ? one : two);
-        }
+        const auto b = [&](int k) { return B + (ib * 2 * mb + k) * 128 + lane; };
+        const auto x = [&](int k) { return XT + (jb * 2 * mb + k) * 128 + (lane ^ (8 * (k & 1) + 4 * (lane >> 5))); };
         if constexpr (kOwn <= 2) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) one[e] += two[e];
+            for (int k = 0; k < 2 * mb; ++k) {
+                if (turned) multiply(x(k)[0], x(k)[64], b(k)[0], b(k)[64], one, two);
+                else multiply(b(k)[0], b(k)[64], x(k)[0], x(k)[64], one, two);
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) one[e] = __builtin_fmaf(two[e], 1.0f / kScaleLo, one[e]);
+        } else {
+            // in one sum, the low halves' first, where a wavefront has three blocks: registers
+#pragma unroll
+            for (int k = 0; k < 2 * mb; ++k) {
+                const f16x8 *p = turned ? x(k) : b(k), *q = turned ? b(k) : x(k);
+                one = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[0], q[64], one, 0, 0, 0);
+                one = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[64], q[0], one, 0, 0, 0);
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) one[e] *= 1.0f / kScaleLo;
+#pragma unroll
+            for (int k = 0; k < 2 * mb; ++k) {
+                const f16x8 *p = turned ? x(k) : b(k), *q = turned ? b(k) : x(k);
+                one = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[0], q[0], one, 0, 0, 0);
+            }
         }
         return one;
     };
@@ -822,7 +846,7 @@ __global__ __launch_bounds__(kSmallThreads) void matrix_small(SmallArgs a) {
                 const int end = 2 * nb * (share + 1) / shares;
                 for (int k = 2 * nb * share / shares; k < end; ++k) multiply(turn(ib, k, 0), turn(ib, k, 1), turn(jb, k, 0), turn(jb, k, 1), one, two);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) one[e] += two[e];
+                for (int e = 0; e < 16; ++e) one[e] = __builtin_fmaf(two[e], 1.0f / kScaleLo, one[e]);
                 if (share > 0)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) reinterpret_cast<float*>(left)[((share - 1) * mb * mb + b) * 1024 + e * 64 + lane] = one[e];
@@ -848,13 +872,14 @@ __global__ __launch_bounds__(kSmallThreads) void matrix_small(SmallArgs a) {
                 const f16x8 *p = G + (ib * 2 * mb + k) * 128 + lane, *q = G + (jb * 2 * mb + k) * 128 + lane;
                 multiply(p[0], p[64], q[0], q[64], d[0], two);
             }
-            const float u = cb * theta2 * (scale / kScaleX), v = cc * theta2 * theta2 * (scale / kScaleX / kScaleX);
+            const float u = cb * theta2 * (scale / kScaleX), ul = u * (1.0f / kScaleLo), v = cc * theta2 * theta2 * (scale / kScaleX / kScaleX);
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const f16x4 hi = *half4(G, ib, jb, g, 0, 0), lo = *half4(G, ib, jb, g, 1, 0);
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    d[0][4 * g + e] = __builtin_fmaf((float)hi[e], u, __builtin_fmaf((float)lo[e], u, v * (d[0][4 * g + e] + two[4 * g + e])));
+                    d[0][4 * g + e] = __builtin_fmaf((float)hi[e], u, __builtin_fmaf((float)lo[e], ul,
+                                                     v * __builtin_fmaf(two[4 * g + e], 1.0f / kScaleLo, d[0][4 * g + e])));
             }
             if (ib == jb) {
 #pragma unroll
@@ -1069,7 +1094,7 @@ gmc_status matrices_check(const char* me, const gmc_matrices* p, int32_t dtype, 
         // X and G by 2^13 have to stay below f16's 65504
         if (!(r.x <= 2.5 || (k == steps - 1 && r.x <= 1e6)))
             return op_error(GMC_EINVAL, me, "the coefficients take a singular value beyond 2.5");
-        // values are kept to 2^-37 of 1, and a later step may not take that for more than it is
+        // values are kept to 2^-48 of 1, and a later step may not take that for more than it is
         if (!(r.x >= 0.25) && k < steps - 1) return op_error(GMC_EINVAL, me, "the coefficients take every singular value below 0.25");
         top = r.x;
     }
