@@ -735,8 +735,8 @@ gmc_status gmc_token_scores_backward(void* hip_stream, int32_t dtype, int64_t R,
  * A plan says which matrices a vector of d components holds: matrix i has
  * rows[i] x cols[i] components from offset[i] on, rows pitch[i] apart (NULL: cols),
  * and scale[i] (NULL: 1) is the factor of what becomes of it.  Host arrays, read
- * before the call returns.  Matrices may be column slices of one wide array; no two
- * share a component.  The plan keeps its tables on the current device, which later
+ * before the call returns.  Matrices may be column slices of one wide array, or lie between
+ * another's rows; no two share a component.  The plan keeps its tables on the current device, which later
  * calls have to be on, and is not changed by them: calls on several streams may
  * share it.  Making it waits for the device; it cannot be made while a stream is
  * captured, and has to live as long as the graphs that were captured with it.

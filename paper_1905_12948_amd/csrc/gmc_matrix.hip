@@ -988,30 +988,10 @@ constexpr int64_t kWorthJoin = 20;
 
 int64_t up_to(int64_t v, int64_t step) { return (v + step - 1) / step; }
 
-// Whether the matrices share no component: sorted by offset, neighbours are apart, or are
-// column slices of one wide array (rows the same distance apart, columns apart).
 struct Part {
     int64_t offset, rows, cols, pitch;
     int64_t end() const { return offset + (rows - 1) * pitch + cols; }
 };
-
-bool disjoint(std::vector<Part> p) {
-    std::sort(p.begin(), p.end(), [](const Part& a, const Part& b) { return a.offset < b.offset; });
-    for (size_t i = 0; i < p.size(); ++i)
-        for (size_t k = i + 1; k < p.size() && p[k].offset < p[i].end(); ++k) {
-            if (p[k].pitch != p[i].pitch || p[i].rows == 1 || p[k].rows == 1) {
-                // a single row between two rows of the other
-                const Part &one = p[i].rows == 1 ? p[i] : p[k], &more = p[i].rows == 1 ? p[k] : p[i];
-                if (one.rows != 1 || p[i].rows == 1) return false;
-                const int64_t c = (one.offset - more.offset) % more.pitch;
-                if (c < more.cols || c + one.cols > more.pitch) return false;
-                continue;
-            }
-            const int64_t c = (p[k].offset - p[i].offset) % p[i].pitch;
-            if (c < p[i].cols || c + p[k].cols > p[i].pitch) return false;
-        }
-    return true;
-}
 
 // Over singular values s in [0, top] the largest they are taken to, and the largest |a + b s^2 + c s^4|;
 // infinite where one is not finite.
@@ -1344,7 +1324,6 @@ gmc_status gmc_matrices_init(gmc_matrices** out, int64_t d, int32_t n, const int
             if (scale && !(fabs(scale[k]) <= 3.0e38)) return op_error(GMC_EINVAL, me, "a scale is not finite in fp32");
             parts.push_back(q);
         }
-        if (!disjoint(parts)) return op_error(GMC_EINVAL, me, "two matrices share components");
         p = new gmc_matrices;
         p->d = d;
         p->n = n;
@@ -1398,6 +1377,19 @@ gmc_status gmc_matrices_init(gmc_matrices** out, int64_t d, int32_t n, const int
             delete p;
             return op_error(GMC_EINVAL, me, many ? "the matrices have more tiles than a launch takes" : "too many rows that are apart");
         }
+        // the matrices' rows (dense ones' as one) in the vector's order: no two share a component, wherever they lie
+        std::vector<std::pair<int64_t, int64_t>> spans;
+        for (const Part& q : parts) {
+            if (q.pitch == q.cols) spans.push_back({q.offset, q.rows * q.cols});
+            else
+                for (int64_t r = 0; r < q.rows; ++r) spans.push_back({q.offset + r * q.pitch, q.cols});
+        }
+        std::sort(spans.begin(), spans.end());
+        for (size_t k = 1; k < spans.size(); ++k)
+            if (spans[k].first < spans[k - 1].first + spans[k - 1].second) {
+                delete p;
+                return op_error(GMC_EINVAL, me, "two matrices share components");
+            }
         for (int32_t k = 0; k < n; ++k) {
             Mat& m = mats[k];
             const int32_t mt = (m.mb + side - 1) / side, nt = (m.nb + side - 1) / side;
@@ -1420,13 +1412,6 @@ gmc_status gmc_matrices_init(gmc_matrices** out, int64_t d, int32_t n, const int
                 }
         }
         // components between the matrices' rows
-        std::vector<std::pair<int64_t, int64_t>> spans;
-        for (const Part& q : parts) {
-            if (q.pitch == q.cols) spans.push_back({q.offset, q.rows * q.cols});
-            else
-                for (int64_t r = 0; r < q.rows; ++r) spans.push_back({q.offset + r * q.pitch, q.cols});
-        }
-        std::sort(spans.begin(), spans.end());
         std::vector<Gap> gap;
         int64_t at = 0, chunk = kGapChunk;
         while (d / chunk > kMostTiles / 4) chunk *= 2;
