@@ -18,6 +18,17 @@ QUINTIC = (3.4445, -4.7750, 2.0315)
 STEPS = 5
 
 
+def _whole(v, name: str) -> int:
+    """v as an int; a whole number of any type."""
+    try:
+        n = int(v)
+        if not isinstance(v, str) and n == v:
+            return n
+    except (OverflowError, ValueError):   # infinite or NaN
+        pass
+    raise ValueError("%s must be a whole number, got %s" % (name, v))
+
+
 class Matrices:
     """A plan: which matrices a vector of ``d`` components holds.
 
@@ -29,12 +40,12 @@ class Matrices:
     def __init__(self, d: int, table: Sequence[Sequence[int]], scales: Optional[Sequence[float]] = None, device="cuda"):
         torch = _torch()
         self._lib, self._plan = load(), None
-        rows = [tuple(int(v) for v in entry) for entry in table]
+        d, rows = _whole(d, "d"), [tuple(_whole(v, "the table's entry") for v in entry) for entry in table]
         if any(len(entry) not in (3, 4) for entry in rows):
             raise ValueError("an entry of the table is (offset, rows, cols) or (offset, rows, cols, pitch)")
         if scales is not None and len(scales) != len(rows):
             raise ValueError("scales must hold one factor for each matrix")
-        if any(not -1 << 63 <= v < 1 << 63 for entry in rows for v in entry) or not -1 << 63 <= int(d) < 1 << 63:
+        if any(not -1 << 63 <= v < 1 << 63 for entry in rows for v in entry) or not -1 << 63 <= d < 1 << 63:
             raise ValueError("d and the table must be 64-bit integers")
         self.device = torch.device(device)
         if self.device.type != "cuda":
@@ -47,10 +58,10 @@ class Matrices:
         plan = ctypes.c_void_p()
         with torch.cuda.device(self.device):
             self.device = torch.device("cuda", torch.cuda.current_device())
-            st = self._lib.gmc_matrices_init(ctypes.byref(plan), int(d), n, offset, r, c, pitch, factor)
+            st = self._lib.gmc_matrices_init(ctypes.byref(plan), d, n, offset, r, c, pitch, factor)
         if st != GMC_OK:
             raise GmcError(st, self._lib.gmc_last_error(None).decode())
-        self._plan, self.d, self.n = plan, int(d), n
+        self._plan, self.d, self.n = plan, d, n
         self.workspace = int(self._lib.gmc_matrices_workspace(plan))
 
     def close(self):
@@ -87,7 +98,7 @@ def _typed(plan: Matrices, t, name: str) -> Tuple[int, int]:
 
 def _steps(steps: int, coefficients):
     """(number, host array) of the steps' coefficients: one triple for all, or one a step."""
-    steps = int(steps)
+    steps = _whole(steps, "steps")
     if not 1 <= steps <= 64:
         raise ValueError("steps must be in 1 to 64")
     if len(coefficients) == 3 and not hasattr(coefficients[0], "__len__"):
