@@ -96,16 +96,30 @@ def _typed(plan: Matrices, t, name: str) -> Tuple[int, int]:
     return code, t.data_ptr()
 
 
+def _several(v) -> bool:
+    """Whether v holds several values; a tensor or array of no axes does not."""
+    try:
+        len(v)
+    except TypeError:
+        return False
+    return True
+
+
 def _steps(steps: int, coefficients):
-    """(number, host array) of the steps' coefficients: one triple for all, or one a step."""
+    """(number, host array) of the steps' coefficients: one triple for all, or one a step;
+    sequences, arrays or tensors."""
     steps = _whole(steps, "steps")
     if not 1 <= steps <= 64:
         raise ValueError("steps must be in 1 to 64")
-    if len(coefficients) == 3 and not hasattr(coefficients[0], "__len__"):
-        coefficients = [coefficients] * steps
-    if len(coefficients) != steps or any(len(c) != 3 for c in coefficients):
+    values = None
+    if _several(coefficients):
+        if len(coefficients) == 3 and not _several(coefficients[0]):
+            values = [float(v) for v in coefficients] * steps
+        elif len(coefficients) == steps and all(_several(c) and len(c) == 3 and not _several(c[0]) for c in coefficients):
+            values = [float(v) for c in coefficients for v in c]
+    if values is None:
         raise ValueError("coefficients must be (a, b, c), or one such a step")
-    return steps, (ctypes.c_double * (3 * steps))(*[float(v) for c in coefficients for v in c])
+    return steps, (ctypes.c_double * (3 * steps))(*values)
 
 
 def _plan_of(plan) -> Matrices:
