@@ -738,8 +738,8 @@ gmc_status gmc_token_scores_backward(void* hip_stream, int32_t dtype, int64_t R,
  * before the call returns.  Matrices may be column slices of one wide array, or lie between
  * another's rows; no two share a component.  The plan keeps its tables on the current device, which later
  * calls have to be on, and is not changed by them: calls on several streams may
- * share it.  Making it waits for the device; it cannot be made while a stream is
- * captured, and has to live as long as the graphs that were captured with it.
+ * share it.  Making and destroying it waits for the device: neither can be done while a
+ * stream is captured.  It has to live as long as the graphs that were captured with it.
  *   d <= 2^40; 0 to 8192 matrices of 1 to 2^26 rows and columns, and no more than
  *   2^22 tiles of 64 x 64 (more than any vector of 2^34 components in dense
  *   matrices of 64 rows and columns or more), nor 2^23 rows with a pitch of their own
@@ -747,7 +747,7 @@ gmc_status gmc_token_scores_backward(void* hip_stream, int32_t dtype, int64_t R,
 typedef struct gmc_matrices gmc_matrices;
 gmc_status gmc_matrices_init(gmc_matrices** out, int64_t d, int32_t n, const int64_t* offset, const int64_t* rows,
                              const int64_t* cols, const int64_t* pitch, const double* scale);
-void gmc_matrices_destroy(gmc_matrices* plan); /* waits for the device; NULL is a no-op */
+void gmc_matrices_destroy(gmc_matrices* plan); /* waits for the plan's device; NULL is a no-op */
 
 /* Scratch bytes of the two calls below (256-byte aligned). */
 int64_t gmc_matrices_workspace(const gmc_matrices* plan);

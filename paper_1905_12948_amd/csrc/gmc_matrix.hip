@@ -1523,7 +1523,14 @@ gmc_status gmc_matrices_init(gmc_matrices** out, int64_t d, int32_t n, const int
 
 void gmc_matrices_destroy(gmc_matrices* plan) {
     if (!plan) return;
-    if (plan->table) (void)hipFree(plan->table);
+    if (plan->table) {
+        int current = plan->device;
+        (void)hipGetDevice(&current);
+        const bool waited = hipSetDevice(plan->device) == hipSuccess && hipDeviceSynchronize() == hipSuccess;
+        // (no table is freed that a call may still read)
+        if (!waited || hipFree(plan->table) != hipSuccess) (void)hipGetLastError();
+        if (current != plan->device) (void)hipSetDevice(current);
+    }
     delete plan;
 }
 

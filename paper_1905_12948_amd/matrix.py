@@ -29,13 +29,31 @@ def _whole(v, name: str) -> int:
     raise ValueError("%s must be a whole number, got %s" % (name, v))
 
 
+# plans closed or dropped while a stream was captured: freeing one waits for the device, which would
+# end the capture
+_dropped = []
+
+
+def _free_dropped():
+    if _dropped and not _torch().cuda.is_current_stream_capturing():
+        while True:
+            try:
+                lib, plan = _dropped.pop()
+            except IndexError:   # none left, or another thread took it
+                return
+            lib.gmc_matrices_destroy(plan)
+
+
 class Matrices:
     """A plan: which matrices a vector of ``d`` components holds.
 
     ``table``: (offset, rows, cols) or (offset, rows, cols, pitch) of each, rows ``pitch``
     components apart (cols, if not given); no two share a component.  ``scales``: each
     one's factor (default 1).  The plan belongs to ``device`` and may be shared by streams;
-    it has to live as long as graphs that were captured with it."""
+    it has to live as long as graphs that were captured with it.  Closed or dropped
+    while the thread's current stream is captured it is freed later, with the next plan that
+    is made, closed or dropped; while another thread captures in the global mode it is
+    neither."""
 
     def __init__(self, d: int, table: Sequence[Sequence[int]], scales: Optional[Sequence[float]] = None, device="cuda"):
         torch = _torch()
@@ -50,6 +68,7 @@ class Matrices:
         self.device = torch.device(device)
         if self.device.type != "cuda":
             raise ValueError("device must be a GPU device")
+        _free_dropped()
         n = len(rows)
         column = ctypes.c_int64 * n
         offset, r, c = (column(*[entry[k] for entry in rows]) for k in range(3))
@@ -66,8 +85,9 @@ class Matrices:
 
     def close(self):
         if getattr(self, "_plan", None):
-            self._lib.gmc_matrices_destroy(self._plan)
+            _dropped.append((self._lib, self._plan))
             self._plan = None
+        _free_dropped()
 
     def __del__(self):
         try:
