@@ -8,10 +8,12 @@ and entropies are the tokens' scores).
 Each worker has images of its own few classes (non-IID) and masks of its own; the
 gradients of all K workers go into gmc_iteration, which compresses them and updates
 the shared parameters.  With --orthogonal the server takes the sum of the messages
-through a momentum of its own and orthogonalises the weight matrices' part of it.
+through a momentum of its own and orthogonalises the weight matrices' part of it; with
+--bonus the policy loss has an entropy bonus of that weight.
 
-    python examples/train_workers.py [--orthogonal]
+    python examples/train_workers.py [--orthogonal] [--bonus 0.01]
 """
+import argparse
 import math
 import os
 import sys
@@ -203,5 +205,13 @@ def train(pair_steps=40, policy_steps=40, device="cuda:0", log=print, orthogonal
     return losses[0], losses[-1], rewards[0], rewards[-1]
 
 
+def options(argv):
+    """train's arguments from the command line's."""
+    p = argparse.ArgumentParser(description="K workers train a small captioning policy.")
+    p.add_argument("--orthogonal", action="store_true", help="the server orthogonalises the weight matrices' part of its step")
+    p.add_argument("--bonus", type=float, default=0.0, help="weight of the entropy bonus in the policy loss (default: none)")
+    return vars(p.parse_args(argv))
+
+
 if __name__ == "__main__":
-    train(orthogonal="--orthogonal" in sys.argv[1:])
+    train(**options(sys.argv[1:]))
