@@ -31,9 +31,9 @@
 // product (2048 x 2048: 40 us, turned 41).  Rows and columns are padded with zeros to 32, which the
 // steps keep.
 //
-// What bounds it.  Three products of halves for one in 32 bits: 4096 x 4096 at 1160 to 1220 TFLOP/s of
-// them, 85 to 90 % of the 1366 a library's product of f16 matrices of that size reaches (both hold the
-// clock at 1.6 GHz of 2.4: power).  Many matrices of few rows are bound by what a step's last launch
+// What bounds it.  Three products of halves for one in 32 bits: X's product of 4096 x 4096 at 1230 to 1270 TFLOP/s of
+// them, 90 to 93 % of the 1366 a library's product of f16 matrices of that size reaches, G's and its square at 970 to 1010 of
+// what their tiles compute (all hold the clock at 1.6 GHz of 2.4: power).  Many matrices of few rows are bound by what a step's last launch
 // reads and writes (ResNet-50: 8 bytes a component and step, 3.5 TB/s with the loads that tiles share), small
 // ones by the launches' chains (3 of 768 x 768: 12 us a launch, of which 2.5 us are the launch's and 2.5 its end's).
 #include <math.h>
@@ -672,8 +672,8 @@ constexpr int kSmallSide = 4;                            // the most blocks of t
 // X^T its own, once all have read them.  G's product turns X^T as above; rows of X^T are exchanged by
 // fours within 16 so that this meets all banks.  What shared memory is left takes the parts
 // of G that wavefronts without a block of their own sum, and then the polynomial.  It is bound by that
-// chain, about 4 us a step: 64 x 147 in five steps 30 us (by the launches above 62), 64 x 576 62 (78), 128 x 192 60
-// (66); 600 of 128 x 192, three a CU one after the other, 212 (436).
+// chain, about 4 us a step: 64 x 147 in five steps 31 us (by the launches above 58), 64 x 576 64 (73), 128 x 192 60
+// (67); 600 of 128 x 192, three a CU one after the other, 205 to 243 (444).
 template <int DT, bool kStep, int mb>
 __global__ __launch_bounds__(kSmallThreads) void matrix_small(SmallArgs a) {
     typedef typename Elem<DT>::T T;
@@ -975,15 +975,17 @@ namespace {
 
 constexpr int64_t kMostTiles = int64_t(1) << 22;
 // Tiles of 128 x 128 from which on they are taken: smaller ones read twice the bytes for each product, and
-// pay where they bring more CUs to work.  X's products: 2048 x 2048 (256 tiles) 48 us, by 64 x 64 ones 62;
-// 3 of 768 x 768 (108) 16 us, by 64 x 64 14.4.  G's and its square's, with their joins: 2048 x 2048 (136) 43 and
-// 41 us, by 64 x 64 49 each; ResNet-18's matrices (about 60) 39 and 14 us, by 64 x 64 36 and 10.
+// pay where they bring more CUs to work.  X's products: 2048 x 2048 (256 tiles) 49 us, by 64 x 64 ones 62;
+// 3 of 768 x 768 (108) 16 us, by 64 x 64 14.2.  G's and its square's, with their joins: 2048 x 2048 (136) 43 and
+// 41 us, by 64 x 64 47 and 48; ResNet-18's matrices (about 60) 38 and 14 us, by 64 x 64 34 and 10.
 constexpr int64_t kMany = 256, kManyEven = 100;
 constexpr int64_t kLeastCut = 8;     // blocks of 32 columns, of a part of a contraction
 constexpr int64_t kWorthCut = 48;    // by so many a tile is longer than its share for a cut to pay
 constexpr int64_t kTileCost = 4;     // what a tile costs besides, in such blocks
 // So many blocks for each place, cut and joined, take longer by tiles of 128 x 128 than by whole ones of 64 x 64,
 // which read more: the square of ResNet-50's G's (14) 26 us and 7 for the join, by 64 x 64 26; G's own (30) 55 and 9, by 64 x 64 74.
+// Of 20 plans those on either side of the border: ResNet-50's matrices (square) 822 us, so 865 without the rule; G's of 40 of
+// 256 x 4096 (30) and of 2 of 1280 x 5120 (34) 854 and 1094 us, by 64 x 64 897 and 1158.  Between 14 and 30 nothing was measured.
 constexpr int64_t kWorthJoin = 20;
 
 int64_t up_to(int64_t v, int64_t step) { return (v + step - 1) / step; }
@@ -1121,7 +1123,10 @@ Launch deal(std::vector<Group> groups, bool may_cut) {
     const int64_t fair = std::max<int64_t>(kLeastCut, up_to(work, kPlaces));
     const int64_t rest = tiles > kPlaces && tiles < 4 * kPlaces ? tiles % kPlaces : 0;
     // Where most tiles are as long, a cut spares little of what the launch does at its end, and a joining
-    // launch has to be worth it; where a few are long, or there is one anyway, less will do.
+    // launch has to be worth it; where a few are long, or there is one anyway, less will do.  (Of 20 plans: with
+    // kWorthCut for all, ResNet-50's matrices take 978 us for 822; with a quarter of it for all, 6 of 1024 x 1024 518 for 458,
+    // 2 of 1792 x 1792 793 for 721, 5 of 1100 x 1200 594 for 518.  It is not the best for all: 2 of 1280 x 5120 take
+    // 970 with the quarter for 1094, 4 of 1000 x 4096 998 for 1084.  The other 14 differ by 5 % at most.)
     int64_t long_work = 0;
     bool some = false;
     for (const Group& g : groups)

@@ -22,10 +22,10 @@
 // into pieces, each with its own maximum, sums and largest keys, which a second launch
 // joins.
 //
-// What bounds it.  Batches are memory's: 16 x 1024 x 50257 bf16 170 to 175 us (6.1 to 5.9 TB/s), the gradient of
-// half as many 237 (5.7, reads and writes).  16-bit rows with alternatives and lengths that no line
+// What bounds it.  Batches are memory's: 16 x 1024 x 50257 bf16, 9941 tokens counting, 170 to 194 us (5.9 to 5.2 TB/s),
+// the gradient of half as many 237 (5.6, reads and writes).  16-bit rows with alternatives and lengths that no line
 // divides: the exponentials and each row's chain (6 x 333 x 32003 f16, 8 of them: 13 us of 21).  Few rows: one row's
-// chain of load, maximum, sums and choice (one 7 us, 20 alternatives of 64 rows 11.7).
+// chain of load, maximum, sums and choice (one 9 us, 20 alternatives of 64 rows 13.5).
 #include "gmc_rows.h"
 
 namespace gmc {
@@ -599,7 +599,11 @@ Cut in_pieces(int64_t V, int64_t b, int64_t pieces) {
     return c;
 }
 
-// Rows too long to hold are cut, into more pieces where they leave CUs without one.
+// Rows too long to hold are cut, into more pieces where they leave CUs without one.  Rows of 6657 to 13,312 vectors are
+// held by 1024 threads, of which a CU takes one row at a time: with few rows that spares a launch (f32 x 50257, 64 rows
+// 12.6 us, in pieces 15; 256 rows 11.4 and 15), with many the loads of one do not overlap the sums of another, and pieces
+// of 512 threads, two on a CU, would be faster (4096 rows 150 us, in pieces 126; 1024 rows 43 and 35; bf16 8192 x 65536
+// 261 and 191).
 Cut cut_rows(int32_t dtype, int64_t rows, int64_t V) {
     const int64_t b = type_size(dtype), vecs = V * b / 16;   // at most, whatever the alignment
     if (vecs <= 1024 * 13 || rows == 0) return held_by(vecs, 1, (int32_t)V);

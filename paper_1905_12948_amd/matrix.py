@@ -13,7 +13,8 @@ from typing import Optional, Sequence, Tuple
 from .gmc import GMC_OK, GmcError, _check, _torch, load
 from .worker import _call, _code
 
-# the five usual steps of the iteration: a, b, c of X <- a X + b (X X^T) X + c (X X^T)^2 X
+# the five usual steps of the iteration: a, b, c of X <- a X + b (X X^T) X + c (X X^T)^2 X, the coefficients that were
+# published with the optimizer Muon (K. Jordan and others, 2024)
 QUINTIC = (3.4445, -4.7750, 2.0315)
 STEPS = 5
 
