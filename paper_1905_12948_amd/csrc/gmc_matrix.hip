@@ -341,7 +341,8 @@ __device__ __forceinline__ void finish_blocks(const ProductArgs& a, const Mat& m
                                               int jb0, const f32x16 (&acc)[kWide][kWide], float* turn) {
     const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
     const float theta = kMode == kGram ? 1.0f : a.theta[t.mat * (kMostSteps + 1)];
-    const float ratio = kMode == kApply ? theta / a.theta[t.mat * (kMostSteps + 1) + 1] : 1.0f;
+    // the last step takes X's scale off here: theta may be so small that what it is multiplied with would lose bits by it
+    const float ratio = kMode == kApply ? theta / a.theta[t.mat * (kMostSteps + 1) + 1] : 1.0f / kScaleX;
     // d <- v d, of the polynomial a I + u hi + ul lo + v d
     const float u = a.b * (theta * theta) * (a.scale / kScaleX), ul = u * (1.0f / kScaleLo);
     const float v = kMode == kPoly ? a.c * (theta * theta) * (theta * theta) * (a.scale / kScaleX / kScaleX) : ratio / a.scale;
@@ -405,7 +406,7 @@ __device__ __forceinline__ void finish_blocks(const ProductArgs& a, const Mat& m
             }
             if constexpr (kMode == kLast || kMode == kLastStep) {
                 typedef typename Elem<DT>::T T;
-                const float factor = a.alpha * m.scale * theta * (1.0f / kScaleX);
+                const float factor = a.alpha * m.scale * theta;
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
                     if (known(i, j, e)) {
@@ -891,7 +892,7 @@ __global__ __launch_bounds__(kSmallThreads) void matrix_small(SmallArgs a) {
         __syncthreads();
         const bool last = step + 1 == a.in.steps;
         const float next = last ? 0.0f : next_theta(theta, a.in.growth[step]);
-        const float ratio = last ? 1.0f : theta / next;
+        const float ratio = last ? 1.0f / kScaleX : theta / next;
         // blocks of X, whose entries have their row j in X^T; in the last step as the matrix lies
         const bool turned = last && m.flip;
 #pragma unroll
@@ -905,7 +906,7 @@ __global__ __launch_bounds__(kSmallThreads) void matrix_small(SmallArgs a) {
             asm volatile("" : "+v"(lane), "+s"(wave));
         }
         if (last) {
-            const float factor = a.alpha * m.scale * theta * (1.0f / kScaleX);
+            const float factor = a.alpha * m.scale * theta;
 #pragma unroll
             for (int k = 0; k < kOwn; ++k) {
                 const int b = wave + k * kWaves, ib = m.flip ? b / mb : b % mb, jb = m.flip ? b % mb : b / mb;
