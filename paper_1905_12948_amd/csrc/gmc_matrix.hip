@@ -13,7 +13,7 @@
 // (the polynomial: 2^-46) where that is more.  Without it, 2^-38: rows 10^-5 the size of the others came out
 // 6e-4 off in a 1000 x 1100 matrix, so 2e-6, as with products in 32 bits; rows of 10^-7 4e-5 (32 bits 2e-6).  A product is
 // hi hi + 2^-11 (hi lo + lo hi) on the f16 matrix instructions, in two sums of 32 bits: what is left out, lo lo,
-// is 2^-22 of it.  The result is nearer to the 64-bit one than with products in 32 bits (its error 0.5 to 0.75 of theirs).
+// is 2^-22 of it.  The result is nearer to the 64-bit one than with products in 32 bits (its error 0.4 to 0.75 of theirs).
 //
 // Where |M| is not far above eps X is small, as small as M, and would leave f16's range: what
 // is held is Y = X / theta, theta <= 1 a number of the matrix and the step: at first
